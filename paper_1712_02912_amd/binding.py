@@ -23,7 +23,9 @@ LUT_U8 = 1
 EXPORTS = ["pq_create", "pq_destroy", "pq_last_error", "pq_version", "pq_build_luts", "pq_quantize_luts",
            "pq_qmax_prescan", "pq_adc_scan_topk", "pq_rerank_f32", "ivf_adc_search", "pq_encode", "pq_rotate", "pq_derived_search", "pq_set_profiling",
            "pq_last_scan_kernel_ms", "pq_calibration_copy", "pq_set_option", "pq_unset_option", "pq_last_scan_info", "pq_adc_scan_topk_noalloc",
-           "ivf_quick_adc_search"]
+           "ivf_quick_adc_search", "pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens"]
+
+ELEMS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # pq_elem
 
 _lib = None
 
@@ -32,6 +34,16 @@ class IvfLists(ctypes.Structure):
     _fields_ = [("coarse_centroids", ctypes.c_void_p), ("list_offsets", ctypes.c_void_p),
                 ("codes", ctypes.c_void_p), ("ids", ctypes.c_void_p),
                 ("nlist", ctypes.c_int), ("d", ctypes.c_int), ("ntotal", ctypes.c_int64)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("key_strides", ctypes.c_int64 * 3),
+                ("value_strides", ctypes.c_int64 * 3), ("nblocks", ctypes.c_int64), ("block_size", ctypes.c_int),
+                ("heads", ctypes.c_int), ("dim", ctypes.c_int), ("elem", ctypes.c_int)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 def load():
@@ -64,6 +76,11 @@ def load():
     lib.pq_rotate.argtypes = [vp, vp, vp, i64, ci, vp]
     lib.pq_encode.argtypes = [vp, vp, vp, i64, ci, ci, ci, ci, vp]
     lib.pq_derived_search.argtypes = [vp, vp, i64, vp, vp, ci, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, i64]
+    cf, cache, heads = ctypes.c_float, ctypes.POINTER(KvCache), ctypes.POINTER(Heads)
+    lib.pq_kv_plan.argtypes = [vp, vp, vp, ci, vp, ci, vp, ci, ci, i64, vp, vp, vp, vp, vp]
+    lib.pq_kv_append.argtypes = [vp, cache, heads, ci, heads, heads, i64, vp, vp, vp, vp, i64, ci, ci, ci, vp, vp, cf, vp]
+    lib.pq_kv_attention.argtypes = [vp, cache, heads, ci, i64, vp, vp, ci, vp, ci, ci, cf, ci, vp, vp]
+    lib.pq_sample_tokens.argtypes = [vp, vp, ci, i64, ci, ci, vp, i64, vp, vp, vp, vp, vp, vp]
     lib.pq_calibration_copy.argtypes = [vp, vp, vp, ctypes.c_size_t]
     lib.pq_set_profiling.argtypes = [vp, ci]
     lib.pq_last_scan_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
@@ -90,6 +107,50 @@ def _dev(t, dtype, name):
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     return t.contiguous()
+
+
+def _in_place(t, dtype, name, shape=None):
+    """A tensor that the library reads and writes where it lies (no copy is made of it)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _heads(t, dtype, shape, name):
+    """Rows [tokens][heads][dim] of any strides but the last, as pq_heads."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and shape[2] > 1 and t.numel() > 0:
+        raise ValueError(f"the dimensions of a row of {name} must be contiguous")
+    return Heads(t.data_ptr(), s0, s1)
+
+
+def _cache(key_cache, value_cache):
+    """A paged cache [blocks][block size][heads][dim] of any strides but the last, as pq_kv_cache."""
+    for t, name in ((key_cache, "key_cache"), (value_cache, "value_cache")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a GPU tensor")
+        if t.dtype not in ELEMS or t.dtype != key_cache.dtype:
+            raise TypeError(f"{name} has dtype {t.dtype}: float32, float16 or bfloat16, the same for keys and values")
+        if t.dim() != 4 or t.shape != key_cache.shape:
+            raise ValueError(f"{name} must have shape [blocks][block size][heads][dim], the same for keys and values")
+        if t.stride(3) != 1 and t.shape[3] > 1 and t.numel() > 0:
+            raise ValueError(f"the dimensions of a row of {name} must be contiguous")
+    nblocks, block_size, heads, dim = key_cache.shape
+    ks, vs = key_cache.stride(), value_cache.stride()
+    return KvCache(key_cache.data_ptr(), value_cache.data_ptr(), ks[:3], vs[:3], nblocks, block_size, heads, dim,
+                   ELEMS[key_cache.dtype])
 
 
 class Context:
@@ -307,3 +368,95 @@ class Context:
                                                   nq, nprobe, init, kprime, topk, _ptr(dist), _ptr(out_ids),
                                                   _ptr(probes)))
         return (dist, out_ids, probes) if return_probes else (dist, out_ids)
+
+    # -- The reading step (include/pq_read.h) ----------------------------------------------------
+    def pq_kv_plan(self, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, out=None):
+        """Positions and slots of the new tokens; block_tables [nreq][width] gets the fresh blocks.
+        Returns (cu_new, kv_lens, positions, slots, taken), `out` if it is given."""
+        i32 = torch.int32
+        nreq, width = block_tables.shape
+        if out is None:
+            out = tuple(torch.empty(n, dtype=dt, device=block_tables.device)
+                        for n, dt in ((nreq + 1, i32), (nreq, i32), (ntokens, i32), (ntokens, torch.int64), (1, i32)))
+        cu_new, kv_lens, positions, slots, taken = out
+        self._check(self.lib.pq_kv_plan(
+            self.handle, _in_place(new_lens, i32, "new_lens", (nreq,)), _in_place(cached_lens, i32, "cached_lens", (nreq,)), nreq,
+            _in_place(block_tables, i32, "block_tables"), width, _in_place(free_blocks, i32, "free_blocks"), free_blocks.numel(),
+            block_size, ntokens, _in_place(cu_new, i32, "cu_new", (nreq + 1,)), _in_place(kv_lens, i32, "kv_lens", (nreq,)),
+            _in_place(positions, i32, "positions", (ntokens,)), _in_place(slots, torch.int64, "slots", (ntokens,)),
+            _in_place(taken, i32, "taken", (1,))))
+        return out
+
+    def pq_kv_append(self, q, k, v, positions, slots, key_cache, value_cache, cos=None, sin=None, q_weight=None, k_weight=None,
+                     eps=1e-6, norm=True, pairs=False, out=None):
+        """Norm and rotation of q [tokens][q heads][dim] and k [tokens][heads][dim]; k and v go into the cache
+        [blocks][block size][heads][dim].  cos, sin [positions][rot/2]; without them nothing is rotated.  Returns the queries
+        (None if q is None)."""
+        cache = _cache(key_cache, value_cache)
+        dtype, f32, heads, dim = key_cache.dtype, torch.float32, cache.heads, cache.dim
+        t = k.shape[0]
+        q_heads = 0 if q is None else q.shape[1]
+        if q is not None and out is None:
+            out = torch.empty((t, q_heads, dim), dtype=dtype, device=q.device)
+        if (cos is None) != (sin is None):
+            raise ValueError("cos and sin go together")
+        positions_max, half = (0, 0) if cos is None else cos.shape
+        rows_q = None if q is None else ctypes.byref(_heads(q, dtype, (t, q_heads, dim), "q"))
+        self._check(self.lib.pq_kv_append(
+            self.handle, ctypes.byref(cache), rows_q, q_heads, ctypes.byref(_heads(k, dtype, (t, heads, dim), "k")),
+            ctypes.byref(_heads(v, dtype, (t, heads, dim), "v")), t, _in_place(positions, torch.int32, "positions", (t,)),
+            _in_place(slots, torch.int64, "slots", (t,)), None if cos is None else _in_place(cos, f32, "cos"),
+            None if sin is None else _in_place(sin, f32, "sin", (positions_max, half)), positions_max, 2 * half, 1 if pairs else 0,
+            1 if norm else 0, None if q_weight is None else _in_place(q_weight, f32, "q_weight", (dim,)),
+            None if k_weight is None else _in_place(k_weight, f32, "k_weight", (dim,)), eps,
+            None if q is None else _in_place(out, dtype, "out", (t, q_heads, dim))))
+        return out if q is not None else None
+
+    def pq_kv_attention(self, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new, scale=None, window=0, out=None,
+                        lse=None):
+        """Attention of q [tokens][q heads][dim] over the paged cache; scale None: 1 / sqrt(dim).  Returns (out, lse)."""
+        cache = _cache(key_cache, value_cache)
+        t, q_heads = q.shape[0], q.shape[1]
+        nreq, width = block_tables.shape
+        if out is None:
+            out = torch.empty((t, q_heads, cache.dim), dtype=key_cache.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((t, q_heads), dtype=torch.float32, device=q.device)
+        i32, shape = torch.int32, (t, q_heads, cache.dim)
+        self._check(self.lib.pq_kv_attention(
+            self.handle, ctypes.byref(cache), ctypes.byref(_heads(q, key_cache.dtype, shape, "q")), q_heads, t,
+            _in_place(cu_new, i32, "cu_new", (nreq + 1,)), _in_place(kv_lens, i32, "kv_lens", (nreq,)), nreq,
+            _in_place(block_tables, i32, "block_tables"), width, max_new, cache.dim ** -0.5 if scale is None else scale, window,
+            _in_place(out, key_cache.dtype, "out", shape), _in_place(lse, torch.float32, "lse", (t, q_heads))))
+        return out, lse
+
+    def pq_sample_tokens(self, logits, noise, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
+        """One token for each row of logits [rows][vocab]; noise [rows][vocab] uniform in (0, 1), None: the largest logits.
+        Returns (tokens, logprobs)."""
+        if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+            raise TypeError("logits must be a GPU tensor")
+        if logits.dtype not in ELEMS:
+            raise TypeError(f"logits have dtype {logits.dtype}: float32, float16 or bfloat16")
+        rows, vocab = logits.shape
+        f32 = torch.float32
+        for t, dtype, name in ((logits, logits.dtype, "logits"), (noise, f32, "noise")):
+            if t is None:
+                continue
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+                raise TypeError(f"{name} must be a GPU tensor of dtype {dtype}")
+            if tuple(t.shape) != (rows, vocab):
+                raise ValueError(f"{name} must have shape {[rows, vocab]}, got {list(t.shape)}")
+            if t.stride(1) != 1 and vocab > 1 and rows > 0:
+                raise ValueError(f"the entries of a row of {name} must be contiguous")
+        if out is None:
+            out = (torch.empty(rows, dtype=torch.int64, device=logits.device), torch.empty(rows, dtype=f32, device=logits.device))
+
+        def per_row(t, dtype, name):
+            return None if t is None else _in_place(t, dtype, name, (rows,))
+
+        self._check(self.lib.pq_sample_tokens(
+            self.handle, _ptr(logits), ELEMS[logits.dtype], logits.stride(0), rows, vocab, _ptr(noise),
+            0 if noise is None else noise.stride(0), per_row(temperature, f32, "temperature"), per_row(top_k, torch.int32, "top_k"),
+            per_row(top_p, f32, "top_p"), per_row(min_p, f32, "min_p"), per_row(out[0], torch.int64, "tokens"),
+            per_row(out[1], f32, "logprobs")))
+        return out

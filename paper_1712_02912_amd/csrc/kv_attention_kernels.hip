@@ -1,0 +1,144 @@
+// Attention of new tokens over a paged cache (pq_kv_attention).
+#include <limits.h>
+
+#include "elem.h"
+#include "pq_internal.h"
+
+namespace pq {
+
+struct attention_args {
+    pq_kv_cache cache;
+    pq_heads q;
+    const int32_t *cu, *kv_lens, *tables;
+    void *out;
+    float *lse;
+    int64_t ntokens;
+    int q_heads, nreq, width, window;
+    float scale_log2;   // scale * log2(e): softmax in powers of two
+};
+
+// The request whose rows hold token t; -1 behind the last one.
+__device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, int64_t t) {
+    if (t >= cu[nreq]) return -1;
+    int low = 0, high = nreq;
+    while (high - low > 1) {
+        const int mid = (low + high) >> 1;
+        if (cu[mid] <= t) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
+// Position j of a request as (block, place); blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
+__device__ __forceinline__ void attention_place(const attention_args &a, int r, int j, int64_t &block, int &place) {
+    const int column = (int)((unsigned)j / (unsigned)a.cache.block_size);
+    place = j - column * a.cache.block_size;
+    const int32_t b = column < a.width ? a.tables[(int64_t)r * a.width + column] : 0;
+    block = (unsigned)b < (uint64_t)a.cache.nblocks ? b : 0;
+}
+
+// ---- any type and layout ------------------------------------------------------------------------------
+//
+// One block per row.  Each wave takes 64 keys at a time: a lane forms the product with one key, the wave updates the running
+// maximum and sum, then the lanes hold the dimensions and add up the weighted values.  The four waves' results are joined
+// at the end.  Keys are read by one lane each and no row shares what another one reads: simple, not fast.
+constexpr int GENERAL_WAVES = 4;
+constexpr int GENERAL_DIM = 512;
+
+template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_attention_general_kernel(attention_args a) {
+    __shared__ float q[GENERAL_DIM], acc[GENERAL_WAVES][GENERAL_DIM], stat[GENERAL_WAVES][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dim = a.cache.dim;
+    const int64_t t = blockIdx.x / a.q_heads;
+    const int h = (int)(blockIdx.x - t * a.q_heads), kvh = h / (a.q_heads / a.cache.heads);
+    const int r = attention_request(a.cu, a.nreq, t);
+    if (r < 0) return;
+    const int kv = a.kv_lens[r], at = kv - (a.cu[r + 1] - (int)t);   // this token's position
+    const int from = a.window > 0 ? max(0, at - a.window + 1) : 0;
+    const T *qrow = (const T *)a.q.p + t * a.q.token_stride + h * a.q.head_stride;
+    for (int i = tid; i < dim; i += 64 * GENERAL_WAVES) q[i] = (float)qrow[i];
+    for (int i = lane; i < dim; i += 64) acc[wave][i] = 0.f;
+    __syncthreads();
+    float top = -INFINITY, sum = 0.f, part[GENERAL_DIM / 64] = {};
+    for (int base = from + wave * 64; base <= at; base += 64 * GENERAL_WAVES) {
+        const int j = base + lane;
+        float s = -INFINITY;
+        int64_t block = 0;
+        int place = 0;
+        if (j <= at) {
+            attention_place(a, r, j, block, place);
+            const T *k = (const T *)a.cache.keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1] + kvh * a.cache.key_strides[2];
+            s = 0.f;
+            for (int i = 0; i < dim; ++i) s += q[i] * (float)k[i];
+            s *= a.scale_log2;
+        }
+        float high = s;
+        for (int d = 32; d > 0; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
+        high = fmaxf(high, top);
+        // (all weights so far zero, as by products of -inf: nothing to scale, and -inf - -inf is not formed)
+        const float ref = high == -INFINITY ? 0.f : high;
+        const float shrink = exp2f(top - ref), w = exp2f(s - ref);
+        top = high;
+        sum = sum * shrink + w;
+        const int64_t row = block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
+        for (int e = 0; e < GENERAL_DIM / 64; ++e) part[e] *= shrink;
+        const int count = min(64, at - base + 1);
+        for (int l = 0; l < count; ++l) {
+            const float wl = __shfl(w, l);
+            const T *v = (const T *)a.cache.values + __shfl((long long)row, l) + kvh * a.cache.value_strides[2];
+#pragma unroll
+            for (int e = 0; e < GENERAL_DIM / 64; ++e)
+                if (e * 64 + lane < dim) part[e] += wl * (float)v[e * 64 + lane];
+        }
+    }
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+#pragma unroll
+    for (int e = 0; e < GENERAL_DIM / 64; ++e)
+        if (e * 64 + lane < dim) acc[wave][e * 64 + lane] = part[e];
+    if (lane == 0) {
+        stat[wave][0] = top;
+        stat[wave][1] = sum;
+    }
+    __syncthreads();
+    float all = -INFINITY, total = 0.f, share[GENERAL_WAVES];
+    for (int w = 0; w < GENERAL_WAVES; ++w) all = fmaxf(all, stat[w][0]);
+    const float ref = all == -INFINITY ? 0.f : all;
+    for (int w = 0; w < GENERAL_WAVES; ++w) {
+        share[w] = exp2f(stat[w][0] - ref);
+        total += share[w] * stat[w][1];
+    }
+    T *out = (T *)a.out + (t * a.q_heads + h) * dim;
+    for (int i = tid; i < dim; i += 64 * GENERAL_WAVES) {
+        float o = 0.f;
+        for (int w = 0; w < GENERAL_WAVES; ++w) o += share[w] * acc[w][i];
+        out[i] = (T)(total != 0.f ? o / total : 0.f);
+    }
+    if (tid == 0 && a.lse) a.lse[t * a.q_heads + h] = total != 0.f ? (ref + log2f(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
+                        const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width,
+                        int max_new, float scale, int window, void *out, float *lse) {
+    attention_args a = {};
+    a.cache = *cache;
+    a.q = *q;
+    a.cu = cu_new;
+    a.kv_lens = kv_lens;
+    a.tables = block_tables;
+    a.out = out;
+    a.lse = lse;
+    a.ntokens = ntokens;
+    a.q_heads = q_heads;
+    a.nreq = nreq;
+    a.width = width;
+    a.window = window;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    const int64_t grid = ntokens * q_heads;
+    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
+    if (cache->elem == PQ_ELEM_F32) kv_attention_general_kernel<float><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
+    else if (cache->elem == PQ_ELEM_F16) kv_attention_general_kernel<_Float16><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
+    else kv_attention_general_kernel<__bf16><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+}  // namespace pq

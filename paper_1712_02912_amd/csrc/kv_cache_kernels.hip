@@ -1,0 +1,463 @@
+// The paged cache of the reading step: the plan (pq_kv_plan) and the append (pq_kv_append).
+#include <limits.h>
+
+#include "elem.h"
+#include "pq_internal.h"
+
+namespace pq {
+
+// ---- plan -------------------------------------------------------------------------------------------
+//
+// Two prefix sums over the requests (new tokens, needed blocks), then one thread per new token that finds its request by
+// bisection.  A fresh block begins with a new token, so the thread of that token also writes the block's entry in the
+// table; tokens of fresh blocks take the block from free_blocks, never from the table, so no thread reads what another
+// one writes.  There is next to nothing to move (12 bytes a token); what counts is that it is one launch: every block
+// forms the sums for itself (PLAN_MAX requests: 8 per thread, a few thousand cycles), rather than wait for another kernel.
+constexpr int PLAN_THREADS = 512;
+constexpr int PLAN_MAX = 4096;   // requests whose sums a block keeps in shared memory
+
+struct plan_args {
+    const int32_t *new_lens, *cached_lens;
+    int32_t *tables;
+    const int32_t *free_blocks;
+    int nreq, width, nfree, block_size;
+    int64_t ntokens;
+    int32_t *cu, *kv, *positions;
+    int64_t *slots;
+    int32_t *taken;
+};
+
+struct plan_request {
+    int64_t fresh_tokens, cached, need;
+    bool fits;
+};
+__device__ __forceinline__ plan_request plan_load(const plan_args &a, int r) {
+    plan_request p;
+    p.fresh_tokens = max(a.new_lens[r], 0);
+    p.cached = max(a.cached_lens[r], 0);
+    const int64_t b = a.block_size, have = (p.cached + b - 1) / b, full = (p.cached + p.fresh_tokens + b - 1) / b;
+    p.fits = full <= a.width;
+    p.need = p.fits ? full - have : 0;
+    return p;
+}
+__device__ __forceinline__ int32_t clamp_i32(int64_t x) { return (int32_t)min(x, (int64_t)INT_MAX); }
+__device__ __forceinline__ bool plan_served(const plan_args &a, const plan_request &p, int64_t tokens_to, int64_t blocks_to) {
+    return p.fits && blocks_to <= a.nfree && tokens_to <= a.ntokens;
+}
+
+// Sums of new tokens and needed blocks up to every request, as [nreq + 1] each with 0 in front, by one block; the block
+// that `writes` also writes the results that belong to requests.
+__device__ void plan_sums(const plan_args &a, int32_t *cu, int32_t *blocks, bool writes) {
+    __shared__ int64_t wave_sum[2][PLAN_THREADS / 64];
+    __shared__ int taken;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int64_t carry_t = 0, carry_b = 0;
+    int mine = 0;
+    if (tid == 0) cu[0] = blocks[0] = taken = 0;
+    for (int base = 0; base < a.nreq; base += PLAN_THREADS) {
+        const int r = base + tid;
+        plan_request p = {0, 0, 0, false};
+        if (r < a.nreq) p = plan_load(a, r);
+        int64_t t = p.fresh_tokens, b = p.need;
+        for (int d = 1; d < 64; d *= 2) {
+            const int64_t tt = __shfl_up(t, d), bb = __shfl_up(b, d);
+            if (lane >= d) {
+                t += tt;
+                b += bb;
+            }
+        }
+        if (lane == 63) {
+            wave_sum[0][wave] = t;
+            wave_sum[1][wave] = b;
+        }
+        __syncthreads();
+        t += carry_t;
+        b += carry_b;
+        for (int w = 0; w < PLAN_THREADS / 64; ++w) {
+            const int64_t st = wave_sum[0][w], sb = wave_sum[1][w];
+            if (w < wave) {
+                t += st;
+                b += sb;
+            }
+            carry_t += st;
+            carry_b += sb;
+        }
+        if (r < a.nreq) {
+            cu[r + 1] = clamp_i32(t);
+            blocks[r + 1] = clamp_i32(b);
+            if (writes) {
+                const bool served = plan_served(a, p, t, b);
+                if (a.cu != cu) a.cu[r + 1] = clamp_i32(t);
+                a.kv[r] = served ? (int32_t)(p.cached + p.fresh_tokens) : -1;
+                if (served) mine += (int)p.need;
+            }
+        }
+        __syncthreads();
+    }
+    if (writes) {
+        if (mine) atomicAdd(&taken, mine);   // (whole numbers: the order does not matter)
+        __syncthreads();
+        if (tid == 0) {
+            if (a.cu != cu) a.cu[0] = 0;
+            *a.taken = taken;
+        }
+    }
+    __syncthreads();
+}
+
+__device__ void plan_token(const plan_args &a, const int32_t *cu, const int32_t *blocks, int64_t t) {
+    int32_t position = -1;
+    int64_t slot = -1;
+    if (t < cu[a.nreq]) {
+        int low = 0, high = a.nreq;   // the request with cu[low] <= t < cu[low + 1]
+        while (high - low > 1) {
+            const int mid = (low + high) >> 1;
+            if (cu[mid] <= t) low = mid;
+            else high = mid;
+        }
+        const plan_request p = plan_load(a, low);
+        if (plan_served(a, p, cu[low + 1], blocks[low + 1])) {
+            position = (int32_t)p.cached + (int32_t)(t - cu[low]);
+            const int b = a.block_size, column = position / b, have = (int)((p.cached + b - 1) / b);
+            int32_t *entry = a.tables + (size_t)low * a.width + column;
+            int32_t block;
+            if (column < have) {
+                block = *entry;
+            } else {
+                block = a.free_blocks[blocks[low] + column - have];
+                if (position == column * b) *entry = block;
+            }
+            slot = (int64_t)block * b + position % b;
+        }
+    }
+    a.positions[t] = position;
+    a.slots[t] = slot;
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(plan_args a) {
+    __shared__ int32_t cu[PLAN_MAX + 1], blocks[PLAN_MAX + 1];
+    plan_sums(a, cu, blocks, blockIdx.x == 0);
+    const int64_t step = (int64_t)gridDim.x * PLAN_THREADS;
+    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; t < a.ntokens; t += step) plan_token(a, cu, blocks, t);
+}
+
+// more requests: the sums by one block first, then the tokens
+__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_sums_kernel(plan_args a, int32_t *blocks) { plan_sums(a, a.cu, blocks, true); }
+__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_tokens_kernel(plan_args a, const int32_t *blocks) {
+    const int64_t step = (int64_t)gridDim.x * PLAN_THREADS;
+    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; t < a.ntokens; t += step) plan_token(a, a.cu, blocks, t);
+}
+
+int launch_kv_plan(pq_ctx *ctx, const int32_t *new_lens, const int32_t *cached_lens, int nreq, int32_t *tables, int width,
+                   const int32_t *free_blocks, int nfree, int block_size, int64_t ntokens, int32_t *cu, int32_t *kv,
+                   int32_t *positions, int64_t *slots, int32_t *taken) {
+    const plan_args a = {new_lens, cached_lens, tables, free_blocks, nreq, width, nfree, block_size, ntokens, cu, kv, positions, slots, taken};
+    // one token per thread up to four blocks per compute unit, each of which forms the sums
+    const int64_t wanted = (ntokens + PLAN_THREADS - 1) / PLAN_THREADS;
+    const int grid = (int)(wanted < 1 ? 1 : wanted > 4 * ctx->num_cu ? 4 * ctx->num_cu : wanted);
+    if (nreq <= PLAN_MAX) {
+        kv_plan_kernel<<<grid, PLAN_THREADS, 0, ctx->stream>>>(a);
+    } else {
+        const int rc = buf_reserve(ctx, &ctx->read_ws, ((size_t)nreq + 1) * sizeof(int32_t), "the plan of a paged cache");
+        if (rc) return rc;
+        kv_plan_sums_kernel<<<1, PLAN_THREADS, 0, ctx->stream>>>(a, (int32_t *)ctx->read_ws.p);
+        kv_plan_tokens_kernel<<<grid, PLAN_THREADS, 0, ctx->stream>>>(a, (const int32_t *)ctx->read_ws.p);
+    }
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+// ---- append -----------------------------------------------------------------------------------------
+//
+// A head is held by a group of lanes, each with one unit of 2 V elements: V firsts and V seconds of rotated pairs, or 2 V
+// neighbours of the part that is not rotated.  So a rotation needs no exchange between lanes, only the norm's sum does,
+// and every element is read and written once, 16 bytes at a time where the layout allows it.  Bound by memory.
+struct append_args {
+    pq_heads q, k, v;
+    pq_kv_cache cache;
+    const int32_t *positions;
+    const int64_t *slots;
+    const float *cos_table, *sin_table, *q_weight, *k_weight;
+    void *q_out;
+    int64_t ntokens, max_positions;
+    float eps;
+    int q_heads, rot, norm, rows;   // rows of a token: q_heads + 2 cache.heads
+    int chunks;                     // groups of lanes that share the rows of a token
+};
+
+struct append_row {
+    const void *from;
+    void *to;             // null: nowhere
+    const float *weight;
+    bool turned;          // query or key: norm and rotation
+    bool zero;            // query of a token without a position
+};
+
+template <class T> __device__ __forceinline__ append_row append_locate(const append_args &a, int64_t t, int row, bool placed, int64_t slot) {
+    append_row r;
+    const pq_kv_cache &c = a.cache;
+    if (row < a.q_heads) {
+        r.from = (const T *)a.q.p + t * a.q.token_stride + row * a.q.head_stride;
+        r.to = (T *)a.q_out + (t * a.q_heads + row) * c.dim;
+        r.weight = a.q_weight;
+        r.turned = true;
+        r.zero = !placed;
+        return r;
+    }
+    const bool is_key = row < a.q_heads + c.heads;
+    const int h = row - a.q_heads - (is_key ? 0 : c.heads);
+    const int64_t place = slot % c.block_size, block = slot / c.block_size;
+    const int64_t *strides = is_key ? c.key_strides : c.value_strides;
+    const pq_heads &from = is_key ? a.k : a.v;
+    r.from = (const T *)from.p + t * from.token_stride + h * from.head_stride;
+    r.to = placed && slot >= 0 && block < c.nblocks ? (T *)(is_key ? c.keys : c.values) + block * strides[0] + place * strides[1] + h * strides[2] : nullptr;
+    r.weight = a.k_weight;
+    r.turned = is_key;
+    r.zero = false;
+    return r;
+}
+
+// The places of unit u: element i of the first half at x + i * step, of the second half at y + i * step.
+template <int V, bool PAIRS> struct append_unit {
+    int first, second, angle;   // angle: entry of the rotation tables, -1 in the part that is not rotated
+    __device__ __forceinline__ append_unit(int u, int rot) {
+        const int turned = rot / 2 / V;
+        if (u < turned) {
+            first = PAIRS ? 2 * V * u : V * u;
+            second = PAIRS ? first + V : first + rot / 2;
+            angle = V * u;
+        } else {
+            first = rot + 2 * V * (u - turned);
+            second = first + V;
+            angle = -1;
+        }
+    }
+};
+
+// rotates a unit in place; x, y: its halves as they lie in memory
+template <int V, bool PAIRS> __device__ __forceinline__ void append_turn(float (&x)[V], float (&y)[V], const float (&c)[V], const float (&s)[V]) {
+    if constexpr (!PAIRS) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float a = x[i], b = y[i];
+            x[i] = a * c[i] - b * s[i];
+            y[i] = a * s[i] + b * c[i];
+        }
+    } else {   // pair i: elements 2 i and 2 i + 1 of x followed by y
+        float z[2 * V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            z[i] = x[i];
+            z[V + i] = y[i];
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float a = z[2 * i], b = z[2 * i + 1];
+            z[2 * i] = a * c[i] - b * s[i];
+            z[2 * i + 1] = a * s[i] + b * c[i];
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            x[i] = z[i];
+            y[i] = z[V + i];
+        }
+    }
+}
+
+constexpr int APPEND_THREADS = 256;
+
+// GL lanes per head (a power of two, at least the number of units), ROWS heads of one token one after the other, all of
+// them read before the first is written.
+template <class T, int V, bool PAIRS, int ROWS>
+__global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(append_args a, int gl) {
+    const int64_t group = ((int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x) / gl;
+    const int u = threadIdx.x & (gl - 1), dim = a.cache.dim;
+    const int64_t t = group / a.chunks;
+    if (t >= a.ntokens) return;
+    const int row0 = (int)(group - t * a.chunks) * ROWS;
+    const bool active = u < dim / (2 * V);
+    const append_unit<V, PAIRS> unit(active ? u : 0, a.rot);
+    typedef elem_vec<T, V> vec;
+    typedef elem_vec<float, V> fvec;
+
+    const int32_t p = a.positions[t];
+    const int64_t slot = a.slots[t];
+    const bool placed = p >= 0 && (a.rot == 0 || p < a.max_positions);
+    append_row row[ROWS];
+    vec x[ROWS], y[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        row[i].to = nullptr;
+        if (row0 + i < a.rows) row[i] = append_locate<T>(a, t, row0 + i, placed, slot);
+        if (active && row[i].to) {
+            x[i] = *(const vec *)((const T *)row[i].from + unit.first);
+            y[i] = *(const vec *)((const T *)row[i].from + unit.second);
+        }
+    }
+    fvec c, s;
+    if (active && placed && unit.angle >= 0) {
+        c = *(const fvec *)(a.cos_table + (int64_t)p * (a.rot / 2) + unit.angle);
+        s = *(const fvec *)(a.sin_table + (int64_t)p * (a.rot / 2) + unit.angle);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        // (a group's lanes take every branch here together: to, turned and norm are the row's)
+        if (!row[i].to) continue;
+        if (row[i].turned) {
+            float fx[V], fy[V], sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                fx[e] = active ? (float)x[i].v[e] : 0.f;
+                fy[e] = active ? (float)y[i].v[e] : 0.f;
+                sum += fx[e] * fx[e] + fy[e] * fy[e];
+            }
+            if (a.norm) {
+                for (int d = gl / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+                const float r = 1.f / sqrtf(sum / (float)dim + a.eps);
+                if (active && row[i].weight) {
+                    const fvec wx = *(const fvec *)(row[i].weight + unit.first), wy = *(const fvec *)(row[i].weight + unit.second);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        fx[e] *= r * wx.v[e];
+                        fy[e] *= r * wy.v[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        fx[e] *= r;
+                        fy[e] *= r;
+                    }
+                }
+            }
+            if (active && placed && unit.angle >= 0) append_turn<V, PAIRS>(fx, fy, c.v, s.v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[i].v[e] = (T)(row[i].zero ? 0.f : fx[e]);
+                y[i].v[e] = (T)(row[i].zero ? 0.f : fy[e]);
+            }
+        }
+        if (active) {
+            *(vec *)((T *)row[i].to + unit.first) = x[i];
+            *(vec *)((T *)row[i].to + unit.second) = y[i];
+        }
+    }
+}
+
+// Any even dim and layout: one wave per head, element pairs one at a time, the row read again after the norm.
+template <class T, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void kv_append_general_kernel(append_args a) {
+    const int lane = threadIdx.x & 63, dim = a.cache.dim;
+    const int64_t item = ((int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x) / 64;
+    const int64_t t = item / a.rows;
+    if (t >= a.ntokens) return;
+    const int32_t p = a.positions[t];
+    const bool placed = p >= 0 && (a.rot == 0 || p < a.max_positions);
+    const append_row row = append_locate<T>(a, t, (int)(item - t * a.rows), placed, a.slots[t]);
+    if (!row.to) return;
+    const T *from = (const T *)row.from;
+    T *to = (T *)row.to;
+    float r = 1.f;
+    if (row.turned && a.norm) {
+        float sum = 0.f;
+        for (int i = lane; i < dim; i += 64) sum += (float)from[i] * (float)from[i];
+        for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+        r = 1.f / sqrtf(sum / (float)dim + a.eps);
+    }
+    for (int u = lane; u < dim / 2; u += 64) {
+        const append_unit<1, PAIRS> unit(u, a.rot);
+        if (!row.turned) {
+            to[unit.first] = from[unit.first];
+            to[unit.second] = from[unit.second];
+            continue;
+        }
+        float x[1] = {(float)from[unit.first]}, y[1] = {(float)from[unit.second]};
+        if (a.norm) {
+            x[0] *= r * (row.weight ? row.weight[unit.first] : 1.f);
+            y[0] *= r * (row.weight ? row.weight[unit.second] : 1.f);
+        }
+        if (placed && unit.angle >= 0) {
+            const float c[1] = {a.cos_table[(int64_t)p * (a.rot / 2) + unit.angle]}, s[1] = {a.sin_table[(int64_t)p * (a.rot / 2) + unit.angle]};
+            append_turn<1, PAIRS>(x, y, c, s);
+        }
+        to[unit.first] = (T)(row.zero ? 0.f : x[0]);
+        to[unit.second] = (T)(row.zero ? 0.f : y[0]);
+    }
+}
+
+template <class T, int V, bool PAIRS> static int append_vector(pq_ctx *ctx, append_args &a) {
+    int gl = 1;
+    while (gl < a.cache.dim / (2 * V)) gl *= 2;
+    // four heads per group of lanes once that still gives every compute unit its 32 waves (the loads of four heads are then
+    // in flight together, and the rotation's row is read once for them)
+    const int64_t lanes = a.ntokens * a.rows * gl;
+    const int rows = lanes >= (int64_t)ctx->num_cu * 2048 * 4 ? 4 : 1;
+    a.chunks = (a.rows + rows - 1) / rows;
+    const int64_t grid = (a.ntokens * a.chunks * gl + APPEND_THREADS - 1) / APPEND_THREADS;
+    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
+    if (rows == 4) kv_append_kernel<T, V, PAIRS, 4><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a, gl);
+    else kv_append_kernel<T, V, PAIRS, 1><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a, gl);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+// elements per access that every row's address, the pairs and the rest of the head allow
+static int append_width(const append_args &a, int most) {
+    const pq_kv_cache &c = a.cache;
+    const size_t e = elem_bytes(c.elem);
+    uint64_t bits = (uint64_t)(a.rot / 2) * e | (uint64_t)((c.dim - a.rot) / 2) * e | (uint64_t)(uintptr_t)c.keys | (uint64_t)(uintptr_t)c.values;
+    for (int i = 0; i < 3; ++i) bits |= (uint64_t)c.key_strides[i] * e | (uint64_t)c.value_strides[i] * e;
+    for (const pq_heads *h : {&a.q, &a.k, &a.v})
+        if (h != &a.q || a.q_heads > 0) bits |= (uint64_t)(uintptr_t)h->p | (uint64_t)h->token_stride * e | (uint64_t)h->head_stride * e;
+    if (a.q_heads > 0) bits |= (uint64_t)(uintptr_t)a.q_out | (uint64_t)c.dim * e;
+    // the tables and weights are read by the same number of fp32 elements
+    uint64_t wide = (uint64_t)(uintptr_t)a.q_weight | (uint64_t)(uintptr_t)a.k_weight;
+    if (a.rot > 0) wide |= (uint64_t)(uintptr_t)a.cos_table | (uint64_t)(uintptr_t)a.sin_table | (uint64_t)(a.rot / 2) * 4;
+    int v = most;
+    while (v > 1 && (bits % (v * e) != 0 || wide % (v * 4) != 0)) v /= 2;
+    return v;
+}
+
+template <class T, bool PAIRS> static int append_typed(pq_ctx *ctx, append_args &a) {
+    constexpr int most = 16 / sizeof(T);
+    const int v = append_width(a, most);
+    if (a.cache.dim <= 64 * 2 * v) {   // the units of a head fit a wave
+        if (v == 8 && most == 8) return append_vector<T, most, PAIRS>(ctx, a);
+        if (v >= 4) return append_vector<T, 4, PAIRS>(ctx, a);
+    }
+    const int64_t grid = (a.ntokens * a.rows + APPEND_THREADS / 64 - 1) / (APPEND_THREADS / 64);
+    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
+    kv_append_general_kernel<T, PAIRS><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+int launch_kv_append(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, const pq_heads *k, const pq_heads *v,
+                     int64_t ntokens, const int32_t *positions, const int64_t *slots, const float *cos_table,
+                     const float *sin_table, int64_t max_positions, int rot, int pairs, int norm, const float *q_weight,
+                     const float *k_weight, float eps, void *q_out) {
+    append_args a = {};
+    if (q_heads > 0) a.q = *q;
+    a.k = *k;
+    a.v = *v;
+    a.cache = *cache;
+    a.positions = positions;
+    a.slots = slots;
+    a.cos_table = cos_table;
+    a.sin_table = sin_table;
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.q_out = q_out;
+    a.ntokens = ntokens;
+    a.max_positions = max_positions;
+    a.eps = eps;
+    a.q_heads = q_heads;
+    a.rot = rot;
+    a.norm = norm;
+    a.rows = q_heads + 2 * cache->heads;
+    switch (cache->elem) {
+    case PQ_ELEM_F32: return pairs ? append_typed<float, true>(ctx, a) : append_typed<float, false>(ctx, a);
+    case PQ_ELEM_F16: return pairs ? append_typed<_Float16, true>(ctx, a) : append_typed<_Float16, false>(ctx, a);
+    default: return pairs ? append_typed<__bf16, true>(ctx, a) : append_typed<__bf16, false>(ctx, a);
+    }
+}
+
+}  // namespace pq

@@ -185,6 +185,7 @@ int pq_destroy(pq_ctx *ctx) {
     if (ctx->lut_ws) (void)hipFree(ctx->lut_ws);
     if (ctx->encode_images.p) (void)hipFree(ctx->encode_images.p);
     if (ctx->derived_lists.p) (void)hipFree(ctx->derived_lists.p);
+    if (ctx->read_ws.p) (void)hipFree(ctx->read_ws.p);
     if (ctx->host_pin) (void)hipHostFree(ctx->host_pin);
     if (ctx->aux_stream) {
         (void)hipStreamSynchronize(ctx->aux_stream);

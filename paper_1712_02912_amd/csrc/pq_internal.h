@@ -6,6 +6,7 @@
 
 #include "pq_adc.h"
 #include "pq_adc_bench.h"
+#include "pq_read.h"
 
 // Tuning and test switches (pq_set_option).  PQ_OPT_UNSET = the kernel's own default.
 enum pq_option_id {
@@ -32,6 +33,7 @@ struct pq_ctx {
     // (buffers of their own: a captured Tables step holds the address of lut_ws, which these calls must not move)
     pq_buf encode_images;   // pq_encode: the centroids as matrix operands
     pq_buf derived_lists;   // pq_derived_search: candidate lists, result lists, tables of Step 2
+    pq_buf read_ws;         // the reading step: sums of the plan, parts of the attention and of the draws
     void *host_pin;    // 256 bytes of pinned host memory for the few words a call reads back
     hipStream_t aux_stream;          // ivf_adc_search: work that does not depend on the tables runs beside them
     hipEvent_t aux_fork, aux_join;
@@ -120,5 +122,20 @@ int launch_derived_search(pq_ctx *ctx, const uint16_t *codes16, int64_t n, const
 int launch_ivf(pq_ctx *ctx, const ivf_lists *lists, const float *codebooks, int m, int k, int cf,
                const float *queries, int nq, int nprobe, int topk, float *out_dist, int64_t *out_ids,
                int32_t *probe_out, int init, int kprime);   // (init, kprime: Quick ADC over packed 4-bit codes only)
+
+// The reading step (pq_read.h).
+int launch_kv_plan(pq_ctx *ctx, const int32_t *new_lens, const int32_t *cached_lens, int nreq, int32_t *tables, int width,
+                   const int32_t *free_blocks, int nfree, int block_size, int64_t ntokens, int32_t *cu, int32_t *kv,
+                   int32_t *positions, int64_t *slots, int32_t *taken);
+int launch_kv_append(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, const pq_heads *k, const pq_heads *v,
+                     int64_t ntokens, const int32_t *positions, const int64_t *slots, const float *cos_table,
+                     const float *sin_table, int64_t max_positions, int rot, int pairs, int norm, const float *q_weight,
+                     const float *k_weight, float eps, void *q_out);
+int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
+                        const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width,
+                        int max_new, float scale, int window, void *out, float *lse);
+int launch_sample_tokens(pq_ctx *ctx, const void *logits, int elem, int64_t row_stride, int rows, int vocab, const float *noise,
+                         int64_t noise_stride, const float *temperature, const int32_t *top_k, const float *top_p,
+                         const float *min_p, int64_t *tokens, float *logprobs);
 
 }  // namespace pq

@@ -1,0 +1,533 @@
+"""The reading step (include/pq_read.h) against its oracle in 64 bits, at the sizes, layouts and masks where it can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import read_oracle as orc
+from paper_1712_02912_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+UNIT = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}   # half a unit in the last place, relative
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context(0)
+    yield c
+    torch.cuda.synchronize()
+    c.close()
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def host(t):
+    """Values of a tensor in double (whole numbers as they are)."""
+    return (t.double() if t.is_floating_point() else t).cpu().numpy()
+
+
+# ---- plan -------------------------------------------------------------------------------------------------------------
+def run_plan(ctx, new, cached, tables, free, block_size, ntokens):
+    t = dev(tables.astype(np.int32))
+    out = ctx.pq_kv_plan(dev(new.astype(np.int32)), dev(cached.astype(np.int32)), t, dev(free.astype(np.int32)), block_size, ntokens)
+    return (host(t),) + tuple(host(x) for x in out)
+
+
+def check_plan(ctx, new, cached, width, nfree, block_size, ntokens, seed=0):
+    r = np.random.default_rng(seed)
+    tables = np.full((len(new), width), -1, np.int32)
+    free = r.permutation(10 ** 6)[:nfree].astype(np.int32) + 10 ** 6
+    for i, c in enumerate(cached):
+        n = min(width, -(-max(int(c), 0) // block_size))
+        tables[i, :n] = r.integers(0, 10 ** 6, n)
+    t, cu, kv, positions, slots, taken = orc.plan(new, cached, tables, free, block_size, ntokens)
+    gt, gcu, gkv, gpos, gslots, gtaken = run_plan(ctx, new, cached, tables, free, block_size, ntokens)
+    assert np.array_equal(gcu, cu) and np.array_equal(gkv, kv)
+    assert np.array_equal(gpos, positions) and np.array_equal(gslots, slots)
+    assert np.array_equal(gt, t) and gtaken[0] == taken
+    return kv
+
+
+@pytest.mark.parametrize("nreq", [1, 2, 63, 512, 513, 4096, 4097])
+@pytest.mark.parametrize("block_size", [1, 16, 24])
+def test_plan_of_ragged_requests(ctx, nreq, block_size):
+    r = np.random.default_rng(nreq)
+    new, cached = r.integers(0, 12, nreq), r.integers(0, 70, nreq)
+    check_plan(ctx, new, cached, -(-82 // block_size), 12 * nreq + 1, block_size, int(new.sum()) + 3)
+
+
+@pytest.mark.parametrize("nreq", [5, 700, 5000])
+def test_plan_refuses_what_does_not_fit(ctx, nreq):
+    r = np.random.default_rng(nreq)
+    new, cached = r.integers(0, 40, nreq), r.integers(0, 60, nreq)
+    new[nreq // 3] = 4000                                  # more blocks than the table's row has
+    total = int(new.sum())
+    kv = check_plan(ctx, new, cached, 8, 5 * nreq, 16, total)
+    assert kv[nreq // 3] == -1 and (kv >= 0).sum() > nreq // 3
+    kv = check_plan(ctx, new, cached, 8, nreq // 2, 16, total)       # the free blocks end
+    assert (kv[-2:] == -1).any()
+    check_plan(ctx, new, cached, 8, 0, 16, total)
+    check_plan(ctx, new, cached, 8, 5 * nreq, 16, total // 2)        # the rows end
+
+
+def test_plan_of_odd_lengths(ctx):
+    check_plan(ctx, np.array([-3, 0, 5, 0]), np.array([4, -7, 16, 0]), 4, 9, 16, 9)
+    check_plan(ctx, np.array([2 ** 31 - 1, 2 ** 31 - 1, 1]), np.array([2 ** 31 - 1, 0, 0]), 4, 9, 16, 9)
+    check_plan(ctx, np.array([0]), np.array([0]), 1, 1, 16, 0)
+    empty = np.zeros(0, np.int32)
+    _, cu, _, positions, slots, taken = run_plan(ctx, empty, empty, np.zeros((0, 4), np.int32), np.zeros(2, np.int32), 16, 5)
+    assert cu.tolist() == [0] and taken[0] == 0 and (positions == -1).all() and (slots == -1).all()
+
+
+def test_plan_refusals(ctx):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    lens, table, free = torch.ones(2, **i32), torch.zeros((2, 4), **i32), torch.zeros(9, **i32)
+    with pytest.raises(binding.PqError):
+        ctx.pq_kv_plan(lens, lens, table, free, 0, 4)
+    with pytest.raises(binding.PqError) as e:
+        ctx.pq_kv_plan(lens, lens, table, free, 2 ** 30, 4)
+    assert e.value.code == -3
+    with pytest.raises(ValueError):
+        ctx.pq_kv_plan(lens[:1], lens, table, free, 16, 4)
+    with pytest.raises(TypeError):
+        ctx.pq_kv_plan(lens.long(), lens, table, free, 16, 4)
+    with pytest.raises(ValueError):
+        ctx.pq_kv_plan(lens, lens, torch.zeros((2, 8), **i32)[:, ::2], free, 16, 4)
+
+
+# ---- append -----------------------------------------------------------------------------------------------------------
+def check_append(ctx, tokens, q_heads, heads, dim, rot, pairs, dtype, norm=True, weights=True, layout="packed", block_size=16, eps=1e-6,
+                 seed=0):
+    r = np.random.default_rng(seed)
+    qkv = dev(r.standard_normal((tokens, q_heads + 2 * heads, dim)) * 3, dtype)
+    if layout == "odd":       # rows that begin at odd elements
+        wide = torch.zeros((tokens, q_heads + 2 * heads, dim + 3), dtype=dtype, device="cuda")
+        wide[:, :, 1:dim + 1] = qkv
+        qkv = wide[:, :, 1:dim + 1]
+    q, k, v = qkv[:, :q_heads], qkv[:, q_heads:q_heads + heads], qkv[:, q_heads + heads:]
+    blocks = -(-tokens // block_size) + 1
+    keys, values = (dev(r.standard_normal((blocks, block_size, heads, dim)), dtype) for _ in range(2))
+    if layout == "heads first":
+        keys = keys.transpose(1, 2).contiguous().transpose(1, 2)
+        values = values.transpose(1, 2).contiguous().transpose(1, 2)
+    before = [host(keys), host(values)]
+    positions = r.integers(0, 50, tokens).astype(np.int32)
+    slots = r.permutation(blocks * block_size)[:tokens].astype(np.int64)
+    if tokens >= 6:           # no position, a position behind the tables, no slot, a slot behind the cache
+        positions[1], positions[2], slots[3], slots[4] = -1, 50, -1, blocks * block_size
+    angle = r.uniform(-3, 3, (50, rot // 2))
+    cos, sin = np.cos(angle).astype(np.float32), np.sin(angle).astype(np.float32)
+    qw, kw = (r.uniform(0.5, 2, dim).astype(np.float32) if norm and weights else None for _ in range(2))
+    out = ctx.pq_kv_append(q if q_heads else None, k, v, dev(positions), dev(slots), keys, values, dev(cos) if rot else None,
+                           dev(sin) if rot else None, q_weight=None if qw is None else dev(qw), k_weight=None if kw is None else dev(kw),
+                           eps=eps, norm=norm, pairs=pairs)
+    placed = (positions >= 0) & ((positions < 50) if rot else True)
+    p = np.where(placed, positions, 0)
+    written = placed & (slots >= 0) & (slots < blocks * block_size)
+    u = UNIT[dtype]
+    for x, weight, got in ((q, qw, out), (k, kw, keys)):
+        if x.shape[1] == 0:
+            assert got is None
+            continue
+        want = orc.turn(host(x), p, cos if rot else None, sin if rot else None, weight, eps, norm, pairs)
+        # rounding of the result, and the fp32 steps before it (sum of squares, root, weight, two products and their sum, each in
+        # proportion to the size of a pair, at most twice the larger of the two)
+        size = np.abs(orc.turn(host(x), p, None, None, weight, eps, norm, pairs))
+        size = np.broadcast_to(size.max(axis=2, keepdims=True), size.shape)
+        bound = u * np.abs(want) * 1.01 + (8 + dim / 64) * 2.0 ** -24 * 2 * size + 2.0 ** -25 * (dtype == F16)
+        got = host(got)
+        if got.ndim == 3:
+            want = np.where(placed[:, None, None], want, 0)
+            assert (np.abs(got - want) <= np.where(placed[:, None, None], bound, 0)).all()
+        else:
+            rows = got.reshape(-1, *got.shape[2:])
+            assert (np.abs(rows[slots[written]] - want[written]) <= bound[written]).all()
+            rest = np.setdiff1d(np.arange(blocks * block_size), slots[written])
+            assert np.array_equal(rows[rest], before[0].reshape(rows.shape)[rest])
+    got = host(values).reshape(-1, heads, dim)
+    want = before[1].reshape(got.shape).copy()
+    want[slots[written]] = host(v)[written]
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dim,rot", [(128, 128), (64, 32), (80, 32), (96, 96), (256, 64), (2, 2), (10, 6), (512, 512), (130, 0), (1024, 26)])
+def test_append(ctx, dtype, pairs, dim, rot):
+    check_append(ctx, 37, 5, 2, dim, rot, pairs, dtype, seed=dim)
+
+
+@pytest.mark.parametrize("tokens", [1, 6, 1031, 12000])
+def test_append_of_many_tokens(ctx, tokens):
+    check_append(ctx, tokens, 8, 2, 64, 64, False, BF16, block_size=24, seed=tokens)
+
+
+@pytest.mark.parametrize("layout", ["odd", "heads first"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_append_layouts(ctx, dtype, layout):
+    check_append(ctx, 19, 4, 4, 128, 64, False, dtype, layout=layout)
+
+
+def test_append_without_norm_weights_queries(ctx):
+    check_append(ctx, 19, 4, 2, 64, 64, False, BF16, norm=False)
+    check_append(ctx, 19, 4, 2, 64, 64, True, F32, weights=False)
+    check_append(ctx, 19, 0, 2, 64, 64, False, F16)
+    check_append(ctx, 19, 3, 1, 64, 0, False, F32, norm=False)
+    check_append(ctx, 0, 3, 1, 64, 64, False, F32)
+
+
+def test_append_of_zero_heads_and_large_values(ctx):
+    """A head of zeros stays zero with eps > 0; squares are summed in fp32, so f16 heads of 60000 have a norm."""
+    for dtype, value in ((F16, 0.0), (F16, 60000.0), (BF16, 1e15)):
+        q = torch.full((1, 1, 64), value, dtype=dtype, device="cuda")
+        cache = torch.zeros((1, 4, 1, 64), dtype=dtype, device="cuda")
+        out = ctx.pq_kv_append(q, q, q, torch.zeros(1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int64, device="cuda"),
+                               cache, cache.clone())
+        assert bool((out == (1.0 if value else 0.0)).all()) and bool((cache[0, 1] == out[0]).all())
+
+
+def test_append_refusals(ctx):
+    x = torch.zeros((4, 2, 64), device="cuda")
+    cache = torch.zeros((2, 4, 2, 64), device="cuda")
+    positions, slots = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.arange(4, device="cuda")
+    table = torch.zeros((8, 40), device="cuda")
+    for bad in (dict(cos=table, sin=table), dict(eps=-1.0)):
+        with pytest.raises(binding.PqError):
+            ctx.pq_kv_append(x, x, x, positions, slots, cache, cache, **bad)
+    odd = torch.zeros((4, 2, 63), device="cuda")
+    odd_cache = torch.zeros((2, 4, 2, 63), device="cuda")
+    with pytest.raises(binding.PqError) as e:
+        ctx.pq_kv_append(odd, odd, odd, positions, slots, odd_cache, odd_cache)
+    assert e.value.code == -3
+    with pytest.raises(TypeError):
+        ctx.pq_kv_append(x.half(), x, x, positions, slots, cache, cache)
+    with pytest.raises(ValueError):
+        ctx.pq_kv_append(x, x[:, :1], x, positions, slots, cache, cache)
+    with pytest.raises(ValueError):
+        ctx.pq_kv_append(x, x, x, positions, slots, cache, cache, cos=table)
+    with pytest.raises(ValueError):
+        ctx.pq_kv_append(x, x, x, positions[:3], slots, cache, cache)
+    assert bool((cache == 0).all())
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+def attention_bound(dtype, q, keys, spread, out, scale, most, dim):
+    """Rounding of the result, of the weights to the cache's type, and of the fp32 products, sums and powers: scores are sums of
+    dim products, off by up to dim units of their terms' sizes, and a weight's relative error is its score's absolute one."""
+    u = UNIT[dtype]
+    size = np.abs(q).max() * np.abs(keys[np.isfinite(keys)]).max(initial=0.0) * scale * dim ** 0.5 * 4
+    fp32 = 2.0 ** -24 * (4 * dim ** 0.5 * max(1.0, size) + 64)
+    # (f16 weights below 2^-14 are rounded to multiples of 2^-24)
+    return u * np.abs(out) * 1.01 + (u * (dtype != F32) + fp32) * 2 * spread + (2.0 ** -24 * most if dtype == F16 else 0.0), fp32
+
+
+def make_cache(r, kv, heads, dim, block_size, dtype, fill, layout):
+    """A cache with the requests' blocks in no order; every place that holds no key has `fill`."""
+    counts = [-(-max(k, 0) // block_size) for k in kv]
+    width = max(counts + [1]) + 1
+    total = sum(counts) + 2
+    pool = r.permutation(total).astype(np.int32)
+    tables = np.full((len(kv), width), -1, np.int32)
+    keys, values = (np.full((total, block_size, heads, dim), fill) for _ in range(2))
+    at = 0
+    for i, (k, n) in enumerate(zip(kv, counts)):
+        tables[i, :n] = pool[at:at + n]
+        at += n
+        j = np.arange(max(k, 0))
+        block, place = tables[i, j // block_size], j % block_size
+        keys[block, place] = r.standard_normal((len(j), heads, dim))
+        values[block, place] = r.standard_normal((len(j), heads, dim)) + 0.5
+    keys, values = dev(keys, dtype), dev(values, dtype)
+    if layout == "heads first":
+        keys, values = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (keys, values))
+    elif layout == "side by side":        # keys and values of a place in one row
+        both = torch.stack([keys, values], dim=3)
+        keys, values = both[:, :, :, 0], both[:, :, :, 1]
+    elif layout == "odd":
+        wide = torch.zeros((total, block_size, heads, dim + 1), dtype=dtype, device="cuda")
+        wide[..., 1:] = keys
+        keys = wide[..., 1:]
+    return tables, keys, values
+
+
+def check_attention(ctx, new, kv, q_heads, heads, dim, dtype, block_size=16, window=0, fill=np.nan, layout="plain", gain=1.0, seed=0,
+                    extra=0, scale=None, max_new=None):
+    r = np.random.default_rng(seed)
+    tables, keys, values = make_cache(r, kv, heads, dim, block_size, dtype, fill, layout)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    t = int(cu[-1]) + extra
+    q = dev(r.standard_normal((t, q_heads, dim)) * gain, dtype)
+    if layout == "odd":
+        wide = torch.zeros((t, q_heads, dim + 1), dtype=dtype, device="cuda")
+        wide[..., 1:] = q
+        q = wide[..., 1:]
+    kv = np.array(kv, np.int32)
+    out = torch.full((t, q_heads, dim), 7.0, dtype=dtype, device="cuda")
+    lse = torch.full((t, q_heads), 7.0, device="cuda")
+    ctx.pq_kv_attention(q, keys, values, dev(tables), dev(cu), dev(kv), max(new) if max_new is None else max_new, scale=scale,
+                        window=window, out=out, lse=lse)
+    scale = dim ** -0.5 if scale is None else scale
+    want, want_lse, spread = orc.attention(host(q), host(keys), host(values), tables, cu, kv, scale, window)
+    got, got_lse = host(out), host(lse)
+    end = int(cu[-1])
+    assert (got[end:] == 7).all() and (got_lse[end:] == 7).all()
+    if end == 0:
+        return
+    got, got_lse, want, want_lse, spread = got[:end], got_lse[:end], want[:end], want_lse[:end], spread[:end]
+    empty = np.isneginf(want_lse)
+    assert np.array_equal(empty, np.isneginf(got_lse)) and (got[empty] == 0).all()
+    bound, fp32 = attention_bound(dtype, host(q), host(keys), spread, want, abs(scale), max(1, kv.max()), dim)
+    assert (np.abs(got - want) <= bound).all(), np.abs((got - want) / bound).max()
+    assert (np.abs(got_lse - want_lse)[~empty] <= 2 * fp32 + 1e-6 * np.abs(want_lse[~empty])).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256, 80, 2, 512])
+def test_attention_of_single_tokens(ctx, dtype, dim):
+    check_attention(ctx, [1] * 7, [1, 2, 31, 64, 65, 300, 1], 8, 2, dim, dtype, seed=dim)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256, 80])
+def test_attention_of_chunks(ctx, dtype, dim):
+    check_attention(ctx, [33, 1, 70, 5], [33, 200, 129, 64], 4, 2, dim, dtype, seed=dim)
+
+
+@pytest.mark.parametrize("q_heads,heads", [(1, 1), (3, 3), (6, 2), (7, 1), (16, 2), (24, 1), (40, 1)])
+@pytest.mark.parametrize("new", [1, 2, 3, 19])
+def test_attention_head_layouts(ctx, q_heads, heads, new):
+    check_attention(ctx, [new, 1, new], [new, 90, 150], q_heads, heads, 64, BF16, seed=q_heads + new)
+
+
+@pytest.mark.parametrize("block_size", [1, 3, 8, 16, 24, 64, 100])
+@pytest.mark.parametrize("new", [1, 50])
+def test_attention_pages(ctx, block_size, new):
+    check_attention(ctx, [new, 1, new], [new + 60, 131, new + 190], 4, 2, 128, F16, block_size=block_size, seed=block_size)
+
+
+@pytest.mark.parametrize("window", [1, 2, 17, 64, 65, 200, 100000])
+@pytest.mark.parametrize("new", [1, 90])
+def test_attention_windows(ctx, window, new):
+    check_attention(ctx, [new, 1, new], [new, 131, new + 190], 4, 2, 64, BF16, window=window, seed=window)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_of_rows_that_see_nothing(ctx, new, dtype):
+    """Refused requests, empty ones, and lengths below the number of new tokens, whose first rows see nothing."""
+    check_attention(ctx, [new, new, 0, new, new], [-1, new + 5, 9, 0, new - 1 if new > 1 else 7], 4, 2, 64, dtype, extra=3)
+    check_attention(ctx, [new], [-1], 4, 2, 128, dtype)
+    check_attention(ctx, [0, 0], [5, 0], 4, 2, 128, dtype, extra=2, max_new=1)
+
+
+@pytest.mark.parametrize("layout", ["heads first", "side by side", "odd"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_layouts(ctx, layout, new):
+    check_attention(ctx, [new, 2], [new + 100, 77], 8, 2, 128, BF16, layout=layout)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("fill", [np.nan, np.inf, -60000.0])
+def test_attention_ignores_what_no_row_sees(ctx, new, dtype, fill):
+    check_attention(ctx, [new, new, 1], [new, 33 + new, 1], 4, 1, 128, dtype, block_size=64, fill=fill)
+
+
+@pytest.mark.parametrize("new", [1, 33])
+def test_attention_of_sharp_scores(ctx, new):
+    """Scores of some hundreds: one key takes all the weight, and running maxima jump."""
+    check_attention(ctx, [new, 1], [new + 500, 400], 4, 2, 64, BF16, gain=30.0)
+    check_attention(ctx, [new, 1], [new + 500, 400], 4, 2, 64, F16, gain=30.0)
+    check_attention(ctx, [new, 1], [new + 500, 400], 4, 2, 64, BF16, scale=0.0)
+    check_attention(ctx, [new, 1], [new + 500, 400], 4, 2, 64, BF16, scale=-0.2)
+
+
+@pytest.mark.parametrize("new", [1, 4, 130])
+def test_attention_of_long_contexts(ctx, new):
+    check_attention(ctx, [new, 1, new], [9000 + new, 5000, 301 + new], 4, 1, 128, BF16, block_size=48, seed=new)
+
+
+def test_attention_of_many_requests(ctx):
+    r = np.random.default_rng(5)
+    kv = r.integers(1, 40, 2500)
+    check_attention(ctx, [1] * 2500, kv.tolist(), 2, 1, 64, BF16)
+    new = np.minimum(r.integers(0, 4, 600), 3)
+    check_attention(ctx, new.tolist(), (r.integers(4, 40, 600)).tolist(), 24, 2, 64, BF16)
+
+
+def test_attention_refusals(ctx):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    q, cache = torch.zeros((2, 4, 64), dtype=BF16, device="cuda"), torch.zeros((3, 16, 2, 64), dtype=BF16, device="cuda")
+    table, cu, kv = torch.zeros((2, 1), **i32), torch.tensor([0, 1, 2], **i32), torch.tensor([4, 5], **i32)
+    with pytest.raises(binding.PqError) as e:
+        ctx.pq_kv_attention(q[:, :3], cache, cache, table, cu, kv, 1)
+    assert e.value.code == -2
+    with pytest.raises(binding.PqError):
+        ctx.pq_kv_attention(q, cache, cache, table, cu, kv, 1, window=-1)
+    with pytest.raises(binding.PqError):
+        ctx.pq_kv_attention(q, cache, cache, table, cu, kv, 1, scale=float("nan"))
+    with pytest.raises(binding.PqError):
+        ctx.pq_kv_attention(q, cache, cache, torch.zeros((2, 0), **i32), cu, kv, 1)
+    wide, wide_cache = torch.zeros((2, 4, 514), dtype=BF16, device="cuda"), torch.zeros((3, 16, 2, 514), dtype=BF16, device="cuda")
+    with pytest.raises(binding.PqError) as e:
+        ctx.pq_kv_attention(wide, wide_cache, wide_cache, table, cu, kv, 1)
+    assert e.value.code == -3
+    with pytest.raises(TypeError):
+        ctx.pq_kv_attention(q.half(), cache, cache, table, cu, kv, 1)
+    with pytest.raises(TypeError):
+        ctx.pq_kv_attention(q, cache, cache.half(), table, cu, kv, 1)
+    with pytest.raises(ValueError):
+        ctx.pq_kv_attention(q, cache, cache, table, cu[:2], kv, 1)
+    with pytest.raises(ValueError):
+        ctx.pq_kv_attention(q, cache, cache.transpose(2, 3), table, cu, kv, 1)
+
+
+# ---- draw -------------------------------------------------------------------------------------------------------------
+def check_sample(ctx, logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
+    rows, vocab = logits.shape
+
+    def per_row(values, dtype):
+        return None if values is None else torch.tensor(values, dtype=dtype, device="cuda")
+
+    tokens, logprobs = ctx.pq_sample_tokens(logits, noise, temperature=per_row(temperature, F32), top_k=per_row(top_k, torch.int32),
+                                            top_p=per_row(top_p, F32), min_p=per_row(min_p, F32))
+    tokens, logprobs, l, u = host(tokens), host(logprobs), host(logits), None if noise is None else host(noise)
+    for r in range(rows):
+        args = [np.float64(np.float32(d if v is None else v[r])) for v, d in ((temperature, 1.0), (top_k, 0), (top_p, 1.0), (min_p, 0.0))]
+        token, logprob, scores, margin = orc.sample(l[r], None if u is None else u[r], args[0], int(args[1]), args[2], args[3])
+        if tokens[r] != token:
+            # only where two scores are as near as fp32 rounds them (x and the logarithms: a few units of numbers up to 100)
+            assert tokens[r] in scores and scores[token] - scores[int(tokens[r])] < 2e-5, (r, token, tokens[r])
+            continue
+        # (a limit of top_p passed within the rounding of the weights may take one token more or less along)
+        assert logprobs[r] == logprob or abs(logprobs[r] - logprob) < 2e-6 * (1 + abs(logprob)) + (1e-4 if margin < 1e-6 else 0), (r, logprob, logprobs[r])
+    return tokens
+
+
+def rows_of(r, rows, vocab, dtype, spread=3.0):
+    l = r.standard_normal((rows, vocab)) * spread
+    l[:, r.integers(0, vocab, max(1, vocab // 50))] = -np.inf
+    if vocab > 1:
+        l[:, r.integers(0, vocab)] = 0.5
+    return dev(l, dtype), dev(r.random((rows, vocab)).astype(np.float32).clip(1e-7, 1 - 1e-7))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 1000, 32000, 50021])
+def test_sample_filters_together(ctx, dtype, vocab):
+    r = np.random.default_rng(vocab)
+    logits, noise = rows_of(r, 24, vocab, dtype)
+    pick = lambda *choices: [choices[i] for i in r.integers(0, len(choices), 24)]   # noqa: E731
+    check_sample(ctx, logits, noise, pick(0.0, 0.3, 0.7, 1.0, 2.0), pick(0, 1, 5, 50, 3000, 10 ** 6), pick(0.0, 0.3, 0.9, 0.999, 1.0),
+                 pick(0.0, 0.0, 0.05, 1.0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", [dict(), dict(top_k=40), dict(top_k=20000), dict(top_p=0.95), dict(top_p=1e-9), dict(min_p=0.1),
+                                  dict(top_k=5000, top_p=0.7), dict(temperature=0.01), dict(temperature=50.0, top_p=0.5)])
+def test_sample_one_filter(ctx, dtype, case):
+    r = np.random.default_rng(7)
+    logits, noise = rows_of(r, 9, 40007, dtype, 2.0)
+    check_sample(ctx, logits, noise, **{k: [v] * 9 for k, v in case.items()})
+
+
+@pytest.mark.parametrize("dtype", [F32, F16])
+@pytest.mark.parametrize("case", [dict(), dict(top_k=1), dict(top_k=7777), dict(top_p=0.5), dict(top_p=0.123, top_k=9999), dict(min_p=1.0)])
+def test_sample_of_equal_logits(ctx, dtype, case):
+    """Equal logits, more of them than are sorted at once: those of the smaller indexes stay."""
+    r = np.random.default_rng(8)
+    logits, noise = torch.full((3, 30011), -2.5, dtype=dtype, device="cuda"), dev(r.random((3, 30011)).astype(np.float32))
+    logits[1, ::2] = 1.0
+    logits[2, 100:] = -2.4
+    check_sample(ctx, logits, noise, **{k: [v] * 3 for k, v in case.items()})
+
+
+def test_sample_greedy_and_special_values(ctx):
+    r = np.random.default_rng(9)
+    logits, noise = rows_of(r, 6, 999, F32)
+    logits[0] = -float("inf")
+    logits[1] = float("nan")
+    logits[2, 5], logits[2, 500:503] = float("nan"), float("inf")
+    logits[3, :] = -float("inf")
+    logits[3, 77] = -3e38
+    logits[4] = logits[4].clamp(min=-1)
+    logits[4, [3, 600]] = logits[4].max() + 1
+    tokens = check_sample(ctx, logits, noise, temperature=[0.7] * 6)
+    assert tokens[0] == -1 and tokens[1] == -1 and tokens[2] in (500, 501, 502) and tokens[3] == 77
+    for filters in (dict(top_k=[2] * 6), dict(top_p=[0.6] * 6), dict(min_p=[0.5] * 6)):
+        check_sample(ctx, logits, noise, **filters)
+    tokens = check_sample(ctx, logits, noise, temperature=[0.0] * 6)
+    assert tokens[2] == 500 and tokens[4] == 3
+    check_sample(ctx, logits, None)
+    check_sample(ctx, logits, noise, temperature=[-1.0, 0.0, 1e-38, 1e-30, 3e38, 1e-5])
+
+
+def test_sample_layouts_and_frequencies(ctx):
+    r = np.random.default_rng(10)
+    wide, noise = rows_of(r, 5, 1003, BF16)
+    check_sample(ctx, wide[:, 3:1000], noise[:, 1:998], top_p=[0.9] * 5)
+    check_sample(ctx, wide[::2, :501], noise[::2, :501])
+    # a thousand rows of one distribution: five standard deviations of a share
+    p = np.array([0.5, 0.2, 0.15, 0.1, 0.05])
+    logits = dev(np.log(np.tile(p, (20000, 1))).astype(np.float32))
+    tokens, _ = ctx.pq_sample_tokens(logits, dev(r.random((20000, 5)).astype(np.float32)))
+    share = np.bincount(host(tokens), minlength=5) / 20000
+    assert (np.abs(share - p) < 5 * np.sqrt(p * (1 - p) / 20000)).all()
+
+
+def test_sample_refusals(ctx):
+    l, u = torch.zeros((2, 50), device="cuda"), torch.rand((2, 50), device="cuda")
+    with pytest.raises(TypeError):
+        ctx.pq_sample_tokens(l.double(), u)
+    with pytest.raises(TypeError):
+        ctx.pq_sample_tokens(l, u.half())
+    with pytest.raises(ValueError):
+        ctx.pq_sample_tokens(l, u[:, :49])
+    with pytest.raises(ValueError):
+        ctx.pq_sample_tokens(l, u, top_p=torch.ones(3, device="cuda"))
+    with pytest.raises(binding.PqError) as e:
+        big = torch.zeros((1, 2 ** 21 + 1), device="cuda")
+        ctx.pq_sample_tokens(big, big)
+    assert e.value.code == -3
+    with pytest.raises(binding.PqError):
+        ctx.pq_sample_tokens(torch.zeros((2, 0), device="cuda"), torch.zeros((2, 0), device="cuda"))
+
+
+# ---- together ---------------------------------------------------------------------------------------------------------
+def test_a_captured_step_replays(ctx):
+    """Plan, append, attention and draw in one HIP graph, replayed on new inputs with eager work in between."""
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        c = binding.Context(0, side)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        new, cached = torch.ones(3, **i32), torch.tensor([5, 16, 40], **i32)
+        tables = torch.arange(12, **i32).view(3, 4)
+        free = torch.arange(12, 20, **i32)
+        keys, values = (torch.randn((20, 16, 2, 64), device="cuda").to(BF16) for _ in range(2))
+        qkv = torch.zeros((3, 8, 64), dtype=BF16, device="cuda")
+        noise = torch.zeros((3, 256), device="cuda")
+
+        def step():
+            cu, kv, positions, slots, _ = c.pq_kv_plan(new, cached, tables, free, 16, 3)
+            q = c.pq_kv_append(qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], positions, slots, keys, values)
+            out, lse = c.pq_kv_attention(q, keys, values, tables, cu, kv, 1)
+            return (out, lse) + tuple(c.pq_sample_tokens(out.view(3, 256), noise, top_p=torch.full((3,), 0.9, device="cuda")))
+
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            captured = step()
+        for k in range(4):
+            qkv.copy_(torch.randn((3, 8, 64), device="cuda").to(BF16))
+            noise.copy_(torch.rand((3, 256), device="cuda"))
+            eager = [x.clone() for x in step()]
+            side.synchronize()
+            graph.replay()
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(eager, captured)), k
+        c.close()
