@@ -1,0 +1,101 @@
+// What the attention kernels share (kv_attention_kernels.hip, kv_attention_few.hip, kv_attention_chunk.hip).
+#pragma once
+#include <limits.h>
+
+#include "elem.h"
+#include "pq_internal.h"
+
+namespace pq {
+
+// n / d for 0 <= n < 2^31, as a product
+struct fast_div {
+    uint32_t d, mul, shift;
+    fast_div() = default;
+    explicit fast_div(uint32_t by) : d(by), shift(0) {
+        while (((uint64_t)1 << shift) < by) ++shift;
+        mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - by)) / by + 1);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(mul, n) + n) >> shift; }
+};
+
+struct attention_args {
+    pq_kv_cache cache;
+    pq_heads q;
+    const int32_t *cu, *kv_lens, *tables;
+    void *out;
+    float *lse;
+    int64_t ntokens;
+    int q_heads, nreq, width, window;
+    int group;          // query heads that read one head of the cache
+    fast_div by_block, by_group;
+    float scale_log2;   // scale * log2(e): softmax in powers of two
+};
+
+constexpr float LN2 = 0.6931471805599453f;
+// Reference of a running softmax that has seen no key: below every score, and finite, so that no -inf - -inf is formed.
+constexpr float NO_SCORE = -3e38f;
+
+// Keys of a request as its table can hold them (kv_lens is the caller's: memory is read by it).
+__device__ __forceinline__ int attention_keys(const attention_args &a, int r) { return min(a.kv_lens[r], a.width * a.cache.block_size); }
+
+// Position j of a request as (block, place); blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
+__device__ __forceinline__ void attention_place(const attention_args &a, int r, int j, int64_t &block, int &place) {
+    const int column = (int)a.by_block.div((uint32_t)j);
+    place = j - column * a.cache.block_size;
+    const int32_t b = a.tables[(int64_t)r * a.width + column];
+    block = (unsigned)b < (uint64_t)a.cache.nblocks ? b : 0;
+}
+
+// ---- the matrix cores on 16-bit elements ---------------------------------------------------------------
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));   // eight elements, as they are moved
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct mfma_of;
+template <> struct mfma_of<_Float16> {
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x4 m16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 m32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+};
+template <> struct mfma_of<__bf16> {
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ f32x4 m16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 m32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+};
+
+// four elements of a column: lane 4 r + c of 16 gives the address of part c of row r, lane n gets column n of the four rows
+__device__ __forceinline__ uint2 read_transposed(const void *lds) {
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lds));
+}
+
+template <class T> __device__ __forceinline__ u32x4 pack8(const float *p) {
+    typename mfma_of<T>::v8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (T)p[i];
+    return __builtin_bit_cast(u32x4, v);
+}
+
+// Rows of keys or values in shared memory: bytes from row to row, and the 16-byte chunk of a row that chunk c of row k lies
+// in.  Sixteen rows' equal chunks lie in different banks (rows written by a lane each, columns of keys read), and so do the
+// even pairs of chunks of four rows that one transposing read takes.
+template <int D> struct lds_row {
+    static constexpr int bytes = D <= 64 ? 128 : D <= 128 ? 256 : 512;
+    static __device__ __forceinline__ int chunk(int k, int c) {
+        return c ^ (bytes == 128 ? ((k >> 1) & 3) << 1 | ((k >> 3) & 1) : (k & 7) << 1 | ((k >> 3) & 1));
+    }
+};
+
+int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int max_new);
+int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, int max_new);
+
+}  // namespace pq

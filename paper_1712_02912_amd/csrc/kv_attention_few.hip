@@ -1,0 +1,339 @@
+// Attention of few rows per head of the cache (single tokens, and short chunks): at most 16 rows, which is one tile of the
+// matrix cores.  Bound by memory: every key and value is read once and used for at most 16 rows.
+//
+// Scores are formed transposed, S^T = K Q^T: keys are rows of the first operand, which lanes load straight from the cache, 16
+// bytes each, and a lane holds scores of one row of queries only.  The weights then are the second operand of
+// O^T = V^T P^T as they lie in the registers (the order of the keys within a product is free, so V's keys are read in the
+// order that the scores have).  V^T needs columns of what the cache holds in rows: values go through shared memory, each
+// wave's through its own part, and are read back transposed.
+//
+// Work is cut by what it is, not by request: all keys of all requests and heads form one line of units of 128 keys, and every
+// block takes an equal stretch of it, so contexts of any lengths fill the chip evenly.  A (request, head) that lies
+// within one block is finished there; of others each block leaves a part (maximum, sum, weighted values), and a second kernel
+// joins the parts, always in the same order.
+#include "kv_attention.h"
+
+namespace pq {
+
+constexpr int FEW_ROWS = 16;
+constexpr int FEW_WAVES = 4;
+constexpr int FEW_TILE = 32;                        // keys that a wave takes at a time
+constexpr int FEW_UNIT = FEW_WAVES * FEW_TILE;
+constexpr int FEW_THREADS = 64 * FEW_WAVES;
+constexpr int FEW_MAX = 1024;                       // requests whose line a block adds up in shared memory
+
+struct few_line {
+    const int64_t *starts;   // [nreq + 1] units of one head before each request, where the block does not add them up itself
+    int64_t *starts_out;     // the same, for the kernel that joins the parts
+    float *parts, *stats;    // [blocks][2][rows][D], [blocks][2][rows][2]
+    int blocks;
+};
+
+struct few_range {
+    int fresh, held, keys, from;   // new tokens, those of them that have a row of the queries
+    int64_t units;
+};
+// Keys that the rows of a request see; a request without any that still has rows is one unit (its rows are written).
+__device__ __forceinline__ few_range few_load(const attention_args &a, int r) {
+    few_range x;
+    x.fresh = a.cu[r + 1] - a.cu[r];
+    x.held = (int)min((int64_t)x.fresh, a.ntokens - a.cu[r]);
+    const int kv = a.kv_lens[r];
+    x.keys = max(0, attention_keys(a, r));
+    x.from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - x.fresh - a.window + 1) : 0;
+    x.units = x.held <= 0 ? 0 : max((int64_t)1, ((int64_t)x.keys - x.from + FEW_UNIT - 1) / FEW_UNIT);
+    return x;
+}
+
+// Units of one head before every request, by one block of THREADS; starts: [nreq + 1].
+template <int THREADS> __device__ void few_starts(const attention_args &a, int64_t *starts) {
+    __shared__ int64_t wave_sum[THREADS / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int64_t carry = 0;
+    if (tid == 0) starts[0] = 0;
+    for (int base = 0; base < a.nreq; base += THREADS) {
+        int64_t u = base + tid < a.nreq ? few_load(a, base + tid).units : 0;
+        for (int d = 1; d < 64; d *= 2) {
+            const int64_t v = __shfl_up((long long)u, d);
+            if (lane >= d) u += v;
+        }
+        if (lane == 63) wave_sum[wave] = u;
+        __syncthreads();
+        u += carry;
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < wave) u += wave_sum[w];
+            carry += wave_sum[w];
+        }
+        if (base + tid < a.nreq) starts[base + tid + 1] = u;
+        __syncthreads();
+    }
+}
+__global__ __launch_bounds__(1024) void kv_attention_starts_kernel(attention_args a, int64_t *starts) { few_starts<1024>(a, starts); }
+
+__device__ __forceinline__ int64_t few_begin(int64_t total, int blocks, int b) { return total * b / blocks; }
+
+// where keys and values of a lane's two places of a tile are, in elements
+struct few_places {
+    int64_t k[2], v[2];
+};
+
+template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_attention_few_kernel(attention_args a, few_line line) {
+    typedef lds_row<D> row;
+    constexpr int STEPS = D / 32;   // products over the dimensions
+    constexpr int OUTS = D / 16;    // tiles of the result
+    __shared__ __attribute__((aligned(16))) unsigned char shared[FEW_WAVES][FEW_TILE * row::bytes];
+    static_assert(FEW_TILE * row::bytes >= FEW_ROWS * D * 4, "results of a wave fit its part");
+    __shared__ float stat[FEW_WAVES][FEW_ROWS][2];
+    __shared__ int64_t own_starts[FEW_MAX + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    unsigned char *const mine = shared[wave];
+
+    const int64_t *starts = line.starts;
+    if (!starts) {
+        few_starts<FEW_THREADS>(a, own_starts);
+        starts = own_starts;
+        if (blockIdx.x == 0)
+            for (int i = tid; i <= a.nreq; i += FEW_THREADS) line.starts_out[i] = own_starts[i];
+    }
+    const int heads = a.cache.heads;
+    const int64_t total = starts[a.nreq] * heads;
+    const int64_t begin = few_begin(total, line.blocks, blockIdx.x), end = few_begin(total, line.blocks, blockIdx.x + 1);
+
+    for (int64_t at = begin; at < end;) {
+        // the request and head at this place of the line
+        int low = 0, high = a.nreq;
+        while (high - low > 1) {
+            const int mid = (low + high) >> 1;
+            if (starts[mid] * heads <= at) low = mid;
+            else high = mid;
+        }
+        const int r = low;
+        const few_range x = few_load(a, r);
+        const int64_t in_request = at - starts[r] * heads;
+        const int h = (int)(in_request / x.units);
+        const int64_t first = in_request - h * x.units, count = min(x.units - first, end - at);
+        const bool whole = count == x.units;
+        const int part = at == begin ? 0 : 1;
+        at += count;
+
+        // rows: token n / group, head n % group of the group
+        const int kv = a.kv_lens[r];
+        const int rows = (int)min((int64_t)FEW_ROWS, (int64_t)x.held * a.group);
+        const int token = (int)a.by_group.div((uint32_t)n), sub = n - token * a.group;
+        const int last = kv - x.fresh + token;                                       // the last key that this lane's row sees
+        const int64_t first_seen = a.window > 0 ? (int64_t)last - a.window + 1 : 0;  // and the first
+        const int64_t qrow = a.cu[r] + (n < rows ? token : 0);
+        u32x4 q[STEPS];
+        {
+            const T *p = (const T *)a.q.p + qrow * a.q.token_stride + (h * a.group + (n < rows ? sub : 0)) * a.q.head_stride + 8 * g;
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + 32 * t);
+        }
+        f32x4 out[OUTS];
+#pragma unroll
+        for (int f = 0; f < OUTS; ++f) out[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float ref = NO_SCORE, sum = 0.f;
+
+        const int tile0 = x.from + (int)first * FEW_UNIT + wave * FEW_TILE;   // this wave's first key; the next ones follow by units
+        const int tiles = x.keys > tile0 ? (int)min(count, (int64_t)(x.keys - tile0 + FEW_UNIT - 1) / FEW_UNIT) : 0;
+        const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2] + 8 * g;
+        const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2] + 8 * g;
+        auto places = [&](int i) {
+            few_places p;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                int64_t block;
+                int place;
+                attention_place(a, r, min(tile0 + i * FEW_UNIT + 16 * s + n, x.keys - 1), block, place);
+                p.k[s] = block * a.cache.key_strides[0] + place * a.cache.key_strides[1];
+                p.v[s] = block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
+            }
+            return p;
+        };
+        u32x4 k[2][STEPS], v[2][STEPS];
+        auto load_k = [&](const few_places &p) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) k[s][t] = *(const u32x4 *)(keys + p.k[s] + 32 * t);
+        };
+        auto load_v = [&](const few_places &p) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) v[s][t] = *(const u32x4 *)(values + p.v[s] + 32 * t);
+        };
+        few_places next;
+        if (tiles > 0) {
+            next = places(0);
+            load_k(next);
+            load_v(next);
+            next = places(min(1, tiles - 1));
+        }
+        for (int i = 0; i < tiles; ++i) {
+            const int tile = tile0 + i * FEW_UNIT;
+            f32x4 s[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t) s[j] = mfma_of<T>::m16(k[j][t], q[t], s[j]);
+            }
+            if (i + 1 < tiles) load_k(next);
+            // a lane's scores: keys 16 j + 4 g + e of the tile for row n
+            float p[8], high_score = NO_SCORE;
+            const bool all_seen = tile + FEW_TILE - 1 <= kv - x.fresh && (a.window == 0 || tile >= (int64_t)kv - a.window);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = tile + 16 * j + 4 * g + e;
+                    float y = s[j][e] * a.scale_log2;
+                    if (!all_seen && !(key <= last && key >= first_seen && key < x.keys)) y = -INFINITY;
+                    p[4 * j + e] = y;
+                    high_score = fmaxf(high_score, y);
+                }
+            // The reference of a row moves only when a score passes it by 2^8: weights stay below 256 times their
+            // sum's smallest term, which neither the sums nor the weights' type minds, and nearly no tile scales the results.
+            if (__any(high_score > ref + 8.f)) {
+                high_score = fmaxf(high_score, __shfl_xor(high_score, 16));
+                high_score = fmaxf(high_score, __shfl_xor(high_score, 32));
+                const float moved = fmaxf(ref, high_score), shrink = exp2f(ref - moved);
+                ref = moved;
+                sum *= shrink;
+#pragma unroll
+                for (int f = 0; f < OUTS; ++f) out[f] *= shrink;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+                sum += p[e];
+            }
+            const u32x4 weights = pack8<T>(p);
+            // values: rows of the tile into shared memory, zeros for places that hold no key (they may hold NaN)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const bool held = tile + 16 * j + n < x.keys;
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t)
+                    *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = held ? v[j][t] : u32x4{0, 0, 0, 0};
+            }
+            if (i + 1 < tiles) {
+                load_v(next);
+                next = places(min(i + 2, tiles - 1));
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int f = 0; f < OUTS; ++f) {
+                u32x4 vt;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int key = 16 * j + 4 * g + (n >> 2);
+                    const uint2 c = read_transposed(mine + key * row::bytes + 16 * row::chunk(key, 2 * f + ((n >> 1) & 1)) + 8 * (n & 1));
+                    vt[2 * j] = c.x;
+                    vt[2 * j + 1] = c.y;
+                }
+                out[f] = mfma_of<T>::m16(vt, weights, out[f]);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+
+        // the four waves' results: dimensions 16 f + 4 g + e of row n
+#pragma unroll
+        for (int f = 0; f < OUTS; ++f) *(f32x4 *)(mine + (n * D + 16 * f + 4 * g) * 4) = out[f];
+        if (g == 0) {
+            stat[wave][n][0] = ref;
+            stat[wave][n][1] = sum;
+        }
+        __syncthreads();
+        for (int i = tid; i < rows * D; i += FEW_THREADS) {
+            const int m = i / D, d = i % D;
+            float top = NO_SCORE, all = 0.f, o = 0.f;
+            for (int w = 0; w < FEW_WAVES; ++w) top = fmaxf(top, stat[w][m][0]);
+            for (int w = 0; w < FEW_WAVES; ++w) {
+                const float share = __builtin_amdgcn_exp2f(stat[w][m][0] - top);
+                all += share * stat[w][m][1];
+                o += share * ((const float *)shared[w])[m * D + d];
+            }
+            if (whole) {
+                const int tok = (int)a.by_group.div((uint32_t)m);
+                const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (m - tok * a.group);
+                ((T *)a.out)[at_row * D + d] = (T)(all != 0.f ? o / all : 0.f);
+                if (d == 0 && a.lse) a.lse[at_row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
+            } else {
+                const int64_t at_row = ((int64_t)blockIdx.x * 2 + part) * FEW_ROWS + m;
+                line.parts[at_row * D + d] = o;
+                if (d == 0) {
+                    line.stats[2 * at_row] = top;
+                    line.stats[2 * at_row + 1] = all;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the parts of one row of one (request, head); D threads.
+template <class T, int D> __global__ __launch_bounds__(D) void kv_attention_few_join_kernel(attention_args a, few_line line) {
+    const int heads = a.cache.heads, r = blockIdx.x / heads, h = blockIdx.x - r * heads, m = blockIdx.y, d = threadIdx.x;
+    const int64_t start = line.starts_out[r], units = line.starts_out[r + 1] - start;
+    if (units == 0 || m >= (int64_t)few_load(a, r).held * a.group) return;
+    const int64_t total = line.starts_out[a.nreq] * heads, from = start * heads + h * units, to = from + units;
+    int b = (int)(from * line.blocks / total);   // the block that holds unit `from`
+    while (b > 0 && few_begin(total, line.blocks, b) > from) --b;
+    while (few_begin(total, line.blocks, b + 1) <= from) ++b;
+    if (few_begin(total, line.blocks, b + 1) >= to) return;   // all in one block: done there
+    float top = NO_SCORE, all = 0.f, o = 0.f;
+    for (int64_t begin = few_begin(total, line.blocks, b); begin < to; ++b) {
+        const int64_t end = few_begin(total, line.blocks, b + 1);
+        if (end > begin) {
+            const int64_t row = ((int64_t)b * 2 + (begin >= from ? 0 : 1)) * FEW_ROWS + m;
+            const float ref = line.stats[2 * row], sum = line.stats[2 * row + 1], part = line.parts[row * D + d];
+            const float moved = fmaxf(top, ref), keep = __builtin_amdgcn_exp2f(top - moved), share = __builtin_amdgcn_exp2f(ref - moved);
+            all = all * keep + sum * share;
+            o = o * keep + part * share;
+            top = moved;
+        }
+        begin = end;
+    }
+    const int tok = (int)a.by_group.div((uint32_t)m);
+    const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (m - tok * a.group);
+    ((T *)a.out)[at_row * D + d] = (T)(all != 0.f ? o / all : 0.f);
+    if (d == 0 && a.lse) a.lse[at_row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
+}
+
+template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int max_new) {
+    few_line line = {};
+    line.blocks = ctx->num_cu * (D > 128 ? 1 : 2);
+    const size_t starts = align_up(((size_t)a.nreq + 1) * sizeof(int64_t), 256), slots = (size_t)line.blocks * 2 * FEW_ROWS;
+    if (const int rc = buf_reserve(ctx, &ctx->read_ws, starts + slots * (D + 2) * sizeof(float), "parts of the attention")) return rc;
+    line.starts_out = (int64_t *)ctx->read_ws.p;
+    line.parts = (float *)((char *)ctx->read_ws.p + starts);
+    line.stats = line.parts + slots * D;
+    if (a.nreq > FEW_MAX) {
+        kv_attention_starts_kernel<<<1, 1024, 0, ctx->stream>>>(a, line.starts_out);
+        line.starts = line.starts_out;
+    }
+    kv_attention_few_kernel<T, D><<<line.blocks, FEW_THREADS, 0, ctx->stream>>>(a, line);
+    const int rows = (int)(max_new * (int64_t)a.group < FEW_ROWS ? max_new * a.group : FEW_ROWS);
+    kv_attention_few_join_kernel<T, D><<<dim3(a.nreq * a.cache.heads, rows), D, 0, ctx->stream>>>(a, line);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+template <class T> static int few_dim(pq_ctx *ctx, const attention_args &a, int max_new) {
+    switch (a.cache.dim) {
+    case 64: return few_typed<T, 64>(ctx, a, max_new);
+    case 96: return few_typed<T, 96>(ctx, a, max_new);
+    case 128: return few_typed<T, 128>(ctx, a, max_new);
+    default: return few_typed<T, 256>(ctx, a, max_new);
+    }
+}
+
+int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int max_new) {
+    return a.cache.elem == PQ_ELEM_F16 ? few_dim<_Float16>(ctx, a, max_new) : few_dim<__bf16>(ctx, a, max_new);
+}
+
+}  // namespace pq

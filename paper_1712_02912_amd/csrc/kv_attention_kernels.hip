@@ -1,21 +1,7 @@
 // Attention of new tokens over a paged cache (pq_kv_attention).
-#include <limits.h>
-
-#include "elem.h"
-#include "pq_internal.h"
+#include "kv_attention.h"
 
 namespace pq {
-
-struct attention_args {
-    pq_kv_cache cache;
-    pq_heads q;
-    const int32_t *cu, *kv_lens, *tables;
-    void *out;
-    float *lse;
-    int64_t ntokens;
-    int q_heads, nreq, width, window;
-    float scale_log2;   // scale * log2(e): softmax in powers of two
-};
 
 // The request whose rows hold token t; -1 behind the last one.
 __device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, int64_t t) {
@@ -27,14 +13,6 @@ __device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, in
         else high = mid;
     }
     return low;
-}
-
-// Position j of a request as (block, place); blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
-__device__ __forceinline__ void attention_place(const attention_args &a, int r, int j, int64_t &block, int &place) {
-    const int column = (int)((unsigned)j / (unsigned)a.cache.block_size);
-    place = j - column * a.cache.block_size;
-    const int32_t b = column < a.width ? a.tables[(int64_t)r * a.width + column] : 0;
-    block = (unsigned)b < (uint64_t)a.cache.nblocks ? b : 0;
 }
 
 // ---- any type and layout ------------------------------------------------------------------------------
@@ -52,7 +30,7 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
     const int h = (int)(blockIdx.x - t * a.q_heads), kvh = h / (a.q_heads / a.cache.heads);
     const int r = attention_request(a.cu, a.nreq, t);
     if (r < 0) return;
-    const int kv = a.kv_lens[r], at = kv - (a.cu[r + 1] - (int)t);   // this token's position
+    const int at = min(a.kv_lens[r] - (a.cu[r + 1] - (int)t), attention_keys(a, r) - 1);   // this token's position
     const int from = a.window > 0 ? max(0, at - a.window + 1) : 0;
     const T *qrow = (const T *)a.q.p + t * a.q.token_stride + h * a.q.head_stride;
     for (int i = tid; i < dim; i += 64 * GENERAL_WAVES) q[i] = (float)qrow[i];
@@ -115,6 +93,16 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
     if (tid == 0 && a.lse) a.lse[t * a.q_heads + h] = total != 0.f ? (ref + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
+// rows of 16-bit elements that 16-byte accesses fit, in the dimensions that are built
+static bool attention_on_matrix_cores(const attention_args &a) {
+    const pq_kv_cache &c = a.cache;
+    if (c.elem == PQ_ELEM_F32 || (c.dim != 64 && c.dim != 96 && c.dim != 128 && c.dim != 256)) return false;
+    uint64_t bits = (uint64_t)(uintptr_t)c.keys | (uint64_t)(uintptr_t)c.values | (uint64_t)(uintptr_t)a.q.p | (uint64_t)(uintptr_t)a.out;
+    for (int i = 0; i < 3; ++i) bits |= (uint64_t)(c.key_strides[i] | c.value_strides[i]) * 2;
+    bits |= (uint64_t)(a.q.token_stride | a.q.head_stride) * 2;
+    return bits % 16 == 0;
+}
+
 int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
                         const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width,
                         int max_new, float scale, int window, void *out, float *lse) {
@@ -131,7 +119,13 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
     a.nreq = nreq;
     a.width = width;
     a.window = window;
+    a.group = q_heads / cache->heads;
+    a.by_block = fast_div((uint32_t)cache->block_size);
+    a.by_group = fast_div((uint32_t)a.group);
     a.scale_log2 = scale * 1.4426950408889634f;
+    if (attention_on_matrix_cores(a)) {
+        if ((int64_t)max_new * a.group <= 16) return launch_kv_attention_few(ctx, a, max_new);
+    }
     const int64_t grid = ntokens * q_heads;
     if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
     if (cache->elem == PQ_ELEM_F32) kv_attention_general_kernel<float><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);

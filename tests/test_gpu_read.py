@@ -359,6 +359,23 @@ def test_attention_of_many_requests(ctx):
     check_attention(ctx, new.tolist(), (r.integers(4, 40, 600)).tolist(), 24, 2, 64, BF16)
 
 
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_of_requests_behind_the_rows(ctx, new):
+    """Requests that a plan refused because the rows ended: nothing is written behind the last row."""
+    r = np.random.default_rng(new)
+    tables, keys, values = make_cache(r, [90, 80, 70], 2, 64, 16, BF16, np.nan, "plain")
+    t = new + new // 2
+    q = dev(r.standard_normal((t, 4, 64)), BF16)
+    wide, wide_lse = torch.full((t + 50, 4, 64), 7.0, dtype=BF16, device="cuda"), torch.full((t + 50, 4), 7.0, device="cuda")
+    cu = np.array([0, new, 2 * new, 2 ** 31 - 1], np.int32)
+    ctx.pq_kv_attention(q, keys, values, dev(tables), dev(cu), dev(np.array([90, -1, -1], np.int32)), new, out=wide[:t], lse=wide_lse[:t])
+    want, want_lse, spread = orc.attention(host(q)[:new], host(keys), host(values), tables[:1], cu[:2], np.array([90]), 0.125, 0)
+    bound, fp32 = attention_bound(BF16, host(q), host(keys), spread, want, 0.125, 90, 64)
+    got, lse = host(wide), host(wide_lse)
+    assert (np.abs(got[:new] - want) <= bound).all()
+    assert (got[new:t] == 0).all() and np.isneginf(lse[new:t]).all() and (got[t:] == 7).all() and (lse[t:] == 7).all()
+
+
 def test_attention_refusals(ctx):
     i32 = dict(dtype=torch.int32, device="cuda")
     q, cache = torch.zeros((2, 4, 64), dtype=BF16, device="cuda"), torch.zeros((3, 16, 2, 64), dtype=BF16, device="cuda")
