@@ -1,0 +1,257 @@
+// Attention of chunks of new tokens: bound by the matrix cores.
+//
+// A block holds 32 rows of queries per wave in registers (rows: token, head of the group, so the heads that share keys
+// share them here too) and walks over the keys in tiles of 64, which its waves read from shared memory.  Scores are formed
+// transposed, S^T = K Q^T, so a lane holds scores of one row only, its maximum and sum need no exchange between lanes in most
+// tiles, and the weights are, as they lie, the second operand of O^T = V^T P^T (the order of the keys within a product is
+// free: V's are read in the order that the scores have, transposed by the reads from shared memory).
+//
+// Keys and values go through registers into one of two buffers while the other one is computed on, so one barrier per tile is
+// enough and loads have a tile's time to arrive.  Places that hold no key become zeros on that way.
+#include "kv_attention.h"
+
+namespace pq {
+
+constexpr int CHUNK_TILE = 64;
+
+struct chunk_split {
+    int splits;            // blocks that share the keys of a tile of rows
+    float *parts, *stats;  // [ntokens * q_heads][splits][D], [..][splits][2]
+};
+
+// Tiles of rows: request r owns the indexes from cu[r] * group / M + r on, which leaves it at least as many as it has tiles.
+template <int M> __device__ __forceinline__ int64_t chunk_index(const attention_args &a, int r) { return (int64_t)a.cu[r] * a.group / M + r; }
+
+template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
+    typedef lds_row<D> row;
+    constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
+    constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
+    constexpr int ALL = CHUNK_TILE * CHUNKS, MOVES = (ALL + THREADS - 1) / THREADS;   // chunks of 16 bytes that a thread moves per tile
+    static_assert(ALL % 64 == 0, "whole waves move");
+    __shared__ __attribute__((aligned(16))) unsigned char lds_k[2][CHUNK_TILE * row::bytes], lds_v[2][CHUNK_TILE * row::bytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
+
+    // heads vary fastest: blocks that read the same head's keys are on the same XCD where the heads are a multiple of eight
+    const int heads = a.cache.heads, h = blockIdx.x % heads, part = blockIdx.y;
+    const int64_t index = blockIdx.x / heads;
+    int low = 0, high = a.nreq;
+    while (high - low > 1) {
+        const int mid = (low + high) >> 1;
+        if (chunk_index<M>(a, mid) <= index) low = mid;
+        else high = mid;
+    }
+    const int r = low, fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
+    const int64_t rows = (int64_t)held * a.group, tiles_of_r = (rows + M - 1) / M;
+    // the last rows see the most keys: they come first
+    const int64_t mine = tiles_of_r - 1 - (index - chunk_index<M>(a, r));
+    if (held <= 0 || mine < 0) return;
+
+    const int kv = a.kv_lens[r], nkeys = attention_keys(a, r);
+    // this lane's row
+    const int64_t my_row = mine * M + wave * 32 + n;
+    const bool valid = my_row < rows;
+    const int token = valid ? (int)a.by_group.div((uint32_t)my_row) : 0, sub = valid ? (int)(my_row - (int64_t)token * a.group) : 0;
+    const int last = kv - fresh + token;
+    const int64_t first_seen = a.window > 0 ? (int64_t)last - a.window + 1 : 0;
+    // the keys that the tile's rows see, and those that all of them see
+    const int token0 = (int)a.by_group.div((uint32_t)(mine * M)), token1 = (int)a.by_group.div((uint32_t)(min(rows, (mine + 1) * M) - 1));
+    const int to = min(nkeys, kv - fresh + token1 + 1);
+    const int from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + token0 - a.window + 1) : 0;
+    const int all_from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + token1 - a.window + 1) : 0, all_to = min(nkeys, kv - fresh + token0 + 1);
+    const int tiles_all = to > from ? (to - from + CHUNK_TILE - 1) / CHUNK_TILE : 0;
+    const int tile_begin = (int)((int64_t)tiles_all * part / split.splits), tile_end = (int)((int64_t)tiles_all * (part + 1) / split.splits);
+
+    u32x4 q[STEPS];
+    {
+        const T *p = (const T *)a.q.p + (a.cu[r] + token) * a.q.token_stride + (h * a.group + sub) * a.q.head_stride + 8 * g;
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + 16 * t);
+    }
+    f32x16 out[OUTS];
+#pragma unroll
+    for (int f = 0; f < OUTS; ++f)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) out[f][i] = 0.f;
+    float ref = NO_SCORE, sum = 0.f;
+
+    // this thread's chunks of a tile
+    const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2];
+    const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2];
+    u32x4 mk[MOVES], mv[MOVES];
+    auto load = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < MOVES; ++i) {
+            const int c = tid + THREADS * i, key = c / CHUNKS, chunk = c % CHUNKS;
+            if (ALL % THREADS != 0 && c >= ALL) continue;
+            int64_t block;
+            int place;
+            attention_place(a, r, min(from + tile * CHUNK_TILE + key, to - 1), block, place);
+            mk[i] = *(const u32x4 *)(keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1] + 8 * chunk);
+            mv[i] = *(const u32x4 *)(values + block * a.cache.value_strides[0] + place * a.cache.value_strides[1] + 8 * chunk);
+        }
+    };
+    auto store = [&](int tile, int buffer) {
+#pragma unroll
+        for (int i = 0; i < MOVES; ++i) {
+            const int c = tid + THREADS * i, key = c / CHUNKS, chunk = c % CHUNKS;
+            if (ALL % THREADS != 0 && c >= ALL) continue;
+            const int at = key * row::bytes + 16 * row::chunk(key, chunk);
+            *(u32x4 *)(lds_k[buffer] + at) = mk[i];
+            *(u32x4 *)(lds_v[buffer] + at) = from + tile * CHUNK_TILE + key < to ? mv[i] : u32x4{0, 0, 0, 0};
+        }
+    };
+    if (tile_begin < tile_end) {
+        load(tile_begin);
+        store(tile_begin, 0);
+        if (tile_begin + 1 < tile_end) load(tile_begin + 1);
+    }
+    for (int tile = tile_begin; tile < tile_end; ++tile) {
+        const int buffer = (tile - tile_begin) & 1, key0 = from + tile * CHUNK_TILE;
+        __syncthreads();   // this tile is written, and the one before it read
+        if (tile + 1 < tile_end) store(tile + 1, buffer ^ 1);
+        if (tile + 2 < tile_end) load(tile + 2);
+
+        f32x16 s[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) {
+                const u32x4 k = *(const u32x4 *)(lds_k[buffer] + (32 * j + n) * row::bytes + 16 * row::chunk(32 * j + n, 2 * t + g));
+                s[j] = mfma_of<T>::m32(k, q[t], s[j]);
+            }
+        }
+        // scores of this lane: keys 32 j + 8 (i / 4) + 4 g + i % 4 of the tile
+        float p[32], high_score = NO_SCORE;
+        const bool all_seen = key0 >= all_from && key0 + CHUNK_TILE <= all_to;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[16 * j + i] = s[j][i] * a.scale_log2;
+        if (!all_seen) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = key0 + 32 * j + 8 * (i / 4) + 4 * g + i % 4;
+                    if (!(key <= last && key >= first_seen && key < nkeys)) p[16 * j + i] = -INFINITY;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) high_score = fmaxf(high_score, p[i]);
+        // (the reference moves only when a score passes it by 2^8, see kv_attention_few.hip)
+        if (__any(high_score > ref + 8.f)) {
+            high_score = fmaxf(high_score, __shfl_xor(high_score, 32));
+            const float moved = fmaxf(ref, high_score), shrink = __builtin_amdgcn_exp2f(ref - moved);
+            ref = moved;
+            sum *= shrink;
+#pragma unroll
+            for (int f = 0; f < OUTS; ++f) out[f] *= shrink;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
+            sum += p[i];
+        }
+#pragma unroll
+        for (int b = 0; b < CHUNK_TILE / 16; ++b) {
+            const u32x4 weights = pack8<T>(p + 8 * b);
+#pragma unroll
+            for (int f = 0; f < OUTS; ++f) {
+                u32x4 vt;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int key = 16 * b + 8 * e + 4 * g + ((lane >> 2) & 3), chunk = 4 * f + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+                    const uint2 c = read_transposed(lds_v[buffer] + key * row::bytes + 16 * row::chunk(key, chunk) + 8 * (lane & 1));
+                    vt[2 * e] = c.x;
+                    vt[2 * e + 1] = c.y;
+                }
+                out[f] = mfma_of<T>::m32(vt, weights, out[f]);
+            }
+        }
+    }
+    sum += __shfl_xor(sum, 32);
+    if (!valid) return;
+    const int64_t at_row = (int64_t)(a.cu[r] + token) * a.q_heads + h * a.group + sub;
+    // dimensions 32 f + 8 (i / 4) + 4 g + i % 4 of this lane's row
+    if (split.splits > 1) {
+        const int64_t slot = at_row * split.splits + part;
+#pragma unroll
+        for (int f = 0; f < OUTS; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(f32x4 *)(split.parts + slot * D + 32 * f + 8 * i + 4 * g) = f32x4{out[f][4 * i], out[f][4 * i + 1], out[f][4 * i + 2], out[f][4 * i + 3]};
+        if (g == 0) {
+            split.stats[2 * slot] = ref;
+            split.stats[2 * slot + 1] = sum;
+        }
+        return;
+    }
+    const float scale = sum != 0.f ? 1.f / sum : 0.f;
+    T *const to_row = (T *)a.out + at_row * D;
+#pragma unroll
+    for (int f = 0; f < OUTS; ++f)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            elem_vec<T, 4> v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v.v[e] = (T)(sum != 0.f ? out[f][4 * i + e] * scale : 0.f);
+            *(elem_vec<T, 4> *)(to_row + 32 * f + 8 * i + 4 * g) = v;
+        }
+    if (g == 0 && a.lse) a.lse[at_row] = sum != 0.f ? (ref + log2f(sum)) * LN2 : -INFINITY;
+}
+
+// Joins the parts of a row: D threads per row, in the order of the keys.
+template <class T, int D> __global__ __launch_bounds__(D) void kv_attention_chunk_join_kernel(attention_args a, chunk_split split) {
+    const int64_t row = blockIdx.x;
+    if (row >= (int64_t)a.cu[a.nreq] * a.q_heads) return;
+    float top = NO_SCORE, all = 0.f, o = 0.f;
+    for (int s = 0; s < split.splits; ++s) top = fmaxf(top, split.stats[2 * (row * split.splits + s)]);
+    for (int s = 0; s < split.splits; ++s) {
+        const int64_t slot = row * split.splits + s;
+        const float share = __builtin_amdgcn_exp2f(split.stats[2 * slot] - top);
+        all += share * split.stats[2 * slot + 1];
+        o += share * split.parts[slot * D + threadIdx.x];
+    }
+    ((T *)a.out)[row * D + threadIdx.x] = (T)(all != 0.f ? o / all : 0.f);
+    if (threadIdx.x == 0 && a.lse) a.lse[row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
+}
+
+template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const attention_args &a) {
+    constexpr int M = 32 * WAVES;
+    const int64_t indexes = a.ntokens * a.group / M + a.nreq, rows = a.ntokens * a.q_heads;
+    if (indexes * a.cache.heads > INT_MAX || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
+    // Fewer tiles of rows than twice the compute units: the keys of each are split, down to 512 keys a part.
+    const int64_t tiles = ((a.ntokens * a.group + M - 1) / M) * a.cache.heads;
+    int64_t splits = (2 * ctx->num_cu + tiles - 1) / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
+    if (a.window > 0 && most > (a.window + 511) / 512) most = (a.window + 511) / 512;
+    if (splits > most) splits = most;
+    chunk_split split = {splits < 1 ? 1 : (int)splits, nullptr, nullptr};
+    if (split.splits > 1) {
+        const size_t slots = (size_t)rows * split.splits;
+        if (const int rc = buf_reserve(ctx, &ctx->read_ws, slots * (D + 2) * sizeof(float), "parts of the attention")) return rc;
+        split.parts = (float *)ctx->read_ws.p;
+        split.stats = split.parts + slots * D;
+    }
+    kv_attention_chunk_kernel<T, D, WAVES><<<dim3((unsigned)(indexes * a.cache.heads), split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
+    if (split.splits > 1) kv_attention_chunk_join_kernel<T, D><<<(int)rows, D, 0, ctx->stream>>>(a, split);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+template <class T> static int chunk_dim(pq_ctx *ctx, const attention_args &a) {
+    const bool many = a.ntokens * a.group >= (int64_t)a.nreq * 192;
+    switch (a.cache.dim) {
+    case 64: return many ? chunk_run<T, 64, 8>(ctx, a) : chunk_run<T, 64, 4>(ctx, a);
+    case 96: return many ? chunk_run<T, 96, 8>(ctx, a) : chunk_run<T, 96, 4>(ctx, a);
+    case 128: return many ? chunk_run<T, 128, 8>(ctx, a) : chunk_run<T, 128, 4>(ctx, a);
+    default: return chunk_run<T, 256, 4>(ctx, a);
+    }
+}
+
+int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, int) {
+    return a.cache.elem == PQ_ELEM_F16 ? chunk_dim<_Float16>(ctx, a) : chunk_dim<__bf16>(ctx, a);
+}
+
+}  // namespace pq

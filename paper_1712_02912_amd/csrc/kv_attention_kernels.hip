@@ -125,6 +125,7 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
     a.scale_log2 = scale * 1.4426950408889634f;
     if (attention_on_matrix_cores(a)) {
         if ((int64_t)max_new * a.group <= 16) return launch_kv_attention_few(ctx, a, max_new);
+        return launch_kv_attention_chunk(ctx, a, max_new);
     }
     const int64_t grid = ntokens * q_heads;
     if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
