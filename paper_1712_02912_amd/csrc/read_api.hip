@@ -103,7 +103,7 @@ int pq_sample_tokens(pq_ctx *ctx, const void *logits, pq_elem elem, int64_t row_
     if (!ctx) return PQ_EINVAL;
     if (const int rc = check_elem(ctx, "sample_tokens", elem)) return rc;
     if (rows < 0 || vocab <= 0 || row_stride < 0 || noise_stride < 0) return fail(ctx, PQ_EINVAL, "sample_tokens: bad size");
-    if (vocab > 1 << 21) return fail(ctx, PQ_EUNSUPPORTED, "sample_tokens: vocab=%d above 2^21", vocab);
+    if (vocab >= 1 << 20) return fail(ctx, PQ_EUNSUPPORTED, "sample_tokens: vocab=%d not below 2^20", vocab);
     if (rows == 0) return PQ_OK;
     if (!logits || !tokens) return fail(ctx, PQ_EINVAL, "sample_tokens: null pointer");
     if (!aligned_to(logits, elem_bytes(elem))) return fail(ctx, PQ_EINVAL, "sample_tokens: logits are not aligned to their elements");

@@ -1,10 +1,20 @@
 // The draw of the next tokens (pq_sample_tokens).
 //
 // A row's tokens are ordered by key = (falling logit, index), so what the filters leave is always a beginning of that order
-// and a cut is one key.  The draw itself is a race: the token with the largest x_i - log(-log u_i) among those that stay is
-// a sample of their softmax, and takes one pass without any running sum over the vocabulary, so it does not depend on how
-// sums round.  Weights are summed as whole numbers of 2^-42: the sums, and with them the cuts, do not depend on the order
-// of additions.
+// and a cut is one key.  The draw itself is a race: with weights w_i and e_i = -log u_i the token with the largest w_i / e_i
+// among those that stay is a sample of their softmax.  It takes one pass without a running sum over the vocabulary, so it
+// does not depend on how sums round; and since e_i >= 1 - u_i, a token whose w_i is below (best so far) * (1 - u_i) cannot
+// win, which spares nearly all of them the logarithm.
+//
+// Cuts: one pass puts every token into one of 2048 bins of 1/16 octave of weight, count and weight in one 64-bit word (all
+// weights of a bin have the same power of two, so they add up as whole numbers, in any order to the same sum).  The bin in
+// which a limit is reached is then known, and the next pass collects the tokens of the bins up to it, or of that bin alone
+// where those are too many for the list.  Finer bins of the list end at 64 keys or fewer, which one wave sorts.  Where the
+// list holds all that stay, the draw is from it, else from one more pass over the row.
+//
+// Weights are relative to a logit that a first look at a part of the row has found, not to the largest: so the pass that fills
+// the bins also finds the largest, and the row is read from memory once.  A row whose largest logit lies far above
+// that look is passed over again.
 #include "elem.h"
 #include "pq_internal.h"
 #include "topk_device.h"
@@ -12,11 +22,15 @@
 namespace pq {
 
 constexpr int SAMPLE_THREADS = 1024;
-constexpr int SAMPLE_BINS = 2048;
-constexpr float SAMPLE_BINS_PER_UNIT = 23.5f;   // bins of x: 2048 of them reach down to x = -87, where exp(x) leaves fp32
-constexpr float SAMPLE_LOWEST = -87.f;
-constexpr int SAMPLE_LIST = 2 * SAMPLE_THREADS;   // keys that are sorted
-constexpr double SAMPLE_MASS = 4398046511104.;    // 2^42
+constexpr int SAMPLE_WAVES = SAMPLE_THREADS / 64;
+static_assert(SAMPLE_WAVES == 16, "the waves' results are joined by one row of 16 lanes");
+constexpr int SAMPLE_V = 8;                // tokens that a thread reads at once
+constexpr int SAMPLE_BINS = 2048;          // and one more for what is below them
+constexpr int SAMPLE_ABOVE = 512;          // of them above weight 1: 32 octaves; 96 octaves below
+constexpr int SAMPLE_LIST = 4096;
+constexpr int SAMPLE_COUNT_BIT = 44;       // a bin: count << 44 | weights in 2^-23 of the bin's power of two
+constexpr float SAMPLE_TOP = 48.f;         // octaves above the reference that weights and their sums stay in fp32
+constexpr int SAMPLE_NONE = 0x7fffffff;
 
 struct sample_args {
     const void *logits;
@@ -28,314 +42,496 @@ struct sample_args {
     float *logprobs;
 };
 
-// falling logit, then index: smaller keys come first
-__device__ __forceinline__ uint64_t sample_key(float l, int i) { return (uint64_t)(~f32_to_ord(l)) << 32 | (uint32_t)i; }
+// falling logit, then index: smaller keys come first (both zeros are equal)
+__device__ __forceinline__ uint64_t sample_key(float l, int i) { return (uint64_t)(~f32_to_ord(l + 0.f)) << 32 | (uint32_t)i; }
 __device__ __forceinline__ float sample_key_logit(uint64_t key) { return ord_to_f32(~(uint32_t)(key >> 32)); }
-__device__ __forceinline__ uint64_t sample_mass(float w) { return (uint64_t)((double)w * SAMPLE_MASS); }
 
-// one row's logits, eight at a time; f(index, logit) for each, NaN read as -inf
-template <class T, class F> __device__ __forceinline__ void sample_each(const T *row, int vocab, F f) {
-    constexpr int V = 8;
-    struct __attribute__((packed, aligned(sizeof(T)))) vec { T v[V]; };
-    const int whole = vocab / V * V;
-    for (int i = threadIdx.x * V; i < whole; i += SAMPLE_THREADS * V) {
-        const vec l = *(const vec *)(row + i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float x = (float)l.v[e];
-            f(i + e, x == x ? x : -INFINITY);
-        }
+// ---- sums and minima over a wave and a block -----------------------------------------------------------
+template <int CTRL, int ROWS, class V> __device__ __forceinline__ V from_lane(V none, V v) {
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+    } else {
+        const int2 n = __builtin_bit_cast(int2, none), x = __builtin_bit_cast(int2, v);
+        return __builtin_bit_cast(V, int2{__builtin_amdgcn_update_dpp(n.x, x.x, CTRL, ROWS, 0xf, false),
+                                          __builtin_amdgcn_update_dpp(n.y, x.y, CTRL, ROWS, 0xf, false)});
     }
-    for (int i = whole + threadIdx.x; i < vocab; i += SAMPLE_THREADS) {
-        const float x = (float)row[i];
-        f(i, x == x ? x : -INFINITY);
+}
+template <class V> __device__ __forceinline__ V read_lane(V v, int lane) {
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    } else {
+        const int2 x = __builtin_bit_cast(int2, v);
+        return __builtin_bit_cast(V, int2{__builtin_amdgcn_readlane(x.x, lane), __builtin_amdgcn_readlane(x.y, lane)});
     }
+}
+struct op_add {
+    template <class V> static __device__ __forceinline__ V none() { return V(0); }
+    template <class V> static __device__ __forceinline__ V of(V a, V b) { return a + b; }
+};
+struct op_min_u64 {
+    template <class V> static __device__ __forceinline__ V none() { return KEY_EMPTY; }
+    template <class V> static __device__ __forceinline__ V of(V a, V b) { return min(a, b); }
+};
+// every lane gets what the lanes up to and with it come to, within its row of 16
+template <class OP, class V> __device__ __forceinline__ V row_scan(V v) {
+    v = OP::template of<V>(v, from_lane<0x111, 0xf>(OP::template none<V>(), v));
+    v = OP::template of<V>(v, from_lane<0x112, 0xf>(OP::template none<V>(), v));
+    v = OP::template of<V>(v, from_lane<0x114, 0xf>(OP::template none<V>(), v));
+    return OP::template of<V>(v, from_lane<0x118, 0xf>(OP::template none<V>(), v));
+}
+template <class OP, class V> __device__ __forceinline__ V wave_scan(V v) {
+    v = row_scan<OP>(v);
+    v = OP::template of<V>(v, from_lane<0x142, 0xa>(OP::template none<V>(), v));
+    return OP::template of<V>(v, from_lane<0x143, 0xc>(OP::template none<V>(), v));
 }
 
 struct sample_shared {
-    uint32_t count[SAMPLE_BINS];
-    uint64_t mass[SAMPLE_BINS];
-    uint64_t list[SAMPLE_LIST];
-    uint64_t wave64[SAMPLE_THREADS / 64], wave64b[SAMPLE_THREADS / 64];
-    uint32_t nlist;
+    unsigned long long bins[SAMPLE_BINS + 1], fine[SAMPLE_BINS];
+    unsigned long long list[SAMPLE_LIST], last[64];
+    unsigned long long wave64[2][SAMPLE_WAVES];   // two of each, used in turn: one barrier per use
+    double wave_d[2][SAMPLE_WAVES];
+    uint32_t wave32[2][SAMPLE_WAVES];
+    unsigned long long cut;
+    double mass;
+    uint32_t count, nlist, nlast, best;
     int bin;
-    uint64_t before_count, before_mass, low, high, cut, upto;
 };
 
-// x = (logit - max) / T of a row, and its weight
+// what a limit is reached by: so many tokens, or so much weight
+struct sample_limit {
+    bool by_count;
+    uint32_t count;
+    double mass;
+    __device__ __forceinline__ bool reached(uint32_t c, double m) const { return by_count ? c >= count : m >= mass; }
+};
+
+// Weights of a row's logits, as exponents of two: y = log2(w).
 struct sample_scale {
-    float top, inv;
-    __device__ __forceinline__ float x(float l) const {
-        if (!(l > -INFINITY)) return -INFINITY;
-        return l == top ? 0.f : (l - top) * inv;   // (max +inf: the infinite ones share the weight)
+    float c, at, ref;   // y = l * c + at, rounded once
+    bool far;           // products beyond fp32 (a tiny temperature): differences from the reference decide, one by one
+    __device__ __forceinline__ sample_scale(float reference, float inv_t) {
+        ref = reference;
+        c = fminf(fmaxf(inv_t * 1.4426950408889634f, 1.17549435e-38f), 3.402823466e38f);
+        at = -reference * c;
+        far = !(fabsf(at) < 1e30f);
     }
-    __device__ __forceinline__ float weight(float xv) const { return xv >= SAMPLE_LOWEST ? expf(xv) : 0.f; }
-    __device__ __forceinline__ int bin(float xv) const { return min(SAMPLE_BINS - 1, (int)(-xv * SAMPLE_BINS_PER_UNIT)); }
+    __device__ __forceinline__ float y(float l) const { return far ? (l == ref ? 0.f : (l - ref) * c) : fmaf(l, c, at); }
+    static __device__ __forceinline__ float weight(float y) { return __builtin_amdgcn_exp2f(y); }
 };
+// sixteenths of an octave, from the top; what is below the bins is in bin SAMPLE_BINS
+__device__ __forceinline__ int bin_of(float y) {
+    const int k = (int)fmaxf(floorf(y * 16.f), (float)(SAMPLE_ABOVE - 1 - SAMPLE_BINS));   // (y may be -inf)
+    return max(SAMPLE_ABOVE - 1 - k, 0);
+}
+// a weight within its bin, one unit of the count above it
+__device__ __forceinline__ unsigned long long bin_word(float y) {
+    const uint32_t q = (__float_as_uint(__builtin_amdgcn_exp2f(__builtin_amdgcn_fractf(y))) & 0x7fffffu) | 0x800000u;
+    return (unsigned long long)1 << SAMPLE_COUNT_BIT | q;
+}
+__device__ __forceinline__ uint32_t bin_count(unsigned long long b) { return (uint32_t)(b >> SAMPLE_COUNT_BIT); }
+__device__ __forceinline__ double bin_mass(unsigned long long b, int octave) {
+    // (2^octave by its exponent bits: octaves are -96 ... 31)
+    const double unit = __longlong_as_double((long long)(1023 + octave - 23) << 52);
+    return (double)(b & (((unsigned long long)1 << SAMPLE_COUNT_BIT) - 1)) * unit;
+}
+__device__ __forceinline__ int bin_octave(int bin) { return (SAMPLE_ABOVE - 1 - bin) >> 4; }
 
-__device__ __forceinline__ uint64_t wave_min_u64(uint64_t v) {
-    for (int d = 32; d > 0; d /= 2) v = min(v, (uint64_t)__shfl_xor((unsigned long long)v, d));
-    return v;
-}
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
-    for (int d = 32; d > 0; d /= 2) v += (uint64_t)__shfl_xor((unsigned long long)v, d);
-    return v;
-}
-__device__ uint64_t block_min_u64(sample_shared &sh, uint64_t v) {
-    v = wave_min_u64(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.wave64[threadIdx.x >> 6] = v;
-    __syncthreads();
-    for (int w = 0; w < SAMPLE_THREADS / 64; ++w) v = min(v, sh.wave64[w]);
-    return v;
-}
-__device__ uint64_t block_sum_u64(sample_shared &sh, uint64_t v) {
-    v = wave_sum_u64(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.wave64[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0;
-    for (int w = 0; w < SAMPLE_THREADS / 64; ++w) v += sh.wave64[w];
-    return v;
-}
+template <class T> struct sample_row {
+    const sample_args &a;
+    sample_shared &sh;
+    const T *row;
+    const float *noise;
+    int turn;
 
-// Sums (count, mass) up to and with this thread's entry, in thread order.
-__device__ void block_scan_pair(sample_shared &sh, uint64_t &c, uint64_t &m) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t cc = __shfl_up((unsigned long long)c, d), mm = __shfl_up((unsigned long long)m, d);
-        if (lane >= d) {
-            c += cc;
-            m += mm;
+    // The row's logits: f(first index, logits) for vectors of eight on 16 bytes, two of them on their way at a time, and
+    // g(index, logit) for the few before and behind.  NaN reads as -inf.
+    template <class F, class G> __device__ __forceinline__ void each_vector(int vocab, F f, G g) {
+        struct alignas(16) vec { T v[SAMPLE_V]; };
+        constexpr int STEP = SAMPLE_THREADS * SAMPLE_V;
+        const int before = min(vocab, (int)((16 - ((uintptr_t)row & 15)) % 16 / sizeof(T)));
+        const int whole = before + (vocab - before) / SAMPLE_V * SAMPLE_V;
+        auto take = [&](const vec &l, int i) {
+            float x[SAMPLE_V];
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) x[e] = fmaxf((float)l.v[e], -INFINITY);
+            f(i, x);
+        };
+        int i = before + threadIdx.x * SAMPLE_V;
+        for (; i + STEP < whole; i += 2 * STEP) {
+            const vec p = *(const vec *)(row + i), q = *(const vec *)(row + i + STEP);
+            take(p, i);
+            take(q, i + STEP);
+        }
+        if (i < whole) take(*(const vec *)(row + i), i);
+        const int t = (int)threadIdx.x < before ? threadIdx.x : whole + threadIdx.x - before;
+        if (t < vocab) g(t, fmaxf((float)row[t], -INFINITY));
+    }
+    template <class F> __device__ __forceinline__ void each(int vocab, F f) {
+        each_vector(vocab, [&](int i, const float (&l)[SAMPLE_V]) {
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) f(i + e, l[e]);
+        }, f);
+    }
+
+    __device__ __forceinline__ uint64_t block_min(uint64_t v) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        turn ^= 1;
+        v = wave_scan<op_min_u64>(v);
+        if (lane == 63) sh.wave64[turn][wave] = v;
+        __syncthreads();
+        v = row_scan<op_min_u64>((uint64_t)sh.wave64[turn][lane & 15]);
+        return read_lane(v, 15);
+    }
+    __device__ __forceinline__ double block_sum(double v) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        turn ^= 1;
+        v = wave_scan<op_add>(v);
+        if (lane == 63) sh.wave_d[turn][wave] = v;
+        __syncthreads();
+        v = row_scan<op_add>(sh.wave_d[turn][lane & 15]);
+        return read_lane(v, 15);
+    }
+    // sums of counts and weights up to and with this thread's, in thread order
+    __device__ __forceinline__ void block_scan(uint32_t &c, double &m) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        turn ^= 1;
+        c = wave_scan<op_add>(c);
+        m = wave_scan<op_add>(m);
+        if (lane == 63) {
+            sh.wave32[turn][wave] = c;
+            sh.wave_d[turn][wave] = m;
+        }
+        __syncthreads();
+        const uint32_t cw = row_scan<op_add>(sh.wave32[turn][lane & 15]);
+        const double mw = row_scan<op_add>(sh.wave_d[turn][lane & 15]);
+        if (wave > 0) {
+            c += read_lane(cw, wave - 1);
+            m += read_lane(mw, wave - 1);
         }
     }
-    __syncthreads();
-    if (lane == 63) {
-        sh.wave64[wave] = c;
-        sh.wave64b[wave] = m;
-    }
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) {
-        c += sh.wave64[w];
-        m += sh.wave64b[w];
-    }
-}
 
-// The bin of the histogram in which a limit is reached: the first whose sums, on top of those before the histogram, come to
-// `target` tokens (by_count) or weight.  Sets bin, before_count, before_mass; bin = SAMPLE_BINS if the limit is not reached.
-__device__ void sample_find_bin(sample_shared &sh, bool by_count, uint64_t target) {
-    const int b = 2 * threadIdx.x;
-    const uint64_t c0 = sh.count[b], m0 = sh.mass[b], c1 = sh.count[b + 1], m1 = sh.mass[b + 1];
-    uint64_t c = c0 + c1, m = m0 + m1;
-    block_scan_pair(sh, c, m);
-    const uint64_t bc = sh.before_count, bm = sh.before_mass;
-    __syncthreads();
-    if (threadIdx.x == 0) sh.bin = SAMPLE_BINS;
-    __syncthreads();
-    c += bc;
-    m += bm;
-    const uint64_t at = by_count ? c : m, step1 = by_count ? c1 : m1, step0 = by_count ? c0 : m0;
-    if (at >= target && at - step1 - step0 < target) {
-        const bool second = at - step1 < target;
-        sh.bin = b + second;
-        sh.before_count = c - c1 - (second ? 0 : c0);
-        sh.before_mass = m - m1 - (second ? 0 : m0);
+    __device__ __forceinline__ void done(int64_t token, float logprob) {
+        if (threadIdx.x != 0) return;
+        a.tokens[blockIdx.x] = token;
+        if (a.logprobs) a.logprobs[blockIdx.x] = logprob;
     }
-    __syncthreads();
-}
 
-// Sorts the list's keys (two per thread), smallest first; those behind n are empty.
-__device__ void sample_sort(sample_shared &sh, int n) {
-    for (int i = threadIdx.x; i < SAMPLE_LIST; i += SAMPLE_THREADS)
-        if (i >= n) sh.list[i] = KEY_EMPTY;
-    int size = 2;
-    while (size < n) size *= 2;
-    __syncthreads();
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-            for (int p = threadIdx.x; p < size / 2; p += SAMPLE_THREADS) {
-                const int i = 2 * p - (p & (j - 1)), o = i + j;   // the pair whose members differ in bit j
-                const uint64_t a = sh.list[i], b = sh.list[o];
-                if ((a > b) == ((i & k) == 0)) {
-                    sh.list[i] = b;
-                    sh.list[o] = a;
-                }
+    __device__ __forceinline__ uint64_t first_key(int vocab) {
+        uint64_t first = KEY_EMPTY;
+        each(vocab, [&](int i, float l) { first = min(first, sample_key(l, i)); });
+        return block_min(first);
+    }
+
+    // the best of a thread's race: largest w / e, then smallest index; sh.best: the best of the block so far, as a bound
+    struct race {
+        float best = -1.f;
+        int token = SAMPLE_NONE;
+        __device__ __forceinline__ void enter(float w, float u, int i) {
+            const float r = w / fmaxf(-logf(u), 1e-30f);
+            if (r > best || (r == best && i < token)) {
+                best = r;
+                token = i;
             }
-            __syncthreads();
         }
-}
-
-// The cut at which a limit is reached: the key of the `target`-th token, or that of the token at which the weights reach
-// `target`.  sh.cut is that key and sh.upto the weights up to and with it; all keys and weights if the limit is not reached.
-// The histogram of x is in sh.count, sh.mass.
-template <class T> __device__ void sample_find_cut(sample_shared &sh, const T *row, int vocab, const sample_scale &s, bool by_count, uint64_t target,
-                                                   uint64_t all_mass) {
-    const int tid = threadIdx.x;
-    if (tid == 0) {
-        sh.before_count = sh.before_mass = 0;
-        sh.nlist = 0;
-        sh.cut = KEY_EMPTY;
-        sh.upto = all_mass;
-        sh.low = KEY_EMPTY;
-        sh.high = 0;
-    }
-    __syncthreads();
-    sample_find_bin(sh, by_count, target);
-    const int bin = sh.bin;
-    if (bin >= SAMPLE_BINS) return;
-    uint32_t n = sh.count[bin];
-    uint64_t low = 0, high = KEY_EMPTY;   // the keys of the bin that are still in question
-    if (n > SAMPLE_LIST) {
-        // too many for the list: the bin's range of keys is split into 2048 parts, and the part with the limit again, until the
-        // rest fits (equal logits are told apart by their indexes, so it ends).  The first histogram is needed again: it goes.
-        sample_each(row, vocab, [&](int i, float l) {
-            const float x = s.x(l);
-            if (x >= SAMPLE_LOWEST && s.bin(x) == bin) {
-                const uint64_t key = sample_key(l, i);
-                atomicMin((unsigned long long *)&sh.low, key);
-                atomicMax((unsigned long long *)&sh.high, key);
+        __device__ __forceinline__ void enter_certain(float w, int i) {   // without noise: the largest weight
+            if (w > best || (w == best && i < token)) {
+                best = w;
+                token = i;
             }
+        }
+    };
+    // The race's token, and the log of its share of the weights that stay.
+    __device__ __forceinline__ void finish(const race &x, const sample_scale &s, double mass) {
+        mass = block_sum(mass);
+        uint64_t best = block_min(x.token == SAMPLE_NONE ? KEY_EMPTY : sample_key(x.best, x.token));
+        if (best == KEY_EMPTY) best = first_key(a.vocab);   // (noise that is no number)
+        if (threadIdx.x != 0) return;
+        const int token = (int)(uint32_t)best;
+        done((int64_t)token, (float)((double)s.y((float)row[token]) * 0.6931471805599453 - log(mass)));
+    }
+
+    // Race over the whole row among keys up to `cut` and weights of at least `least`.  Returns false if the reference is too
+    // low for the row's largest logit, `top`.
+    __device__ __forceinline__ bool draw(const sample_scale &s, uint64_t cut, float least, float &top) {
+        struct __attribute__((packed, aligned(4))) noises { float v[SAMPLE_V]; };
+        race best;
+        float high = -INFINITY, sum[SAMPLE_V] = {};
+        const float bound = cut == KEY_EMPTY ? -INFINITY : sample_key_logit(cut);
+        if (threadIdx.x == 0) sh.best = 0;
+        __syncthreads();
+        auto weight = [&](int i, float l) {   // 0: does not stay
+            const float w = s.weight(s.y(l));
+            return l >= bound && l > -INFINITY && w >= least && !(l == bound && sample_key(l, i) > cut) ? w : 0.f;
+        };
+        each_vector(a.vocab, [&](int i, const float (&l)[SAMPLE_V]) {
+            float w[SAMPLE_V], any = 0.f;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) {
+                high = fmaxf(high, l[e]);
+                w[e] = weight(i + e, l[e]);
+                sum[e] += w[e];
+                any += w[e];
+            }
+            if (!(any > 0.f)) return;
+            if (!noise) {
+#pragma unroll
+                for (int e = 0; e < SAMPLE_V; ++e)
+                    if (w[e] > 0.f) best.enter_certain(w[e], i + e);
+                return;
+            }
+            const noises u = *(const noises *)(noise + i);
+            const float so_far = __uint_as_float(__hip_atomic_load(&sh.best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+            bool wins = false;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) wins |= w[e] > 0.f && w[e] >= so_far * (1.f - u.v[e]);
+            if (!wins) return;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e)
+                if (w[e] > 0.f && w[e] >= so_far * (1.f - u.v[e])) best.enter(w[e], u.v[e], i + e);
+            if (best.best > so_far) atomicMax(&sh.best, __float_as_uint(best.best));
+        }, [&](int i, float l) {
+            high = fmaxf(high, l);
+            const float w = weight(i, l);
+            sum[0] += w;
+            if (!(w > 0.f)) return;
+            if (noise) best.enter(w, noise[i], i);
+            else best.enter_certain(w, i);
+        });
+        top = sample_key_logit(block_min(sample_key(high, 0)));
+        if (!(s.y(top) <= SAMPLE_TOP)) return false;
+        double mass = 0.;
+#pragma unroll
+        for (int e = 0; e < SAMPLE_V; ++e) mass += (double)sum[e];
+        finish(best, s, mass);
+        return true;
+    }
+
+    // Bins of the whole row.  Returns false if a weight lies above them; top: the largest logit.
+    __device__ __forceinline__ bool fill_bins(const sample_scale &s, float &top) {
+        for (int b = threadIdx.x; b <= SAMPLE_BINS; b += SAMPLE_THREADS) sh.bins[b] = 0;
+        __syncthreads();
+        float high = -INFINITY;
+        each(a.vocab, [&](int, float l) {
+            high = fmaxf(high, l);
+            const float y = s.y(l);
+            const int b = bin_of(y);
+            if (b < SAMPLE_BINS) atomicAdd(&sh.bins[b], bin_word(y));
+        });
+        top = sample_key_logit(block_min(sample_key(high, 0)));
+        return s.y(top) < (float)(SAMPLE_ABOVE / 16);
+    }
+
+    // The bin in which a limit is reached, counting from c, m before the bins: the bin (SAMPLE_BINS: it is not reached), and
+    // in c, m the sums before it.  octave(bin): the power of two of a bin's weights.
+    template <class O> __device__ __forceinline__ int find_bin(const unsigned long long *bins, const sample_limit &limit, uint32_t &c0, double &m0, O octave) {
+        const int b = 2 * threadIdx.x;
+        const unsigned long long v0 = bins[b], v1 = bins[b + 1];
+        const double w0 = bin_mass(v0, octave(b)), w1 = bin_mass(v1, octave(b + 1));
+        uint32_t c = bin_count(v0) + bin_count(v1);
+        double m = w0 + w1;
+        if (threadIdx.x == 0) sh.bin = SAMPLE_BINS;
+        block_scan(c, m);   // (its barrier comes before the minimum)
+        c += c0;
+        m += m0;
+        // (an empty bin reaches nothing, so rounding of the sums cannot name one)
+        if (bin_count(v0) && limit.reached(c - bin_count(v1), m - w1)) atomicMin(&sh.bin, b);
+        else if (bin_count(v1) && limit.reached(c, m)) atomicMin(&sh.bin, b + 1);
+        __syncthreads();
+        const int found = sh.bin;
+        if (found >> 1 == (int)threadIdx.x && found < SAMPLE_BINS) {
+            sh.count = c - bin_count(v1) - (found & 1 ? 0 : bin_count(v0));
+            sh.mass = m - w1 - (found & 1 ? 0. : w0);
+        }
+        __syncthreads();
+        if (found < SAMPLE_BINS) {
+            c0 = sh.count;
+            m0 = sh.mass;
+        }
+        return found;
+    }
+
+    // Adds the tokens of bins first ... last with keys low ... high to the list (there is room); returns their number.
+    __device__ __forceinline__ int collect(const sample_scale &s, int first, int last, uint64_t low, uint64_t high) {
+        if (threadIdx.x == 0) sh.nlist = 0;
+        __syncthreads();
+        const float lowest = (float)(SAMPLE_ABOVE - 1 - last) * 0.0625f, highest = first == 0 ? INFINITY : (float)(SAMPLE_ABOVE - first) * 0.0625f;
+        each(a.vocab, [&](int i, float l) {
+            const float y = s.y(l);
+            if (!(y >= lowest && y < highest)) return;
+            const uint64_t key = sample_key(l, i);
+            if (key >= low && key <= high) sh.list[atomicAdd(&sh.nlist, 1u)] = key;
         });
         __syncthreads();
-        low = sh.low;
-        high = sh.high;
-        uint32_t keep_count[2];
-        uint64_t keep_mass[2];
-        for (int e = 0; e < 2; ++e) {
-            keep_count[e] = sh.count[2 * tid + e];
-            keep_mass[e] = sh.mass[2 * tid + e];
-        }
-        while (n > SAMPLE_LIST) {
+        return (int)sh.nlist;
+    }
+
+    // The key in `bin` at which a limit is reached on top of c, m; the weight up to and with it in m.  The bin's keys are split
+    // into 2048 parts, the part with the limit again, until 64 or fewer are left (equal logits are told apart by their
+    // indexes, so it ends), which a wave sorts.  They come from the list of `listed` keys, or, where the bin has too many for
+    // it (listed < 0), from the row until the rest fits.
+    __device__ __forceinline__ uint64_t find_cut(const sample_scale &s, int bin, int listed, sample_limit limit, uint32_t c, double &m) {
+        const int tid = threadIdx.x, octave = bin_octave(bin);
+        auto in_bin = [&](float y) { return bin_of(y) == bin; };
+        auto from_list = [&](auto f) {
+            for (int i = tid; i < listed; i += SAMPLE_THREADS) {
+                const uint64_t key = sh.list[i];
+                const float y = s.y(sample_key_logit(key));
+                if (in_bin(y)) f(key, y);
+            }
+        };
+        auto from_row = [&](auto f) {
+            each(a.vocab, [&](int i, float l) {
+                const float y = s.y(l);
+                if (in_bin(y)) f(sample_key(l, i), y);
+            });
+        };
+        uint64_t lo = KEY_EMPTY, hi = 0;
+        auto range = [&](uint64_t key, float) {
+            lo = min(lo, key);
+            hi = max(hi, key);
+        };
+        if (listed >= 0) from_list(range);
+        else from_row(range);
+        uint64_t low = block_min(lo), high = ~block_min(~hi);
+        for (uint32_t n = bin_count(sh.bins[bin]); n > 64;) {
             int shift = 0;
             while ((high - low) >> shift >= SAMPLE_BINS) ++shift;
             __syncthreads();
-            for (int e = 0; e < 2; ++e) sh.count[2 * tid + e] = 0, sh.mass[2 * tid + e] = 0;
+            for (int b = tid; b < SAMPLE_BINS; b += SAMPLE_THREADS) sh.fine[b] = 0;
             __syncthreads();
-            sample_each(row, vocab, [&](int i, float l) {
-                const uint64_t key = sample_key(l, i);
-                const float x = s.x(l);
-                if (key < low || key > high || !(x >= SAMPLE_LOWEST) || s.bin(x) != bin) return;
-                const int part = (int)((key - low) >> shift);
-                atomicAdd(&sh.count[part], 1u);
-                atomicAdd((unsigned long long *)&sh.mass[part], (unsigned long long)sample_mass(s.weight(x)));
-            });
+            auto add = [&](uint64_t key, float y) {
+                if (key >= low && key <= high) atomicAdd(&sh.fine[(key - low) >> shift], bin_word(y));
+            };
+            if (listed >= 0) from_list(add);
+            else from_row(add);
             __syncthreads();
-            sample_find_bin(sh, by_count, target);
-            const uint64_t part = sh.bin;
-            n = sh.count[part];
-            low += part << shift;
+            const int part = find_bin(sh.fine, limit, c, m, [&](int) { return octave; });
+            if (part >= SAMPLE_BINS) {   // (reached by the sums of the bins, but not by these, which round differently)
+                limit.mass *= 1. - 1e-12;
+                continue;
+            }
+            n = bin_count(sh.fine[part]);
+            low += (uint64_t)part << shift;
             high = min(high, low + ((uint64_t)1 << shift) - 1);
+            if (listed < 0 && n <= SAMPLE_LIST) listed = collect(s, bin, bin, low, high);
+        }
+        if (listed < 0) listed = collect(s, bin, bin, low, high);   // (never: such a bin has more keys than the list)
+        if (tid == 0) sh.nlast = 0;
+        if (tid < 64) sh.last[tid] = KEY_EMPTY;
+        __syncthreads();
+        from_list([&](uint64_t key, float) {
+            if (key >= low && key <= high) sh.last[atomicAdd(&sh.nlast, 1u)] = key;
+        });
+        __syncthreads();
+        if (tid < 64) {
+            const int n = (int)sh.nlast;
+            const uint64_t mine = sh.last[tid];
+            int rank = 0;
+            for (int i = 0; i < n; ++i) rank += read_lane(mine, i) < mine;
+            __builtin_amdgcn_wave_barrier();
+            if (tid < n) sh.last[rank] = mine;
+            __builtin_amdgcn_wave_barrier();
+            const uint64_t key = sh.last[tid];
+            const double w = tid < n ? (double)s.weight(s.y(sample_key_logit(key))) : 0.;
+            const double upto = wave_scan<op_add>(w) + m;
+            const uint64_t there = __ballot(tid < n && limit.reached(c + tid + 1, upto));
+            const int at = there ? __ffsll((unsigned long long)there) - 1 : n - 1;   // (not reached: rounding, the last one)
+            if (tid == at) {
+                sh.cut = key;
+                sh.mass = upto;
+            }
         }
         __syncthreads();
-        for (int e = 0; e < 2; ++e) {
-            sh.count[2 * tid + e] = keep_count[e];
-            sh.mass[2 * tid + e] = keep_mass[e];
+        m = sh.mass;
+        const uint64_t cut = sh.cut;
+        return cut;
+    }
+
+    __device__ __forceinline__ void run() {
+        const int tid = threadIdx.x, r = blockIdx.x;
+        const float t = a.temperature ? a.temperature[r] : 1.f;
+        const int64_t top_k = a.top_k ? a.top_k[r] : 0;
+        const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
+        const bool greedy = !(t > 0.f) || min_p > 1.f;   // (the first token alone stays)
+        const bool by_k = top_k > 0 && top_k < a.vocab, by_p = top_p < 1.f;
+
+        // the reference: the largest of a part of the row, or of all of it where that is needed anyway
+        float ref = -INFINITY;
+        if (!greedy && !(min_p > 0.f && !by_k && !by_p))
+            ref = sample_key_logit(first_key(min(a.vocab, SAMPLE_THREADS * SAMPLE_V)));
+        if (!(ref > -INFINITY)) {
+            const uint64_t first = first_key(a.vocab);
+            ref = sample_key_logit(first);
+            if (!(ref > -INFINITY)) return done(-1, -INFINITY);
+            if (greedy) return done((int64_t)(uint32_t)first, 0.f);
         }
-        __syncthreads();
+        const float inv = 1.f / t;
+        float top;
+        if (!by_k && !by_p) {
+            // (with min_p the reference is the largest logit; its weight is 1 up to the rounding of y)
+            sample_scale s(ref, inv);
+            const float least = min_p > 0.f ? min_p * s.weight(s.y(ref)) : 0.f;
+            if (!draw(s, KEY_EMPTY, least, top)) draw(sample_scale(top, inv), KEY_EMPTY, least, top);
+            return;
+        }
+        if (!fill_bins(sample_scale(ref, inv), top)) {
+            ref = top;
+            fill_bins(sample_scale(ref, inv), top);
+        }
+        const sample_scale s(ref, inv);
+        const float least = min_p > 0.f ? min_p * s.weight(s.y(top)) : 0.f;
+
+        // Each limit in turn: its bin, the list if it is not there, its cut.
+        double all = block_sum(bin_mass(sh.bins[2 * tid], bin_octave(2 * tid)) + bin_mass(sh.bins[2 * tid + 1], bin_octave(2 * tid + 1)));
+        uint64_t cut = KEY_EMPTY;
+        int listed = 0;                       // > 0: the list holds the tokens of all bins up to `complete`
+        int complete = -1;
+        for (int step = 0; step < 2; ++step) {
+            if (step == 0 ? !by_k : !by_p) continue;
+            sample_limit limit;
+            limit.by_count = step == 0;
+            limit.count = (uint32_t)top_k;
+            limit.mass = (double)fmaxf(top_p, 0.f) * all;   // a token stays while the weights before it are below: up to the one that reaches it
+            uint32_t c = 0;
+            double m = 0.;
+            const int bin = find_bin(sh.bins, limit, c, m, bin_octave);
+            if (bin >= SAMPLE_BINS) continue;   // not reached: all stay
+            int have = listed;
+            if (bin > complete) {
+                const uint32_t n = bin_count(sh.bins[bin]);
+                const bool fits = c + n <= SAMPLE_LIST;
+                have = n > SAMPLE_LIST ? -1 : collect(s, fits ? 0 : bin, bin, 0, KEY_EMPTY);
+                listed = fits ? have : 0;
+                complete = fits ? bin : -1;
+            }
+            cut = min(cut, find_cut(s, bin, have, limit, c, m));
+            all = m;
+        }
+        if (complete < 0) {
+            draw(s, cut, least, top);
+            return;
+        }
+        // the race on the list
+        race best;
+        double mass = 0.;
+        for (int i = tid; i < listed; i += SAMPLE_THREADS) {
+            const uint64_t key = sh.list[i];
+            const float w = s.weight(s.y(sample_key_logit(key)));
+            const int token = (int)(uint32_t)key;
+            if (key > cut || !(w > 0.f) || w < least) continue;
+            mass += (double)w;
+            if (noise) best.enter(w, noise[token], token);
+            else best.enter_certain(w, token);
+        }
+        finish(best, s, mass);
     }
-    sample_each(row, vocab, [&](int i, float l) {
-        const uint64_t key = sample_key(l, i);
-        const float x = s.x(l);
-        if (key < low || key > high || !(x >= SAMPLE_LOWEST) || s.bin(x) != bin) return;
-        sh.list[atomicAdd(&sh.nlist, 1u)] = key;
-    });
-    __syncthreads();
-    sample_sort(sh, (int)n);
-    const uint64_t k0 = sh.list[2 * tid], k1 = sh.list[2 * tid + 1];
-    const uint64_t m0 = k0 == KEY_EMPTY ? 0 : sample_mass(s.weight(s.x(sample_key_logit(k0))));
-    const uint64_t m1 = k1 == KEY_EMPTY ? 0 : sample_mass(s.weight(s.x(sample_key_logit(k1))));
-    uint64_t c = (k0 != KEY_EMPTY) + (k1 != KEY_EMPTY), m = m0 + m1;
-    block_scan_pair(sh, c, m);
-    c += sh.before_count;
-    m += sh.before_mass;
-    const uint64_t at = by_count ? c : m, step1 = by_count ? k1 != KEY_EMPTY : m1, step0 = by_count ? k0 != KEY_EMPTY : m0;
-    if (at >= target && at - step1 - step0 < target) {
-        const bool second = at - step1 < target;
-        sh.cut = second ? k1 : k0;
-        sh.upto = second ? m : m - m1;
-    }
-    __syncthreads();
-}
+};
 
 template <class T> __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(sample_args a) {
     __shared__ sample_shared sh;
-    const int r = blockIdx.x, tid = threadIdx.x;
-    const T *row = (const T *)a.logits + r * a.row_stride;
-    const float *noise = a.noise ? a.noise + r * a.noise_stride : nullptr;
-
-    uint64_t first = KEY_EMPTY;
-    sample_each(row, a.vocab, [&](int i, float l) { first = min(first, sample_key(l, i)); });
-    first = block_min_u64(sh, first);
-    sample_scale s;
-    s.top = sample_key_logit(first);
-    const float t = a.temperature ? a.temperature[r] : 1.f;
-    if (!(s.top > -INFINITY)) {
-        if (tid == 0) {
-            a.tokens[r] = -1;
-            if (a.logprobs) a.logprobs[r] = -INFINITY;
-        }
-        return;
-    }
-    const bool greedy = !(t > 0.f);
-    if (greedy && (tid == 0)) {
-        a.tokens[r] = (int64_t)(uint32_t)first;
-        if (a.logprobs) a.logprobs[r] = 0.f;
-    }
-    if (greedy) return;
-    s.inv = fminf(1.f / t, 3.402823466e38f);
-    const int64_t top_k = a.top_k ? a.top_k[r] : 0;
-    const float top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
-    const bool by_k = top_k > 0 && top_k < a.vocab, by_p = top_p < 1.f;
-
-    uint64_t cut = KEY_EMPTY;
-    if (by_k || by_p) {
-        for (int b = tid; b < SAMPLE_BINS; b += SAMPLE_THREADS) sh.count[b] = 0, sh.mass[b] = 0;
-        __syncthreads();
-        sample_each(row, a.vocab, [&](int, float l) {
-            const float x = s.x(l);
-            if (!(x >= SAMPLE_LOWEST)) return;
-            const int b = s.bin(x);
-            atomicAdd(&sh.count[b], 1u);
-            atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)sample_mass(s.weight(x)));
-        });
-        __syncthreads();
-        uint64_t all = block_sum_u64(sh, sh.mass[2 * tid] + sh.mass[2 * tid + 1]);
-        if (by_k) {
-            sample_find_cut(sh, row, a.vocab, s, true, (uint64_t)top_k, all);
-            cut = sh.cut;
-            all = sh.upto;
-            __syncthreads();
-        }
-        if (by_p) {
-            // a token stays while the weights before it are below top_p * all: up to the one that reaches the next whole number
-            const double limit = ceil(fmax(0., (double)top_p) * (double)all);
-            sample_find_cut(sh, row, a.vocab, s, false, max((uint64_t)1, (uint64_t)limit), all);
-            cut = min(cut, sh.cut);
-        }
-    }
-
-    // the race among the keys up to the cut: the largest score, then the smallest index
-    uint64_t best = KEY_EMPTY, mass = 0;
-    float drawn = 0.f;
-    sample_each(row, a.vocab, [&](int i, float l) {
-        const uint64_t key = sample_key(l, i);
-        if (key > cut) return;
-        const float x = s.x(l);
-        const float w = s.weight(x);
-        if (!(w > 0.f) || (w < min_p && key != first)) return;
-        mass += sample_mass(w);
-        const float score = noise ? x - logf(-logf(noise[i])) : x;
-        best = min(best, sample_key(score, i));
-    });
-    // (a score that is NaN, from noise outside 0 ... 1, sorts behind or before the others: some token is drawn all the same)
-    const uint64_t all_best = block_min_u64(sh, best);
-    mass = block_sum_u64(sh, mass);
-    const int token = (int)(uint32_t)all_best;
-    if (tid == 0) {
-        a.tokens[r] = token;
-        drawn = s.x((float)row[token]);
-        if (a.logprobs) a.logprobs[r] = (float)((double)drawn - log((double)mass / SAMPLE_MASS));
-    }
+    const int64_t r = blockIdx.x;
+    sample_row<T> row = {a, sh, (const T *)a.logits + r * a.row_stride, a.noise ? a.noise + r * a.noise_stride : nullptr, 0};
+    row.run();
 }
 
 int launch_sample_tokens(pq_ctx *ctx, const void *logits, int elem, int64_t row_stride, int rows, int vocab, const float *noise,

@@ -507,7 +507,7 @@ def test_sample_refusals(ctx):
     with pytest.raises(ValueError):
         ctx.pq_sample_tokens(l, u, top_p=torch.ones(3, device="cuda"))
     with pytest.raises(binding.PqError) as e:
-        big = torch.zeros((1, 2 ** 21 + 1), device="cuda")
+        big = torch.zeros((1, 2 ** 20), device="cuda")
         ctx.pq_sample_tokens(big, big)
     assert e.value.code == -3
     with pytest.raises(binding.PqError):
