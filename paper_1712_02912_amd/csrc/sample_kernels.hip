@@ -25,7 +25,7 @@ constexpr int SAMPLE_THREADS = 1024;
 constexpr int SAMPLE_WAVES = SAMPLE_THREADS / 64;
 static_assert(SAMPLE_WAVES == 16, "the waves' results are joined by one row of 16 lanes");
 constexpr int SAMPLE_V = 8;                // tokens that a thread reads at once
-constexpr int SAMPLE_BINS = 2048;          // and one more for what is below them
+constexpr int SAMPLE_BINS = 2048;          // and one more for what is below them (SAMPLE_FLOOR)
 constexpr int SAMPLE_ABOVE = 512;          // of them above weight 1: 32 octaves; 96 octaves below
 constexpr int SAMPLE_LIST = 4096;
 constexpr int SAMPLE_COUNT_BIT = 44;       // a bin: count << 44 | weights in 2^-23 of the bin's power of two
@@ -72,6 +72,10 @@ struct op_min_u64 {
     template <class V> static __device__ __forceinline__ V none() { return KEY_EMPTY; }
     template <class V> static __device__ __forceinline__ V of(V a, V b) { return min(a, b); }
 };
+struct op_max {
+    template <class V> static __device__ __forceinline__ V none() { return -INFINITY; }
+    template <class V> static __device__ __forceinline__ V of(V a, V b) { return fmaxf(a, b); }
+};
 // every lane gets what the lanes up to and with it come to, within its row of 16
 template <class OP, class V> __device__ __forceinline__ V row_scan(V v) {
     v = OP::template of<V>(v, from_lane<0x111, 0xf>(OP::template none<V>(), v));
@@ -105,23 +109,25 @@ struct sample_limit {
     __device__ __forceinline__ bool reached(uint32_t c, double m) const { return by_count ? c >= count : m >= mass; }
 };
 
-// Weights of a row's logits, as exponents of two: y = log2(w).
+// Weights of a row's logits, as exponents of two: y = log2(w).  What is far below the bins is cut off there, so is what is no
+// number (the middle of three is the smallest then), and what is above them at SAMPLE_CAP.
+constexpr float SAMPLE_FLOOR = -100.f, SAMPLE_CAP = 1e30f;
 struct sample_scale {
-    float c, at, ref;   // y = l * c + at, rounded once
-    bool far;           // products beyond fp32 (a tiny temperature): differences from the reference decide, one by one
+    float c, ref, low, high;   // y = c * (l - ref), the difference within low ... high
     __device__ __forceinline__ sample_scale(float reference, float inv_t) {
-        ref = reference;
-        c = fminf(fmaxf(inv_t * 1.4426950408889634f, 1.17549435e-38f), 3.402823466e38f);
-        at = -reference * c;
-        far = !(fabsf(at) < 1e30f);
+        ref = fminf(reference, 3.402823466e38f);
+        c = fminf(fmaxf(inv_t * 1.4426950408889634f, 1e-36f), 1e36f);
+        low = SAMPLE_FLOOR / c;
+        high = reference < INFINITY ? fminf(SAMPLE_CAP / c, 3.402823466e38f) : 0.f;   // (+inf and the largest number share the weight)
     }
-    __device__ __forceinline__ float y(float l) const { return far ? (l == ref ? 0.f : (l - ref) * c) : fmaf(l, c, at); }
+    __device__ __forceinline__ float y(float l) const { return __builtin_amdgcn_fmed3f(l - ref, low, high) * c; }
     static __device__ __forceinline__ float weight(float y) { return __builtin_amdgcn_exp2f(y); }
 };
-// sixteenths of an octave, from the top; what is below the bins is in bin SAMPLE_BINS
+// Bins are sixteenths of an octave, in the order of falling weight; bin SAMPLE_BINS is what lies below.
 __device__ __forceinline__ int bin_of(float y) {
-    const int k = (int)fmaxf(floorf(y * 16.f), (float)(SAMPLE_ABOVE - 1 - SAMPLE_BINS));   // (y may be -inf)
-    return max(SAMPLE_ABOVE - 1 - k, 0);
+    int k;   // floor
+    asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(k) : "v"(y * 16.f));
+    return max(SAMPLE_ABOVE - 1 - max(k, SAMPLE_ABOVE - 1 - SAMPLE_BINS), 0);
 }
 // a weight within its bin, one unit of the count above it
 __device__ __forceinline__ unsigned long long bin_word(float y) {
@@ -143,31 +149,46 @@ template <class T> struct sample_row {
     const float *noise;
     int turn;
 
-    // The row's logits: f(first index, logits) for vectors of eight on 16 bytes, two of them on their way at a time, and
-    // g(index, logit) for the few before and behind.  NaN reads as -inf.
-    template <class F, class G> __device__ __forceinline__ void each_vector(int vocab, F f, G g) {
-        struct alignas(16) vec { T v[SAMPLE_V]; };
-        constexpr int STEP = SAMPLE_THREADS * SAMPLE_V;
-        const int before = min(vocab, (int)((16 - ((uintptr_t)row & 15)) % 16 / sizeof(T)));
-        const int whole = before + (vocab - before) / SAMPLE_V * SAMPLE_V;
+    // The row as vectors of eight on 16 bytes and the few logits before and behind them.  A thread keeps its vector of the
+    // first 1024 in registers (the first look; empty places hold -inf) until the pass over the rest.
+    struct alignas(16) vec { T v[SAMPLE_V]; };
+    static constexpr int STEP = SAMPLE_THREADS * SAMPLE_V;
+    int before, whole;      // vectors are at before ... whole
+    float look[SAMPLE_V];
+    __device__ __forceinline__ void load_look() {
+        before = min(a.vocab, (int)((16 - ((uintptr_t)row & 15)) % 16 / sizeof(T)));
+        whole = before + (a.vocab - before) / SAMPLE_V * SAMPLE_V;
+        const int i = before + threadIdx.x * SAMPLE_V;
+        if (i < whole) {
+            const vec l = *(const vec *)(row + i);
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) look[e] = (float)l.v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) look[e] = -INFINITY;
+        }
+    }
+    // f(first index, logits) for the vectors, g(index, logit) for the few others; two vectors are on their way at a time.
+    // `rest`: without the first look.
+    template <class F, class G> __device__ __forceinline__ void each_vector(bool rest, F f, G g) {
         auto take = [&](const vec &l, int i) {
             float x[SAMPLE_V];
 #pragma unroll
-            for (int e = 0; e < SAMPLE_V; ++e) x[e] = fmaxf((float)l.v[e], -INFINITY);
+            for (int e = 0; e < SAMPLE_V; ++e) x[e] = (float)l.v[e];
             f(i, x);
         };
-        int i = before + threadIdx.x * SAMPLE_V;
+        int i = before + threadIdx.x * SAMPLE_V + (rest ? STEP : 0);
         for (; i + STEP < whole; i += 2 * STEP) {
             const vec p = *(const vec *)(row + i), q = *(const vec *)(row + i + STEP);
             take(p, i);
             take(q, i + STEP);
         }
         if (i < whole) take(*(const vec *)(row + i), i);
-        const int t = (int)threadIdx.x < before ? threadIdx.x : whole + threadIdx.x - before;
-        if (t < vocab) g(t, fmaxf((float)row[t], -INFINITY));
+        const int t = (int)threadIdx.x < before ? (int)threadIdx.x : whole + (int)threadIdx.x - before;
+        if (t < a.vocab) g(t, (float)row[t]);
     }
-    template <class F> __device__ __forceinline__ void each(int vocab, F f) {
-        each_vector(vocab, [&](int i, const float (&l)[SAMPLE_V]) {
+    template <class F> __device__ __forceinline__ void each(F f) {
+        each_vector(false, [&](int i, const float (&l)[SAMPLE_V]) {
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) f(i + e, l[e]);
         }, f);
@@ -182,6 +203,15 @@ template <class T> struct sample_row {
         v = row_scan<op_min_u64>((uint64_t)sh.wave64[turn][lane & 15]);
         return read_lane(v, 15);
     }
+    __device__ __forceinline__ float block_max(float v) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        turn ^= 1;
+        v = wave_scan<op_max>(v);
+        if (lane == 63) sh.wave32[turn][wave] = __float_as_uint(v);
+        __syncthreads();
+        v = row_scan<op_max>(__uint_as_float(sh.wave32[turn][lane & 15]));
+        return read_lane(v, 15);
+    }
     __device__ __forceinline__ double block_sum(double v) {
         const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
         turn ^= 1;
@@ -191,38 +221,19 @@ template <class T> struct sample_row {
         v = row_scan<op_add>(sh.wave_d[turn][lane & 15]);
         return read_lane(v, 15);
     }
-    // sums of counts and weights up to and with this thread's, in thread order
-    __device__ __forceinline__ void block_scan(uint32_t &c, double &m) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-        turn ^= 1;
-        c = wave_scan<op_add>(c);
-        m = wave_scan<op_add>(m);
-        if (lane == 63) {
-            sh.wave32[turn][wave] = c;
-            sh.wave_d[turn][wave] = m;
-        }
-        __syncthreads();
-        const uint32_t cw = row_scan<op_add>(sh.wave32[turn][lane & 15]);
-        const double mw = row_scan<op_add>(sh.wave_d[turn][lane & 15]);
-        if (wave > 0) {
-            c += read_lane(cw, wave - 1);
-            m += read_lane(mw, wave - 1);
-        }
-    }
-
     __device__ __forceinline__ void done(int64_t token, float logprob) {
         if (threadIdx.x != 0) return;
         a.tokens[blockIdx.x] = token;
         if (a.logprobs) a.logprobs[blockIdx.x] = logprob;
     }
 
-    __device__ __forceinline__ uint64_t first_key(int vocab) {
+    __device__ __forceinline__ uint64_t first_key() {
         uint64_t first = KEY_EMPTY;
-        each(vocab, [&](int i, float l) { first = min(first, sample_key(l, i)); });
+        each([&](int i, float l) { first = min(first, sample_key(fmaxf(l, -INFINITY), i)); });   // (NaN reads as -inf)
         return block_min(first);
     }
 
-    // the best of a thread's race: largest w / e, then smallest index; sh.best: the best of the block so far, as a bound
+    // the best of a thread's race: largest w / e, then smallest index
     struct race {
         float best = -1.f;
         int token = SAMPLE_NONE;
@@ -244,61 +255,79 @@ template <class T> struct sample_row {
     __device__ __forceinline__ void finish(const race &x, const sample_scale &s, double mass) {
         mass = block_sum(mass);
         uint64_t best = block_min(x.token == SAMPLE_NONE ? KEY_EMPTY : sample_key(x.best, x.token));
-        if (best == KEY_EMPTY) best = first_key(a.vocab);   // (noise that is no number)
+        if (best == KEY_EMPTY) best = first_key();   // (noise that is no number)
         if (threadIdx.x != 0) return;
         const int token = (int)(uint32_t)best;
-        done((int64_t)token, (float)((double)s.y((float)row[token]) * 0.6931471805599453 - log(mass)));
+        const float octaves = (float)__builtin_amdgcn_frexp_exp(mass);
+        done((int64_t)token, (s.y((float)row[token]) - octaves - log2f((float)__builtin_amdgcn_frexp_mant(mass))) * 0.6931471805599453f);
     }
 
     // Race over the whole row among keys up to `cut` and weights of at least `least`.  Returns false if the reference is too
-    // low for the row's largest logit, `top`.
-    __device__ __forceinline__ bool draw(const sample_scale &s, uint64_t cut, float least, float &top) {
+    // low for the row's largest logit.
+    // A bound on the winner, w / e, is found first, on the first look: e = -log u is at most (1 - u) / u.
+    __device__ __forceinline__ bool draw(const sample_scale &s, uint64_t cut, float least) {
         struct __attribute__((packed, aligned(4))) noises { float v[SAMPLE_V]; };
         race best;
         float high = -INFINITY, sum[SAMPLE_V] = {};
-        const float bound = cut == KEY_EMPTY ? -INFINITY : sample_key_logit(cut);
-        if (threadIdx.x == 0) sh.best = 0;
-        __syncthreads();
-        auto weight = [&](int i, float l) {   // 0: does not stay
-            const float w = s.weight(s.y(l));
-            return l >= bound && l > -INFINITY && w >= least && !(l == bound && sample_key(l, i) > cut) ? w : 0.f;
+        const bool all_stay = cut == KEY_EMPTY;   // (but for weights below least): noise is read beside the logits, not after them
+        const float bound = all_stay ? -INFINITY : sample_key_logit(cut);
+        least = fmaxf(least, 1e-30f);             // (what is cut off at SAMPLE_FLOOR does not stay)
+        auto weight = [&](int i, float l, float y) {   // 0: does not stay
+            const float w = s.weight(y);
+            if (all_stay) return w >= least ? w : 0.f;
+            return w >= least && (l > bound || (l == bound && sample_key(l, i) <= cut)) ? w : 0.f;
         };
-        each_vector(a.vocab, [&](int i, const float (&l)[SAMPLE_V]) {
-            float w[SAMPLE_V], any = 0.f;
+        float bounded = 0.f;
+        if (noise) {
+            const int i = before + threadIdx.x * SAMPLE_V;
+            if (i < whole) {
+                const noises u = *(const noises *)(noise + i);
+#pragma unroll
+                for (int e = 0; e < SAMPLE_V; ++e) bounded = fmaxf(bounded, weight(i + e, look[e], s.y(look[e])) * u.v[e] * __builtin_amdgcn_rcpf(1.f - u.v[e]));
+            }
+            bounded = block_max(bounded) * (1.f - 1e-6f);   // (rounded down)
+            if (threadIdx.x == 0) sh.best = __float_as_uint(bounded < INFINITY ? bounded : 0.f);
+            __syncthreads();
+        }
+        each_vector(false, [&](int i, const float (&l)[SAMPLE_V]) {
+            noises u;
+            if (noise && all_stay) u = *(const noises *)(noise + i);
+            float w[SAMPLE_V], most = 0.f;
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) {
-                high = fmaxf(high, l[e]);
-                w[e] = weight(i + e, l[e]);
+                const float y = s.y(l[e]);
+                high = fmaxf(high, y);
+                w[e] = weight(i + e, l[e], y);
                 sum[e] += w[e];
-                any += w[e];
+                most = fmaxf(most, w[e]);
             }
-            if (!(any > 0.f)) return;
+            if (!(most > 0.f)) return;
             if (!noise) {
 #pragma unroll
                 for (int e = 0; e < SAMPLE_V; ++e)
                     if (w[e] > 0.f) best.enter_certain(w[e], i + e);
                 return;
             }
-            const noises u = *(const noises *)(noise + i);
+            if (!all_stay) u = *(const noises *)(noise + i);
             const float so_far = __uint_as_float(__hip_atomic_load(&sh.best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
             bool wins = false;
 #pragma unroll
-            for (int e = 0; e < SAMPLE_V; ++e) wins |= w[e] > 0.f && w[e] >= so_far * (1.f - u.v[e]);
+            for (int e = 0; e < SAMPLE_V; ++e) wins |= w[e] >= so_far * (1.f - u.v[e]);   // (weights of 0 are sorted out below)
             if (!wins) return;
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e)
                 if (w[e] > 0.f && w[e] >= so_far * (1.f - u.v[e])) best.enter(w[e], u.v[e], i + e);
             if (best.best > so_far) atomicMax(&sh.best, __float_as_uint(best.best));
         }, [&](int i, float l) {
-            high = fmaxf(high, l);
-            const float w = weight(i, l);
+            const float y = s.y(l);
+            high = fmaxf(high, y);
+            const float w = weight(i, l, y);
             sum[0] += w;
             if (!(w > 0.f)) return;
             if (noise) best.enter(w, noise[i], i);
             else best.enter_certain(w, i);
         });
-        top = sample_key_logit(block_min(sample_key(high, 0)));
-        if (!(s.y(top) <= SAMPLE_TOP)) return false;
+        if (!(block_max(high) <= SAMPLE_TOP)) return false;
         double mass = 0.;
 #pragma unroll
         for (int e = 0; e < SAMPLE_V; ++e) mass += (double)sum[e];
@@ -306,48 +335,117 @@ template <class T> struct sample_row {
         return true;
     }
 
-    // Bins of the whole row.  Returns false if a weight lies above them; top: the largest logit.
-    __device__ __forceinline__ bool fill_bins(const sample_scale &s, float &top) {
-        for (int b = threadIdx.x; b <= SAMPLE_BINS; b += SAMPLE_THREADS) sh.bins[b] = 0;
+    // Bins of the whole row; top: the largest y, which has to lie below them.  The bins of the first look at the row say from
+    // which bin on about `wanted` tokens are to be expected, and these go into the list on the way: listed = the last bin that
+    // the list then holds with all before it, -1 if they were too many.
+    __device__ __forceinline__ void fill_bins(const sample_scale &s, uint32_t wanted, float &top, int &listed) {
+        const int tid = threadIdx.x;
+        for (int b = tid; b <= SAMPLE_BINS; b += SAMPLE_THREADS) sh.bins[b] = 0;
+        if (tid == 0) sh.nlist = 0;
         __syncthreads();
         float high = -INFINITY;
-        each(a.vocab, [&](int, float l) {
-            high = fmaxf(high, l);
+        const int first = before + tid * SAMPLE_V;
+        if (first < whole) {
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) {
+                const float y = s.y(look[e]);
+                high = fmaxf(high, y);
+                atomicAdd(&sh.bins[bin_of(y)], bin_word(y));
+            }
+        }
+        __syncthreads();
+        uint32_t c = 0;
+        double m = 0.;
+        wanted = max(1u, (uint32_t)((float)wanted * (float)min(whole - before, STEP) / (float)a.vocab));
+        const int last = min(find_bin(sh.bins, sample_limit{true, wanted, 0.}, c, m, bin_octave), SAMPLE_BINS - 1);
+        const float lowest = (float)(SAMPLE_ABOVE - 1 - last) * 0.0625f;
+        auto list = [&](int i, const float (&y)[SAMPLE_V], float most) {   // (indexes first, in the place of the keys)
+            if (!(most >= lowest)) return;
+            uint32_t which = 0;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) which |= (uint32_t)(y[e] >= lowest) << e;
+            for (; which; which &= which - 1) {
+                const uint32_t at = atomicAdd(&sh.nlist, 1u);
+                if (at < SAMPLE_LIST) sh.list[at] = (uint32_t)(i + __ffs(which) - 1);
+            }
+        };
+        if (first < whole) {
+            float y[SAMPLE_V], most = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) most = fmaxf(most, y[e] = s.y(look[e]));
+            list(first, y, most);
+        }
+        each_vector(true, [&](int i, const float (&l)[SAMPLE_V]) {
+            float y[SAMPLE_V], most = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) {
+                y[e] = s.y(l[e]);
+                most = fmaxf(most, y[e]);
+                atomicAdd(&sh.bins[bin_of(y[e])], bin_word(y[e]));
+            }
+            high = fmaxf(high, most);
+            list(i, y, most);
+        }, [&](int i, float l) {
             const float y = s.y(l);
-            const int b = bin_of(y);
-            if (b < SAMPLE_BINS) atomicAdd(&sh.bins[b], bin_word(y));
+            high = fmaxf(high, y);
+            atomicAdd(&sh.bins[bin_of(y)], bin_word(y));
+            if (y >= lowest) {
+                const uint32_t at = atomicAdd(&sh.nlist, 1u);
+                if (at < SAMPLE_LIST) sh.list[at] = (uint32_t)i;
+            }
         });
-        top = sample_key_logit(block_min(sample_key(high, 0)));
-        return s.y(top) < (float)(SAMPLE_ABOVE / 16);
+        top = block_max(high);
+        const uint32_t n = min(sh.nlist, (uint32_t)SAMPLE_LIST);
+        for (uint32_t i = tid; i < n; i += SAMPLE_THREADS) {
+            const int at = (int)sh.list[i];
+            sh.list[i] = sample_key((float)row[at], at);
+        }
+        listed = sh.nlist <= SAMPLE_LIST ? last : -1;
+        __syncthreads();
     }
 
     // The bin in which a limit is reached, counting from c, m before the bins: the bin (SAMPLE_BINS: it is not reached), and
     // in c, m the sums before it.  octave(bin): the power of two of a bin's weights.
     template <class O> __device__ __forceinline__ int find_bin(const unsigned long long *bins, const sample_limit &limit, uint32_t &c0, double &m0, O octave) {
-        const int b = 2 * threadIdx.x;
+        const int b = 2 * threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
         const unsigned long long v0 = bins[b], v1 = bins[b + 1];
         const double w0 = bin_mass(v0, octave(b)), w1 = bin_mass(v1, octave(b + 1));
-        uint32_t c = bin_count(v0) + bin_count(v1);
-        double m = w0 + w1;
-        if (threadIdx.x == 0) sh.bin = SAMPLE_BINS;
-        block_scan(c, m);   // (its barrier comes before the minimum)
-        c += c0;
-        m += m0;
-        // (an empty bin reaches nothing, so rounding of the sums cannot name one)
-        if (bin_count(v0) && limit.reached(c - bin_count(v1), m - w1)) atomicMin(&sh.bin, b);
-        else if (bin_count(v1) && limit.reached(c, m)) atomicMin(&sh.bin, b + 1);
-        __syncthreads();
-        const int found = sh.bin;
-        if (found >> 1 == (int)threadIdx.x && found < SAMPLE_BINS) {
-            sh.count = c - bin_count(v1) - (found & 1 ? 0 : bin_count(v0));
-            sh.mass = m - w1 - (found & 1 ? 0. : w0);
+        turn ^= 1;
+        uint32_t c = wave_scan<op_add>(bin_count(v0) + bin_count(v1));
+        double m = wave_scan<op_add>(w0 + w1);
+        if (lane == 63) {
+            sh.wave32[turn][wave] = c;
+            sh.wave_d[turn][wave] = m;
         }
         __syncthreads();
-        if (found < SAMPLE_BINS) {
-            c0 = sh.count;
-            m0 = sh.mass;
+        const uint32_t cw = row_scan<op_add>(sh.wave32[turn][lane & 15]) + c0;
+        const double mw = row_scan<op_add>(sh.wave_d[turn][lane & 15]) + m0;
+        if (!limit.reached(read_lane(cw, 15), read_lane(mw, 15))) return SAMPLE_BINS;
+        // one wave: the first whose sum reaches the limit; in it the first bin that does (an empty one reaches nothing; if the
+        // rounding of the sums lets none, the last that is not empty)
+        const uint32_t cb = wave > 0 ? read_lane(cw, wave - 1) : c0;
+        const double mb = wave > 0 ? read_lane(mw, wave - 1) : m0;
+        if ((wave == 0 || !limit.reached(cb, mb)) && limit.reached(read_lane(cw, wave), read_lane(mw, wave))) {
+            c += cb;
+            m += mb;
+            const uint32_t n0 = bin_count(v0), n1 = bin_count(v1);
+            bool at0 = n0 && limit.reached(c - n1, m - w1), at1 = n1 && limit.reached(c, m);
+            uint64_t there = __ballot(at0 || at1);
+            if (!there) {
+                at0 = !n1;
+                there = __ballot(n0 || n1);
+                there = there ? 1ull << (63 - __clzll((long long)there)) : 1;
+            }
+            if (lane == __ffsll((unsigned long long)there) - 1) {
+                sh.bin = at0 ? b : b + 1;
+                sh.count = c - n1 - (at0 ? n0 : 0);
+                sh.mass = m - w1 - (at0 ? w0 : 0.);
+            }
         }
-        return found;
+        __syncthreads();
+        c0 = sh.count;
+        m0 = sh.mass;
+        return sh.bin;
     }
 
     // Adds the tokens of bins first ... last with keys low ... high to the list (there is room); returns their number.
@@ -355,7 +453,7 @@ template <class T> struct sample_row {
         if (threadIdx.x == 0) sh.nlist = 0;
         __syncthreads();
         const float lowest = (float)(SAMPLE_ABOVE - 1 - last) * 0.0625f, highest = first == 0 ? INFINITY : (float)(SAMPLE_ABOVE - first) * 0.0625f;
-        each(a.vocab, [&](int i, float l) {
+        each([&](int i, float l) {
             const float y = s.y(l);
             if (!(y >= lowest && y < highest)) return;
             const uint64_t key = sample_key(l, i);
@@ -380,7 +478,7 @@ template <class T> struct sample_row {
             }
         };
         auto from_row = [&](auto f) {
-            each(a.vocab, [&](int i, float l) {
+            each([&](int i, float l) {
                 const float y = s.y(l);
                 if (in_bin(y)) f(sample_key(l, i), y);
             });
@@ -390,10 +488,15 @@ template <class T> struct sample_row {
             lo = min(lo, key);
             hi = max(hi, key);
         };
-        if (listed >= 0) from_list(range);
-        else from_row(range);
-        uint64_t low = block_min(lo), high = ~block_min(~hi);
-        for (uint32_t n = bin_count(sh.bins[bin]); n > 64;) {
+        uint64_t low = 0, high = KEY_EMPTY;
+        uint32_t n = bin_count(sh.bins[bin]);
+        if (n > 64) {
+            if (listed >= 0) from_list(range);
+            else from_row(range);
+            low = block_min(lo);
+            high = ~block_min(~hi);
+        }
+        while (n > 64) {
             int shift = 0;
             while ((high - low) >> shift >= SAMPLE_BINS) ++shift;
             __syncthreads();
@@ -455,43 +558,53 @@ template <class T> struct sample_row {
         const bool greedy = !(t > 0.f) || min_p > 1.f;   // (the first token alone stays)
         const bool by_k = top_k > 0 && top_k < a.vocab, by_p = top_p < 1.f;
 
-        // the reference: the largest of a part of the row, or of all of it where that is needed anyway
-        float ref = -INFINITY;
-        if (!greedy && !(min_p > 0.f && !by_k && !by_p))
-            ref = sample_key_logit(first_key(min(a.vocab, SAMPLE_THREADS * SAMPLE_V)));
-        if (!(ref > -INFINITY)) {
-            const uint64_t first = first_key(a.vocab);
-            ref = sample_key_logit(first);
-            if (!(ref > -INFINITY)) return done(-1, -INFINITY);
-            if (greedy) return done((int64_t)(uint32_t)first, 0.f);
+        load_look();
+        if (greedy) {
+            const uint64_t first = first_key();
+            return sample_key_logit(first) > -INFINITY ? done((int64_t)(uint32_t)first, 0.f) : done(-1, -INFINITY);
         }
+        // the reference: the largest of a part of the row, or of all of it where that is needed anyway
+        auto largest = [&]() {
+            float high = -INFINITY;
+            each([&](int, float l) { high = fmaxf(high, l); });
+            return block_max(high);
+        };
+        float ref = -INFINITY;
+        if (!(min_p > 0.f && !by_k && !by_p)) {
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) ref = fmaxf(ref, look[e]);
+            ref = block_max(ref);
+        }
+        if (!(ref > -INFINITY)) ref = largest();
+        if (!(ref > -INFINITY)) return done(-1, -INFINITY);
         const float inv = 1.f / t;
-        float top;
         if (!by_k && !by_p) {
-            // (with min_p the reference is the largest logit; its weight is 1 up to the rounding of y)
-            sample_scale s(ref, inv);
-            const float least = min_p > 0.f ? min_p * s.weight(s.y(ref)) : 0.f;
-            if (!draw(s, KEY_EMPTY, least, top)) draw(sample_scale(top, inv), KEY_EMPTY, least, top);
+            // (with min_p the reference is the largest logit, of weight 1)
+            if (!draw(sample_scale(ref, inv), KEY_EMPTY, min_p)) draw(sample_scale(largest(), inv), KEY_EMPTY, min_p);
             return;
         }
-        if (!fill_bins(sample_scale(ref, inv), top)) {
-            ref = top;
-            fill_bins(sample_scale(ref, inv), top);
+        float top;
+        int complete;   // the list holds the tokens of all bins up to this one; -1: of none
+        // (half as many again as top_k asks for, or some, for top_p, which may ask for any number)
+        const uint32_t wanted = by_k ? (uint32_t)min((int64_t)(SAMPLE_LIST / 2), top_k + top_k / 2 + 64) : SAMPLE_LIST / 4;
+        fill_bins(sample_scale(ref, inv), wanted, top, complete);
+        if (!(top < (float)(SAMPLE_ABOVE / 16))) {
+            ref = largest();
+            fill_bins(sample_scale(ref, inv), wanted, top, complete);
         }
         const sample_scale s(ref, inv);
-        const float least = min_p > 0.f ? min_p * s.weight(s.y(top)) : 0.f;
+        const float least = min_p > 0.f ? min_p * s.weight(top) : 0.f;
 
         // Each limit in turn: its bin, the list if it is not there, its cut.
         double all = block_sum(bin_mass(sh.bins[2 * tid], bin_octave(2 * tid)) + bin_mass(sh.bins[2 * tid + 1], bin_octave(2 * tid + 1)));
         uint64_t cut = KEY_EMPTY;
-        int listed = 0;                       // > 0: the list holds the tokens of all bins up to `complete`
-        int complete = -1;
+        int listed = complete >= 0 ? (int)sh.nlist : 0;
         for (int step = 0; step < 2; ++step) {
             if (step == 0 ? !by_k : !by_p) continue;
             sample_limit limit;
             limit.by_count = step == 0;
             limit.count = (uint32_t)top_k;
-            limit.mass = (double)fmaxf(top_p, 0.f) * all;   // a token stays while the weights before it are below: up to the one that reaches it
+            limit.mass = fmax((double)top_p * all, 1e-300);   // a token stays while the weights before it are below: up to the one that reaches it
             uint32_t c = 0;
             double m = 0.;
             const int bin = find_bin(sh.bins, limit, c, m, bin_octave);
@@ -508,7 +621,7 @@ template <class T> struct sample_row {
             all = m;
         }
         if (complete < 0) {
-            draw(s, cut, least, top);
+            draw(s, cut, least);
             return;
         }
         // the race on the list
@@ -518,7 +631,7 @@ template <class T> struct sample_row {
             const uint64_t key = sh.list[i];
             const float w = s.weight(s.y(sample_key_logit(key)));
             const int token = (int)(uint32_t)key;
-            if (key > cut || !(w > 0.f) || w < least) continue;
+            if (key > cut || !(w >= fmaxf(least, 1e-30f))) continue;
             mass += (double)w;
             if (noise) best.enter(w, noise[token], token);
             else best.enter_certain(w, token);
@@ -530,7 +643,7 @@ template <class T> struct sample_row {
 template <class T> __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(sample_args a) {
     __shared__ sample_shared sh;
     const int64_t r = blockIdx.x;
-    sample_row<T> row = {a, sh, (const T *)a.logits + r * a.row_stride, a.noise ? a.noise + r * a.noise_stride : nullptr, 0};
+    sample_row<T> row = {a, sh, (const T *)a.logits + r * a.row_stride, a.noise ? a.noise + r * a.noise_stride : nullptr, 0, 0, 0, {}};
     row.run();
 }
 
