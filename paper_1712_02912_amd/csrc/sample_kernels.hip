@@ -111,7 +111,7 @@ struct sample_limit {
 
 // Weights of a row's logits, as exponents of two: y = log2(w).  What is far below the bins is cut off there, so is what is no
 // number (the middle of three is the smallest then), and what is above them at SAMPLE_CAP.
-constexpr float SAMPLE_FLOOR = -100.f, SAMPLE_CAP = 1e30f;
+constexpr float SAMPLE_FLOOR = -100.f, SAMPLE_LEAST = -95.f, SAMPLE_CAP = 1e30f;
 struct sample_scale {
     float c, ref, low, high;   // y = c * (l - ref), the difference within low ... high
     __device__ __forceinline__ sample_scale(float reference, float inv_t) {
@@ -262,46 +262,58 @@ template <class T> struct sample_row {
         done((int64_t)token, (s.y((float)row[token]) - octaves - log2f((float)__builtin_amdgcn_frexp_mant(mass))) * 0.6931471805599453f);
     }
 
-    // Race over the whole row among keys up to `cut` and weights of at least `least`.  Returns false if the reference is too
-    // low for the row's largest logit.
+    // Race over the whole row: tokens with y of at least `upper` and `least` stay; those from `lower` to below `upper`, which
+    // are the bin of the cut, all go into the list (there is room; `cut` KEY_EMPTY), or stay if their key is not behind `cut`
+    // (and y at least `least`).  Returns the largest y.
     // A bound on the winner, w / e, is found first, on the first look: e = -log u is at most (1 - u) / u.
-    __device__ __forceinline__ bool draw(const sample_scale &s, uint64_t cut, float least) {
+    __device__ __forceinline__ float draw(const sample_scale &s, float upper, float lower, float least, uint64_t cut, race &best, double &mass) {
         struct __attribute__((packed, aligned(4))) noises { float v[SAMPLE_V]; };
-        race best;
+        const float edge = fmaxf(upper, least);
         float high = -INFINITY, sum[SAMPLE_V] = {};
-        const bool all_stay = cut == KEY_EMPTY;   // (but for weights below least): noise is read beside the logits, not after them
-        const float bound = all_stay ? -INFINITY : sample_key_logit(cut);
-        least = fmaxf(least, 1e-30f);             // (what is cut off at SAMPLE_FLOOR does not stay)
-        auto weight = [&](int i, float l, float y) {   // 0: does not stay
-            const float w = s.weight(y);
-            if (all_stay) return w >= least ? w : 0.f;
-            return w >= least && (l > bound || (l == bound && sample_key(l, i) <= cut)) ? w : 0.f;
+        auto weight = [&](float y) { return y >= edge ? s.weight(y) : 0.f; };
+        auto border = [&](int i, float l) {   // a token of the cut's bin
+            if (cut == KEY_EMPTY) {
+                sh.list[atomicAdd(&sh.nlist, 1u)] = sample_key(l, i);
+            } else if (sample_key(l, i) <= cut && s.y(l) >= least) {
+                const float w = s.weight(s.y(l));
+                sum[0] += w;
+                if (noise) best.enter(w, noise[i], i);
+                else best.enter_certain(w, i);
+            }
         };
         float bounded = 0.f;
-        if (noise) {
-            const int i = before + threadIdx.x * SAMPLE_V;
-            if (i < whole) {
-                const noises u = *(const noises *)(noise + i);
+        const int first = before + threadIdx.x * SAMPLE_V;
+        if (noise && first < whole) {
+            const noises u = *(const noises *)(noise + first);
 #pragma unroll
-                for (int e = 0; e < SAMPLE_V; ++e) bounded = fmaxf(bounded, weight(i + e, look[e], s.y(look[e])) * u.v[e] * __builtin_amdgcn_rcpf(1.f - u.v[e]));
-            }
-            bounded = block_max(bounded) * (1.f - 1e-6f);   // (rounded down)
-            if (threadIdx.x == 0) sh.best = __float_as_uint(bounded < INFINITY ? bounded : 0.f);
-            __syncthreads();
+            for (int e = 0; e < SAMPLE_V; ++e) bounded = fmaxf(bounded, weight(s.y(look[e])) * u.v[e] * __builtin_amdgcn_rcpf(1.f - u.v[e]));
         }
+        bounded = block_max(bounded) * (1.f - 1e-6f);   // (rounded down)
+        if (threadIdx.x == 0) {
+            sh.best = __float_as_uint(bounded < INFINITY ? bounded : 0.f);
+            sh.nlist = 0;
+        }
+        __syncthreads();
+        const bool all_stay = upper < SAMPLE_LEAST;   // noise is read beside the logits, not after them
         each_vector(false, [&](int i, const float (&l)[SAMPLE_V]) {
             noises u;
             if (noise && all_stay) u = *(const noises *)(noise + i);
-            float w[SAMPLE_V], most = 0.f;
+            float w[SAMPLE_V], most = -INFINITY;
+            uint32_t which = 0;
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) {
                 const float y = s.y(l[e]);
-                high = fmaxf(high, y);
-                w[e] = weight(i + e, l[e], y);
+                most = fmaxf(most, y);
+                w[e] = weight(y);
                 sum[e] += w[e];
-                most = fmaxf(most, w[e]);
+                which |= (uint32_t)(y >= lower && y < upper) << e;
             }
-            if (!(most > 0.f)) return;
+            high = fmaxf(high, most);
+            for (; which; which &= which - 1) {
+                const int e = __ffs(which) - 1;
+                border(i + e, (float)row[i + e]);
+            }
+            if (!(most >= edge)) return;
             if (!noise) {
 #pragma unroll
                 for (int e = 0; e < SAMPLE_V; ++e)
@@ -319,20 +331,29 @@ template <class T> struct sample_row {
                 if (w[e] > 0.f && w[e] >= so_far * (1.f - u.v[e])) best.enter(w[e], u.v[e], i + e);
             if (best.best > so_far) atomicMax(&sh.best, __float_as_uint(best.best));
         }, [&](int i, float l) {
-            const float y = s.y(l);
+            const float y = s.y(l), w = weight(y);
             high = fmaxf(high, y);
-            const float w = weight(i, l, y);
             sum[0] += w;
+            if (y >= lower && y < upper) border(i, l);
             if (!(w > 0.f)) return;
             if (noise) best.enter(w, noise[i], i);
             else best.enter_certain(w, i);
         });
-        if (!(block_max(high) <= SAMPLE_TOP)) return false;
-        double mass = 0.;
 #pragma unroll
         for (int e = 0; e < SAMPLE_V; ++e) mass += (double)sum[e];
-        finish(best, s, mass);
-        return true;
+        return block_max(high);
+    }
+    // The race on the list's keys up to `cut`.
+    __device__ __forceinline__ void draw_list(const sample_scale &s, int listed, float least, uint64_t cut, race &best, double &mass) {
+        for (int i = threadIdx.x; i < listed; i += SAMPLE_THREADS) {
+            const uint64_t key = sh.list[i];
+            const float y = s.y(sample_key_logit(key)), w = s.weight(y);
+            const int token = (int)(uint32_t)key;
+            if (key > cut || !(y >= least)) continue;
+            mass += (double)w;
+            if (noise) best.enter(w, noise[token], token);
+            else best.enter_certain(w, token);
+        }
     }
 
     // Bins of the whole row; top: the largest y, which has to lie below them.  The bins of the first look at the row say from
@@ -464,10 +485,10 @@ template <class T> struct sample_row {
     }
 
     // The key in `bin` at which a limit is reached on top of c, m; the weight up to and with it in m.  The bin's keys are split
-    // into 2048 parts, the part with the limit again, until 64 or fewer are left (equal logits are told apart by their
-    // indexes, so it ends), which a wave sorts.  They come from the list of `listed` keys, or, where the bin has too many for
+    // into 2048 parts, the part with the limit again, until 64 or fewer are left, which a wave sorts (the range of
+    // keys shrinks to a 1024th at least, and no two keys are equal, so it ends after six rounds at most).  They come from the list of `listed` keys, or, where the bin has too many for
     // it (listed < 0), from the row until the rest fits.
-    __device__ __forceinline__ uint64_t find_cut(const sample_scale &s, int bin, int listed, sample_limit limit, uint32_t c, double &m) {
+    __device__ __forceinline__ uint64_t find_cut(const sample_scale &s, int bin, int listed, const sample_limit &limit, uint32_t c, double &m) {
         const int tid = threadIdx.x, octave = bin_octave(bin);
         auto in_bin = [&](float y) { return bin_of(y) == bin; };
         auto from_list = [&](auto f) {
@@ -509,9 +530,9 @@ template <class T> struct sample_row {
             else from_row(add);
             __syncthreads();
             const int part = find_bin(sh.fine, limit, c, m, [&](int) { return octave; });
-            if (part >= SAMPLE_BINS) {   // (reached by the sums of the bins, but not by these, which round differently)
-                limit.mass *= 1. - 1e-12;
-                continue;
+            if (part >= SAMPLE_BINS) {   // reached by the sums of the bins, but not by these, which round differently: the last key
+                m = limit.mass;
+                return high;
             }
             n = bin_count(sh.fine[part]);
             low += (uint64_t)part << shift;
@@ -578,64 +599,77 @@ template <class T> struct sample_row {
         if (!(ref > -INFINITY)) ref = largest();
         if (!(ref > -INFINITY)) return done(-1, -INFINITY);
         const float inv = 1.f / t;
-        if (!by_k && !by_p) {
-            // (with min_p the reference is the largest logit, of weight 1)
-            if (!draw(sample_scale(ref, inv), KEY_EMPTY, min_p)) draw(sample_scale(largest(), inv), KEY_EMPTY, min_p);
-            return;
-        }
-        float top;
-        int complete;   // the list holds the tokens of all bins up to this one; -1: of none
-        // (half as many again as top_k asks for, or some, for top_p, which may ask for any number)
-        const uint32_t wanted = by_k ? (uint32_t)min((int64_t)(SAMPLE_LIST / 2), top_k + top_k / 2 + 64) : SAMPLE_LIST / 4;
-        fill_bins(sample_scale(ref, inv), wanted, top, complete);
-        if (!(top < (float)(SAMPLE_ABOVE / 16))) {
-            ref = largest();
-            fill_bins(sample_scale(ref, inv), wanted, top, complete);
-        }
-        const sample_scale s(ref, inv);
-        const float least = min_p > 0.f ? min_p * s.weight(top) : 0.f;
-
-        // Each limit in turn: its bin, the list if it is not there, its cut.
-        double all = block_sum(bin_mass(sh.bins[2 * tid], bin_octave(2 * tid)) + bin_mass(sh.bins[2 * tid + 1], bin_octave(2 * tid + 1)));
+        sample_scale s(ref, inv);
+        // (without limits, min_p takes the largest logit for the reference: of weight 1)
+        float least = min_p > 0.f ? fmaxf(log2f(min_p), SAMPLE_LEAST) : SAMPLE_LEAST;
         uint64_t cut = KEY_EMPTY;
-        int listed = complete >= 0 ? (int)sh.nlist : 0;
-        for (int step = 0; step < 2; ++step) {
-            if (step == 0 ? !by_k : !by_p) continue;
-            sample_limit limit;
-            limit.by_count = step == 0;
-            limit.count = (uint32_t)top_k;
-            limit.mass = fmax((double)top_p * all, 1e-300);   // a token stays while the weights before it are below: up to the one that reaches it
-            uint32_t c = 0;
-            double m = 0.;
-            const int bin = find_bin(sh.bins, limit, c, m, bin_octave);
-            if (bin >= SAMPLE_BINS) continue;   // not reached: all stay
-            int have = listed;
-            if (bin > complete) {
-                const uint32_t n = bin_count(sh.bins[bin]);
-                const bool fits = c + n <= SAMPLE_LIST;
-                have = n > SAMPLE_LIST ? -1 : collect(s, fits ? 0 : bin, bin, 0, KEY_EMPTY);
-                listed = fits ? have : 0;
-                complete = fits ? bin : -1;
+        sample_limit limit = {};
+        uint32_t c = 0;       // tokens and weight before the bin of the cut
+        double m = 0.;
+        int listed = 0;       // keys in the list
+        int cut_bin = SAMPLE_BINS;
+        bool on_list = false, later = false;   // the list holds all that stay; the cut is to be found after the pass over the row
+
+        if (by_k || by_p) {
+            // (half as many again as top_k asks for, or some, for top_p, which may ask for any number)
+            const uint32_t wanted = by_k ? (uint32_t)min((int64_t)(SAMPLE_LIST / 2), top_k + top_k / 2 + 64) : SAMPLE_LIST / 4;
+            float top;
+            int complete;   // the list holds the tokens of all bins up to this one; -1: of none
+            for (int round = 0; round < 2; ++round) {   // (the second with the largest logit for the reference)
+                fill_bins(s, wanted, top, complete);
+                if (top < (float)(SAMPLE_ABOVE / 16) || round == 1) break;
+                s = sample_scale(largest(), inv);
             }
-            cut = min(cut, find_cut(s, bin, have, limit, c, m));
-            all = m;
+            least = min_p > 0.f ? fmaxf(top + log2f(min_p), SAMPLE_LEAST) : SAMPLE_LEAST;
+            listed = complete >= 0 ? (int)sh.nlist : 0;
+            // each limit in turn: its bin, the list if it is not there, its cut
+            double all = block_sum(bin_mass(sh.bins[2 * tid], bin_octave(2 * tid)) + bin_mass(sh.bins[2 * tid + 1], bin_octave(2 * tid + 1)));
+            for (int step = 0; step < 2; ++step) {
+                if (step == 0 ? !by_k : !by_p) continue;
+                limit.by_count = step == 0;
+                limit.count = (uint32_t)top_k;
+                limit.mass = fmax((double)top_p * all, 1e-300);   // a token stays while the weights before it are below: up to the one that reaches it
+                c = 0;
+                m = 0.;
+                const int bin = find_bin(sh.bins, limit, c, m, bin_octave);
+                if (bin >= SAMPLE_BINS) continue;   // not reached: all stay
+                cut_bin = bin;
+                int have = listed;
+                if (bin > complete) {
+                    const uint32_t n = bin_count(sh.bins[bin]);
+                    const bool fits = c + n <= SAMPLE_LIST;
+                    if (!fits && n <= SAMPLE_LIST && (step == 1 || !by_p)) {
+                        later = true;
+                        break;
+                    }
+                    have = n > SAMPLE_LIST ? -1 : collect(s, fits ? 0 : bin, bin, 0, KEY_EMPTY);
+                    listed = fits ? have : 0;
+                    complete = fits ? bin : -1;
+                }
+                cut = min(cut, find_cut(s, bin, have, limit, c, m));
+                all = m;
+            }
+            on_list = complete >= 0 && cut != KEY_EMPTY;
         }
-        if (complete < 0) {
-            draw(s, cut, least);
-            return;
-        }
-        // the race on the list
         race best;
         double mass = 0.;
-        for (int i = tid; i < listed; i += SAMPLE_THREADS) {
-            const uint64_t key = sh.list[i];
-            const float w = s.weight(s.y(sample_key_logit(key)));
-            const int token = (int)(uint32_t)key;
-            if (key > cut || !(w >= fmaxf(least, 1e-30f))) continue;
-            mass += (double)w;
-            if (noise) best.enter(w, noise[token], token);
-            else best.enter_certain(w, token);
+        if (!on_list) {
+            // from the row: what lies before the bin of the cut stays, the bin itself is listed for later, or the cut is there
+            const float lower = cut_bin < SAMPLE_BINS ? (float)(SAMPLE_ABOVE - 1 - cut_bin) * 0.0625f : -INFINITY;
+            const float upper = cut_bin < SAMPLE_BINS ? lower + 0.0625f : -INFINITY;
+            for (int round = 0; round < 2; ++round) {   // (the second with the largest logit for the reference)
+                const float high = draw(s, upper, lower, least, later ? KEY_EMPTY : cut, best, mass);
+                if (high <= SAMPLE_TOP || round == 1) break;
+                s = sample_scale(largest(), inv);
+                best = race();
+                mass = 0.;
+            }
+            if (later) {
+                listed = (int)sh.nlist;
+                cut = min(cut, find_cut(s, cut_bin, listed, limit, c, m));
+            }
         }
+        if (on_list || later) draw_list(s, listed, least, cut, best, mass);
         finish(best, s, mass);
     }
 };
