@@ -8,6 +8,8 @@
 //
 // Keys and values go through registers into one of two buffers while the other one is computed on, so one barrier per tile is
 // enough and loads have a tile's time to arrive.  Places that hold no key become zeros on that way.
+#include <type_traits>
+
 #include "kv_attention.h"
 
 namespace pq {
@@ -26,8 +28,8 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     typedef lds_row<D> row;
     constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
-    constexpr int ALL = CHUNK_TILE * CHUNKS, MOVES = (ALL + THREADS - 1) / THREADS;   // chunks of 16 bytes that a thread moves per tile
-    static_assert(ALL % 64 == 0, "whole waves move");
+    // a thread moves chunks of 16 bytes of one key (and value) of a tile, every LANES-th from its own on
+    constexpr int LANES = THREADS / CHUNK_TILE, MOVES = (CHUNKS + LANES - 1) / LANES;
     __shared__ __attribute__((aligned(16))) unsigned char lds_k[2][CHUNK_TILE * row::bytes], lds_v[2][CHUNK_TILE * row::bytes];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
 
@@ -51,8 +53,9 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     const int64_t my_row = mine * M + wave * 32 + n;
     const bool valid = my_row < rows;
     const int token = valid ? (int)a.by_group.div((uint32_t)my_row) : 0, sub = valid ? (int)(my_row - (int64_t)token * a.group) : 0;
-    const int last = kv - fresh + token;
-    const int64_t first_seen = a.window > 0 ? (int64_t)last - a.window + 1 : 0;
+    // the keys that it sees: `seen` of them from first_seen on
+    const int last = kv - fresh + token, first_seen = a.window > 0 ? (int)max((int64_t)0, (int64_t)last - a.window + 1) : 0;
+    const uint32_t seen = (uint32_t)max(0, min(last, nkeys - 1) - first_seen + 1);
     // the keys that the tile's rows see, and those that all of them see
     const int token0 = (int)a.by_group.div((uint32_t)(mine * M)), token1 = (int)a.by_group.div((uint32_t)(min(rows, (mine + 1) * M) - 1));
     const int to = min(nkeys, kv - fresh + token1 + 1);
@@ -61,97 +64,97 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     const int tiles_all = to > from ? (to - from + CHUNK_TILE - 1) / CHUNK_TILE : 0;
     const int tile_begin = (int)((int64_t)tiles_all * part / split.splits), tile_end = (int)((int64_t)tiles_all * (part + 1) / split.splits);
 
+    // (a negative scale is the queries' sign: scores are compared before they are scaled)
+    const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+    const float scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-37f);   // (0 times the -inf of a key that is not seen is no number)
     u32x4 q[STEPS];
     {
         const T *p = (const T *)a.q.p + (a.cu[r] + token) * a.q.token_stride + (h * a.group + sub) * a.q.head_stride + 8 * g;
 #pragma unroll
-        for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + 16 * t);
+        for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + 16 * t) ^ sign;
     }
     f32x16 out[OUTS];
 #pragma unroll
     for (int f = 0; f < OUTS; ++f)
 #pragma unroll
         for (int i = 0; i < 16; ++i) out[f][i] = 0.f;
-    float ref = NO_SCORE, sum = 0.f;
+    float ref = NO_SCORE, sum = 0.f;   // ref: of the scaled scores
 
     // this thread's chunks of a tile
-    const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2];
-    const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2];
+    const int my_key = tid / LANES, my_chunk = tid % LANES;
+    const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2] + 8 * my_chunk;
+    const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2] + 8 * my_chunk;
     u32x4 mk[MOVES], mv[MOVES];
     auto load = [&](int tile) {
+        int64_t block;
+        int place;
+        attention_place(a, r, min(from + tile * CHUNK_TILE + my_key, to - 1), block, place);
+        const T *const k = keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1];
+        const T *const v = values + block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
-            const int c = tid + THREADS * i, key = c / CHUNKS, chunk = c % CHUNKS;
-            if (ALL % THREADS != 0 && c >= ALL) continue;
-            int64_t block;
-            int place;
-            attention_place(a, r, min(from + tile * CHUNK_TILE + key, to - 1), block, place);
-            mk[i] = *(const u32x4 *)(keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1] + 8 * chunk);
-            mv[i] = *(const u32x4 *)(values + block * a.cache.value_strides[0] + place * a.cache.value_strides[1] + 8 * chunk);
+            if (CHUNKS % LANES != 0 && my_chunk + LANES * i >= CHUNKS) continue;
+            mk[i] = *(const u32x4 *)(k + 8 * LANES * i);
+            mv[i] = *(const u32x4 *)(v + 8 * LANES * i);
         }
     };
     auto store = [&](int tile, int buffer) {
+        const bool held = from + tile * CHUNK_TILE + my_key < to;
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
-            const int c = tid + THREADS * i, key = c / CHUNKS, chunk = c % CHUNKS;
-            if (ALL % THREADS != 0 && c >= ALL) continue;
-            const int at = key * row::bytes + 16 * row::chunk(key, chunk);
+            const int chunk = my_chunk + LANES * i;
+            if (CHUNKS % LANES != 0 && chunk >= CHUNKS) continue;
+            const int at = my_key * row::bytes + 16 * row::chunk(my_key, chunk);
             *(u32x4 *)(lds_k[buffer] + at) = mk[i];
-            *(u32x4 *)(lds_v[buffer] + at) = from + tile * CHUNK_TILE + key < to ? mv[i] : u32x4{0, 0, 0, 0};
+            *(u32x4 *)(lds_v[buffer] + at) = held ? mv[i] : u32x4{0, 0, 0, 0};
         }
     };
-    if (tile_begin < tile_end) {
-        load(tile_begin);
-        store(tile_begin, 0);
-        if (tile_begin + 1 < tile_end) load(tile_begin + 1);
-    }
-    for (int tile = tile_begin; tile < tile_end; ++tile) {
-        const int buffer = (tile - tile_begin) & 1, key0 = from + tile * CHUNK_TILE;
-        __syncthreads();   // this tile is written, and the one before it read
-        if (tile + 1 < tile_end) store(tile + 1, buffer ^ 1);
-        if (tile + 2 < tile_end) load(tile + 2);
+    // Where this lane reads: key n of 32 and chunk g, key 4 g + (lane / 4) % 4 of 16 and its part of chunk pair 0.  Other chunks
+    // differ in bits that the row's swizzle only turns over, so their places are one exclusive or away.
+    const int k_at = n * row::bytes + 16 * row::chunk(n, g);
+    const int v_key = 4 * g + ((lane >> 2) & 3);
+    const int v_at = v_key * row::bytes + 16 * row::chunk(v_key, 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 8 * (lane & 1);
 
+    auto compute = [&](int tile, auto buffer_of) {
+        constexpr int buffer = decltype(buffer_of)::value;
+        const int key0 = from + tile * CHUNK_TILE;
         f32x16 s[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
-#pragma unroll
-            for (int t = 0; t < STEPS; ++t) {
-                const u32x4 k = *(const u32x4 *)(lds_k[buffer] + (32 * j + n) * row::bytes + 16 * row::chunk(32 * j + n, 2 * t + g));
-                s[j] = mfma_of<T>::m32(k, q[t], s[j]);
-            }
-        }
-        // scores of this lane: keys 32 j + 8 (i / 4) + 4 g + i % 4 of the tile
-        float p[32], high_score = NO_SCORE;
-        const bool all_seen = key0 >= all_from && key0 + CHUNK_TILE <= all_to;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[16 * j + i] = s[j][i] * a.scale_log2;
-        if (!all_seen) {
+            for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s[j] = mfma_of<T>::m32(*(const u32x4 *)(lds_k[buffer] + (k_at ^ (32 * t)) + 32 * j * row::bytes), q[t], s[j]);
+        // scores of this lane: keys 32 j + 8 (i / 4) + 4 g + i % 4 of the tile
+        if (key0 < all_from || key0 + CHUNK_TILE > all_to) {   // some row does not see some key
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = key0 + 32 * j + 8 * (i / 4) + 4 * g + i % 4;
-                    if (!(key <= last && key >= first_seen && key < nkeys)) p[16 * j + i] = -INFINITY;
+                    if ((uint32_t)(key - first_seen) >= seen) s[j][i] = -INFINITY;
                 }
         }
+        float high_score = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) high_score = fmaxf(high_score, p[i]);
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) high_score = fmaxf(high_score, s[j][i]);
         // (the reference moves only when a score passes it by 2^8, see kv_attention_few.hip)
-        if (__any(high_score > ref + 8.f)) {
+        if (__any(high_score * scale_log2 > ref + 8.f)) {
             high_score = fmaxf(high_score, __shfl_xor(high_score, 32));
-            const float moved = fmaxf(ref, high_score), shrink = __builtin_amdgcn_exp2f(ref - moved);
+            const float moved = fmaxf(ref, high_score * scale_log2), shrink = __builtin_amdgcn_exp2f(ref - moved);
             ref = moved;
             sum *= shrink;
 #pragma unroll
             for (int f = 0; f < OUTS; ++f) out[f] *= shrink;
         }
+        float p[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(p[i] - ref);
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale_log2, -ref));
             sum += p[i];
         }
 #pragma unroll
@@ -162,14 +165,31 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
                 u32x4 vt;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int key = 16 * b + 8 * e + 4 * g + ((lane >> 2) & 3), chunk = 4 * f + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-                    const uint2 c = read_transposed(lds_v[buffer] + key * row::bytes + 16 * row::chunk(key, chunk) + 8 * (lane & 1));
+                    // (keys 8 on change the swizzle's last bit, but in rows of 128 bytes, too)
+                    const uint2 c = read_transposed(lds_v[buffer] + (v_at ^ (64 * f) ^ (16 * e)) + (16 * b + 8 * e) * row::bytes);
                     vt[2 * e] = c.x;
                     vt[2 * e + 1] = c.y;
                 }
                 out[f] = mfma_of<T>::m32(vt, weights, out[f]);
             }
         }
+    };
+
+    if (tile_begin < tile_end) {
+        load(tile_begin);
+        store(tile_begin, 0);
+        if (tile_begin + 1 < tile_end) load(tile_begin + 1);
+    }
+    for (int tile = tile_begin; tile < tile_end; tile += 2) {
+        __syncthreads();   // this tile is written, and the one before it read
+        if (tile + 1 < tile_end) store(tile + 1, 1);
+        if (tile + 2 < tile_end) load(tile + 2);
+        compute(tile, std::integral_constant<int, 0>());
+        if (tile + 1 >= tile_end) break;
+        __syncthreads();
+        if (tile + 2 < tile_end) store(tile + 2, 0);
+        if (tile + 3 < tile_end) load(tile + 3);
+        compute(tile + 1, std::integral_constant<int, 1>());
     }
     sum += __shfl_xor(sum, 32);
     if (!valid) return;

@@ -120,8 +120,9 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
         const int kv = a.kv_lens[r];
         const int rows = (int)min((int64_t)FEW_ROWS, (int64_t)x.held * a.group);
         const int token = (int)a.by_group.div((uint32_t)n), sub = n - token * a.group;
-        const int last = kv - x.fresh + token;                                       // the last key that this lane's row sees
-        const int64_t first_seen = a.window > 0 ? (int64_t)last - a.window + 1 : 0;  // and the first
+        // the keys that this lane's row sees: `seen` of them from first_seen on
+        const int last = kv - x.fresh + token, first_seen = a.window > 0 ? (int)max((int64_t)0, (int64_t)last - a.window + 1) : 0;
+        const uint32_t seen = (uint32_t)max(0, min(last, x.keys - 1) - first_seen + 1);
         const int64_t qrow = a.cu[r] + (n < rows ? token : 0);
         u32x4 q[STEPS];
         {
@@ -189,7 +190,7 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
                 for (int e = 0; e < 4; ++e) {
                     const int key = tile + 16 * j + 4 * g + e;
                     float y = s[j][e] * a.scale_log2;
-                    if (!all_seen && !(key <= last && key >= first_seen && key < x.keys)) y = -INFINITY;
+                    if (!all_seen && (uint32_t)(key - first_seen) >= seen) y = -INFINITY;
                     p[4 * j + e] = y;
                     high_score = fmaxf(high_score, y);
                 }
