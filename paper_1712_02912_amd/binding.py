@@ -9,6 +9,7 @@ fallback.
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -34,16 +35,6 @@ class IvfLists(ctypes.Structure):
     _fields_ = [("coarse_centroids", ctypes.c_void_p), ("list_offsets", ctypes.c_void_p),
                 ("codes", ctypes.c_void_p), ("ids", ctypes.c_void_p),
                 ("nlist", ctypes.c_int), ("d", ctypes.c_int), ("ntotal", ctypes.c_int64)]
-
-
-class KvCache(ctypes.Structure):
-    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("key_strides", ctypes.c_int64 * 3),
-                ("value_strides", ctypes.c_int64 * 3), ("nblocks", ctypes.c_int64), ("block_size", ctypes.c_int),
-                ("heads", ctypes.c_int), ("dim", ctypes.c_int), ("elem", ctypes.c_int)]
-
-
-class Heads(ctypes.Structure):
-    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 def load():
@@ -76,7 +67,7 @@ def load():
     lib.pq_rotate.argtypes = [vp, vp, vp, i64, ci, vp]
     lib.pq_encode.argtypes = [vp, vp, vp, i64, ci, ci, ci, ci, vp]
     lib.pq_derived_search.argtypes = [vp, vp, i64, vp, vp, ci, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, i64]
-    cf, cache, heads = ctypes.c_float, ctypes.POINTER(KvCache), ctypes.POINTER(Heads)
+    cf, cache, heads = ctypes.c_float, vp, vp   # (structures as their bytes, see _cache and _heads)
     lib.pq_kv_plan.argtypes = [vp, vp, vp, ci, vp, ci, vp, ci, ci, i64, vp, vp, vp, vp, vp]
     lib.pq_kv_append.argtypes = [vp, cache, heads, ci, heads, heads, i64, vp, vp, vp, vp, i64, ci, ci, ci, vp, vp, cf, vp]
     lib.pq_kv_attention.argtypes = [vp, cache, heads, ci, i64, vp, vp, ci, vp, ci, ci, cf, ci, vp, vp]
@@ -110,47 +101,55 @@ def _dev(t, dtype, name):
 
 
 def _in_place(t, dtype, name, shape=None):
-    """A tensor that the library reads and writes where it lies (no copy is made of it)."""
+    """Address of a tensor that the library reads and writes where it lies (no copy is made of it)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
-    return ctypes.c_void_p(t.data_ptr())
+    raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+
+
+_pack_heads = struct.Struct("@Pqq").pack            # pq_heads
+_pack_cache = struct.Struct("@PP6qqiiii").pack      # pq_kv_cache
 
 
 def _heads(t, dtype, shape, name):
-    """Rows [tokens][heads][dim] of any strides but the last, as pq_heads."""
+    """Rows [tokens][heads][dim] of any strides but the last, as the bytes of a pq_heads."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
     s0, s1, s2 = t.stride()
     if s2 != 1 and shape[2] > 1 and t.numel() > 0:
         raise ValueError(f"the dimensions of a row of {name} must be contiguous")
-    return Heads(t.data_ptr(), s0, s1)
+    return _pack_heads(t.data_ptr(), s0, s1)
 
 
 def _cache(key_cache, value_cache):
-    """A paged cache [blocks][block size][heads][dim] of any strides but the last, as pq_kv_cache."""
+    """A paged cache [blocks][block size][heads][dim] of any strides but the last, as the bytes of a pq_kv_cache; its dtype and
+    shape."""
+    dtype, shape = key_cache.dtype, key_cache.shape
     for t, name in ((key_cache, "key_cache"), (value_cache, "value_cache")):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError(f"{name} must be a GPU tensor")
-        if t.dtype not in ELEMS or t.dtype != key_cache.dtype:
+        if t.dtype not in ELEMS or t.dtype is not dtype:
             raise TypeError(f"{name} has dtype {t.dtype}: float32, float16 or bfloat16, the same for keys and values")
-        if t.dim() != 4 or t.shape != key_cache.shape:
+        if len(shape) != 4 or t.shape != shape:
             raise ValueError(f"{name} must have shape [blocks][block size][heads][dim], the same for keys and values")
-        if t.stride(3) != 1 and t.shape[3] > 1 and t.numel() > 0:
+        if t.stride(3) != 1 and shape[3] > 1 and t.numel() > 0:
             raise ValueError(f"the dimensions of a row of {name} must be contiguous")
-    nblocks, block_size, heads, dim = key_cache.shape
-    ks, vs = key_cache.stride(), value_cache.stride()
-    return KvCache(key_cache.data_ptr(), value_cache.data_ptr(), ks[:3], vs[:3], nblocks, block_size, heads, dim,
-                   ELEMS[key_cache.dtype])
+    nblocks, block_size, heads, dim = shape
+    k0, k1, k2, _ = key_cache.stride()
+    v0, v1, v2, _ = value_cache.stride()
+    packed = _pack_cache(key_cache.data_ptr(), value_cache.data_ptr(), k0, k1, k2, v0, v1, v2, nblocks, block_size, heads, dim,
+                         ELEMS[dtype])
+    return packed, dtype, heads, dim
 
 
 class Context:
@@ -392,8 +391,8 @@ class Context:
         """Norm and rotation of q [tokens][q heads][dim] and k [tokens][heads][dim]; k and v go into the cache
         [blocks][block size][heads][dim].  cos, sin [positions][rot/2]; without them nothing is rotated.  Returns the queries
         (None if q is None)."""
-        cache = _cache(key_cache, value_cache)
-        dtype, f32, heads, dim = key_cache.dtype, torch.float32, cache.heads, cache.dim
+        cache, dtype, heads, dim = _cache(key_cache, value_cache)
+        f32 = torch.float32
         t = k.shape[0]
         q_heads = 0 if q is None else q.shape[1]
         if q is not None and out is None:
@@ -401,10 +400,10 @@ class Context:
         if (cos is None) != (sin is None):
             raise ValueError("cos and sin go together")
         positions_max, half = (0, 0) if cos is None else cos.shape
-        rows_q = None if q is None else ctypes.byref(_heads(q, dtype, (t, q_heads, dim), "q"))
+        rows_q = None if q is None else _heads(q, dtype, (t, q_heads, dim), "q")
         self._check(self.lib.pq_kv_append(
-            self.handle, ctypes.byref(cache), rows_q, q_heads, ctypes.byref(_heads(k, dtype, (t, heads, dim), "k")),
-            ctypes.byref(_heads(v, dtype, (t, heads, dim), "v")), t, _in_place(positions, torch.int32, "positions", (t,)),
+            self.handle, cache, rows_q, q_heads, _heads(k, dtype, (t, heads, dim), "k"),
+            _heads(v, dtype, (t, heads, dim), "v"), t, _in_place(positions, torch.int32, "positions", (t,)),
             _in_place(slots, torch.int64, "slots", (t,)), None if cos is None else _in_place(cos, f32, "cos"),
             None if sin is None else _in_place(sin, f32, "sin", (positions_max, half)), positions_max, 2 * half, 1 if pairs else 0,
             1 if norm else 0, None if q_weight is None else _in_place(q_weight, f32, "q_weight", (dim,)),
@@ -415,19 +414,19 @@ class Context:
     def pq_kv_attention(self, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new, scale=None, window=0, out=None,
                         lse=None):
         """Attention of q [tokens][q heads][dim] over the paged cache; scale None: 1 / sqrt(dim).  Returns (out, lse)."""
-        cache = _cache(key_cache, value_cache)
+        cache, dtype, _, dim = _cache(key_cache, value_cache)
         t, q_heads = q.shape[0], q.shape[1]
         nreq, width = block_tables.shape
+        shape, i32 = (t, q_heads, dim), torch.int32
         if out is None:
-            out = torch.empty((t, q_heads, cache.dim), dtype=key_cache.dtype, device=q.device)
+            out = torch.empty(shape, dtype=dtype, device=q.device)
         if lse is None:
             lse = torch.empty((t, q_heads), dtype=torch.float32, device=q.device)
-        i32, shape = torch.int32, (t, q_heads, cache.dim)
         self._check(self.lib.pq_kv_attention(
-            self.handle, ctypes.byref(cache), ctypes.byref(_heads(q, key_cache.dtype, shape, "q")), q_heads, t,
-            _in_place(cu_new, i32, "cu_new", (nreq + 1,)), _in_place(kv_lens, i32, "kv_lens", (nreq,)), nreq,
-            _in_place(block_tables, i32, "block_tables"), width, max_new, cache.dim ** -0.5 if scale is None else scale, window,
-            _in_place(out, key_cache.dtype, "out", shape), _in_place(lse, torch.float32, "lse", (t, q_heads))))
+            self.handle, cache, _heads(q, dtype, shape, "q"), q_heads, t, _in_place(cu_new, i32, "cu_new", (nreq + 1,)),
+            _in_place(kv_lens, i32, "kv_lens", (nreq,)), nreq, _in_place(block_tables, i32, "block_tables"), width, max_new,
+            dim ** -0.5 if scale is None else scale, window, _in_place(out, dtype, "out", shape),
+            _in_place(lse, torch.float32, "lse", (t, q_heads))))
         return out, lse
 
     def pq_sample_tokens(self, logits, noise, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
@@ -442,9 +441,9 @@ class Context:
         for t, dtype, name in ((logits, logits.dtype, "logits"), (noise, f32, "noise")):
             if t is None:
                 continue
-            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype:
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype:
                 raise TypeError(f"{name} must be a GPU tensor of dtype {dtype}")
-            if tuple(t.shape) != (rows, vocab):
+            if t.shape != (rows, vocab):
                 raise ValueError(f"{name} must have shape {[rows, vocab]}, got {list(t.shape)}")
             if t.stride(1) != 1 and vocab > 1 and rows > 0:
                 raise ValueError(f"the entries of a row of {name} must be contiguous")

@@ -70,7 +70,20 @@ template <int THREADS> __device__ void few_starts(const attention_args &a, int64
 }
 __global__ __launch_bounds__(1024) void kv_attention_starts_kernel(attention_args a, int64_t *starts) { few_starts<1024>(a, starts); }
 
-__device__ __forceinline__ int64_t few_begin(int64_t total, int blocks, int b) { return total * b / blocks; }
+// The stretches of the line: the first total % blocks of them are one unit longer.
+struct few_cut {
+    int64_t each, longer;
+    __device__ __forceinline__ few_cut(int64_t total, int blocks) {
+        each = (uint64_t)total >> 32 ? total / blocks : (int64_t)((uint32_t)total / (uint32_t)blocks);
+        longer = total - each * blocks;
+    }
+    __device__ __forceinline__ int64_t begin(int b) const { return each * b + min((int64_t)b, longer); }
+    __device__ __forceinline__ int block_of(int64_t unit) const {   // the block that holds it
+        const int64_t in_longer = longer * (each + 1);
+        const uint64_t n = unit < in_longer ? unit : unit - in_longer, d = unit < in_longer ? each + 1 : each;
+        return (int)((unit < in_longer ? 0 : longer) + (int64_t)(n >> 32 | d >> 32 ? n / d : (uint32_t)n / (uint32_t)d));
+    }
+};
 
 // where keys and values of a lane's two places of a tile are, in elements
 struct few_places {
@@ -97,7 +110,8 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
     }
     const int heads = a.cache.heads;
     const int64_t total = starts[a.nreq] * heads;
-    const int64_t begin = few_begin(total, line.blocks, blockIdx.x), end = few_begin(total, line.blocks, blockIdx.x + 1);
+    const few_cut cut(total, line.blocks);
+    const int64_t begin = cut.begin(blockIdx.x), end = cut.begin(blockIdx.x + 1);
 
     for (int64_t at = begin; at < end;) {
         // the request and head at this place of the line
@@ -276,33 +290,50 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
     }
 }
 
-// Joins the parts of one row of one (request, head); D threads.
-template <class T, int D> __global__ __launch_bounds__(D) void kv_attention_few_join_kernel(attention_args a, few_line line) {
-    const int heads = a.cache.heads, r = blockIdx.x / heads, h = blockIdx.x - r * heads, m = blockIdx.y, d = threadIdx.x;
+// Joins the parts of one row of one (request, head): each wave sums up every JOIN_WAVES-th, then the waves are added, always in
+// the same order.
+constexpr int JOIN_WAVES = 8;
+template <class T, int D> __global__ __launch_bounds__(64 * JOIN_WAVES) void kv_attention_few_join_kernel(attention_args a, few_line line) {
+    __shared__ float sums[JOIN_WAVES][D], alls[JOIN_WAVES];
+    constexpr int E = (D + 63) / 64;
+    const int heads = a.cache.heads, r = blockIdx.x / heads, h = blockIdx.x - r * heads, m = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t start = line.starts_out[r], units = line.starts_out[r + 1] - start;
     if (units == 0 || m >= (int64_t)few_load(a, r).held * a.group) return;
-    const int64_t total = line.starts_out[a.nreq] * heads, from = start * heads + h * units, to = from + units;
-    int b = (int)(from * line.blocks / total);   // the block that holds unit `from`
-    while (b > 0 && few_begin(total, line.blocks, b) > from) --b;
-    while (few_begin(total, line.blocks, b + 1) <= from) ++b;
-    if (few_begin(total, line.blocks, b + 1) >= to) return;   // all in one block: done there
-    float top = NO_SCORE, all = 0.f, o = 0.f;
-    for (int64_t begin = few_begin(total, line.blocks, b); begin < to; ++b) {
-        const int64_t end = few_begin(total, line.blocks, b + 1);
-        if (end > begin) {
-            const int64_t row = ((int64_t)b * 2 + (begin >= from ? 0 : 1)) * FEW_ROWS + m;
-            const float ref = line.stats[2 * row], sum = line.stats[2 * row + 1], part = line.parts[row * D + d];
-            const float moved = fmaxf(top, ref), keep = __builtin_amdgcn_exp2f(top - moved), share = __builtin_amdgcn_exp2f(ref - moved);
-            all = all * keep + sum * share;
-            o = o * keep + part * share;
-            top = moved;
-        }
-        begin = end;
+    const few_cut cut(line.starts_out[a.nreq] * heads, line.blocks);
+    const int64_t from = start * heads + h * units, to = from + units;
+    const int first = cut.block_of(from), last = cut.block_of(to - 1);
+    if (first == last) return;   // all in one block: done there
+    // the part of block b: its first one, but where the (request, head) begins inside the block
+    auto slot = [&](int b) { return ((int64_t)b * 2 + (cut.begin(b) >= from ? 0 : 1)) * FEW_ROWS + m; };
+    float top = NO_SCORE;
+    for (int b = first + lane; b <= last; b += 64) top = fmaxf(top, line.stats[2 * slot(b)]);
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    float all = 0.f, o[E] = {};
+#pragma unroll 4
+    for (int b = first + wave; b <= last; b += JOIN_WAVES) {
+        const int64_t at = slot(b);
+        const float share = __builtin_amdgcn_exp2f(line.stats[2 * at] - top);
+        all += share * line.stats[2 * at + 1];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (D % 64 == 0 || e * 64 + lane < D) o[e] += share * line.parts[at * D + e * 64 + lane];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (D % 64 == 0 || e * 64 + lane < D) sums[wave][e * 64 + lane] = o[e];
+    if (lane == 0) alls[wave] = all;
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d >= D) return;
+    float total = 0.f, sum = 0.f;
+    for (int w = 0; w < JOIN_WAVES; ++w) {
+        total += alls[w];
+        sum += sums[w][d];
     }
     const int tok = (int)a.by_group.div((uint32_t)m);
     const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (m - tok * a.group);
-    ((T *)a.out)[at_row * D + d] = (T)(all != 0.f ? o / all : 0.f);
-    if (d == 0 && a.lse) a.lse[at_row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
+    ((T *)a.out)[at_row * D + d] = (T)(total != 0.f ? sum / total : 0.f);
+    if (d == 0 && a.lse) a.lse[at_row] = total != 0.f ? (top + log2f(total)) * LN2 : -INFINITY;
 }
 
 template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int max_new) {
@@ -319,7 +350,7 @@ template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args
     }
     kv_attention_few_kernel<T, D><<<line.blocks, FEW_THREADS, 0, ctx->stream>>>(a, line);
     const int rows = (int)(max_new * (int64_t)a.group < FEW_ROWS ? max_new * a.group : FEW_ROWS);
-    kv_attention_few_join_kernel<T, D><<<dim3(a.nreq * a.cache.heads, rows), D, 0, ctx->stream>>>(a, line);
+    kv_attention_few_join_kernel<T, D><<<dim3(a.nreq * a.cache.heads, rows), 64 * JOIN_WAVES, 0, ctx->stream>>>(a, line);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
