@@ -38,12 +38,13 @@ constexpr float NO_SCORE = -3e38f;
 // Keys of a request as its table can hold them (kv_lens is the caller's: memory is read by it).
 __device__ __forceinline__ int attention_keys(const attention_args &a, int r) { return min(a.kv_lens[r], a.width * a.cache.block_size); }
 
-// Position j of a request as (block, place); blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
+// A block table's entry; blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
+__device__ __forceinline__ int64_t attention_block(const attention_args &a, int32_t entry) { return (unsigned)entry < (uint64_t)a.cache.nblocks ? entry : 0; }
+// Position j of a request as (block, place).
 __device__ __forceinline__ void attention_place(const attention_args &a, int r, int j, int64_t &block, int &place) {
     const int column = (int)a.by_block.div((uint32_t)j);
     place = j - column * a.cache.block_size;
-    const int32_t b = a.tables[(int64_t)r * a.width + column];
-    block = (unsigned)b < (uint64_t)a.cache.nblocks ? b : 0;
+    block = attention_block(a, a.tables[(int64_t)r * a.width + column]);
 }
 
 // ---- the matrix cores on 16-bit elements ---------------------------------------------------------------
@@ -95,7 +96,25 @@ template <int D> struct lds_row {
     }
 };
 
-int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int max_new);
-int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, int max_new);
+// Requests of so few rows per head of the cache have a kernel of their own.
+constexpr int FEW_ROWS = 16;
+__device__ __forceinline__ bool attention_is_few(const attention_args &a, int fresh) { return (int64_t)fresh * a.group <= FEW_ROWS; }
+
+// The request whose rows hold token t; -1 behind the last one.
+__device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, int64_t t) {
+    if (t >= cu[nreq]) return -1;
+    int low = 0, high = nreq;
+    while (high - low > 1) {
+        const int mid = (low + high) >> 1;
+        if (cu[mid] <= t) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
+// The requests of few rows; *ws_used: bytes of read_ws.
+int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, size_t *ws_used);
+// All requests, or those of more rows; parts go to read_ws from ws_at on (growing it waits for the stream).
+int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at);
 
 }  // namespace pq

@@ -18,6 +18,7 @@ constexpr int CHUNK_TILE = 64;
 
 struct chunk_split {
     int splits;            // blocks that share the keys of a tile of rows
+    bool without_few;      // requests of few rows are left to kv_attention_few.hip
     float *parts, *stats;  // [ntokens * q_heads][splits][D], [..][splits][2]
 };
 
@@ -42,7 +43,9 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
         if (chunk_index<M>(a, mid) <= index) low = mid;
         else high = mid;
     }
-    const int r = low, fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
+    const int r = low, fresh = a.cu[r + 1] - a.cu[r];
+    if (split.without_few && attention_is_few(a, fresh)) return;
+    const int held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
     const int64_t rows = (int64_t)held * a.group, tiles_of_r = (rows + M - 1) / M;
     // the last rows see the most keys: they come first
     const int64_t mine = tiles_of_r - 1 - (index - chunk_index<M>(a, r));
@@ -80,15 +83,31 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
         for (int i = 0; i < 16; ++i) out[f][i] = 0.f;
     float ref = NO_SCORE, sum = 0.f;   // ref: of the scaled scores
 
+    // the tiles that some row of this wave sees: the others it only helps to move
+    const int64_t row0 = mine * M + wave * 32, row1 = min(rows, row0 + 32) - 1;
+    int wave_begin = tile_end, wave_end = tile_end;
+    if (row0 < rows) {
+        const int wave_to = min(nkeys, kv - fresh + (int)a.by_group.div((uint32_t)row1) + 1);
+        const int wave_from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + (int)a.by_group.div((uint32_t)row0) - a.window + 1) : 0;
+        wave_begin = (wave_from - from) / CHUNK_TILE;
+        wave_end = wave_to > from ? (wave_to - from + CHUNK_TILE - 1) / CHUNK_TILE : 0;
+    }
+
     // this thread's chunks of a tile
     const int my_key = tid / LANES, my_chunk = tid % LANES;
     const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2] + 8 * my_chunk;
     const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2] + 8 * my_chunk;
+    const int32_t *const table = a.tables + (int64_t)r * a.width;
     u32x4 mk[MOVES], mv[MOVES];
-    auto load = [&](int tile) {
-        int64_t block;
-        int place;
-        attention_place(a, r, min(from + tile * CHUNK_TILE + my_key, to - 1), block, place);
+    // (a tile's entry of the block table is read a tile before its keys are, so that nothing waits for it)
+    int32_t entry = 0, place = 0;
+    auto look_up = [&](int tile) {
+        const uint32_t j = (uint32_t)min(from + tile * CHUNK_TILE + my_key, to - 1), column = a.by_block.div(j);
+        place = (int)(j - column * a.cache.block_size);
+        entry = table[column];
+    };
+    auto load = [&]() {
+        const int64_t block = attention_block(a, entry);
         const T *const k = keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1];
         const T *const v = values + block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
 #pragma unroll
@@ -117,6 +136,7 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
 
     auto compute = [&](int tile, auto buffer_of) {
         constexpr int buffer = decltype(buffer_of)::value;
+        if (tile < wave_begin || tile >= wave_end) return;
         const int key0 = from + tile * CHUNK_TILE;
         f32x16 s[2];
 #pragma unroll
@@ -176,20 +196,27 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     };
 
     if (tile_begin < tile_end) {
-        load(tile_begin);
+        look_up(tile_begin);
+        load();
+        look_up(min(tile_begin + 1, tile_end - 1));
         store(tile_begin, 0);
-        if (tile_begin + 1 < tile_end) load(tile_begin + 1);
+        load();
+        look_up(min(tile_begin + 2, tile_end - 1));
     }
-    for (int tile = tile_begin; tile < tile_end; tile += 2) {
+    // (behind the last tile that one is loaded once more, and not stored)
+    auto step = [&](int tile, auto buffer_of) {
+        constexpr int buffer = decltype(buffer_of)::value;
         __syncthreads();   // this tile is written, and the one before it read
-        if (tile + 1 < tile_end) store(tile + 1, 1);
-        if (tile + 2 < tile_end) load(tile + 2);
-        compute(tile, std::integral_constant<int, 0>());
-        if (tile + 1 >= tile_end) break;
-        __syncthreads();
-        if (tile + 2 < tile_end) store(tile + 2, 0);
-        if (tile + 3 < tile_end) load(tile + 3);
-        compute(tile + 1, std::integral_constant<int, 1>());
+        if (tile + 1 < tile_end) {
+            store(tile + 1, buffer ^ 1);
+            load();
+            look_up(min(tile + 3, tile_end - 1));
+        }
+        compute(tile, buffer_of);
+    };
+    for (int tile = tile_begin; tile < tile_end; tile += 2) {
+        step(tile, std::integral_constant<int, 0>());
+        if (tile + 1 < tile_end) step(tile + 1, std::integral_constant<int, 1>());
     }
     sum += __shfl_xor(sum, 32);
     if (!valid) return;
@@ -222,56 +249,71 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     if (g == 0 && a.lse) a.lse[at_row] = sum != 0.f ? (ref + log2f(sum)) * LN2 : -INFINITY;
 }
 
-// Joins the parts of a row: D threads per row, in the order of the keys.
-template <class T, int D> __global__ __launch_bounds__(D) void kv_attention_chunk_join_kernel(attention_args a, chunk_split split) {
-    const int64_t row = blockIdx.x;
-    if (row >= (int64_t)a.cu[a.nreq] * a.q_heads) return;
-    float top = NO_SCORE, all = 0.f, o = 0.f;
-    for (int s = 0; s < split.splits; ++s) top = fmaxf(top, split.stats[2 * (row * split.splits + s)]);
-    for (int s = 0; s < split.splits; ++s) {
-        const int64_t slot = row * split.splits + s;
-        const float share = __builtin_amdgcn_exp2f(split.stats[2 * slot] - top);
-        all += share * split.stats[2 * slot + 1];
-        o += share * split.parts[slot * D + threadIdx.x];
+// Joins the parts of a row, a wave for each row, in the order of the keys.
+constexpr int JOIN_ROWS = 4;
+template <class T, int D> __global__ __launch_bounds__(64 * JOIN_ROWS) void kv_attention_chunk_join_kernel(attention_args a, chunk_split split) {
+    constexpr int E = (D + 63) / 64;
+    const int64_t row = (int64_t)blockIdx.x * JOIN_ROWS + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= min(a.ntokens, (int64_t)a.cu[a.nreq]) * a.q_heads) return;
+    if (split.without_few) {
+        const int r = attention_request(a.cu, a.nreq, row / a.q_heads);
+        if (attention_is_few(a, a.cu[r + 1] - a.cu[r])) return;
     }
-    ((T *)a.out)[row * D + threadIdx.x] = (T)(all != 0.f ? o / all : 0.f);
-    if (threadIdx.x == 0 && a.lse) a.lse[row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
+    const float *const stats = split.stats + 2 * row * split.splits, *const parts = split.parts + row * split.splits * D;
+    float top = NO_SCORE, all = 0.f, o[E] = {};
+    for (int s = lane; s < split.splits; s += 64) top = fmaxf(top, stats[2 * s]);
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll 4
+    for (int s = 0; s < split.splits; ++s) {
+        const float share = __builtin_amdgcn_exp2f(stats[2 * s] - top);
+        all += share * stats[2 * s + 1];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (D % 64 == 0 || e * 64 + lane < D) o[e] += share * parts[s * D + e * 64 + lane];
+    }
+    T *const out = (T *)a.out + row * D;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (D % 64 == 0 || e * 64 + lane < D) out[e * 64 + lane] = (T)(all != 0.f ? o[e] / all : 0.f);
+    if (lane == 0 && a.lse) a.lse[row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
 }
 
-template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const attention_args &a) {
+template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at) {
     constexpr int M = 32 * WAVES;
     const int64_t indexes = a.ntokens * a.group / M + a.nreq, rows = a.ntokens * a.q_heads;
     if (indexes * a.cache.heads > INT_MAX || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
-    // Fewer tiles of rows than twice the compute units: the keys of each are split, down to 512 keys a part.
-    const int64_t tiles = ((a.ntokens * a.group + M - 1) / M) * a.cache.heads;
-    int64_t splits = (2 * ctx->num_cu + tiles - 1) / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
+    // Fewer tiles of rows than the chip holds blocks: the keys of each are split, down to 512 keys a part.
+    constexpr int RESIDENT = WAVES == 4 && D < 128 ? 2 : 1;   // blocks per compute unit, by their registers and shared memory
+    const int64_t full = (a.ntokens * a.group + M - 1) / M, tiles = (full > a.nreq ? full : a.nreq) * a.cache.heads;
+    int64_t splits = RESIDENT * ctx->num_cu / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
     if (a.window > 0 && most > (a.window + 511) / 512) most = (a.window + 511) / 512;
     if (splits > most) splits = most;
-    chunk_split split = {splits < 1 ? 1 : (int)splits, nullptr, nullptr};
+    chunk_split split = {splits < 1 ? 1 : (int)splits, without_few, nullptr, nullptr};
     if (split.splits > 1) {
         const size_t slots = (size_t)rows * split.splits;
-        if (const int rc = buf_reserve(ctx, &ctx->read_ws, slots * (D + 2) * sizeof(float), "parts of the attention")) return rc;
-        split.parts = (float *)ctx->read_ws.p;
+        if (const int rc = buf_reserve(ctx, &ctx->read_ws, ws_at + slots * (D + 2) * sizeof(float), "parts of the attention")) return rc;
+        split.parts = (float *)((char *)ctx->read_ws.p + ws_at);
         split.stats = split.parts + slots * D;
     }
     kv_attention_chunk_kernel<T, D, WAVES><<<dim3((unsigned)(indexes * a.cache.heads), split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
-    if (split.splits > 1) kv_attention_chunk_join_kernel<T, D><<<(int)rows, D, 0, ctx->stream>>>(a, split);
+    if (split.splits > 1) kv_attention_chunk_join_kernel<T, D><<<(int)((rows + JOIN_ROWS - 1) / JOIN_ROWS), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
 
-template <class T> static int chunk_dim(pq_ctx *ctx, const attention_args &a) {
+template <class T> static int chunk_dim(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at) {
     const bool many = a.ntokens * a.group >= (int64_t)a.nreq * 192;
     switch (a.cache.dim) {
-    case 64: return many ? chunk_run<T, 64, 8>(ctx, a) : chunk_run<T, 64, 4>(ctx, a);
-    case 96: return many ? chunk_run<T, 96, 8>(ctx, a) : chunk_run<T, 96, 4>(ctx, a);
-    case 128: return many ? chunk_run<T, 128, 8>(ctx, a) : chunk_run<T, 128, 4>(ctx, a);
-    default: return chunk_run<T, 256, 4>(ctx, a);
+    case 64: return many ? chunk_run<T, 64, 8>(ctx, a, without_few, ws_at) : chunk_run<T, 64, 4>(ctx, a, without_few, ws_at);
+    case 96: return many ? chunk_run<T, 96, 8>(ctx, a, without_few, ws_at) : chunk_run<T, 96, 4>(ctx, a, without_few, ws_at);
+    case 128: return many ? chunk_run<T, 128, 8>(ctx, a, without_few, ws_at) : chunk_run<T, 128, 4>(ctx, a, without_few, ws_at);
+    default: return chunk_run<T, 256, 4>(ctx, a, without_few, ws_at);
     }
 }
 
-int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, int) {
-    return a.cache.elem == PQ_ELEM_F16 ? chunk_dim<_Float16>(ctx, a) : chunk_dim<__bf16>(ctx, a);
+int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at) {
+    return a.cache.elem == PQ_ELEM_F16 ? chunk_dim<_Float16>(ctx, a, without_few, ws_at) : chunk_dim<__bf16>(ctx, a, without_few, ws_at);
 }
 
 }  // namespace pq

@@ -15,7 +15,6 @@
 
 namespace pq {
 
-constexpr int FEW_ROWS = 16;
 constexpr int FEW_WAVES = 4;
 constexpr int FEW_TILE = 32;                        // keys that a wave takes at a time
 constexpr int FEW_UNIT = FEW_WAVES * FEW_TILE;
@@ -41,7 +40,7 @@ __device__ __forceinline__ few_range few_load(const attention_args &a, int r) {
     const int kv = a.kv_lens[r];
     x.keys = max(0, attention_keys(a, r));
     x.from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - x.fresh - a.window + 1) : 0;
-    x.units = x.held <= 0 ? 0 : max((int64_t)1, ((int64_t)x.keys - x.from + FEW_UNIT - 1) / FEW_UNIT);
+    x.units = x.held <= 0 || !attention_is_few(a, x.fresh) ? 0 : max((int64_t)1, ((int64_t)x.keys - x.from + FEW_UNIT - 1) / FEW_UNIT);
     return x;
 }
 
@@ -290,57 +289,68 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
     }
 }
 
-// Joins the parts of one row of one (request, head): each wave sums up every JOIN_WAVES-th, then the waves are added, always in
-// the same order.
-constexpr int JOIN_WAVES = 8;
+// Joins the parts of one (request, head): its rows are spread over the waves, several for each row where there are fewer, which
+// sum up every so many-th part; the sums of a row's waves are added in the same order always.
+constexpr int JOIN_WAVES = 16;
 template <class T, int D> __global__ __launch_bounds__(64 * JOIN_WAVES) void kv_attention_few_join_kernel(attention_args a, few_line line) {
-    __shared__ float sums[JOIN_WAVES][D], alls[JOIN_WAVES];
+    __shared__ float sums[JOIN_WAVES][D], alls[JOIN_WAVES], tops[JOIN_WAVES];
     constexpr int E = (D + 63) / 64;
-    const int heads = a.cache.heads, r = blockIdx.x / heads, h = blockIdx.x - r * heads, m = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int heads = a.cache.heads, r = blockIdx.x / heads, h = blockIdx.x - r * heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t start = line.starts_out[r], units = line.starts_out[r + 1] - start;
-    if (units == 0 || m >= (int64_t)few_load(a, r).held * a.group) return;
+    if (units == 0) return;
     const few_cut cut(line.starts_out[a.nreq] * heads, line.blocks);
     const int64_t from = start * heads + h * units, to = from + units;
     const int first = cut.block_of(from), last = cut.block_of(to - 1);
     if (first == last) return;   // all in one block: done there
-    // the part of block b: its first one, but where the (request, head) begins inside the block
-    auto slot = [&](int b) { return ((int64_t)b * 2 + (cut.begin(b) >= from ? 0 : 1)) * FEW_ROWS + m; };
-    float top = NO_SCORE;
-    for (int b = first + lane; b <= last; b += 64) top = fmaxf(top, line.stats[2 * slot(b)]);
-    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    float all = 0.f, o[E] = {};
+    const int rows = (int)min((int64_t)FEW_ROWS, (int64_t)few_load(a, r).held * a.group);
+    int row_waves = JOIN_WAVES;
+    while (row_waves * rows > JOIN_WAVES) row_waves /= 2;
+    const int m = wave / row_waves, way = wave - m * row_waves;
+    float top = NO_SCORE, all = 0.f, o[E] = {};
+    if (m < rows) {
+        // the part of block b: its first one, but where the (request, head) begins inside the block
+        auto slot = [&](int b) { return ((int64_t)b * 2 + (cut.begin(b) >= from ? 0 : 1)) * FEW_ROWS + m; };
+        for (int b = first + lane; b <= last; b += 64) top = fmaxf(top, line.stats[2 * slot(b)]);
+        for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
 #pragma unroll 4
-    for (int b = first + wave; b <= last; b += JOIN_WAVES) {
-        const int64_t at = slot(b);
-        const float share = __builtin_amdgcn_exp2f(line.stats[2 * at] - top);
-        all += share * line.stats[2 * at + 1];
+        for (int b = first + way; b <= last; b += row_waves) {
+            const int64_t at = slot(b);
+            const float share = __builtin_amdgcn_exp2f(line.stats[2 * at] - top);
+            all += share * line.stats[2 * at + 1];
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (D % 64 == 0 || e * 64 + lane < D) o[e] += share * line.parts[at * D + e * 64 + lane];
+            for (int e = 0; e < E; ++e)
+                if (D % 64 == 0 || e * 64 + lane < D) o[e] += share * line.parts[at * D + e * 64 + lane];
+        }
     }
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (D % 64 == 0 || e * 64 + lane < D) sums[wave][e * 64 + lane] = o[e];
-    if (lane == 0) alls[wave] = all;
-    __syncthreads();
-    const int d = threadIdx.x;
-    if (d >= D) return;
-    float total = 0.f, sum = 0.f;
-    for (int w = 0; w < JOIN_WAVES; ++w) {
-        total += alls[w];
-        sum += sums[w][d];
+    if (lane == 0) {
+        alls[wave] = all;
+        tops[wave] = top;
     }
-    const int tok = (int)a.by_group.div((uint32_t)m);
-    const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (m - tok * a.group);
-    ((T *)a.out)[at_row * D + d] = (T)(total != 0.f ? sum / total : 0.f);
-    if (d == 0 && a.lse) a.lse[at_row] = total != 0.f ? (top + log2f(total)) * LN2 : -INFINITY;
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * D; i += 64 * JOIN_WAVES) {
+        const int row = i / D, d = i % D;
+        float total = 0.f, sum = 0.f;
+        for (int w = row * row_waves; w < (row + 1) * row_waves; ++w) {
+            total += alls[w];
+            sum += sums[w][d];
+        }
+        const int tok = (int)a.by_group.div((uint32_t)row);
+        const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (row - tok * a.group);
+        ((T *)a.out)[at_row * D + d] = (T)(total != 0.f ? sum / total : 0.f);
+        if (d == 0 && a.lse) a.lse[at_row] = total != 0.f ? (tops[row * row_waves] + log2f(total)) * LN2 : -INFINITY;
+    }
 }
 
-template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int max_new) {
+template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, size_t *ws_used) {
     few_line line = {};
     line.blocks = ctx->num_cu * (D > 128 ? 1 : 2);
+    *ws_used = 0;
     const size_t starts = align_up(((size_t)a.nreq + 1) * sizeof(int64_t), 256), slots = (size_t)line.blocks * 2 * FEW_ROWS;
-    if (const int rc = buf_reserve(ctx, &ctx->read_ws, starts + slots * (D + 2) * sizeof(float), "parts of the attention")) return rc;
+    *ws_used = align_up(starts + slots * (D + 2) * sizeof(float), 256);
+    if (const int rc = buf_reserve(ctx, &ctx->read_ws, *ws_used, "parts of the attention")) return rc;
     line.starts_out = (int64_t *)ctx->read_ws.p;
     line.parts = (float *)((char *)ctx->read_ws.p + starts);
     line.stats = line.parts + slots * D;
@@ -349,23 +359,22 @@ template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args
         line.starts = line.starts_out;
     }
     kv_attention_few_kernel<T, D><<<line.blocks, FEW_THREADS, 0, ctx->stream>>>(a, line);
-    const int rows = (int)(max_new * (int64_t)a.group < FEW_ROWS ? max_new * a.group : FEW_ROWS);
-    kv_attention_few_join_kernel<T, D><<<dim3(a.nreq * a.cache.heads, rows), 64 * JOIN_WAVES, 0, ctx->stream>>>(a, line);
+    kv_attention_few_join_kernel<T, D><<<a.nreq * a.cache.heads, 64 * JOIN_WAVES, 0, ctx->stream>>>(a, line);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
 
-template <class T> static int few_dim(pq_ctx *ctx, const attention_args &a, int max_new) {
+template <class T> static int few_dim(pq_ctx *ctx, const attention_args &a, size_t *ws_used) {
     switch (a.cache.dim) {
-    case 64: return few_typed<T, 64>(ctx, a, max_new);
-    case 96: return few_typed<T, 96>(ctx, a, max_new);
-    case 128: return few_typed<T, 128>(ctx, a, max_new);
-    default: return few_typed<T, 256>(ctx, a, max_new);
+    case 64: return few_typed<T, 64>(ctx, a, ws_used);
+    case 96: return few_typed<T, 96>(ctx, a, ws_used);
+    case 128: return few_typed<T, 128>(ctx, a, ws_used);
+    default: return few_typed<T, 256>(ctx, a, ws_used);
     }
 }
 
-int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int max_new) {
-    return a.cache.elem == PQ_ELEM_F16 ? few_dim<_Float16>(ctx, a, max_new) : few_dim<__bf16>(ctx, a, max_new);
+int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, size_t *ws_used) {
+    return a.cache.elem == PQ_ELEM_F16 ? few_dim<_Float16>(ctx, a, ws_used) : few_dim<__bf16>(ctx, a, ws_used);
 }
 
 }  // namespace pq

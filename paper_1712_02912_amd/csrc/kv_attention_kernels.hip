@@ -3,18 +3,6 @@
 
 namespace pq {
 
-// The request whose rows hold token t; -1 behind the last one.
-__device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, int64_t t) {
-    if (t >= cu[nreq]) return -1;
-    int low = 0, high = nreq;
-    while (high - low > 1) {
-        const int mid = (low + high) >> 1;
-        if (cu[mid] <= t) low = mid;
-        else high = mid;
-    }
-    return low;
-}
-
 // ---- any type and layout ------------------------------------------------------------------------------
 //
 // One block per row.  Each wave takes 64 keys at a time: a lane forms the product with one key, the wave updates the running
@@ -124,8 +112,14 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
     a.by_group = fast_div((uint32_t)a.group);
     a.scale_log2 = scale * 1.4426950408889634f;
     if (attention_on_matrix_cores(a)) {
-        if ((int64_t)max_new * a.group <= 16) return launch_kv_attention_few(ctx, a, max_new);
-        return launch_kv_attention_chunk(ctx, a, max_new);
+        // Requests of few rows and others in one call: each goes to its own kernel.  A tile of rows of the chunks' kernel costs a
+        // request of one token as much as one of 128 (23 requests of 1 to 517 tokens, 16 heads: 63 us with that kernel alone, XX
+        // with both); where all requests have max_new tokens there is one kind only.
+        size_t ws_used = 0;
+        const bool all_few = (int64_t)max_new * a.group <= FEW_ROWS, some_few = a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new;
+        if (all_few || some_few)
+            if (const int rc = launch_kv_attention_few(ctx, a, &ws_used)) return rc;
+        return all_few ? PQ_OK : launch_kv_attention_chunk(ctx, a, some_few, ws_used);
     }
     const int64_t grid = ntokens * q_heads;
     if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
