@@ -25,7 +25,7 @@ struct chunk_split {
 // Tiles of rows: request r owns the indexes from cu[r] * group / M + r on, which leaves it at least as many as it has tiles.
 template <int M> __device__ __forceinline__ int64_t chunk_index(const attention_args &a, int r) { return (int64_t)a.cu[r] * a.group / M + r; }
 
-template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
+template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
     typedef lds_row<D> row;
     constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
@@ -284,7 +284,7 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
     const int64_t indexes = a.ntokens * a.group / M + a.nreq, rows = a.ntokens * a.q_heads;
     if (indexes * a.cache.heads > INT_MAX || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
     // Fewer tiles of rows than the chip holds blocks: the keys of each are split, down to 512 keys a part.
-    constexpr int RESIDENT = WAVES == 4 && D < 128 ? 2 : 1;   // blocks per compute unit, by their registers and shared memory
+    constexpr int RESIDENT = WAVES == 4 && D <= 128 ? 2 : 1;   // blocks per compute unit, by their registers and shared memory
     const int64_t full = (a.ntokens * a.group + M - 1) / M, tiles = (full > a.nreq ? full : a.nreq) * a.cache.heads;
     int64_t splits = RESIDENT * ctx->num_cu / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
     if (a.window > 0 && most > (a.window + 511) / 512) most = (a.window + 511) / 512;
