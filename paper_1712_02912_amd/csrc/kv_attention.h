@@ -73,6 +73,29 @@ template <> struct mfma_of<__bf16> {
     }
 };
 
+// Whether one of eight elements is inf or NaN (the exponent's bits are all set).
+template <class T> __device__ __forceinline__ bool any_not_finite(u32x4 x) {
+    constexpr uint32_t e = __is_same(T, _Float16) ? 0x7c00u : 0x7f80u;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) found |= (x[i] & e) == e || (x[i] >> 16 & e) == e;
+    return found;
+}
+// The same eight with those as zeros.
+template <class T> __device__ __forceinline__ u32x4 finite_only(u32x4 x) {
+    constexpr uint32_t e = __is_same(T, _Float16) ? 0x7c00u : 0x7f80u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = ((x[i] & e) == e ? 0u : x[i] & 0xffffu) | ((x[i] >> 16 & e) == e ? 0u : x[i] & 0xffff0000u);
+    return x;
+}
+
+// Adds those of four elements of a row of values that are inf or NaN.
+template <class T, class V> __device__ __forceinline__ void add_not_finite(const T *v, V &out, int at) {
+    const elem_vec<T, 4> x = *(const elem_vec<T, 4> *)v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[at + e] += !(fabsf((float)x.v[e]) < INFINITY) ? (float)x.v[e] : 0.f;
+}
+
 // four elements of a column: lane 4 r + c of 16 gives the address of part c of row r, lane n gets column n of the four rows
 __device__ __forceinline__ uint2 read_transposed(const void *lds) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;

@@ -1,7 +1,7 @@
 // Attention of chunks of new tokens: bound by the matrix cores.
 //
 // A block holds 32 rows of queries per wave in registers (rows: token, head of the group, so the heads that share keys
-// share them here too) and walks over the keys in tiles of 64, which its waves read from shared memory.  Scores are formed
+// share them here too) and walks over the keys in tiles of 64 (32), which its waves read from shared memory.  Scores are formed
 // transposed, S^T = K Q^T, so a lane holds scores of one row only, its maximum and sum need no exchange between lanes in most
 // tiles, and the weights are, as they lie, the second operand of O^T = V^T P^T (the order of the keys within a product is
 // free: V's are read in the order that the scores have, transposed by the reads from shared memory).
@@ -14,8 +14,6 @@
 
 namespace pq {
 
-constexpr int CHUNK_TILE = 64;
-
 struct chunk_split {
     int splits;            // blocks that share the keys of a tile of rows
     bool without_few;      // requests of few rows are left to kv_attention_few.hip
@@ -25,13 +23,14 @@ struct chunk_split {
 // Tiles of rows: request r owns the indexes from cu[r] * group / M + r on, which leaves it at least as many as it has tiles.
 template <int M> __device__ __forceinline__ int64_t chunk_index(const attention_args &a, int r) { return (int64_t)a.cu[r] * a.group / M + r; }
 
-template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
+template <class T, int D, int WAVES, int TILE> __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
     typedef lds_row<D> row;
     constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
     // a thread moves chunks of 16 bytes of one key (and value) of a tile, every LANES-th from its own on
-    constexpr int LANES = THREADS / CHUNK_TILE, MOVES = (CHUNKS + LANES - 1) / LANES;
-    __shared__ __attribute__((aligned(16))) unsigned char lds_k[2][CHUNK_TILE * row::bytes], lds_v[2][CHUNK_TILE * row::bytes];
+    constexpr int LANES = THREADS / TILE, MOVES = (CHUNKS + LANES - 1) / LANES;
+    __shared__ __attribute__((aligned(16))) unsigned char lds_k[2][TILE * row::bytes], lds_v[2][TILE * row::bytes];
+    __shared__ int taken_out;   // values were (see below)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
 
     // heads vary fastest: blocks that read the same head's keys are on the same XCD where the heads are a multiple of eight
@@ -64,7 +63,7 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
     const int to = min(nkeys, kv - fresh + token1 + 1);
     const int from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + token0 - a.window + 1) : 0;
     const int all_from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + token1 - a.window + 1) : 0, all_to = min(nkeys, kv - fresh + token0 + 1);
-    const int tiles_all = to > from ? (to - from + CHUNK_TILE - 1) / CHUNK_TILE : 0;
+    const int tiles_all = to > from ? (to - from + TILE - 1) / TILE : 0;
     const int tile_begin = (int)((int64_t)tiles_all * part / split.splits), tile_end = (int)((int64_t)tiles_all * (part + 1) / split.splits);
 
     // (a negative scale is the queries' sign: scores are compared before they are scaled)
@@ -89,8 +88,8 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
     if (row0 < rows) {
         const int wave_to = min(nkeys, kv - fresh + (int)a.by_group.div((uint32_t)row1) + 1);
         const int wave_from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + (int)a.by_group.div((uint32_t)row0) - a.window + 1) : 0;
-        wave_begin = (wave_from - from) / CHUNK_TILE;
-        wave_end = wave_to > from ? (wave_to - from + CHUNK_TILE - 1) / CHUNK_TILE : 0;
+        wave_begin = (wave_from - from) / TILE;
+        wave_end = wave_to > from ? (wave_to - from + TILE - 1) / TILE : 0;
     }
 
     // this thread's chunks of a tile
@@ -102,7 +101,7 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
     // (a tile's entry of the block table is read a tile before its keys are, so that nothing waits for it)
     int32_t entry = 0, place = 0;
     auto look_up = [&](int tile) {
-        const uint32_t j = (uint32_t)min(from + tile * CHUNK_TILE + my_key, to - 1), column = a.by_block.div(j);
+        const uint32_t j = (uint32_t)min(from + tile * TILE + my_key, to - 1), column = a.by_block.div(j);
         place = (int)(j - column * a.cache.block_size);
         entry = table[column];
     };
@@ -118,7 +117,8 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
         }
     };
     auto store = [&](int tile, int buffer) {
-        const bool held = from + tile * CHUNK_TILE + my_key < to;
+        const int key0 = from + tile * TILE;
+        const bool held = key0 + my_key < to;
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
             const int chunk = my_chunk + LANES * i;
@@ -126,6 +126,17 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
             const int at = my_key * row::bytes + 16 * row::chunk(my_key, chunk);
             *(u32x4 *)(lds_k[buffer] + at) = mk[i];
             *(u32x4 *)(lds_v[buffer] + at) = held ? mv[i] : u32x4{0, 0, 0, 0};
+        }
+        // Values that some row does not see must not reach it as 0 times inf: where a tile has rows that do not see all of it,
+        // what is not finite is taken out, and added in the end to the rows that see it.
+        if ((key0 < all_from || key0 + TILE > all_to) && held) {
+#pragma unroll
+            for (int i = 0; i < MOVES; ++i) {
+                const int chunk = my_chunk + LANES * i;
+                if ((CHUNKS % LANES != 0 && chunk >= CHUNKS) || !any_not_finite<T>(mv[i])) continue;
+                *(u32x4 *)(lds_v[buffer] + my_key * row::bytes + 16 * row::chunk(my_key, chunk)) = finite_only<T>(mv[i]);
+                taken_out = 1;
+            }
         }
     };
     // Where this lane reads: key n of 32 and chunk g, key 4 g + (lane / 4) % 4 of 16 and its part of chunk pair 0.  Other chunks
@@ -137,20 +148,20 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
     auto compute = [&](int tile, auto buffer_of) {
         constexpr int buffer = decltype(buffer_of)::value;
         if (tile < wave_begin || tile >= wave_end) return;
-        const int key0 = from + tile * CHUNK_TILE;
-        f32x16 s[2];
+        const int key0 = from + tile * TILE;
+        f32x16 s[TILE / 32];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < TILE / 32; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
 #pragma unroll
         for (int t = 0; t < STEPS; ++t)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) s[j] = mfma_of<T>::m32(*(const u32x4 *)(lds_k[buffer] + (k_at ^ (32 * t)) + 32 * j * row::bytes), q[t], s[j]);
+            for (int j = 0; j < TILE / 32; ++j) s[j] = mfma_of<T>::m32(*(const u32x4 *)(lds_k[buffer] + (k_at ^ (32 * t)) + 32 * j * row::bytes), q[t], s[j]);
         // scores of this lane: keys 32 j + 8 (i / 4) + 4 g + i % 4 of the tile
-        if (key0 < all_from || key0 + CHUNK_TILE > all_to) {   // some row does not see some key
+        if (key0 < all_from || key0 + TILE > all_to) {   // some row does not see some key
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < TILE / 32; ++j)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = key0 + 32 * j + 8 * (i / 4) + 4 * g + i % 4;
@@ -159,7 +170,7 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
         }
         float high_score = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < TILE / 32; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i) high_score = fmaxf(high_score, s[j][i]);
         // (the reference moves only when a score passes it by 2^8, see kv_attention_few.hip)
@@ -171,14 +182,14 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
 #pragma unroll
             for (int f = 0; f < OUTS; ++f) out[f] *= shrink;
         }
-        float p[32];
+        float p[TILE / 2];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < TILE / 2; ++i) {
             p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale_log2, -ref));
             sum += p[i];
         }
 #pragma unroll
-        for (int b = 0; b < CHUNK_TILE / 16; ++b) {
+        for (int b = 0; b < TILE / 16; ++b) {
             const u32x4 weights = pack8<T>(p + 8 * b);
 #pragma unroll
             for (int f = 0; f < OUTS; ++f) {
@@ -195,6 +206,8 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
         }
     };
 
+    if (tid == 0) taken_out = 0;
+    __syncthreads();
     if (tile_begin < tile_end) {
         look_up(tile_begin);
         load();
@@ -217,6 +230,24 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D 
     for (int tile = tile_begin; tile < tile_end; tile += 2) {
         step(tile, std::integral_constant<int, 0>());
         if (tile + 1 < tile_end) step(tile + 1, std::integral_constant<int, 1>());
+    }
+    if (__builtin_amdgcn_readfirstlane(taken_out)) {
+        // (rare, and so without marks: all values of the tiles that some row does not see all of)
+        for (int tile = max(tile_begin, wave_begin); tile < min(tile_end, wave_end); ++tile) {
+            const int key0 = from + tile * TILE;
+            if (key0 >= all_from && key0 + TILE <= all_to) continue;
+            for (int key = key0; key < min(key0 + TILE, to); ++key) {
+                if ((uint32_t)(key - first_seen) >= seen) continue;
+                int64_t block;
+                int at;
+                attention_place(a, r, key, block, at);
+                const T *const v = (const T *)a.cache.values + h * a.cache.value_strides[2] + block * a.cache.value_strides[0] + at * a.cache.value_strides[1];
+#pragma unroll
+                for (int f = 0; f < OUTS; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) add_not_finite(v + 32 * f + 8 * i + 4 * g, out[f], 4 * i);
+            }
+        }
     }
     sum += __shfl_xor(sum, 32);
     if (!valid) return;
@@ -283,10 +314,10 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
     constexpr int M = 32 * WAVES;
     const int64_t indexes = a.ntokens * a.group / M + a.nreq, rows = a.ntokens * a.q_heads;
     if (indexes * a.cache.heads > INT_MAX || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
-    // Fewer tiles of rows than the chip holds blocks: the keys of each are split, down to 512 keys a part.
-    constexpr int RESIDENT = WAVES == 4 && D <= 128 ? 2 : 1;   // blocks per compute unit, by their registers and shared memory
+    // Fewer tiles of rows than twice the compute units: the keys of each are split, down to 512 keys a part.
+    constexpr int TILE = D > 128 ? 32 : 64;   // (of 256 dimensions, registers and shared memory hold half as many keys)
     const int64_t full = (a.ntokens * a.group + M - 1) / M, tiles = (full > a.nreq ? full : a.nreq) * a.cache.heads;
-    int64_t splits = RESIDENT * ctx->num_cu / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
+    int64_t splits = 2 * ctx->num_cu / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
     if (a.window > 0 && most > (a.window + 511) / 512) most = (a.window + 511) / 512;
     if (splits > most) splits = most;
     chunk_split split = {splits < 1 ? 1 : (int)splits, without_few, nullptr, nullptr};
@@ -296,7 +327,7 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
         split.parts = (float *)((char *)ctx->read_ws.p + ws_at);
         split.stats = split.parts + slots * D;
     }
-    kv_attention_chunk_kernel<T, D, WAVES><<<dim3((unsigned)(indexes * a.cache.heads), split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
+    kv_attention_chunk_kernel<T, D, WAVES, TILE><<<dim3((unsigned)(indexes * a.cache.heads), split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
     if (split.splits > 1) kv_attention_chunk_join_kernel<T, D><<<(int)((rows + JOIN_ROWS - 1) / JOIN_ROWS), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;

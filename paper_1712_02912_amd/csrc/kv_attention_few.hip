@@ -89,7 +89,7 @@ struct few_places {
     int64_t k[2], v[2];
 };
 
-template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_attention_few_kernel(attention_args a, few_line line) {
+template <class T, int D> __global__ __launch_bounds__(FEW_THREADS, D > 128 ? 1 : 2) void kv_attention_few_kernel(attention_args a, few_line line) {
     typedef lds_row<D> row;
     constexpr int STEPS = D / 32;   // products over the dimensions
     constexpr int OUTS = D / 16;    // tiles of the result
@@ -147,6 +147,7 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
 #pragma unroll
         for (int f = 0; f < OUTS; ++f) out[f] = f32x4{0.f, 0.f, 0.f, 0.f};
         float ref = NO_SCORE, sum = 0.f;
+        bool taken_out = false;
 
         const int tile0 = x.from + (int)first * FEW_UNIT + wave * FEW_TILE;   // this wave's first key; the next ones follow by units
         const int tiles = x.keys > tile0 ? (int)min(count, (int64_t)(x.keys - tile0 + FEW_UNIT - 1) / FEW_UNIT) : 0;
@@ -232,6 +233,19 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
                 for (int t = 0; t < STEPS; ++t)
                     *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = held ? v[j][t] : u32x4{0, 0, 0, 0};
             }
+            // (what is not finite and not seen by all rows is taken out, see kv_attention_chunk.hip)
+            if (!all_seen) {
+                bool found = false;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int t = 0; t < STEPS; ++t) {
+                        if (tile + 16 * j + n >= x.keys || !any_not_finite<T>(v[j][t])) continue;
+                        found = true;
+                        *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = finite_only<T>(v[j][t]);
+                    }
+                taken_out |= __any(found);
+            }
             if (i + 1 < tiles) {
                 load_v(next);
                 next = places(min(i + 2, tiles - 1));
@@ -250,6 +264,21 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS) void kv_atte
                 out[f] = mfma_of<T>::m16(vt, weights, out[f]);
             }
             __builtin_amdgcn_wave_barrier();
+        }
+        if (taken_out) {
+            for (int i = 0; i < tiles; ++i) {
+                const int tile = tile0 + i * FEW_UNIT;
+                if (tile + FEW_TILE - 1 <= kv - x.fresh && (a.window == 0 || tile >= (int64_t)kv - a.window)) continue;
+                for (int key = tile; key < min(tile + FEW_TILE, x.keys); ++key) {
+                    if ((uint32_t)(key - first_seen) >= seen) continue;
+                    int64_t block;
+                    int place;
+                    attention_place(a, r, key, block, place);
+                    const T *const row_v = values - 8 * g + block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
+#pragma unroll
+                    for (int f = 0; f < OUTS; ++f) add_not_finite(row_v + 16 * f + 4 * g, out[f], 0);
+                }
+            }
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);

@@ -337,6 +337,42 @@ def test_attention_ignores_what_no_row_sees(ctx, new, dtype, fill):
     check_attention(ctx, [new, new, 1], [new, 33 + new, 1], 4, 1, 128, dtype, block_size=64, fill=fill)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,window", [(3, 0), (3, 20), (70, 0), (70, 40), (300, 0), (300, 130)])
+def test_attention_of_numbers_that_are_none(ctx, dtype, dim, new, window):
+    """Keys and values of inf and NaN reach the rows that see them, and no other row of their chunk."""
+    r = np.random.default_rng(new + dim)
+    kv = [new + 150, new]
+    tables, keys, values = make_cache(r, kv, 2, dim, 16, dtype, np.nan, "plain")
+
+    def place(request, j):
+        return int(tables[request, j // 16]), j % 16
+    b, s = place(0, kv[0] - 2)
+    values[b, s, 0, 3] = float("nan")
+    b, s = place(0, kv[0] - new + 1)
+    values[b, s, 1, dim - 1] = float("inf")
+    b, s = place(0, 149)
+    values[b, s, 0, 40] = -float("inf")
+    b, s = place(1, new - 1)
+    keys[b, s, 1, 5] = float("nan")
+    b, s = place(0, kv[0] - 1)
+    keys[b, s, 0] = float("inf")
+    cu = np.array([0, new, 2 * new], np.int32)
+    q = dev(r.standard_normal((2 * new, 4, dim)), dtype)
+    out, lse = ctx.pq_kv_attention(q, keys, values, dev(tables), dev(cu), dev(np.array(kv, np.int32)), new, window=window)
+    with np.errstate(invalid="ignore"):
+        want, want_lse, spread = orc.attention(host(q), host(keys), host(values), tables, cu, np.array(kv), dim ** -0.5, window)
+    got, got_lse = host(out), host(lse)
+    fine = np.isfinite(want)
+    assert fine.mean() > 0.5 and not fine.all()
+    assert np.array_equal(np.isfinite(got), fine) and np.array_equal(np.isfinite(got_lse), np.isfinite(want_lse))
+    bound, fp32 = attention_bound(dtype, host(q), host(keys), spread, want, dim ** -0.5, max(kv), dim)
+    assert (np.abs(got - want)[fine] <= bound[fine]).all()
+    whole = np.isfinite(want_lse)
+    assert (np.abs(got_lse - want_lse)[whole] <= 2 * fp32 + 1e-6 * np.abs(want_lse[whole])).all()
+
+
 @pytest.mark.parametrize("new", [1, 33])
 def test_attention_of_sharp_scores(ctx, new):
     """Scores of some hundreds: one key takes all the weight, and running maxima jump."""
