@@ -123,6 +123,20 @@ template <int D> struct lds_row {
 constexpr int FEW_ROWS = 16;
 __device__ __forceinline__ bool attention_is_few(const attention_args &a, int fresh) { return (int64_t)fresh * a.group <= FEW_ROWS; }
 
+// The last of 0 ... n - 1 for which f holds; f holds from 0 up to there.  By a whole wave, 64 places at once, so that a
+// search of a few hundred takes two loads one after the other, not nine.
+template <class F> __device__ __forceinline__ int wave_search(int n, F f) {
+    const int lane = threadIdx.x & 63;
+    int low = 0;
+    while (n > 1) {
+        const int step = (n + 63) / 64, i = lane * step;
+        const int last = __popcll(__ballot(i < n && f(low + i))) - 1;
+        low += max(last, 0) * step;
+        n = min(step, n - max(last, 0) * step);
+    }
+    return __builtin_amdgcn_readfirstlane(low);
+}
+
 // The request whose rows hold token t; -1 behind the last one.
 __device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, int64_t t) {
     if (t >= cu[nreq]) return -1;

@@ -114,13 +114,7 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS, D > 128 ? 1 
 
     for (int64_t at = begin; at < end;) {
         // the request and head at this place of the line
-        int low = 0, high = a.nreq;
-        while (high - low > 1) {
-            const int mid = (low + high) >> 1;
-            if (starts[mid] * heads <= at) low = mid;
-            else high = mid;
-        }
-        const int r = low;
+        const int r = wave_search(a.nreq, [&](int i) { return starts[i] * heads <= at; });
         const few_range x = few_load(a, r);
         const int64_t in_request = at - starts[r] * heads;
         const int h = (int)(in_request / x.units);
