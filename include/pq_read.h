@@ -104,7 +104,7 @@ int pq_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, in
  *   -> tokens [rows] i64; logprobs [rows] f32 = log of the token's share of the weights that stay (0 for temperature <= 0),
  *      may be NULL.
  * Logits of -inf and NaN are never drawn; a row that holds nothing else gives token -1, logprob -inf.  If some are +inf,
- * those share the weight.  Weights of less than 2^-95 of the largest count as 0.  Requires vocab < 2^20. */
+ * those share the weight.  Weights of less than 2^-60 of the largest may count as 0.  Requires vocab < 2^20. */
 int pq_sample_tokens(pq_ctx *ctx, const void *logits, pq_elem elem, int64_t row_stride, int rows, int vocab, const float *noise,
                      int64_t noise_stride, const float *temperature, const int32_t *top_k, const float *top_p,
                      const float *min_p, int64_t *tokens, float *logprobs);

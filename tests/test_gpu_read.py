@@ -452,6 +452,9 @@ def check_sample(ctx, logits, noise, temperature=None, top_k=None, top_p=None, m
     for r in range(rows):
         args = [np.float64(np.float32(d if v is None else v[r])) for v, d in ((temperature, 1.0), (top_k, 0), (top_p, 1.0), (min_p, 0.0))]
         token, logprob, scores, margin = orc.sample(l[r], None if u is None else u[r], args[0], int(args[1]), args[2], args[3])
+        if u is not None and np.isnan(u[r]).all():          # noise that is no number: some token of those that stay
+            assert tokens[r] in scores or not scores
+            continue
         if tokens[r] != token:
             # only where two scores are as near as fp32 rounds them (x and the logarithms: a few units of numbers up to 100)
             assert tokens[r] in scores and scores[token] - scores[int(tokens[r])] < 2e-5, (r, token, tokens[r])
@@ -486,6 +489,24 @@ def test_sample_one_filter(ctx, dtype, case):
     r = np.random.default_rng(7)
     logits, noise = rows_of(r, 9, 40007, dtype, 2.0)
     check_sample(ctx, logits, noise, **{k: [v] * 9 for k, v in case.items()})
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [3, 70])
+def test_sample_of_large_vocabularies(ctx, dtype, rows):
+    """Rows whose last pass is shared by several blocks, beside others."""
+    r = np.random.default_rng(rows)
+    vocab = 70001
+    logits, noise = rows_of(r, rows, vocab, dtype, 1.5)
+    logits[1, :vocab // 2] = -2.0                              # a bin of more tokens than are listed
+    logits[2, vocab - 9:] = float("inf") if dtype == F32 else 900.0
+    logits[0, 60000] = 60.0
+    pick = lambda *choices: [choices[i] for i in r.integers(0, len(choices), rows)]   # noqa: E731
+    check_sample(ctx, logits, noise, pick(0.0, 0.8, 1.0, 2.0), pick(0, 0, 50, 20000), pick(0.5, 0.99, 0.999, 1.0), pick(0.0, 0.0, 1e-3))
+    check_sample(ctx, logits, noise, pick(0.0, 0.8, 1.0, 2.0))
+    check_sample(ctx, logits, noise, pick(0.8, 1.0), min_p=pick(0.0, 0.01, 2.0))
+    check_sample(ctx, logits, None, pick(0.8, 1.0), top_p=pick(0.9, 1.0))
+    check_sample(ctx, logits, torch.full_like(noise, float("nan")))
 
 
 @pytest.mark.parametrize("dtype", [F32, F16])
