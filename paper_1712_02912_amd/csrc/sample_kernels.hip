@@ -191,25 +191,36 @@ template <class T> struct sample_row {
     }
     // f(first index, logits) for the vectors, g(index, logit) for the few others; two vectors are on their way at a time.
     // `rest`: without the first look.
-    template <class F, class G> __device__ __forceinline__ void each_vector(bool rest, F f, G g) {
-        auto take = [&](const vec &l, int i) {
+    // With `beside`, f's third argument is the noise of the vector, read together with it.
+    struct __attribute__((packed, aligned(4))) noises { float v[SAMPLE_V]; };
+    template <class F, class G> __device__ __forceinline__ void each_vector(bool rest, bool beside, F f, G g) {
+        auto take = [&](const vec &l, const noises &u, int i) {
             float x[SAMPLE_V];
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) x[e] = (float)l.v[e];
-            f(i, x);
+            f(i, x, u);
         };
         int i = before + threadIdx.x * SAMPLE_V + (rest ? STEP : 0);
         for (; i + STEP < whole; i += 2 * STEP) {
             const vec p = *(const vec *)(row + i), q = *(const vec *)(row + i + STEP);
-            take(p, i);
-            take(q, i + STEP);
+            noises up, uq;
+            if (beside) {
+                up = *(const noises *)(noise + i);
+                uq = *(const noises *)(noise + i + STEP);
+            }
+            take(p, up, i);
+            take(q, uq, i + STEP);
         }
-        if (i < whole) take(*(const vec *)(row + i), i);
+        if (i < whole) {
+            noises u;
+            if (beside) u = *(const noises *)(noise + i);
+            take(*(const vec *)(row + i), u, i);
+        }
         const int t = (int)threadIdx.x < head ? (int)threadIdx.x : tail + (int)threadIdx.x - head;
         if (t < a.vocab) g(t, (float)row[t]);
     }
     template <class F> __device__ __forceinline__ void each(F f) {
-        each_vector(false, [&](int i, const float (&l)[SAMPLE_V]) {
+        each_vector(false, false, [&](int i, const float (&l)[SAMPLE_V], const noises &) {
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) f(i + e, l[e]);
         }, f);
@@ -257,10 +268,25 @@ template <class T> struct sample_row {
         if (a.logprobs) a.logprobs[r] = logprob;
     }
 
+    // The key of the largest logit (NaN reads as -inf): vectors that hold nothing larger than before are passed over.
     __device__ __forceinline__ uint64_t first_key() {
-        uint64_t first = KEY_EMPTY;
-        each([&](int i, float l) { first = min(first, sample_key(fmaxf(l, -INFINITY), i)); });   // (NaN reads as -inf)
-        return block_min(first);
+        float high = -INFINITY;
+        int at = SAMPLE_NONE;
+        auto take = [&](int i, float l) {
+            if (l > high || (l == high && i < at)) {
+                high = l;
+                at = i;
+            }
+        };
+        each_vector(false, false, [&](int i, const float (&l)[SAMPLE_V], const noises &) {
+            float most = l[0];
+#pragma unroll
+            for (int e = 1; e < SAMPLE_V; ++e) most = fmaxf(most, l[e]);
+            if (!(most > high)) return;
+#pragma unroll
+            for (int e = 0; e < SAMPLE_V; ++e) take(i + e, l[e]);
+        }, take);
+        return block_min(sample_key(high, at));
     }
 
     // the best of a thread's race: largest w / e, then smallest index
@@ -295,21 +321,23 @@ template <class T> struct sample_row {
     // Race over the row (or this part): tokens with y of at least `upper` and `least` stay; those from `lower` to below `upper`, which
     // are the bin of the cut, all go into the list (there is room; `cut` KEY_EMPTY), or stay if their key is not behind `cut`
     // (and y at least `least`).  Returns the largest y.
+    // many: of most vectors some token stays, so that their noise is read beside them, not after them.
     // A bound on the winner, w / e, is found first, on the first look: e = -log u is at most (1 - u) / u.
-    __device__ __forceinline__ float draw(const sample_scale &s, float upper, float lower, float least, uint64_t cut, race &best, double &mass) {
-        struct __attribute__((packed, aligned(4))) noises { float v[SAMPLE_V]; };
+    __device__ __forceinline__ float draw(const sample_scale &s, float upper, float lower, float least, uint64_t cut, bool many, race &best, double &mass) {
         const float edge = fmaxf(upper, least);
         float high = -INFINITY, sum[SAMPLE_V] = {};
         auto weight = [&](float y) { return y >= edge ? s.weight(y) : 0.f; };
-        auto border = [&](int i, float l) {   // a token of the cut's bin
+        auto border = [&](int i) {   // a token of the cut's bin (indexes first, in the place of the keys)
             if (cut == KEY_EMPTY) {
-                sh.list[atomicAdd(&sh.nlist, 1u)] = sample_key(l, i);
-            } else if (sample_key(l, i) <= cut && s.y(l) >= least) {
-                const float w = s.weight(s.y(l));
-                sum[0] += w;
-                if (noise) best.enter(w, noise[i], i);
-                else best.enter_certain(w, i);
+                sh.list[atomicAdd(&sh.nlist, 1u)] = (uint32_t)i;
+                return;
             }
+            const float l = (float)row[i], y = s.y(l);
+            if (sample_key(l, i) > cut || !(y >= least)) return;
+            const float w = s.weight(y);
+            sum[0] += w;
+            if (noise) best.enter(w, noise[i], i);
+            else best.enter_certain(w, i);
         };
         float bounded = 0.f;
         const int first = before + threadIdx.x * SAMPLE_V;
@@ -324,10 +352,8 @@ template <class T> struct sample_row {
             sh.nlist = 0;
         }
         __syncthreads();
-        const bool all_stay = upper < SAMPLE_LEAST;   // noise is read beside the logits, not after them
-        each_vector(false, [&](int i, const float (&l)[SAMPLE_V]) {
-            noises u;
-            if (noise && all_stay) u = *(const noises *)(noise + i);
+        many = many && noise;
+        each_vector(false, many, [&](int i, const float (&l)[SAMPLE_V], noises u) {
             float w[SAMPLE_V], most = -INFINITY;
             uint32_t which = 0;
 #pragma unroll
@@ -339,10 +365,7 @@ template <class T> struct sample_row {
                 which |= (uint32_t)(y >= lower && y < upper) << e;
             }
             high = fmaxf(high, most);
-            for (; which; which &= which - 1) {
-                const int e = __ffs(which) - 1;
-                border(i + e, (float)row[i + e]);
-            }
+            for (; which; which &= which - 1) border(i + __ffs(which) - 1);
             if (!(most >= edge)) return;
             if (!noise) {
 #pragma unroll
@@ -350,7 +373,7 @@ template <class T> struct sample_row {
                     if (w[e] > 0.f) best.enter_certain(w[e], i + e);
                 return;
             }
-            if (!all_stay) u = *(const noises *)(noise + i);
+            if (!many) u = *(const noises *)(noise + i);
             const float so_far = __uint_as_float(__hip_atomic_load(&sh.best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
             bool wins = false;
 #pragma unroll
@@ -364,14 +387,24 @@ template <class T> struct sample_row {
             const float y = s.y(l), w = weight(y);
             high = fmaxf(high, y);
             sum[0] += w;
-            if (y >= lower && y < upper) border(i, l);
+            if (y >= lower && y < upper) border(i);
             if (!(w > 0.f)) return;
             if (noise) best.enter(w, noise[i], i);
             else best.enter_certain(w, i);
         });
 #pragma unroll
         for (int e = 0; e < SAMPLE_V; ++e) mass += (double)sum[e];
-        return block_max(high);
+        high = block_max(high);
+        if (cut == KEY_EMPTY) list_keys(sh.nlist);
+        return high;
+    }
+    // The list's n indexes become keys.
+    __device__ __forceinline__ void list_keys(uint32_t n) {
+        for (uint32_t i = threadIdx.x; i < n; i += SAMPLE_THREADS) {
+            const int at = (int)sh.list[i];
+            sh.list[i] = sample_key((float)row[at], at);
+        }
+        __syncthreads();
     }
     // The race on the list's keys up to `cut`.  Returns their weights that stay, summed as whole numbers (the keys are in no
     // order); top: the largest y.
@@ -434,7 +467,7 @@ template <class T> struct sample_row {
             for (int e = 0; e < SAMPLE_V; ++e) most = fmaxf(most, y[e] = s.y(look[e]));
             list(first, y, most);
         }
-        each_vector(true, [&](int i, const float (&l)[SAMPLE_V]) {
+        each_vector(true, false, [&](int i, const float (&l)[SAMPLE_V], const noises &) {
             float y[SAMPLE_V], most = -INFINITY;
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) {
@@ -454,13 +487,8 @@ template <class T> struct sample_row {
             }
         });
         top = block_max(high);
-        const uint32_t n = min(sh.nlist, (uint32_t)SAMPLE_LIST);
-        for (uint32_t i = tid; i < n; i += SAMPLE_THREADS) {
-            const int at = (int)sh.list[i];
-            sh.list[i] = sample_key((float)row[at], at);
-        }
         listed = sh.nlist <= SAMPLE_LIST ? last : -1;
-        __syncthreads();
+        if (listed >= 0) list_keys(sh.nlist);
     }
 
     // The bin in which a limit is reached, counting from c, m before the bins: the bin (SAMPLE_BINS: it is not reached), and
@@ -700,7 +728,7 @@ template <class T> struct sample_row {
             const float lower = cut_bin < SAMPLE_BINS ? (float)(SAMPLE_ABOVE - 1 - cut_bin) * 0.0625f : -INFINITY;
             const float upper = cut_bin < SAMPLE_BINS ? lower + 0.0625f : -INFINITY;
             for (int round = 0; round < 2; ++round) {   // (the second with the largest logit for the reference)
-                const float high = draw(s, upper, lower, least, later ? KEY_EMPTY : cut, best, mass);
+                const float high = draw(s, upper, lower, least, later ? KEY_EMPTY : cut, cut_bin >= SAMPLE_BINS || c > (uint32_t)a.vocab / 32, best, mass);
                 if (high <= SAMPLE_TOP || round == 1) break;
                 s = sample_scale(largest(), inv);
                 best = race();
@@ -738,7 +766,7 @@ template <class T> struct sample_row {
         if (ref > -INFINITY) {
             part_of_row(part, parts);
             load_look();
-            high = draw(sample_scale(ref, 1.f / t), -INFINITY, -INFINITY, SAMPLE_LEAST, 0, best, mass);
+            high = draw(sample_scale(ref, 1.f / t), -INFINITY, -INFINITY, SAMPLE_LEAST, 0, true, best, mass);
         }
         mass = block_sum(mass);
         const uint64_t key = winner(best);
