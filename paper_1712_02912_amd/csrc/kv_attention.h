@@ -4,19 +4,9 @@
 
 #include "elem.h"
 #include "pq_internal.h"
+#include "wave_sums.h"
 
 namespace pq {
-
-// n / d for 0 <= n < 2^31, as a product
-struct fast_div {
-    uint32_t d, mul, shift;
-    fast_div() = default;
-    explicit fast_div(uint32_t by) : d(by), shift(0) {
-        while (((uint64_t)1 << shift) < by) ++shift;
-        mul = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - by)) / by + 1);
-    }
-    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(mul, n) + n) >> shift; }
-};
 
 struct attention_args {
     pq_kv_cache cache;

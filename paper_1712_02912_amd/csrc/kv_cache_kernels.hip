@@ -3,6 +3,7 @@
 
 #include "elem.h"
 #include "pq_internal.h"
+#include "wave_sums.h"
 
 namespace pq {
 
@@ -12,122 +13,111 @@ namespace pq {
 // bisection.  A fresh block begins with a new token, so the thread of that token also writes the block's entry in the
 // table; tokens of fresh blocks take the block from free_blocks, never from the table, so no thread reads what another
 // one writes.  There is next to nothing to move (12 bytes a token); what counts is that it is one launch: every block
-// forms the sums for itself (PLAN_MAX requests: 8 per thread, a few thousand cycles), rather than wait for another kernel.
-constexpr int PLAN_THREADS = 512;
+// forms the sums for itself (PLAN_MAX requests: four rounds of its threads), rather than wait for another kernel.
+constexpr int PLAN_THREADS = 1024;
 constexpr int PLAN_MAX = 4096;   // requests whose sums a block keeps in shared memory
+static_assert(PLAN_THREADS / 64 == 16, "the waves' sums are joined by one row of 16 lanes");
 
 struct plan_args {
     const int32_t *new_lens, *cached_lens;
     int32_t *tables;
     const int32_t *free_blocks;
-    int nreq, width, nfree, block_size;
+    int nreq, width, nfree;
+    fast_div by_block;
     int64_t ntokens;
     int32_t *cu, *kv, *positions;
     int64_t *slots;
     int32_t *taken;
 };
-
-struct plan_request {
-    int64_t fresh_tokens, cached, need;
-    bool fits;
+// of every request: tokens and needed blocks before it (one more of each behind the last), its cached tokens or -1 (refused)
+struct plan_sums {
+    int32_t *tokens, *blocks, *cached;
 };
-__device__ __forceinline__ plan_request plan_load(const plan_args &a, int r) {
-    plan_request p;
-    p.fresh_tokens = max(a.new_lens[r], 0);
-    p.cached = max(a.cached_lens[r], 0);
-    const int64_t b = a.block_size, have = (p.cached + b - 1) / b, full = (p.cached + p.fresh_tokens + b - 1) / b;
-    p.fits = full <= a.width;
-    p.need = p.fits ? full - have : 0;
-    return p;
-}
-__device__ __forceinline__ int32_t clamp_i32(int64_t x) { return (int32_t)min(x, (int64_t)INT_MAX); }
-__device__ __forceinline__ bool plan_served(const plan_args &a, const plan_request &p, int64_t tokens_to, int64_t blocks_to) {
-    return p.fits && blocks_to <= a.nfree && tokens_to <= a.ntokens;
+
+__device__ __forceinline__ int32_t clamp_i32(uint64_t x) { return (int32_t)min(x, (uint64_t)INT_MAX); }
+// ceil(n / block) for 0 <= n < 2^31
+__device__ __forceinline__ uint32_t plan_blocks(const plan_args &a, uint32_t n) {
+    const uint32_t q = a.by_block.div(n);
+    return q + (q * a.by_block.d < n);
 }
 
-// Sums of new tokens and needed blocks up to every request, as [nreq + 1] each with 0 in front, by one block; the block
-// that `writes` also writes the results that belong to requests.
-__device__ void plan_sums(const plan_args &a, int32_t *cu, int32_t *blocks, bool writes) {
-    __shared__ int64_t wave_sum[2][PLAN_THREADS / 64];
+// The sums, by one block; the block that `writes` also writes the results that belong to requests.
+__device__ __forceinline__ void plan_add_up(const plan_args &a, const plan_sums &x, bool writes) {
+    __shared__ uint64_t wave_sum[2][2][16];
     __shared__ int taken;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int64_t carry_t = 0, carry_b = 0;
-    int mine = 0;
-    if (tid == 0) cu[0] = blocks[0] = taken = 0;
-    for (int base = 0; base < a.nreq; base += PLAN_THREADS) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint64_t carry_t = 0, carry_b = 0;
+    int mine = 0, turn = 0;
+    if (tid == 0) x.tokens[0] = x.blocks[0] = taken = 0;
+    for (int base = 0; base < a.nreq; base += PLAN_THREADS, turn ^= 1) {
         const int r = base + tid;
-        plan_request p = {0, 0, 0, false};
-        if (r < a.nreq) p = plan_load(a, r);
-        int64_t t = p.fresh_tokens, b = p.need;
-        for (int d = 1; d < 64; d *= 2) {
-            const int64_t tt = __shfl_up(t, d), bb = __shfl_up(b, d);
-            if (lane >= d) {
-                t += tt;
-                b += bb;
-            }
-        }
-        if (lane == 63) {
-            wave_sum[0][wave] = t;
-            wave_sum[1][wave] = b;
-        }
-        __syncthreads();
-        t += carry_t;
-        b += carry_b;
-        for (int w = 0; w < PLAN_THREADS / 64; ++w) {
-            const int64_t st = wave_sum[0][w], sb = wave_sum[1][w];
-            if (w < wave) {
-                t += st;
-                b += sb;
-            }
-            carry_t += st;
-            carry_b += sb;
-        }
+        uint32_t fresh = 0, cached = 0, need = 0;
+        bool fits = false;
         if (r < a.nreq) {
-            cu[r + 1] = clamp_i32(t);
-            blocks[r + 1] = clamp_i32(b);
-            if (writes) {
-                const bool served = plan_served(a, p, t, b);
-                if (a.cu != cu) a.cu[r + 1] = clamp_i32(t);
-                a.kv[r] = served ? (int32_t)(p.cached + p.fresh_tokens) : -1;
-                if (served) mine += (int)p.need;
-            }
+            fresh = (uint32_t)max(a.new_lens[r], 0);
+            cached = (uint32_t)max(a.cached_lens[r], 0);
+            const uint32_t all = fresh + cached;   // (below 2^32)
+            const uint32_t full = all <= INT_MAX ? plan_blocks(a, all) : UINT_MAX;
+            fits = full <= (uint32_t)a.width;
+            need = fits ? full - plan_blocks(a, cached) : 0;
+        }
+        uint64_t t = wave_scan<op_add>((uint64_t)fresh), b = wave_scan<op_add>((uint64_t)need);
+        if (lane == 63) {
+            wave_sum[turn][0][wave] = t;
+            wave_sum[turn][1][wave] = b;
         }
         __syncthreads();
+        const uint64_t tw = row_scan<op_add>(wave_sum[turn][0][lane & 15]) + carry_t, bw = row_scan<op_add>(wave_sum[turn][1][lane & 15]) + carry_b;
+        t += wave > 0 ? read_lane(tw, wave - 1) : carry_t;
+        b += wave > 0 ? read_lane(bw, wave - 1) : carry_b;
+        carry_t = read_lane(tw, 15);
+        carry_b = read_lane(bw, 15);
+        if (r < a.nreq) {
+            const bool served = fits && b <= (uint64_t)a.nfree && t <= (uint64_t)a.ntokens;
+            x.tokens[r + 1] = clamp_i32(t);
+            x.blocks[r + 1] = clamp_i32(b);
+            x.cached[r] = served ? (int32_t)cached : -1;
+            if (writes) {
+                if (a.cu != x.tokens) a.cu[r + 1] = clamp_i32(t);
+                a.kv[r] = served ? (int32_t)(cached + fresh) : -1;
+                if (served) mine += (int)need;
+            }
+        }
     }
+    __syncthreads();
     if (writes) {
         if (mine) atomicAdd(&taken, mine);   // (whole numbers: the order does not matter)
         __syncthreads();
         if (tid == 0) {
-            if (a.cu != cu) a.cu[0] = 0;
+            if (a.cu != x.tokens) a.cu[0] = 0;
             *a.taken = taken;
         }
     }
-    __syncthreads();
 }
 
-__device__ void plan_token(const plan_args &a, const int32_t *cu, const int32_t *blocks, int64_t t) {
+__device__ __forceinline__ void plan_token(const plan_args &a, const plan_sums &x, int64_t t) {
     int32_t position = -1;
     int64_t slot = -1;
-    if (t < cu[a.nreq]) {
-        int low = 0, high = a.nreq;   // the request with cu[low] <= t < cu[low + 1]
+    if (t < x.tokens[a.nreq]) {
+        int low = 0, high = a.nreq;   // the request with tokens[low] <= t < tokens[low + 1]
         while (high - low > 1) {
             const int mid = (low + high) >> 1;
-            if (cu[mid] <= t) low = mid;
+            if (x.tokens[mid] <= t) low = mid;
             else high = mid;
         }
-        const plan_request p = plan_load(a, low);
-        if (plan_served(a, p, cu[low + 1], blocks[low + 1])) {
-            position = (int32_t)p.cached + (int32_t)(t - cu[low]);
-            const int b = a.block_size, column = position / b, have = (int)((p.cached + b - 1) / b);
+        const int32_t cached = x.cached[low];
+        if (cached >= 0) {
+            position = cached + (int32_t)(t - x.tokens[low]);
+            const int b = (int)a.by_block.d, column = (int)a.by_block.div((uint32_t)position), have = (int)plan_blocks(a, (uint32_t)cached);
             int32_t *entry = a.tables + (size_t)low * a.width + column;
             int32_t block;
             if (column < have) {
                 block = *entry;
             } else {
-                block = a.free_blocks[blocks[low] + column - have];
+                block = a.free_blocks[x.blocks[low] + column - have];
                 if (position == column * b) *entry = block;
             }
-            slot = (int64_t)block * b + position % b;
+            slot = (int64_t)block * b + (position - column * b);
         }
     }
     a.positions[t] = position;
@@ -135,33 +125,35 @@ __device__ void plan_token(const plan_args &a, const int32_t *cu, const int32_t 
 }
 
 __global__ __launch_bounds__(PLAN_THREADS) void kv_plan_kernel(plan_args a) {
-    __shared__ int32_t cu[PLAN_MAX + 1], blocks[PLAN_MAX + 1];
-    plan_sums(a, cu, blocks, blockIdx.x == 0);
+    __shared__ int32_t tokens[PLAN_MAX + 1], blocks[PLAN_MAX + 1], cached[PLAN_MAX];
+    const plan_sums x = {tokens, blocks, cached};
+    plan_add_up(a, x, blockIdx.x == 0);
     const int64_t step = (int64_t)gridDim.x * PLAN_THREADS;
-    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; t < a.ntokens; t += step) plan_token(a, cu, blocks, t);
+    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; t < a.ntokens; t += step) plan_token(a, x, t);
 }
 
 // more requests: the sums by one block first, then the tokens
-__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_sums_kernel(plan_args a, int32_t *blocks) { plan_sums(a, a.cu, blocks, true); }
-__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_tokens_kernel(plan_args a, const int32_t *blocks) {
+__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_sums_kernel(plan_args a, plan_sums x) { plan_add_up(a, x, true); }
+__global__ __launch_bounds__(PLAN_THREADS) void kv_plan_tokens_kernel(plan_args a, plan_sums x) {
     const int64_t step = (int64_t)gridDim.x * PLAN_THREADS;
-    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; t < a.ntokens; t += step) plan_token(a, a.cu, blocks, t);
+    for (int64_t t = (int64_t)blockIdx.x * PLAN_THREADS + threadIdx.x; t < a.ntokens; t += step) plan_token(a, x, t);
 }
 
 int launch_kv_plan(pq_ctx *ctx, const int32_t *new_lens, const int32_t *cached_lens, int nreq, int32_t *tables, int width,
                    const int32_t *free_blocks, int nfree, int block_size, int64_t ntokens, int32_t *cu, int32_t *kv,
                    int32_t *positions, int64_t *slots, int32_t *taken) {
-    const plan_args a = {new_lens, cached_lens, tables, free_blocks, nreq, width, nfree, block_size, ntokens, cu, kv, positions, slots, taken};
-    // one token per thread up to four blocks per compute unit, each of which forms the sums
+    const plan_args a = {new_lens, cached_lens, tables, free_blocks, nreq, width, nfree, fast_div((uint32_t)block_size), ntokens, cu, kv, positions, slots, taken};
+    // one token per thread up to two blocks per compute unit, each of which forms the sums
     const int64_t wanted = (ntokens + PLAN_THREADS - 1) / PLAN_THREADS;
-    const int grid = (int)(wanted < 1 ? 1 : wanted > 4 * ctx->num_cu ? 4 * ctx->num_cu : wanted);
+    const int grid = (int)(wanted < 1 ? 1 : wanted > 2 * ctx->num_cu ? 2 * ctx->num_cu : wanted);
     if (nreq <= PLAN_MAX) {
         kv_plan_kernel<<<grid, PLAN_THREADS, 0, ctx->stream>>>(a);
     } else {
-        const int rc = buf_reserve(ctx, &ctx->read_ws, ((size_t)nreq + 1) * sizeof(int32_t), "the plan of a paged cache");
+        const int rc = buf_reserve(ctx, &ctx->read_ws, 2 * ((size_t)nreq + 1) * sizeof(int32_t), "the plan of a paged cache");
         if (rc) return rc;
-        kv_plan_sums_kernel<<<1, PLAN_THREADS, 0, ctx->stream>>>(a, (int32_t *)ctx->read_ws.p);
-        kv_plan_tokens_kernel<<<grid, PLAN_THREADS, 0, ctx->stream>>>(a, (const int32_t *)ctx->read_ws.p);
+        const plan_sums x = {cu, (int32_t *)ctx->read_ws.p, (int32_t *)ctx->read_ws.p + nreq + 1};
+        kv_plan_sums_kernel<<<1, PLAN_THREADS, 0, ctx->stream>>>(a, x);
+        kv_plan_tokens_kernel<<<grid, PLAN_THREADS, 0, ctx->stream>>>(a, x);
     }
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;

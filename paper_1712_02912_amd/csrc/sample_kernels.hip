@@ -21,6 +21,7 @@
 #include "elem.h"
 #include "pq_internal.h"
 #include "topk_device.h"
+#include "wave_sums.h"
 
 namespace pq {
 
@@ -49,28 +50,6 @@ struct sample_args {
 __device__ __forceinline__ uint64_t sample_key(float l, int i) { return (uint64_t)(~f32_to_ord(l + 0.f)) << 32 | (uint32_t)i; }
 __device__ __forceinline__ float sample_key_logit(uint64_t key) { return ord_to_f32(~(uint32_t)(key >> 32)); }
 
-// ---- sums and minima over a wave and a block -----------------------------------------------------------
-template <int CTRL, int ROWS, class V> __device__ __forceinline__ V from_lane(V none, V v) {
-    if constexpr (sizeof(V) == 4) {
-        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
-    } else {
-        const int2 n = __builtin_bit_cast(int2, none), x = __builtin_bit_cast(int2, v);
-        return __builtin_bit_cast(V, int2{__builtin_amdgcn_update_dpp(n.x, x.x, CTRL, ROWS, 0xf, false),
-                                          __builtin_amdgcn_update_dpp(n.y, x.y, CTRL, ROWS, 0xf, false)});
-    }
-}
-template <class V> __device__ __forceinline__ V read_lane(V v, int lane) {
-    if constexpr (sizeof(V) == 4) {
-        return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
-    } else {
-        const int2 x = __builtin_bit_cast(int2, v);
-        return __builtin_bit_cast(V, int2{__builtin_amdgcn_readlane(x.x, lane), __builtin_amdgcn_readlane(x.y, lane)});
-    }
-}
-struct op_add {
-    template <class V> static __device__ __forceinline__ V none() { return V(0); }
-    template <class V> static __device__ __forceinline__ V of(V a, V b) { return a + b; }
-};
 struct op_min_u64 {
     template <class V> static __device__ __forceinline__ V none() { return KEY_EMPTY; }
     template <class V> static __device__ __forceinline__ V of(V a, V b) { return min(a, b); }
@@ -79,19 +58,6 @@ struct op_max {
     template <class V> static __device__ __forceinline__ V none() { return -INFINITY; }
     template <class V> static __device__ __forceinline__ V of(V a, V b) { return fmaxf(a, b); }
 };
-// every lane gets what the lanes up to and with it come to, within its row of 16
-template <class OP, class V> __device__ __forceinline__ V row_scan(V v) {
-    v = OP::template of<V>(v, from_lane<0x111, 0xf>(OP::template none<V>(), v));
-    v = OP::template of<V>(v, from_lane<0x112, 0xf>(OP::template none<V>(), v));
-    v = OP::template of<V>(v, from_lane<0x114, 0xf>(OP::template none<V>(), v));
-    return OP::template of<V>(v, from_lane<0x118, 0xf>(OP::template none<V>(), v));
-}
-template <class OP, class V> __device__ __forceinline__ V wave_scan(V v) {
-    v = row_scan<OP>(v);
-    v = OP::template of<V>(v, from_lane<0x142, 0xa>(OP::template none<V>(), v));
-    return OP::template of<V>(v, from_lane<0x143, 0xc>(OP::template none<V>(), v));
-}
-
 struct sample_shared {
     unsigned long long bins[SAMPLE_BINS], fine[SAMPLE_BINS];
     unsigned long long list[SAMPLE_LIST], last[64];
