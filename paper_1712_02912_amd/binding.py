@@ -9,9 +9,13 @@ fallback.
 """
 import ctypes
 import os
-import struct
 
 import torch
+
+try:
+    from paper_1712_02912_amd import tensor_views as _views
+except ImportError:   # not built: load() says so
+    _views = None
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpqadc.so")
@@ -25,8 +29,6 @@ EXPORTS = ["pq_create", "pq_destroy", "pq_last_error", "pq_version", "pq_build_l
            "pq_qmax_prescan", "pq_adc_scan_topk", "pq_rerank_f32", "ivf_adc_search", "pq_encode", "pq_rotate", "pq_derived_search", "pq_set_profiling",
            "pq_last_scan_kernel_ms", "pq_calibration_copy", "pq_set_option", "pq_unset_option", "pq_last_scan_info", "pq_adc_scan_topk_noalloc",
            "ivf_quick_adc_search", "pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens"]
-
-ELEMS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # pq_elem
 
 _lib = None
 
@@ -45,6 +47,8 @@ def load():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: build it first (python -m paper_1712_02912_amd.build); "
                            "there is no fallback path")
+    if _views is None:
+        raise RuntimeError("tensor_views.so is missing: build it first (python -m paper_1712_02912_amd.build)")
     lib = ctypes.CDLL(LIB_PATH)
     vp, ci, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
     lib.pq_create.argtypes = [ctypes.POINTER(vp), ci, vp]
@@ -98,58 +102,6 @@ def _dev(t, dtype, name):
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     return t.contiguous()
-
-
-def _in_place(t, dtype, name, shape=None):
-    """Address of a tensor that the library reads and writes where it lies (no copy is made of it)."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and (shape is None or t.shape == shape):
-        return t.data_ptr()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
-
-
-_pack_heads = struct.Struct("@Pqq").pack            # pq_heads
-_pack_cache = struct.Struct("@PP6qqiiii").pack      # pq_kv_cache
-
-
-def _heads(t, dtype, shape, name):
-    """Rows [tokens][heads][dim] of any strides but the last, as the bytes of a pq_heads."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a GPU tensor")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
-    s0, s1, s2 = t.stride()
-    if s2 != 1 and shape[2] > 1 and t.numel() > 0:
-        raise ValueError(f"the dimensions of a row of {name} must be contiguous")
-    return _pack_heads(t.data_ptr(), s0, s1)
-
-
-def _cache(key_cache, value_cache):
-    """A paged cache [blocks][block size][heads][dim] of any strides but the last, as the bytes of a pq_kv_cache; its dtype and
-    shape."""
-    dtype, shape = key_cache.dtype, key_cache.shape
-    for t, name in ((key_cache, "key_cache"), (value_cache, "value_cache")):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be a GPU tensor")
-        if t.dtype not in ELEMS or t.dtype is not dtype:
-            raise TypeError(f"{name} has dtype {t.dtype}: float32, float16 or bfloat16, the same for keys and values")
-        if len(shape) != 4 or t.shape != shape:
-            raise ValueError(f"{name} must have shape [blocks][block size][heads][dim], the same for keys and values")
-        if t.stride(3) != 1 and shape[3] > 1 and t.numel() > 0:
-            raise ValueError(f"the dimensions of a row of {name} must be contiguous")
-    nblocks, block_size, heads, dim = shape
-    k0, k1, k2, _ = key_cache.stride()
-    v0, v1, v2, _ = value_cache.stride()
-    packed = _pack_cache(key_cache.data_ptr(), value_cache.data_ptr(), k0, k1, k2, v0, v1, v2, nblocks, block_size, heads, dim,
-                         ELEMS[dtype])
-    return packed, dtype, heads, dim
 
 
 class Context:
@@ -368,22 +320,25 @@ class Context:
                                                   _ptr(probes)))
         return (dist, out_ids, probes) if return_probes else (dist, out_ids)
 
-    # -- The reading step (include/pq_read.h) ----------------------------------------------------
+    # -- The reading step (include/pq_read.h).  Tensors are taken where they lie: what the library reads with strides may have any
+    # but the last, all others are contiguous; nothing is copied. -------------------------------------------------------------
     def pq_kv_plan(self, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, out=None):
         """Positions and slots of the new tokens; block_tables [nreq][width] gets the fresh blocks.
         Returns (cu_new, kv_lens, positions, slots, taken), `out` if it is given."""
-        i32 = torch.int32
+        i32, i64, at = torch.int32, torch.int64, _views.address
         nreq, width = block_tables.shape
         if out is None:
             out = tuple(torch.empty(n, dtype=dt, device=block_tables.device)
-                        for n, dt in ((nreq + 1, i32), (nreq, i32), (ntokens, i32), (ntokens, torch.int64), (1, i32)))
+                        for n, dt in ((nreq + 1, i32), (nreq, i32), (ntokens, i32), (ntokens, i64), (1, i32)))
         cu_new, kv_lens, positions, slots, taken = out
-        self._check(self.lib.pq_kv_plan(
-            self.handle, _in_place(new_lens, i32, "new_lens", (nreq,)), _in_place(cached_lens, i32, "cached_lens", (nreq,)), nreq,
-            _in_place(block_tables, i32, "block_tables"), width, _in_place(free_blocks, i32, "free_blocks"), free_blocks.numel(),
-            block_size, ntokens, _in_place(cu_new, i32, "cu_new", (nreq + 1,)), _in_place(kv_lens, i32, "kv_lens", (nreq,)),
-            _in_place(positions, i32, "positions", (ntokens,)), _in_place(slots, torch.int64, "slots", (ntokens,)),
-            _in_place(taken, i32, "taken", (1,))))
+        nfree = free_blocks.numel()
+        rc = self.lib.pq_kv_plan(
+            self.handle, at(new_lens, i32, "new_lens", (nreq,)), at(cached_lens, i32, "cached_lens", (nreq,)), nreq,
+            at(block_tables, i32, "block_tables", (nreq, width)), width, at(free_blocks, i32, "free_blocks", (nfree,)), nfree,
+            block_size, ntokens, at(cu_new, i32, "cu_new", (nreq + 1,)), at(kv_lens, i32, "kv_lens", (nreq,)),
+            at(positions, i32, "positions", (ntokens,)), at(slots, i64, "slots", (ntokens,)), at(taken, i32, "taken", (1,)))
+        if rc:
+            self._check(rc)
         return out
 
     def pq_kv_append(self, q, k, v, positions, slots, key_cache, value_cache, cos=None, sin=None, q_weight=None, k_weight=None,
@@ -391,71 +346,69 @@ class Context:
         """Norm and rotation of q [tokens][q heads][dim] and k [tokens][heads][dim]; k and v go into the cache
         [blocks][block size][heads][dim].  cos, sin [positions][rot/2]; without them nothing is rotated.  Returns the queries
         (None if q is None)."""
-        cache, dtype, heads, dim = _cache(key_cache, value_cache)
-        f32 = torch.float32
+        cache, heads, dim = _views.cache(key_cache, value_cache)
+        dtype, f32, at, rows = key_cache.dtype, torch.float32, _views.address, _views.heads
         t = k.shape[0]
-        q_heads = 0 if q is None else q.shape[1]
-        if q is not None and out is None:
-            out = torch.empty((t, q_heads, dim), dtype=dtype, device=q.device)
+        shape, q_rows, q_heads = (t, heads, dim), None, 0
+        if q is not None:
+            q_heads = q.shape[1]
+            q_shape = (t, q_heads, dim)
+            q_rows = rows(q, dtype, "q", q_shape)
+            if out is None:
+                out = torch.empty(q_shape, dtype=dtype, device=q.device)
         if (cos is None) != (sin is None):
             raise ValueError("cos and sin go together")
-        positions_max, half = (0, 0) if cos is None else cos.shape
-        rows_q = None if q is None else _heads(q, dtype, (t, q_heads, dim), "q")
-        self._check(self.lib.pq_kv_append(
-            self.handle, cache, rows_q, q_heads, _heads(k, dtype, (t, heads, dim), "k"),
-            _heads(v, dtype, (t, heads, dim), "v"), t, _in_place(positions, torch.int32, "positions", (t,)),
-            _in_place(slots, torch.int64, "slots", (t,)), None if cos is None else _in_place(cos, f32, "cos"),
-            None if sin is None else _in_place(sin, f32, "sin", (positions_max, half)), positions_max, 2 * half, 1 if pairs else 0,
-            1 if norm else 0, None if q_weight is None else _in_place(q_weight, f32, "q_weight", (dim,)),
-            None if k_weight is None else _in_place(k_weight, f32, "k_weight", (dim,)), eps,
-            None if q is None else _in_place(out, dtype, "out", (t, q_heads, dim))))
+        table = (0, 0) if cos is None else tuple(cos.shape)
+        if len(table) != 2:
+            raise ValueError("cos and sin must be [positions][rot/2]")
+        rc = self.lib.pq_kv_append(
+            self.handle, cache, q_rows, q_heads, rows(k, dtype, "k", shape), rows(v, dtype, "v", shape), t,
+            at(positions, torch.int32, "positions", (t,)), at(slots, torch.int64, "slots", (t,)), at(cos, f32, "cos", table),
+            at(sin, f32, "sin", table), table[0], 2 * table[1], 1 if pairs else 0, 1 if norm else 0,
+            at(q_weight, f32, "q_weight", (dim,)), at(k_weight, f32, "k_weight", (dim,)), eps,
+            None if q is None else at(out, dtype, "out", q_shape))
+        if rc:
+            self._check(rc)
         return out if q is not None else None
 
     def pq_kv_attention(self, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new, scale=None, window=0, out=None,
                         lse=None):
         """Attention of q [tokens][q heads][dim] over the paged cache; scale None: 1 / sqrt(dim).  Returns (out, lse)."""
-        cache, dtype, _, dim = _cache(key_cache, value_cache)
-        t, q_heads = q.shape[0], q.shape[1]
+        cache, _, dim = _views.cache(key_cache, value_cache)
+        dtype, i32, at = key_cache.dtype, torch.int32, _views.address
+        t, q_heads, _ = q.shape
         nreq, width = block_tables.shape
-        shape, i32 = (t, q_heads, dim), torch.int32
+        shape = (t, q_heads, dim)
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=q.device)
         if lse is None:
             lse = torch.empty((t, q_heads), dtype=torch.float32, device=q.device)
-        self._check(self.lib.pq_kv_attention(
-            self.handle, cache, _heads(q, dtype, shape, "q"), q_heads, t, _in_place(cu_new, i32, "cu_new", (nreq + 1,)),
-            _in_place(kv_lens, i32, "kv_lens", (nreq,)), nreq, _in_place(block_tables, i32, "block_tables"), width, max_new,
-            dim ** -0.5 if scale is None else scale, window, _in_place(out, dtype, "out", shape),
-            _in_place(lse, torch.float32, "lse", (t, q_heads))))
+        rc = self.lib.pq_kv_attention(
+            self.handle, cache, _views.heads(q, dtype, "q", shape), q_heads, t, at(cu_new, i32, "cu_new", (nreq + 1,)),
+            at(kv_lens, i32, "kv_lens", (nreq,)), nreq, at(block_tables, i32, "block_tables", (nreq, width)), width, max_new,
+            dim ** -0.5 if scale is None else scale, window, at(out, dtype, "out", shape), at(lse, torch.float32, "lse", (t, q_heads)))
+        if rc:
+            self._check(rc)
         return out, lse
 
     def pq_sample_tokens(self, logits, noise, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
         """One token for each row of logits [rows][vocab]; noise [rows][vocab] uniform in (0, 1), None: the largest logits.
         Returns (tokens, logprobs)."""
-        if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
-            raise TypeError("logits must be a GPU tensor")
-        if logits.dtype not in ELEMS:
-            raise TypeError(f"logits have dtype {logits.dtype}: float32, float16 or bfloat16")
-        rows, vocab = logits.shape
-        f32 = torch.float32
-        for t, dtype, name in ((logits, logits.dtype, "logits"), (noise, f32, "noise")):
-            if t is None:
-                continue
-            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype:
-                raise TypeError(f"{name} must be a GPU tensor of dtype {dtype}")
-            if t.shape != (rows, vocab):
-                raise ValueError(f"{name} must have shape {[rows, vocab]}, got {list(t.shape)}")
-            if t.stride(1) != 1 and vocab > 1 and rows > 0:
-                raise ValueError(f"the entries of a row of {name} must be contiguous")
+        p, elem, stride, rows, vocab = _views.rows(logits, "logits")
+        noise_p, noise_stride, f32, at = None, 0, torch.float32, _views.address
+        if noise is not None:
+            noise_p, noise_elem, noise_stride, noise_rows, noise_vocab = _views.rows(noise, "noise")
+            if noise_elem != 0:
+                raise TypeError(f"noise must have dtype {f32}, got {noise.dtype}")
+            if (noise_rows, noise_vocab) != (rows, vocab):
+                raise ValueError(f"noise must have shape {[rows, vocab]}, got {list(noise.shape)}")
         if out is None:
             out = (torch.empty(rows, dtype=torch.int64, device=logits.device), torch.empty(rows, dtype=f32, device=logits.device))
-
-        def per_row(t, dtype, name):
-            return None if t is None else _in_place(t, dtype, name, (rows,))
-
-        self._check(self.lib.pq_sample_tokens(
-            self.handle, _ptr(logits), ELEMS[logits.dtype], logits.stride(0), rows, vocab, _ptr(noise),
-            0 if noise is None else noise.stride(0), per_row(temperature, f32, "temperature"), per_row(top_k, torch.int32, "top_k"),
-            per_row(top_p, f32, "top_p"), per_row(min_p, f32, "min_p"), per_row(out[0], torch.int64, "tokens"),
-            per_row(out[1], f32, "logprobs")))
+        per_row = (rows,)
+        rc = self.lib.pq_sample_tokens(
+            self.handle, p, elem, stride, rows, vocab, noise_p, noise_stride, at(temperature, f32, "temperature", per_row),
+            at(top_k, torch.int32, "top_k", per_row), at(top_p, f32, "top_p", per_row), at(min_p, f32, "min_p", per_row),
+            at(out[0], torch.int64, "tokens", per_row), at(out[1], f32, "logprobs", per_row))
+        if rc:
+            self._check(rc)
         return out
