@@ -348,7 +348,8 @@ template <class T> struct sample_row {
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e)
                 if (w[e] > 0.f && w[e] >= so_far * (1.f - u.v[e])) best.enter(w[e], u.v[e], i + e);
-            if (best.best > so_far) atomicMax(&sh.best, __float_as_uint(best.best));
+            // (rounded down, so that the logarithm's last bit decides nothing: the winner is the same whoever passes here first)
+            if (best.best > so_far) atomicMax(&sh.best, __float_as_uint(best.best * (1.f - 1e-6f)));
         }, [&](int i, float l) {
             const float y = s.y(l), w = weight(y);
             high = fmaxf(high, y);
