@@ -81,12 +81,14 @@ int pq_kv_append(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q
  *   q rows in cache->elem; out [ntokens][q_heads][dim] in cache->elem; lse [ntokens][q_heads] f32, may be NULL.
  * A row that sees nothing (a refused request, kv_lens below the number of new tokens) is 0, its lse -inf.  Rows behind
  * cu_new[nreq] are left.  max_new: the largest number of new tokens of a request (rows of a request behind it are not
- * written).  Keys and values that no row sees may hold anything, NaN included.  Products of f16 and bf16 are summed in fp32
- * on the matrix cores, softmax statistics are fp32, the weights are rounded to the cache's type for the product with
- * the values.  With block numbers outside the cache among those of a request's keys its rows are unspecified
- * (nothing outside the cache is read).
- * Requires q_heads a multiple of cache->heads; dim 64, 96, 128 or 256 in f16 or bf16 with rows of the queries and the cache on
- * 16 bytes take the matrix cores, any other even dim <= 512 and f32 a general kernel. */
+ * written).  Keys behind the last position of the table are not seen.  Keys and values that no row sees may hold anything,
+ * NaN included, and inf and NaN among values reach only the rows that see them.  Products of f16 and bf16 are summed in fp32
+ * on the matrix cores, softmax statistics are fp32, the weights are rounded to the cache's type for the product with the
+ * values.  With block numbers outside the cache among those of a request's keys its rows are unspecified (nothing outside the
+ * cache is read).
+ * Requires q_heads a multiple of cache->heads, width * block_size < 2^31 - 4096.  dim 64, 96, 128 or 256 in f16 or bf16, with
+ * rows of the queries, the cache and out on 16 bytes, takes the matrix cores, any other even dim <= 512 and f32 a general
+ * kernel. */
 int pq_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
                     const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width, int max_new,
                     float scale, int window, void *out, float *lse);

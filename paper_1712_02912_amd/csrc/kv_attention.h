@@ -25,8 +25,10 @@ constexpr float LN2 = 0.6931471805599453f;
 // Reference of a running softmax that has seen no key: below every score, and finite, so that no -inf - -inf is formed.
 constexpr float NO_SCORE = -3e38f;
 
-// Keys of a request as its table can hold them (kv_lens is the caller's: memory is read by it).
-__device__ __forceinline__ int attention_keys(const attention_args &a, int r) { return min(a.kv_lens[r], a.width * a.cache.block_size); }
+// A request's length (refused requests have -1; so has what lies below, that no difference leaves 32 bits) and its keys as its
+// table can hold them (kv_lens is the caller's: memory is read by it).
+__device__ __forceinline__ int attention_length(const attention_args &a, int r) { return max(a.kv_lens[r], -1); }
+__device__ __forceinline__ int attention_keys(const attention_args &a, int r) { return min(attention_length(a, r), a.width * a.cache.block_size); }
 
 // A block table's entry; blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
 __device__ __forceinline__ int64_t attention_block(const attention_args &a, int32_t entry) { return (unsigned)entry < (uint64_t)a.cache.nblocks ? entry : 0; }
@@ -92,6 +94,11 @@ __device__ __forceinline__ uint2 read_transposed(const void *lds) {
     return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lds));
 }
 
+// Weights are rounded to the cache's type for the product with the values: at most half a unit in the last place each, which
+// is what the values themselves were rounded by, where a product in fp32 would take sixteen times as long.  Their sum is of
+// those before the rounding.  Those of f16, whose least is 2^-24, are scaled by 2^7 (the sum with them): with the 2^8 by which
+// a score may pass the reference the largest is 2^15, and weights of 2^-32 of a row's first still count.
+template <class T> constexpr float WEIGHT_ROOM = __is_same(T, _Float16) ? 7.f : 0.f;
 template <class T> __device__ __forceinline__ u32x4 pack8(const float *p) {
     typename mfma_of<T>::v8 v;
 #pragma unroll

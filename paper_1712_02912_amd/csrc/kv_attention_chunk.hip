@@ -78,7 +78,7 @@ template <class T, int D, int WAVES, int TILE> __global__ __launch_bounds__(64 *
     const int r = at.r, fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
     const int64_t rows = (int64_t)held * a.group, mine = at.tiles - 1 - at.index;   // the last rows see the most keys: they come first
 
-    const int kv = a.kv_lens[r], nkeys = attention_keys(a, r);
+    const int kv = attention_length(a, r), nkeys = attention_keys(a, r);
     // this lane's row
     const int64_t my_row = mine * M + wave * 32 + n;
     const bool valid = my_row < rows;
@@ -202,9 +202,9 @@ template <class T, int D, int WAVES, int TILE> __global__ __launch_bounds__(64 *
 #pragma unroll
             for (int i = 0; i < 16; ++i) high_score = fmaxf(high_score, s[j][i]);
         // (the reference moves only when a score passes it by 2^8, see kv_attention_few.hip)
-        if (__any(high_score * scale_log2 > ref + 8.f)) {
+        if (__any(high_score * scale_log2 > ref + (8.f + WEIGHT_ROOM<T>))) {
             high_score = fmaxf(high_score, __shfl_xor(high_score, 32));
-            const float moved = fmaxf(ref, high_score * scale_log2), shrink = __builtin_amdgcn_exp2f(ref - moved);
+            const float moved = fmaxf(ref, high_score * scale_log2 - WEIGHT_ROOM<T>), shrink = __builtin_amdgcn_exp2f(ref - moved);
             ref = moved;
             sum *= shrink;
 #pragma unroll

@@ -37,7 +37,7 @@ __device__ __forceinline__ few_range few_load(const attention_args &a, int r) {
     few_range x;
     x.fresh = a.cu[r + 1] - a.cu[r];
     x.held = (int)min((int64_t)x.fresh, a.ntokens - a.cu[r]);
-    const int kv = a.kv_lens[r];
+    const int kv = attention_length(a, r);
     x.keys = max(0, attention_keys(a, r));
     x.from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - x.fresh - a.window + 1) : 0;
     x.units = x.held <= 0 || !attention_is_few(a, x.fresh) ? 0 : max((int64_t)1, ((int64_t)x.keys - x.from + FEW_UNIT - 1) / FEW_UNIT);
@@ -124,12 +124,13 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS, D > 128 ? 1 
         at += count;
 
         // rows: token n / group, head n % group of the group
-        const int kv = a.kv_lens[r];
+        const int kv = attention_length(a, r);
         const int rows = (int)min((int64_t)FEW_ROWS, (int64_t)x.held * a.group);
         const int token = (int)a.by_group.div((uint32_t)n), sub = n - token * a.group;
         // the keys that this lane's row sees: `seen` of them from first_seen on
         const int last = kv - x.fresh + token, first_seen = a.window > 0 ? (int)max((int64_t)0, (int64_t)last - a.window + 1) : 0;
         const uint32_t seen = (uint32_t)max(0, min(last, x.keys - 1) - first_seen + 1);
+        const int all_upto = min(kv - x.fresh, x.keys - 1);   // the last key that all rows see
         const int64_t qrow = a.cu[r] + (n < rows ? token : 0);
         u32x4 q[STEPS];
         {
@@ -191,7 +192,7 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS, D > 128 ? 1 
             if (i + 1 < tiles) load_k(next);
             // a lane's scores: keys 16 j + 4 g + e of the tile for row n
             float p[8], high_score = NO_SCORE;
-            const bool all_seen = tile + FEW_TILE - 1 <= kv - x.fresh && (a.window == 0 || tile >= (int64_t)kv - a.window);
+            const bool all_seen = tile + FEW_TILE - 1 <= all_upto && (a.window == 0 || tile >= (int64_t)kv - a.window);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -202,12 +203,12 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS, D > 128 ? 1 
                     p[4 * j + e] = y;
                     high_score = fmaxf(high_score, y);
                 }
-            // The reference of a row moves only when a score passes it by 2^8: weights stay below 256 times their
-            // sum's smallest term, which neither the sums nor the weights' type minds, and nearly no tile scales the results.
-            if (__any(high_score > ref + 8.f)) {
+            // The reference of a row moves only when a score passes it by 2^8: that much neither the sums nor the weights' type
+            // minds, and nearly no tile scales the results.
+            if (__any(high_score > ref + (8.f + WEIGHT_ROOM<T>))) {
                 high_score = fmaxf(high_score, __shfl_xor(high_score, 16));
                 high_score = fmaxf(high_score, __shfl_xor(high_score, 32));
-                const float moved = fmaxf(ref, high_score), shrink = exp2f(ref - moved);
+                const float moved = fmaxf(ref, high_score - WEIGHT_ROOM<T>), shrink = exp2f(ref - moved);
                 ref = moved;
                 sum *= shrink;
 #pragma unroll
@@ -262,7 +263,7 @@ template <class T, int D> __global__ __launch_bounds__(FEW_THREADS, D > 128 ? 1 
         if (taken_out) {
             for (int i = 0; i < tiles; ++i) {
                 const int tile = tile0 + i * FEW_UNIT;
-                if (tile + FEW_TILE - 1 <= kv - x.fresh && (a.window == 0 || tile >= (int64_t)kv - a.window)) continue;
+                if (tile + FEW_TILE - 1 <= all_upto && (a.window == 0 || tile >= (int64_t)kv - a.window)) continue;
                 for (int key = tile; key < min(tile + FEW_TILE, x.keys); ++key) {
                     if ((uint32_t)(key - first_seen) >= seen) continue;
                     int64_t block;

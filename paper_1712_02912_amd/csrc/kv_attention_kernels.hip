@@ -18,8 +18,8 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
     const int h = (int)(blockIdx.x - t * a.q_heads), kvh = h / (a.q_heads / a.cache.heads);
     const int r = attention_request(a.cu, a.nreq, t);
     if (r < 0) return;
-    const int at = min(a.kv_lens[r] - (a.cu[r + 1] - (int)t), attention_keys(a, r) - 1);   // this token's position
-    const int from = a.window > 0 ? max(0, at - a.window + 1) : 0;
+    const int position = attention_length(a, r) - (a.cu[r + 1] - (int)t), at = min(position, attention_keys(a, r) - 1);
+    const int from = a.window > 0 ? (int)max((int64_t)0, (int64_t)position - a.window + 1) : 0;
     const T *qrow = (const T *)a.q.p + t * a.q.token_stride + h * a.q.head_stride;
     for (int i = tid; i < dim; i += 64 * GENERAL_WAVES) q[i] = (float)qrow[i];
     for (int i = lane; i < dim; i += 64) acc[wave][i] = 0.f;
@@ -78,7 +78,7 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
         for (int w = 0; w < GENERAL_WAVES; ++w) o += share[w] * acc[w][i];
         out[i] = (T)(total != 0.f ? o / total : 0.f);
     }
-    if (tid == 0 && a.lse) a.lse[t * a.q_heads + h] = total != 0.f ? (ref + log2f(total)) * 0.6931471805599453f : -INFINITY;
+    if (tid == 0 && a.lse) a.lse[t * a.q_heads + h] = total != 0.f ? (ref + log2f(total)) * LN2 : -INFINITY;
 }
 
 // rows of 16-bit elements that 16-byte accesses fit, in the dimensions that are built

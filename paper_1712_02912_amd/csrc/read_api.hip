@@ -85,7 +85,9 @@ int pq_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, in
     if (q_heads <= 0 || ntokens < 0 || nreq < 0 || width < 0 || max_new < 0 || window < 0) return fail(ctx, PQ_EINVAL, "kv_attention: bad size");
     if (q_heads % cache->heads != 0)
         return fail(ctx, PQ_ESHAPE, "kv_attention: %d query heads are no multiple of the cache's %d", q_heads, cache->heads);
-    if ((int64_t)width * cache->block_size > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: width * block_size must be below 2^31");
+    // (the kernels look some tiles of keys ahead)
+    if ((int64_t)width * cache->block_size > INT_MAX - 4096) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: width * block_size must be below 2^31 - 4096");
+    if ((int64_t)nreq * cache->heads > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", nreq);
     if (ntokens > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: ntokens must be below 2^31");
     if (!isfinite(scale)) return fail(ctx, PQ_EINVAL, "kv_attention: scale must be finite");
     if (ntokens == 0 || nreq == 0 || max_new == 0) return PQ_OK;
@@ -107,6 +109,7 @@ int pq_sample_tokens(pq_ctx *ctx, const void *logits, pq_elem elem, int64_t row_
     if (rows == 0) return PQ_OK;
     if (!logits || !tokens) return fail(ctx, PQ_EINVAL, "sample_tokens: null pointer");
     if (!aligned_to(logits, elem_bytes(elem))) return fail(ctx, PQ_EINVAL, "sample_tokens: logits are not aligned to their elements");
+    if (!aligned_to(noise, 4)) return fail(ctx, PQ_EINVAL, "sample_tokens: noise is not aligned to its elements");
     return launch_sample_tokens(ctx, logits, elem, row_stride, rows, vocab, noise, noise_stride, temperature, top_k, top_p, min_p, tokens,
                                 logprobs);
 }

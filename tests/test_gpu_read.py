@@ -412,6 +412,49 @@ def test_attention_of_requests_behind_the_rows(ctx, new):
     assert (got[new:t] == 0).all() and np.isneginf(lse[new:t]).all() and (got[t:] == 7).all() and (lse[t:] == 7).all()
 
 
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("window", [0, 30])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_of_lengths_that_no_plan_gives(ctx, new, window, dtype):
+    """The least of all lengths sees nothing; keys behind the end of the table are not seen."""
+    r = np.random.default_rng(new)
+    tables, keys, values = make_cache(r, [90, 90, 90], 2, 64, 16, dtype, 0.0, "plain")
+    tables = tables[:, :5]                                  # 80 positions
+    cu = (np.arange(4) * new).astype(np.int32)
+    q = dev(r.standard_normal((3 * new, 4, 64)), dtype)
+    kv = np.array([-2 ** 31, 75, 85], np.int32)
+    out, lse = ctx.pq_kv_attention(q, keys, values, dev(tables), dev(cu), dev(kv), new, window=window)
+    got, got_lse = host(out), host(lse)
+    assert (got[:new] == 0).all() and np.isneginf(got_lse[:new]).all()
+    for i in (1, 2):
+        for t in range(new):
+            at = kv[i] - new + t
+            upto, first = min(at, 79), max(0, at - window + 1) if window else 0
+            # (as one token whose last key is the last seen)
+            row = i * new + t
+            want, _, spread = orc.attention(host(q)[row:row + 1], host(keys), host(values), tables[i:i + 1], np.array([0, 1]),
+                                            np.array([upto + 1]), 0.125, upto - first + 1)
+            bound, _ = attention_bound(dtype, host(q), host(keys), spread, want, 0.125, 90, 64)
+            assert (np.abs(got[row] - want[0]) <= bound[0]).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_adds_up_small_weights(ctx, new):
+    """One key of a large weight and value 0, thousands of 2^-25.5 of it whose values are large: in f16 those weights count."""
+    kv, count = 8192 + new, 8191
+    tables = np.arange(-(-kv // 16), dtype=np.int32)[None]
+    keys, values = (np.zeros((tables.shape[1], 16, 1, 64)) for _ in range(2))
+    keys.reshape(-1, 64)[1:8192, 0], values.reshape(-1, 64)[1:8192] = -17.6875, 1000.0
+    keys.reshape(-1, 64)[8192:, 0] = -60000.0               # (the new tokens themselves)
+    q = np.zeros((new, 1, 64))
+    q[:, 0, 0] = 1.0
+    out, _ = ctx.pq_kv_attention(dev(q, F16), dev(keys, F16), dev(values, F16), dev(tables), dev(np.array([0, new], np.int32)),
+                                 dev(np.array([kv], np.int32)), new, scale=1.0)
+    want = count * np.exp(-17.6875) * 1000 / (1 + count * np.exp(-17.6875))
+    # half of the least weight, 2^-24 of 2^7 of the largest, for each of them; rounding of the result
+    assert (np.abs(host(out) - want) <= count * 1000 * 2.0 ** -32 + 2.0 ** -10 * want).all()
+
+
 def test_attention_refusals(ctx):
     i32 = dict(dtype=torch.int32, device="cuda")
     q, cache = torch.zeros((2, 4, 64), dtype=BF16, device="cuda"), torch.zeros((3, 16, 2, 64), dtype=BF16, device="cuda")
@@ -425,6 +468,10 @@ def test_attention_refusals(ctx):
         ctx.pq_kv_attention(q, cache, cache, table, cu, kv, 1, scale=float("nan"))
     with pytest.raises(binding.PqError):
         ctx.pq_kv_attention(q, cache, cache, torch.zeros((2, 0), **i32), cu, kv, 1)
+    with pytest.raises(binding.PqError) as e:
+        one = torch.zeros((1, 2 ** 16, 1, 64), dtype=BF16, device="cuda")
+        ctx.pq_kv_attention(q, one, one, torch.zeros((2, 2 ** 15), **i32), cu, kv, 1)
+    assert e.value.code == -3
     wide, wide_cache = torch.zeros((2, 4, 514), dtype=BF16, device="cuda"), torch.zeros((3, 16, 2, 514), dtype=BF16, device="cuda")
     with pytest.raises(binding.PqError) as e:
         ctx.pq_kv_attention(wide, wide_cache, wide_cache, table, cu, kv, 1)
