@@ -1,4 +1,4 @@
-// What the attention kernels share (kv_attention_kernels.hip, kv_attention_few.hip, kv_attention_chunk.hip).
+// What the attention kernels share (kv_attention_kernels.hip, kv_attention_few.h, kv_attention_chunk.h).
 #pragma once
 #include <limits.h>
 
@@ -146,9 +146,9 @@ __device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, in
     return low;
 }
 
-// The requests of few rows; *ws_used: bytes of read_ws.
-int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, size_t *ws_used);
-// All requests, or those of more rows; parts go to read_ws from ws_at on (growing it waits for the stream).
-int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at);
+// All requests, none of more than most_rows <= FEW_ROWS rows per head.
+int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int most_rows);
+// All requests; some_few: those of few rows by the blocks of their own kind.
+int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool some_few);
 
 }  // namespace pq

@@ -1,378 +1,86 @@
-// Attention of chunks of new tokens: bound by the matrix cores.
-//
-// A block holds 32 rows of queries per wave in registers (rows: token, head of the group, so the heads that share keys
-// share them here too) and walks over the keys in tiles of 64 (32), which its waves read from shared memory.  Scores are formed
-// transposed, S^T = K Q^T, so a lane holds scores of one row only, its maximum and sum need no exchange between lanes in most
-// tiles, and the weights are, as they lie, the second operand of O^T = V^T P^T (the order of the keys within a product is
-// free: V's are read in the order that the scores have, transposed by the reads from shared memory).
-//
-// Keys and values go through registers into one of two buffers while the other one is computed on, so one barrier per tile is
-// enough and loads have a tile's time to arrive.  Places that hold no key become zeros on that way.
-#include <type_traits>
-
-#include "kv_attention.h"
+// Launches of the attention of chunks (kv_attention_chunk.h), alone or together with that of few rows (kv_attention_few.h).
+#include "kv_attention_chunk.h"
 
 namespace pq {
 
-struct chunk_split {
-    int splits;            // blocks that share the keys of a tile of rows
-    bool without_few;      // requests of few rows are left to kv_attention_few.hip
-    float *parts, *stats;  // [ntokens * q_heads][splits][D], [..][splits][2]
-};
-
-// The tiles of rows, one index each: request after request, the empty indexes behind the last one.  Every wave adds up the
-// requests before its own, 64 at a time.  (Blocks without work between the others are not free: they take their turn in the
-// order in which blocks are dealt to the parts of the chip, so with every second index empty half of the compute units got all
-// the work, and 448 tiles of 128 rows over 1152 keys of 64 dimensions took 51 us, 33 us without.)  Adding up is for
-// CHUNK_ADDED requests; where there are more, request r owns the indexes from cu[r] * group / M + r on, at least as many as it
-// has tiles.
-constexpr int CHUNK_ADDED = 512;
-struct chunk_place {
-    int r, tiles;     // the request (-1: none), its tiles of rows
-    int64_t index;    // among them
-};
-template <int M> __device__ __forceinline__ chunk_place chunk_locate(const attention_args &a, bool without_few, int64_t index) {
-    auto tiles_of = [&](int r) {
-        const int fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
-        return held <= 0 || (without_few && attention_is_few(a, fresh)) ? 0 : (int)(((int64_t)held * a.group + M - 1) / M);
-    };
-    if (a.nreq > CHUNK_ADDED) {
-        const int r = wave_search(a.nreq, [&](int i) { return (int64_t)a.cu[i] * a.group / M + i <= index; });
-        const int tiles = tiles_of(r);
-        index -= (int64_t)a.cu[r] * a.group / M + r;
-        return {index < tiles ? r : -1, tiles, index};
-    }
-    const int lane = threadIdx.x & 63;
-    int64_t before = 0;
-    for (int base = 0; base < a.nreq; base += 64) {
-        const int mine = base + lane < a.nreq ? tiles_of(base + lane) : 0;
-        int upto = mine;
-        for (int d = 1; d < 64; d *= 2) {
-            const int v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
-        const uint64_t there = __ballot(before + upto > index);
-        if (there) {
-            const int at = __ffsll((unsigned long long)there) - 1, tiles = __shfl(mine, at);
-            return {__builtin_amdgcn_readfirstlane(base + at), tiles, index - before - (__shfl(upto, at) - tiles)};
-        }
-        before += __shfl(upto, 63);
-    }
-    return {-1, 0, 0};
+// splits: parts of the keys; blocks of chunks come first, part after part, then those of few rows (the chunks' take longer)
+template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
+    __shared__ __attribute__((aligned(16))) unsigned char pool[CHUNK_POOL<D>];
+    chunk_block<T, D, WAVES>(a, split, blockIdx.x, blockIdx.y, pool);
 }
-
-template <class T, int D, int WAVES, int TILE> __global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
-    typedef lds_row<D> row;
-    constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
-    constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
-    // a thread moves chunks of 16 bytes of one key (and value) of a tile, every LANES-th from its own on
-    constexpr int LANES = THREADS / TILE, MOVES = (CHUNKS + LANES - 1) / LANES;
-    __shared__ __attribute__((aligned(16))) unsigned char lds_k[2][TILE * row::bytes], lds_v[2][TILE * row::bytes];
-    __shared__ int taken_out;   // values were (see below)
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
-
-    // heads vary fastest: blocks that read the same head's keys are on the same XCD where the heads are a multiple of eight
-    const int heads = a.cache.heads, h = blockIdx.x % heads, part = blockIdx.y;
-    const chunk_place at = chunk_locate<M>(a, split.without_few, blockIdx.x / heads);
-    if (at.r < 0) return;
-    const int r = at.r, fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
-    const int64_t rows = (int64_t)held * a.group, mine = at.tiles - 1 - at.index;   // the last rows see the most keys: they come first
-
-    const int kv = attention_length(a, r), nkeys = attention_keys(a, r);
-    // this lane's row
-    const int64_t my_row = mine * M + wave * 32 + n;
-    const bool valid = my_row < rows;
-    const int token = valid ? (int)a.by_group.div((uint32_t)my_row) : 0, sub = valid ? (int)(my_row - (int64_t)token * a.group) : 0;
-    // the keys that it sees: `seen` of them from first_seen on
-    const int last = kv - fresh + token, first_seen = a.window > 0 ? (int)max((int64_t)0, (int64_t)last - a.window + 1) : 0;
-    const uint32_t seen = (uint32_t)max(0, min(last, nkeys - 1) - first_seen + 1);
-    // the keys that the tile's rows see, and those that all of them see
-    const int token0 = (int)a.by_group.div((uint32_t)(mine * M)), token1 = (int)a.by_group.div((uint32_t)(min(rows, (mine + 1) * M) - 1));
-    const int to = min(nkeys, kv - fresh + token1 + 1);
-    const int from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + token0 - a.window + 1) : 0;
-    const int all_from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + token1 - a.window + 1) : 0, all_to = min(nkeys, kv - fresh + token0 + 1);
-    const int tiles_all = to > from ? (to - from + TILE - 1) / TILE : 0;
-    const int tile_begin = (int)((int64_t)tiles_all * part / split.splits), tile_end = (int)((int64_t)tiles_all * (part + 1) / split.splits);
-
-    // (a negative scale is the queries' sign: scores are compared before they are scaled)
-    const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;
-    const float scale_log2 = fmaxf(fabsf(a.scale_log2), 1e-37f);   // (0 times the -inf of a key that is not seen is no number)
-    u32x4 q[STEPS];
-    {
-        const T *p = (const T *)a.q.p + (a.cu[r] + token) * a.q.token_stride + (h * a.group + sub) * a.q.head_stride + 8 * g;
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + 16 * t) ^ sign;
-    }
-    f32x16 out[OUTS];
-#pragma unroll
-    for (int f = 0; f < OUTS; ++f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) out[f][i] = 0.f;
-    float ref = NO_SCORE, sum = 0.f;   // ref: of the scaled scores
-
-    // the tiles that some row of this wave sees: the others it only helps to move
-    const int64_t row0 = mine * M + wave * 32, row1 = min(rows, row0 + 32) - 1;
-    int wave_begin = tile_end, wave_end = tile_end;
-    if (row0 < rows) {
-        const int wave_to = min(nkeys, kv - fresh + (int)a.by_group.div((uint32_t)row1) + 1);
-        const int wave_from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - fresh + (int)a.by_group.div((uint32_t)row0) - a.window + 1) : 0;
-        wave_begin = (wave_from - from) / TILE;
-        wave_end = wave_to > from ? (wave_to - from + TILE - 1) / TILE : 0;
-    }
-
-    // this thread's chunks of a tile
-    const int my_key = tid / LANES, my_chunk = tid % LANES;
-    const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2] + 8 * my_chunk;
-    const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2] + 8 * my_chunk;
-    const int32_t *const table = a.tables + (int64_t)r * a.width;
-    u32x4 mk[MOVES], mv[MOVES];
-    // (a tile's entry of the block table is read a tile before its keys are, so that nothing waits for it)
-    int32_t entry = 0, place = 0;
-    auto look_up = [&](int tile) {
-        const uint32_t j = (uint32_t)min(from + tile * TILE + my_key, to - 1), column = a.by_block.div(j);
-        place = (int)(j - column * a.cache.block_size);
-        entry = table[column];
-    };
-    auto load = [&]() {
-        const int64_t block = attention_block(a, entry);
-        const T *const k = keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1];
-        const T *const v = values + block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
-#pragma unroll
-        for (int i = 0; i < MOVES; ++i) {
-            if (CHUNKS % LANES != 0 && my_chunk + LANES * i >= CHUNKS) continue;
-            mk[i] = *(const u32x4 *)(k + 8 * LANES * i);
-            mv[i] = *(const u32x4 *)(v + 8 * LANES * i);
-        }
-    };
-    auto store = [&](int tile, int buffer) {
-        const int key0 = from + tile * TILE;
-        const bool held = key0 + my_key < to;
-#pragma unroll
-        for (int i = 0; i < MOVES; ++i) {
-            const int chunk = my_chunk + LANES * i;
-            if (CHUNKS % LANES != 0 && chunk >= CHUNKS) continue;
-            const int at = my_key * row::bytes + 16 * row::chunk(my_key, chunk);
-            *(u32x4 *)(lds_k[buffer] + at) = mk[i];
-            *(u32x4 *)(lds_v[buffer] + at) = held ? mv[i] : u32x4{0, 0, 0, 0};
-        }
-        // Values that some row does not see must not reach it as 0 times inf: where a tile has rows that do not see all of it,
-        // what is not finite is taken out, and added in the end to the rows that see it.
-        if ((key0 < all_from || key0 + TILE > all_to) && held) {
-#pragma unroll
-            for (int i = 0; i < MOVES; ++i) {
-                const int chunk = my_chunk + LANES * i;
-                if ((CHUNKS % LANES != 0 && chunk >= CHUNKS) || !any_not_finite<T>(mv[i])) continue;
-                *(u32x4 *)(lds_v[buffer] + my_key * row::bytes + 16 * row::chunk(my_key, chunk)) = finite_only<T>(mv[i]);
-                taken_out = 1;
-            }
-        }
-    };
-    // Where this lane reads: key n of 32 and chunk g, key 4 g + (lane / 4) % 4 of 16 and its part of chunk pair 0.  Other chunks
-    // differ in bits that the row's swizzle only turns over, so their places are one exclusive or away.
-    const int k_at = n * row::bytes + 16 * row::chunk(n, g);
-    const int v_key = 4 * g + ((lane >> 2) & 3);
-    const int v_at = v_key * row::bytes + 16 * row::chunk(v_key, 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 8 * (lane & 1);
-
-    auto compute = [&](int tile, auto buffer_of) {
-        constexpr int buffer = decltype(buffer_of)::value;
-        if (tile < wave_begin || tile >= wave_end) return;
-        const int key0 = from + tile * TILE;
-        f32x16 s[TILE / 32];
-#pragma unroll
-        for (int j = 0; j < TILE / 32; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t)
-#pragma unroll
-            for (int j = 0; j < TILE / 32; ++j) s[j] = mfma_of<T>::m32(*(const u32x4 *)(lds_k[buffer] + (k_at ^ (32 * t)) + 32 * j * row::bytes), q[t], s[j]);
-        // scores of this lane: keys 32 j + 8 (i / 4) + 4 g + i % 4 of the tile
-        if (key0 < all_from || key0 + TILE > all_to) {   // some row does not see some key
-#pragma unroll
-            for (int j = 0; j < TILE / 32; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = key0 + 32 * j + 8 * (i / 4) + 4 * g + i % 4;
-                    if ((uint32_t)(key - first_seen) >= seen) s[j][i] = -INFINITY;
-                }
-        }
-        float high_score = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < TILE / 32; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) high_score = fmaxf(high_score, s[j][i]);
-        // (the reference moves only when a score passes it by 2^8, see kv_attention_few.hip)
-        if (__any(high_score * scale_log2 > ref + (8.f + WEIGHT_ROOM<T>))) {
-            high_score = fmaxf(high_score, __shfl_xor(high_score, 32));
-            const float moved = fmaxf(ref, high_score * scale_log2 - WEIGHT_ROOM<T>), shrink = __builtin_amdgcn_exp2f(ref - moved);
-            ref = moved;
-            sum *= shrink;
-#pragma unroll
-            for (int f = 0; f < OUTS; ++f) out[f] *= shrink;
-        }
-        float p[TILE / 2];
-#pragma unroll
-        for (int i = 0; i < TILE / 2; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale_log2, -ref));
-            sum += p[i];
-        }
-#pragma unroll
-        for (int b = 0; b < TILE / 16; ++b) {
-            const u32x4 weights = pack8<T>(p + 8 * b);
-#pragma unroll
-            for (int f = 0; f < OUTS; ++f) {
-                u32x4 vt;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    // (keys 8 on change the swizzle's last bit, but in rows of 128 bytes, too)
-                    const uint2 c = read_transposed(lds_v[buffer] + (v_at ^ (64 * f) ^ (16 * e)) + (16 * b + 8 * e) * row::bytes);
-                    vt[2 * e] = c.x;
-                    vt[2 * e + 1] = c.y;
-                }
-                out[f] = mfma_of<T>::m32(vt, weights, out[f]);
-            }
-        }
-    };
-
-    if (tid == 0) taken_out = 0;
-    __syncthreads();
-    if (tile_begin < tile_end) {
-        look_up(tile_begin);
-        load();
-        look_up(min(tile_begin + 1, tile_end - 1));
-        store(tile_begin, 0);
-        load();
-        look_up(min(tile_begin + 2, tile_end - 1));
-    }
-    // (behind the last tile that one is loaded once more, and not stored)
-    auto step = [&](int tile, auto buffer_of) {
-        constexpr int buffer = decltype(buffer_of)::value;
-        __syncthreads();   // this tile is written, and the one before it read
-        if (tile + 1 < tile_end) {
-            store(tile + 1, buffer ^ 1);
-            load();
-            look_up(min(tile + 3, tile_end - 1));
-        }
-        compute(tile, buffer_of);
-    };
-    for (int tile = tile_begin; tile < tile_end; tile += 2) {
-        step(tile, std::integral_constant<int, 0>());
-        if (tile + 1 < tile_end) step(tile + 1, std::integral_constant<int, 1>());
-    }
-    if (__builtin_amdgcn_readfirstlane(taken_out)) {
-        // (rare, and so without marks: all values of the tiles that some row does not see all of)
-        for (int tile = max(tile_begin, wave_begin); tile < min(tile_end, wave_end); ++tile) {
-            const int key0 = from + tile * TILE;
-            if (key0 >= all_from && key0 + TILE <= all_to) continue;
-            for (int key = key0; key < min(key0 + TILE, to); ++key) {
-                if ((uint32_t)(key - first_seen) >= seen) continue;
-                int64_t block;
-                int at;
-                attention_place(a, r, key, block, at);
-                const T *const v = (const T *)a.cache.values + h * a.cache.value_strides[2] + block * a.cache.value_strides[0] + at * a.cache.value_strides[1];
-#pragma unroll
-                for (int f = 0; f < OUTS; ++f)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) add_not_finite(v + 32 * f + 8 * i + 4 * g, out[f], 4 * i);
-            }
-        }
-    }
-    sum += __shfl_xor(sum, 32);
-    if (!valid) return;
-    const int64_t at_row = (int64_t)(a.cu[r] + token) * a.q_heads + h * a.group + sub;
-    // dimensions 32 f + 8 (i / 4) + 4 g + i % 4 of this lane's row
-    if (split.splits > 1) {
-        const int64_t slot = at_row * split.splits + part;
-#pragma unroll
-        for (int f = 0; f < OUTS; ++f)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(f32x4 *)(split.parts + slot * D + 32 * f + 8 * i + 4 * g) = f32x4{out[f][4 * i], out[f][4 * i + 1], out[f][4 * i + 2], out[f][4 * i + 3]};
-        if (g == 0) {
-            split.stats[2 * slot] = ref;
-            split.stats[2 * slot + 1] = sum;
-        }
-        return;
-    }
-    const float scale = sum != 0.f ? 1.f / sum : 0.f;
-    T *const to_row = (T *)a.out + at_row * D;
-#pragma unroll
-    for (int f = 0; f < OUTS; ++f)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            elem_vec<T, 4> v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v.v[e] = (T)(sum != 0.f ? out[f][4 * i + e] * scale : 0.f);
-            *(elem_vec<T, 4> *)(to_row + 32 * f + 8 * i + 4 * g) = v;
-        }
-    if (g == 0 && a.lse) a.lse[at_row] = sum != 0.f ? (ref + log2f(sum)) * LN2 : -INFINITY;
-}
-
-// Joins the parts of a row, a wave for each row, in the order of the keys.
-constexpr int JOIN_ROWS = 4;
 template <class T, int D> __global__ __launch_bounds__(64 * JOIN_ROWS) void kv_attention_chunk_join_kernel(attention_args a, chunk_split split) {
-    constexpr int E = (D + 63) / 64;
-    const int64_t row = (int64_t)blockIdx.x * JOIN_ROWS + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= min(a.ntokens, (int64_t)a.cu[a.nreq]) * a.q_heads) return;
-    if (split.without_few) {
-        const int r = attention_request(a.cu, a.nreq, row / a.q_heads);
-        if (attention_is_few(a, a.cu[r + 1] - a.cu[r])) return;
-    }
-    const float *const stats = split.stats + 2 * row * split.splits, *const parts = split.parts + row * split.splits * D;
-    float top = NO_SCORE, all = 0.f, o[E] = {};
-    for (int s = lane; s < split.splits; s += 64) top = fmaxf(top, stats[2 * s]);
-    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-#pragma unroll 4
-    for (int s = 0; s < split.splits; ++s) {
-        const float share = __builtin_amdgcn_exp2f(stats[2 * s] - top);
-        all += share * stats[2 * s + 1];
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (D % 64 == 0 || e * 64 + lane < D) o[e] += share * parts[s * D + e * 64 + lane];
-    }
-    T *const out = (T *)a.out + row * D;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (D % 64 == 0 || e * 64 + lane < D) out[e * 64 + lane] = (T)(all != 0.f ? o[e] / all : 0.f);
-    if (lane == 0 && a.lse) a.lse[row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
+    chunk_join_block<T, D>(a, split, blockIdx.x);
 }
 
-template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at) {
+// Both kinds of requests in one launch, so that neither waits for the other's last blocks: first the chunks' blocks, which take
+// longer, part after part, then those of few rows.
+template <class T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D > 128 ? 1 : 2) void kv_attention_mixed_kernel(attention_args a, chunk_split split, int chunk_blocks, few_line line) {
+    constexpr int POOL = CHUNK_POOL<D> > FEW_POOL<D, WAVES> ? CHUNK_POOL<D> : FEW_POOL<D, WAVES>;
+    __shared__ __attribute__((aligned(16))) unsigned char pool[POOL];
+    const int b = blockIdx.x;
+    if (b < chunk_blocks * split.splits) chunk_block<T, D, WAVES>(a, split, b % chunk_blocks, b / chunk_blocks, pool);
+    else few_block<T, D, WAVES>(a, line, b - chunk_blocks * split.splits, pool);
+}
+template <class T, int D>
+__global__ __launch_bounds__(64 * JOIN_ROWS) void kv_attention_mixed_join_kernel(attention_args a, chunk_split split, int few_blocks, int slices, few_line line) {
+    const int b = blockIdx.x;
+    if (b < few_blocks) few_join_block<T, D, JOIN_ROWS>(a, line, b / slices, b % slices);
+    else chunk_join_block<T, D>(a, split, b - few_blocks);
+}
+
+template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const attention_args &a, bool some_few) {
     constexpr int M = 32 * WAVES;
     const int64_t indexes = a.ntokens * a.group / M + a.nreq, rows = a.ntokens * a.q_heads;
-    if (indexes * a.cache.heads > INT_MAX || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
     // Fewer tiles of rows than twice the compute units: the keys of each are split, down to 512 keys a part.
-    constexpr int TILE = D > 128 ? 32 : 64;   // (of 256 dimensions, registers and shared memory hold half as many keys)
     const int64_t full = (a.ntokens * a.group + M - 1) / M, tiles = (full > a.nreq ? full : a.nreq) * a.cache.heads;
     int64_t splits = 2 * ctx->num_cu / tiles, most = ((int64_t)a.width * a.cache.block_size + 511) / 512;
     if (a.window > 0 && most > (a.window + 511) / 512) most = (a.window + 511) / 512;
     if (splits > most) splits = most;
-    chunk_split split = {splits < 1 ? 1 : (int)splits, without_few, nullptr, nullptr};
+    chunk_split split = {splits < 1 ? 1 : (int)splits, some_few, nullptr, nullptr};
+    const int64_t chunk_blocks = indexes * a.cache.heads;
+    if (chunk_blocks * split.splits > INT_MAX - (1 << 20) || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
+    const size_t slots = split.splits > 1 ? (size_t)rows * split.splits : 0, ws = slots * (D + 2) * sizeof(float);
+    size_t ws_at = 0;
+    few_line line = {};
+    if (some_few) {
+        if (const int rc = few_prepare(ctx, a, WAVES, ws, &line, &ws_at)) return rc;
+        if (line.row_waves > JOIN_ROWS) line.row_waves = JOIN_ROWS;
+    } else if (ws > 0) {
+        if (const int rc = buf_reserve(ctx, &ctx->read_ws, ws, "parts of the attention")) return rc;
+    }
     if (split.splits > 1) {
-        const size_t slots = (size_t)rows * split.splits;
-        if (const int rc = buf_reserve(ctx, &ctx->read_ws, ws_at + slots * (D + 2) * sizeof(float), "parts of the attention")) return rc;
         split.parts = (float *)((char *)ctx->read_ws.p + ws_at);
         split.stats = split.parts + slots * D;
     }
-    kv_attention_chunk_kernel<T, D, WAVES, TILE><<<dim3((unsigned)(indexes * a.cache.heads), split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
-    if (split.splits > 1) kv_attention_chunk_join_kernel<T, D><<<(int)((rows + JOIN_ROWS - 1) / JOIN_ROWS), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split);
+    const int joins = split.splits > 1 ? (int)((rows + JOIN_ROWS - 1) / JOIN_ROWS) : 0;
+    if (some_few) {
+        const int64_t all = chunk_blocks * split.splits + line.blocks;
+        kv_attention_mixed_kernel<T, D, WAVES><<<(unsigned)all, 64 * WAVES, 0, ctx->stream>>>(a, split, (int)chunk_blocks, line);
+        const int slices = few_slices(line, FEW_ROWS, JOIN_ROWS);
+        const int64_t few_blocks = (int64_t)a.nreq * a.cache.heads * slices;
+        if (few_blocks + joins > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", a.nreq);
+        kv_attention_mixed_join_kernel<T, D><<<(unsigned)(few_blocks + joins), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split, (int)few_blocks, slices, line);
+    } else {
+        kv_attention_chunk_kernel<T, D, WAVES><<<dim3((unsigned)chunk_blocks, split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
+        if (joins > 0) kv_attention_chunk_join_kernel<T, D><<<joins, 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split);
+    }
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
 
-template <class T> static int chunk_dim(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at) {
+template <class T> static int chunk_dim(pq_ctx *ctx, const attention_args &a, bool some_few) {
     const bool many = a.ntokens * a.group >= (int64_t)a.nreq * 192;
     switch (a.cache.dim) {
-    case 64: return many ? chunk_run<T, 64, 8>(ctx, a, without_few, ws_at) : chunk_run<T, 64, 4>(ctx, a, without_few, ws_at);
-    case 96: return many ? chunk_run<T, 96, 8>(ctx, a, without_few, ws_at) : chunk_run<T, 96, 4>(ctx, a, without_few, ws_at);
-    case 128: return many ? chunk_run<T, 128, 8>(ctx, a, without_few, ws_at) : chunk_run<T, 128, 4>(ctx, a, without_few, ws_at);
-    default: return chunk_run<T, 256, 4>(ctx, a, without_few, ws_at);
+    case 64: return many ? chunk_run<T, 64, 8>(ctx, a, some_few) : chunk_run<T, 64, 4>(ctx, a, some_few);
+    case 96: return many ? chunk_run<T, 96, 8>(ctx, a, some_few) : chunk_run<T, 96, 4>(ctx, a, some_few);
+    case 128: return many ? chunk_run<T, 128, 8>(ctx, a, some_few) : chunk_run<T, 128, 4>(ctx, a, some_few);
+    default: return chunk_run<T, 256, 4>(ctx, a, some_few);
     }
 }
 
-int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool without_few, size_t ws_at) {
-    return a.cache.elem == PQ_ELEM_F16 ? chunk_dim<_Float16>(ctx, a, without_few, ws_at) : chunk_dim<__bf16>(ctx, a, without_few, ws_at);
+int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool some_few) {
+    return a.cache.elem == PQ_ELEM_F16 ? chunk_dim<_Float16>(ctx, a, some_few) : chunk_dim<__bf16>(ctx, a, some_few);
 }
 
 }  // namespace pq

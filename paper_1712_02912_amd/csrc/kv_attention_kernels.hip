@@ -115,11 +115,9 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
         // Requests of few rows and others in one call: each goes to its own kernel.  A tile of rows of the chunks' kernel costs a
         // request of one token as much as one of 128 (23 requests of 1 to 517 tokens, 16 heads: 63 us with that kernel alone, XX
         // with both); where all requests have max_new tokens there is one kind only.
-        size_t ws_used = 0;
-        const bool all_few = (int64_t)max_new * a.group <= FEW_ROWS, some_few = a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new;
-        if (all_few || some_few)
-            if (const int rc = launch_kv_attention_few(ctx, a, &ws_used)) return rc;
-        return all_few ? PQ_OK : launch_kv_attention_chunk(ctx, a, some_few, ws_used);
+        const int64_t most_rows = (int64_t)max_new * a.group;
+        if (most_rows <= FEW_ROWS) return launch_kv_attention_few(ctx, a, (int)most_rows);
+        return launch_kv_attention_chunk(ctx, a, a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new);
     }
     const int64_t grid = ntokens * q_heads;
     if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
