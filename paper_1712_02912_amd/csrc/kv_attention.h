@@ -17,6 +17,7 @@ struct attention_args {
     int64_t ntokens;
     int q_heads, nreq, width, window;
     int group;          // query heads that read one head of the cache
+    uint32_t k_strides[2], v_strides[2];   // of blocks and places of the cache, where the matrix cores are taken
     fast_div by_block, by_group;
     float scale_log2;   // scale * log2(e): softmax in powers of two
 };
@@ -37,6 +38,14 @@ __device__ __forceinline__ void attention_place(const attention_args &a, int r, 
     const int column = (int)a.by_block.div((uint32_t)j);
     place = j - column * a.cache.block_size;
     block = attention_block(a, a.tables[(int64_t)r * a.width + column]);
+}
+
+// Where a place's keys and values are, in elements (one multiply-add of 32 by 32 bits for each stride).
+__device__ __forceinline__ uint64_t attention_key_at(const attention_args &a, int64_t block, int place) {
+    return (uint64_t)(uint32_t)block * a.k_strides[0] + (uint64_t)(uint32_t)place * a.k_strides[1];
+}
+__device__ __forceinline__ uint64_t attention_value_at(const attention_args &a, int64_t block, int place) {
+    return (uint64_t)(uint32_t)block * a.v_strides[0] + (uint64_t)(uint32_t)place * a.v_strides[1];
 }
 
 // ---- the matrix cores on 16-bit elements ---------------------------------------------------------------

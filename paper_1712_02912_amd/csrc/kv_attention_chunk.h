@@ -72,6 +72,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
     typedef lds_row<D> row;
     constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
+    constexpr int AT_ONCE = D > 128 ? 4 : 1;
     // a thread moves chunks of 16 bytes of one key (and value) of a tile, every LANES-th from its own on
     constexpr int LANES = THREADS / TILE, MOVES = (CHUNKS + LANES - 1) / LANES;
     unsigned char *const lds_k[2] = {pool, pool + TILE * row::bytes}, *const lds_v[2] = {pool + 2 * TILE * row::bytes, pool + 3 * TILE * row::bytes};
@@ -142,8 +143,8 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
     };
     auto load = [&]() {
         const int64_t block = attention_block(a, entry);
-        const T *const k = keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1];
-        const T *const v = values + block * a.cache.value_strides[0] + place * a.cache.value_strides[1];
+        const T *const k = keys + attention_key_at(a, block, place);
+        const T *const v = values + attention_value_at(a, block, place);
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
             if (CHUNKS % LANES != 0 && my_chunk + LANES * i >= CHUNKS) continue;
@@ -153,24 +154,24 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
     };
     auto store = [&](int tile, int buffer) {
         const int key0 = from + tile * TILE;
-        const bool held = key0 + my_key < to;
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
             const int chunk = my_chunk + LANES * i;
             if (CHUNKS % LANES != 0 && chunk >= CHUNKS) continue;
             const int at = my_key * row::bytes + 16 * row::chunk(my_key, chunk);
             *(u32x4 *)(lds_k[buffer] + at) = mk[i];
-            *(u32x4 *)(lds_v[buffer] + at) = held ? mv[i] : u32x4{0, 0, 0, 0};
+            *(u32x4 *)(lds_v[buffer] + at) = mv[i];
         }
         // Values that some row does not see must not reach it as 0 times inf: where a tile has rows that do not see all of it,
-        // what is not finite is taken out, and added in the end to the rows that see it.
-        if ((key0 < all_from || key0 + TILE > all_to) && held) {
+        // what is not finite is taken out, and added in the end to the rows that see it.  Places behind the last key become zeros.
+        if (key0 < all_from || key0 + TILE > all_to) {
+            const bool held = key0 + my_key < to;
 #pragma unroll
             for (int i = 0; i < MOVES; ++i) {
                 const int chunk = my_chunk + LANES * i;
-                if ((CHUNKS % LANES != 0 && chunk >= CHUNKS) || !any_not_finite<T>(mv[i])) continue;
-                *(u32x4 *)(lds_v[buffer] + my_key * row::bytes + 16 * row::chunk(my_key, chunk)) = finite_only<T>(mv[i]);
-                taken_out = 1;
+                if ((CHUNKS % LANES != 0 && chunk >= CHUNKS) || (held && !any_not_finite<T>(mv[i]))) continue;
+                *(u32x4 *)(lds_v[buffer] + my_key * row::bytes + 16 * row::chunk(my_key, chunk)) = held ? finite_only<T>(mv[i]) : u32x4{0, 0, 0, 0};
+                if (held) taken_out = 1;
             }
         }
     };
@@ -189,10 +190,42 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
         for (int j = 0; j < TILE / 32; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
+        constexpr int KS = STEPS * (TILE / 32), VS = (TILE / 16) * OUTS;   // products of either kind
+        u32x4 kf[2][AT_ONCE], vf[2][AT_ONCE];
+        auto read_k = [&](int group) {
 #pragma unroll
-        for (int t = 0; t < STEPS; ++t)
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int u = group * AT_ONCE + i, t = u / (TILE / 32), j = u % (TILE / 32);
+                if (u < KS) kf[group & 1][i] = *(const u32x4 *)(lds_k[buffer] + (k_at ^ (32 * t)) + 32 * j * row::bytes);
+            }
+        };
+        auto read_v = [&](int group) {
 #pragma unroll
-            for (int j = 0; j < TILE / 32; ++j) s[j] = mfma_of<T>::m32(*(const u32x4 *)(lds_k[buffer] + (k_at ^ (32 * t)) + 32 * j * row::bytes), q[t], s[j]);
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int u = group * AT_ONCE + i, b = u / OUTS, f = u % OUTS;
+                if (u >= VS) continue;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    // (keys 8 on change the swizzle's last bit, but in rows of 128 bytes, too)
+                    const uint2 c = read_transposed(lds_v[buffer] + (v_at ^ (64 * f) ^ (16 * e)) + (16 * b + 8 * e) * row::bytes);
+                    vf[group & 1][i][2 * e] = c.x;
+                    vf[group & 1][i][2 * e + 1] = c.y;
+                }
+            }
+        };
+        read_k(0);
+#pragma unroll
+        for (int group = 0; group * AT_ONCE < KS; ++group) {
+            if ((group + 1) * AT_ONCE < KS) read_k(group + 1);
+            if (AT_ONCE > 1) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int u = group * AT_ONCE + i, t = u / (TILE / 32), j = u % (TILE / 32);
+                if (u < KS) s[j] = mfma_of<T>::m32(kf[group & 1][i], q[t], s[j]);
+            }
+            if (AT_ONCE > 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        read_v(0);
         // scores of this lane: keys 32 j + 8 (i / 4) + 4 g + i % 4 of the tile
         if (key0 < all_from || key0 + TILE > all_to) {   // some row does not see some key
 #pragma unroll
@@ -223,21 +256,19 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
             p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 16][i % 16], scale_log2, -ref));
             sum += p[i];
         }
+        u32x4 weights[TILE / 16];
 #pragma unroll
-        for (int b = 0; b < TILE / 16; ++b) {
-            const u32x4 weights = pack8<T>(p + 8 * b);
+        for (int b = 0; b < TILE / 16; ++b) weights[b] = pack8<T>(p + 8 * b);
 #pragma unroll
-            for (int f = 0; f < OUTS; ++f) {
-                u32x4 vt;
+        for (int group = 0; group * AT_ONCE < VS; ++group) {
+            if ((group + 1) * AT_ONCE < VS) read_v(group + 1);
+            if (AT_ONCE > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    // (keys 8 on change the swizzle's last bit, but in rows of 128 bytes, too)
-                    const uint2 c = read_transposed(lds_v[buffer] + (v_at ^ (64 * f) ^ (16 * e)) + (16 * b + 8 * e) * row::bytes);
-                    vt[2 * e] = c.x;
-                    vt[2 * e + 1] = c.y;
-                }
-                out[f] = mfma_of<T>::m32(vt, weights, out[f]);
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int u = group * AT_ONCE + i, b = u / OUTS, f = u % OUTS;
+                if (u < VS) out[f] = mfma_of<T>::m32(vf[group & 1][i], weights[b], out[f]);
             }
+            if (AT_ONCE > 1) __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -276,7 +307,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
                 int64_t block;
                 int at;
                 attention_place(a, r, key, block, at);
-                const T *const v = (const T *)a.cache.values + h * a.cache.value_strides[2] + block * a.cache.value_strides[0] + at * a.cache.value_strides[1];
+                const T *const v = (const T *)a.cache.values + h * a.cache.value_strides[2] + attention_value_at(a, block, at);
 #pragma unroll
                 for (int f = 0; f < OUTS; ++f)
 #pragma unroll

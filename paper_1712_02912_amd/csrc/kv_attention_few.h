@@ -156,8 +156,8 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
                 int64_t page;
                 int place;
                 attention_place(a, r, min(tile0 + i * UNIT + 16 * s + n, x.keys - 1), page, place);
-                p.k[s] = page * a.cache.key_strides[0] + place * a.cache.key_strides[1];
-                p.v[s] = page * a.cache.value_strides[0] + place * a.cache.value_strides[1];
+                p.k[s] = (int64_t)attention_key_at(a, page, place);
+                p.v[s] = (int64_t)attention_value_at(a, page, place);
             }
             return p;
         };
@@ -221,25 +221,25 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
                 sum += p[e];
             }
             const u32x4 weights = pack8<T>(p);
-            // values: rows of the tile into shared memory, zeros for places that hold no key (they may hold NaN)
+            // values: rows of the tile into shared memory
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bool held = tile + 16 * j + n < x.keys;
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int t = 0; t < STEPS; ++t)
-                    *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = held ? v[j][t] : u32x4{0, 0, 0, 0};
-            }
-            // (what is not finite and not seen by all rows is taken out, see kv_attention_chunk.h)
+                    *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = v[j][t];
+            // zeros for places that hold no key; what is not finite and not seen by all rows is taken out, see kv_attention_chunk.h
             if (!all_seen) {
                 bool found = false;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int j = 0; j < 2; ++j) {
+                    const bool held = tile + 16 * j + n < x.keys;
 #pragma unroll
                     for (int t = 0; t < STEPS; ++t) {
-                        if (tile + 16 * j + n >= x.keys || !any_not_finite<T>(v[j][t])) continue;
-                        found = true;
-                        *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = finite_only<T>(v[j][t]);
+                        if (held && !any_not_finite<T>(v[j][t])) continue;
+                        found |= held;
+                        *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = held ? finite_only<T>(v[j][t]) : u32x4{0, 0, 0, 0};
                     }
+                }
                 taken_out |= __any(found);
             }
             if (i + 1 < tiles) {
@@ -270,7 +270,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
                     int64_t page;
                     int place;
                     attention_place(a, r, key, page, place);
-                    const T *const row_v = values - 8 * g + page * a.cache.value_strides[0] + place * a.cache.value_strides[1];
+                    const T *const row_v = values - 8 * g + attention_value_at(a, page, place);
 #pragma unroll
                     for (int f = 0; f < OUTS; ++f) add_not_finite(row_v + 16 * f + 4 * g, out[f], 0);
                 }

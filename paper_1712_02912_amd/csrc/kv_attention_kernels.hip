@@ -87,6 +87,9 @@ static bool attention_on_matrix_cores(const attention_args &a) {
     if (c.elem == PQ_ELEM_F32 || (c.dim != 64 && c.dim != 96 && c.dim != 128 && c.dim != 256)) return false;
     uint64_t bits = (uint64_t)(uintptr_t)c.keys | (uint64_t)(uintptr_t)c.values | (uint64_t)(uintptr_t)a.q.p | (uint64_t)(uintptr_t)a.out;
     for (int i = 0; i < 3; ++i) bits |= (uint64_t)(c.key_strides[i] | c.value_strides[i]) * 2;
+    // (strides of blocks and places are multiplied in 32 bits)
+    for (int i = 0; i < 2; ++i)
+        if (c.key_strides[i] > INT_MAX || c.value_strides[i] > INT_MAX) return false;
     bits |= (uint64_t)(a.q.token_stride | a.q.head_stride) * 2;
     return bits % 16 == 0;
 }
@@ -112,6 +115,10 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
     a.by_group = fast_div((uint32_t)a.group);
     a.scale_log2 = scale * 1.4426950408889634f;
     if (attention_on_matrix_cores(a)) {
+        for (int i = 0; i < 2; ++i) {
+            a.k_strides[i] = (uint32_t)cache->key_strides[i];
+            a.v_strides[i] = (uint32_t)cache->value_strides[i];
+        }
         // Requests of few rows and others in one call: each goes to its own kernel.  A tile of rows of the chunks' kernel costs a
         // request of one token as much as one of 128 (23 requests of 1 to 517 tokens, 16 heads: 63 us with that kernel alone, XX
         // with both); where all requests have max_new tokens there is one kind only.
