@@ -31,6 +31,7 @@ EXPORTS = ["pq_create", "pq_destroy", "pq_last_error", "pq_version", "pq_build_l
            "ivf_quick_adc_search", "pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens"]
 
 _lib = None
+_entries = {}
 
 
 class IvfLists(ctypes.Structure):
@@ -71,7 +72,7 @@ def load():
     lib.pq_rotate.argtypes = [vp, vp, vp, i64, ci, vp]
     lib.pq_encode.argtypes = [vp, vp, vp, i64, ci, ci, ci, ci, vp]
     lib.pq_derived_search.argtypes = [vp, vp, i64, vp, vp, ci, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, i64]
-    cf, cache, heads = ctypes.c_float, vp, vp   # (structures as their bytes, see _cache and _heads)
+    cf, cache, heads = ctypes.c_float, vp, vp   # (structures as their bytes, which the extension module makes)
     lib.pq_kv_plan.argtypes = [vp, vp, vp, ci, vp, ci, vp, ci, ci, i64, vp, vp, vp, vp, vp]
     lib.pq_kv_append.argtypes = [vp, cache, heads, ci, heads, heads, i64, vp, vp, vp, vp, i64, ci, ci, ci, vp, vp, cf, vp]
     lib.pq_kv_attention.argtypes = [vp, cache, heads, ci, i64, vp, vp, ci, vp, ci, ci, cf, ci, vp, vp]
@@ -82,6 +83,9 @@ def load():
     for name in EXPORTS:
         if name not in ("pq_last_error", "pq_version"):
             getattr(lib, name).restype = ci
+    # the addresses of what the extension module calls by itself
+    for name in ("pq_kv_plan", "pq_kv_append"):
+        _entries[name] = ctypes.cast(getattr(lib, name), vp).value
     _lib = lib
     return lib
 
@@ -325,18 +329,11 @@ class Context:
     def pq_kv_plan(self, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, out=None):
         """Positions and slots of the new tokens; block_tables [nreq][width] gets the fresh blocks.
         Returns (cu_new, kv_lens, positions, slots, taken), `out` if it is given."""
-        i32, i64, at = torch.int32, torch.int64, _views.address
-        nreq, width = block_tables.shape
         if out is None:
+            i32, nreq = torch.int32, block_tables.shape[0]
             out = tuple(torch.empty(n, dtype=dt, device=block_tables.device)
-                        for n, dt in ((nreq + 1, i32), (nreq, i32), (ntokens, i32), (ntokens, i64), (1, i32)))
-        cu_new, kv_lens, positions, slots, taken = out
-        nfree = free_blocks.numel()
-        rc = self.lib.pq_kv_plan(
-            self.handle, at(new_lens, i32, "new_lens", (nreq,)), at(cached_lens, i32, "cached_lens", (nreq,)), nreq,
-            at(block_tables, i32, "block_tables", (nreq, width)), width, at(free_blocks, i32, "free_blocks", (nfree,)), nfree,
-            block_size, ntokens, at(cu_new, i32, "cu_new", (nreq + 1,)), at(kv_lens, i32, "kv_lens", (nreq,)),
-            at(positions, i32, "positions", (ntokens,)), at(slots, i64, "slots", (ntokens,)), at(taken, i32, "taken", (1,)))
+                        for n, dt in ((nreq + 1, i32), (nreq, i32), (ntokens, i32), (ntokens, torch.int64), (1, i32)))
+        rc = _views.plan(_entries["pq_kv_plan"], self.handle.value, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, *out)
         if rc:
             self._check(rc)
         return out
@@ -346,27 +343,10 @@ class Context:
         """Norm and rotation of q [tokens][q heads][dim] and k [tokens][heads][dim]; k and v go into the cache
         [blocks][block size][heads][dim].  cos, sin [positions][rot/2]; without them nothing is rotated.  Returns the queries
         (None if q is None)."""
-        cache, heads, dim = _views.cache(key_cache, value_cache)
-        dtype, f32, at, rows = key_cache.dtype, torch.float32, _views.address, _views.heads
-        t = k.shape[0]
-        shape, q_rows, q_heads = (t, heads, dim), None, 0
-        if q is not None:
-            q_heads = q.shape[1]
-            q_shape = (t, q_heads, dim)
-            q_rows = rows(q, dtype, "q", q_shape)
-            if out is None:
-                out = torch.empty(q_shape, dtype=dtype, device=q.device)
-        if (cos is None) != (sin is None):
-            raise ValueError("cos and sin go together")
-        table = (0, 0) if cos is None else tuple(cos.shape)
-        if len(table) != 2:
-            raise ValueError("cos and sin must be [positions][rot/2]")
-        rc = self.lib.pq_kv_append(
-            self.handle, cache, q_rows, q_heads, rows(k, dtype, "k", shape), rows(v, dtype, "v", shape), t,
-            at(positions, torch.int32, "positions", (t,)), at(slots, torch.int64, "slots", (t,)), at(cos, f32, "cos", table),
-            at(sin, f32, "sin", table), table[0], 2 * table[1], 1 if pairs else 0, 1 if norm else 0,
-            at(q_weight, f32, "q_weight", (dim,)), at(k_weight, f32, "k_weight", (dim,)), eps,
-            None if q is None else at(out, dtype, "out", q_shape))
+        if q is not None and out is None:
+            out = torch.empty(q.shape, dtype=key_cache.dtype, device=q.device)
+        rc = _views.append(_entries["pq_kv_append"], self.handle.value, q, k, v, positions, slots, key_cache, value_cache, cos, sin, q_weight,
+                           k_weight, eps, norm, pairs, out)
         if rc:
             self._check(rc)
         return out if q is not None else None

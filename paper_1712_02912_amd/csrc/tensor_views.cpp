@@ -1,11 +1,16 @@
 // What the binding asks of tensors, as an extension module: checks, addresses and strides.  A call of the reading step takes up
 // to a dozen tensors and some microseconds; asked from Python, each tensor costs a third of a microsecond, here a tenth of
-// that.  Errors are raised here; no tensor is kept.
+// that.  The plan and the append of few tokens take less on the GPU than their arguments in Python, so these two are called from
+// here altogether (64 requests: 5.0 us a call of the plan by way of Python's foreign functions, 3.9 us from here).
+// Errors are raised here; no tensor is kept.
 #define PY_SSIZE_T_CLEAN   // (before any header of Python)
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdint.h>
+
+#include <algorithm>
+#include <string>
 
 #include "pq_read.h"
 
@@ -95,22 +100,163 @@ PyObject *rows(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return Py_BuildValue("KiLLL", (unsigned long long)(uintptr_t)t->data_ptr(), elem, (long long)t->stride(0), (long long)t->size(0), (long long)t->size(1));
 }
 
+bool read_cache(PyObject *keys, PyObject *values, pq_kv_cache *c) {
+    const at::Tensor *k = tensor_of(keys, "key_cache"), *v = k ? tensor_of(values, "value_cache") : nullptr;
+    if (!v) return false;
+    const int elem = elem_of(*k, "key_cache");
+    if (elem < 0) return false;
+    if (v->scalar_type() != k->scalar_type()) {
+        PyErr_Format(PyExc_TypeError, "value_cache has dtype %s, key_cache %s", dtype_name(v->scalar_type()), dtype_name(k->scalar_type()));
+        return false;
+    }
+    if (k->dim() != 4 || !v->sizes().equals(k->sizes())) {
+        PyErr_Format(PyExc_ValueError, "keys and values must have one shape [blocks][block size][heads][dim]");
+        return false;
+    }
+    if (!rows_contiguous(*k, "key_cache") || !rows_contiguous(*v, "value_cache")) return false;
+    if (k->size(1) > INT32_MAX || k->size(2) > INT32_MAX || k->size(3) > INT32_MAX) {
+        PyErr_Format(PyExc_ValueError, "the cache is too large");
+        return false;
+    }
+    *c = {k->data_ptr(), v->data_ptr(), {k->stride(0), k->stride(1), k->stride(2)}, {v->stride(0), v->stride(1), v->stride(2)},
+          k->size(0), (int)k->size(1), (int)k->size(2), (int)k->size(3), (pq_elem)elem};
+    return true;
+}
+
 // cache(keys, values): paged [blocks][block size][heads][dim] of any strides but the last -> (bytes of a pq_kv_cache, heads, dim)
 PyObject *cache(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != 2) return PyErr_Format(PyExc_TypeError, "cache takes keys and values");
-    const at::Tensor *k = tensor_of(args[0], "key_cache"), *v = k ? tensor_of(args[1], "value_cache") : nullptr;
-    if (!v) return nullptr;
-    const int elem = elem_of(*k, "key_cache");
-    if (elem < 0) return nullptr;
-    if (v->scalar_type() != k->scalar_type())
-        return PyErr_Format(PyExc_TypeError, "value_cache has dtype %s, key_cache %s", dtype_name(v->scalar_type()), dtype_name(k->scalar_type()));
-    if (k->dim() != 4 || !v->sizes().equals(k->sizes()))
-        return PyErr_Format(PyExc_ValueError, "keys and values must have one shape [blocks][block size][heads][dim]");
-    if (!rows_contiguous(*k, "key_cache") || !rows_contiguous(*v, "value_cache")) return nullptr;
-    if (k->size(1) > INT32_MAX || k->size(2) > INT32_MAX || k->size(3) > INT32_MAX) return PyErr_Format(PyExc_ValueError, "the cache is too large");
-    pq_kv_cache c = {k->data_ptr(), v->data_ptr(), {k->stride(0), k->stride(1), k->stride(2)}, {v->stride(0), v->stride(1), v->stride(2)},
-                     k->size(0), (int)k->size(1), (int)k->size(2), (int)k->size(3), (pq_elem)elem};
+    pq_kv_cache c;
+    if (!read_cache(args[0], args[1], &c)) return nullptr;
     return Py_BuildValue("y#ii", (const char *)&c, (Py_ssize_t)sizeof(c), c.heads, c.dim);
+}
+
+// ---- whole calls ------------------------------------------------------------------------------------------
+bool has_type(const at::Tensor &t, at::ScalarType want, const char *name) {
+    if (t.scalar_type() == want) return true;
+    PyErr_Format(PyExc_TypeError, "%s must have dtype %s, got %s", name, dtype_name(want), dtype_name(t.scalar_type()));
+    return false;
+}
+bool has_sizes(const at::Tensor &t, at::IntArrayRef want, const char *name) {
+    if (t.sizes().equals(want)) return true;
+    std::string text;
+    for (const int64_t n : want) text += (text.empty() ? "" : ", ") + std::to_string(n);
+    PyErr_Format(PyExc_ValueError, "%s does not have shape (%s)", name, text.c_str());
+    return false;
+}
+// The address of a contiguous tensor of that type and shape (null of None, where that may be).
+template <class P> bool in_place(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const char *name, P **p, bool may_be_none = false) {
+    *p = nullptr;
+    if (may_be_none && o == Py_None) return true;
+    const at::Tensor *t = tensor_of(o, name);
+    if (!t || !has_type(*t, type, name)) return false;
+    if (!t->is_contiguous()) {
+        PyErr_Format(PyExc_ValueError, "%s must be contiguous", name);
+        return false;
+    }
+    if (!has_sizes(*t, sizes, name)) return false;
+    *p = (P *)t->data_ptr();
+    return true;
+}
+bool in_rows(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const char *name, pq_heads *h) {
+    const at::Tensor *t = tensor_of(o, name);
+    if (!t || !has_type(*t, type, name) || !has_sizes(*t, sizes, name) || !rows_contiguous(*t, name)) return false;
+    *h = {t->data_ptr(), t->stride(0), t->stride(1)};
+    return true;
+}
+bool whole(PyObject *o, int64_t *x) {
+    *x = PyLong_AsLongLong(o);
+    return *x != -1 || !PyErr_Occurred();
+}
+// The library's function and context, as the binding has them: addresses.
+template <class F> bool entry(PyObject *const *args, F **f, pq_ctx **ctx) {
+    *f = (F *)PyLong_AsVoidPtr(args[0]);
+    *ctx = *f ? (pq_ctx *)PyLong_AsVoidPtr(args[1]) : nullptr;
+    if (*f && *ctx) return true;
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "the context is closed");
+    return false;
+}
+template <class F> PyObject *without_gil(F f) {
+    PyThreadState *const state = PyEval_SaveThread();
+    const int rc = f();
+    PyEval_RestoreThread(state);
+    return PyLong_FromLong(rc);
+}
+
+// plan(function, context, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, cu_new, kv_lens, positions, slots, taken)
+PyObject *plan(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 13) return PyErr_Format(PyExc_TypeError, "plan takes 13 arguments");
+    decltype(pq_kv_plan) *f;
+    pq_ctx *ctx;
+    int64_t block_size, ntokens;
+    if (!entry(args, &f, &ctx) || !whole(args[6], &block_size) || !whole(args[7], &ntokens)) return nullptr;
+    const at::Tensor *tables = tensor_of(args[4], "block_tables"), *free_blocks = tables ? tensor_of(args[5], "free_blocks") : nullptr;
+    if (!free_blocks) return nullptr;
+    if (tables->dim() != 2) return PyErr_Format(PyExc_ValueError, "block_tables must be [requests][width]");
+    const int64_t nreq = tables->size(0), width = tables->size(1), nfree = free_blocks->numel();
+    for (const int64_t x : {nreq, width, nfree, block_size})
+        if (x > INT32_MAX || x < INT32_MIN) return PyErr_Format(PyExc_ValueError, "sizes must be below 2^31");
+    const int32_t *new_lens, *cached_lens, *free_p;
+    int32_t *tables_p, *cu, *kv, *positions, *taken;
+    int64_t *slots;
+    // (a negative ntokens is the library's to refuse)
+    const int64_t rows = std::max<int64_t>(ntokens, 0);
+    if (!in_place(args[2], at::kInt, {nreq}, "new_lens", &new_lens) || !in_place(args[3], at::kInt, {nreq}, "cached_lens", &cached_lens) ||
+        !in_place(args[4], at::kInt, {nreq, width}, "block_tables", &tables_p) || !in_place(args[5], at::kInt, {nfree}, "free_blocks", &free_p) ||
+        !in_place(args[8], at::kInt, {nreq + 1}, "cu_new", &cu) || !in_place(args[9], at::kInt, {nreq}, "kv_lens", &kv) ||
+        !in_place(args[10], at::kInt, {rows}, "positions", &positions) || !in_place(args[11], at::kLong, {rows}, "slots", &slots) ||
+        !in_place(args[12], at::kInt, {1}, "taken", &taken))
+        return nullptr;
+    return without_gil([&] {
+        return f(ctx, new_lens, cached_lens, (int)nreq, tables_p, (int)width, free_p, (int)nfree, (int)block_size, ntokens, cu, kv, positions, slots, taken);
+    });
+}
+
+// append(function, context, q, k, v, positions, slots, key_cache, value_cache, cos, sin, q_weight, k_weight, eps, norm, pairs, out)
+PyObject *append(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 17) return PyErr_Format(PyExc_TypeError, "append takes 17 arguments");
+    decltype(pq_kv_append) *f;
+    pq_ctx *ctx;
+    pq_kv_cache cache;
+    if (!entry(args, &f, &ctx) || !read_cache(args[7], args[8], &cache)) return nullptr;
+    const at::ScalarType type = THPVariable_Unpack(args[7]).scalar_type();
+    const at::Tensor *k = tensor_of(args[3], "k");
+    if (!k) return nullptr;
+    const int64_t t = k->dim() > 0 ? k->size(0) : 0;
+    int64_t q_heads = 0, max_positions = 0, half = 0;
+    pq_heads q_rows = {}, k_rows, v_rows;
+    void *out = nullptr;
+    if (args[2] != Py_None) {
+        const at::Tensor *q = tensor_of(args[2], "q");
+        if (!q) return nullptr;
+        q_heads = q->dim() == 3 ? q->size(1) : 0;
+        if (q_heads > INT32_MAX) return PyErr_Format(PyExc_ValueError, "sizes must be below 2^31");
+        if (!in_rows(args[2], type, {t, q_heads, cache.dim}, "q", &q_rows) || !in_place(args[16], type, {t, q_heads, cache.dim}, "out", &out)) return nullptr;
+    }
+    if ((args[9] == Py_None) != (args[10] == Py_None)) return PyErr_Format(PyExc_ValueError, "cos and sin go together");
+    if (args[9] != Py_None) {
+        const at::Tensor *cos = tensor_of(args[9], "cos");
+        if (!cos) return nullptr;
+        if (cos->dim() != 2 || cos->size(1) > INT32_MAX / 2) return PyErr_Format(PyExc_ValueError, "cos and sin must be [positions][rot/2]");
+        max_positions = cos->size(0);
+        half = cos->size(1);
+    }
+    const int32_t *positions;
+    const int64_t *slots;
+    const float *cos_p, *sin_p, *q_weight, *k_weight;
+    if (!in_rows(args[3], type, {t, cache.heads, cache.dim}, "k", &k_rows) || !in_rows(args[4], type, {t, cache.heads, cache.dim}, "v", &v_rows) ||
+        !in_place(args[5], at::kInt, {t}, "positions", &positions) || !in_place(args[6], at::kLong, {t}, "slots", &slots) ||
+        !in_place(args[9], at::kFloat, {max_positions, half}, "cos", &cos_p, true) || !in_place(args[10], at::kFloat, {max_positions, half}, "sin", &sin_p, true) ||
+        !in_place(args[11], at::kFloat, {cache.dim}, "q_weight", &q_weight, true) || !in_place(args[12], at::kFloat, {cache.dim}, "k_weight", &k_weight, true))
+        return nullptr;
+    const double eps = PyFloat_AsDouble(args[13]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    const int norm = PyObject_IsTrue(args[14]), pairs = PyObject_IsTrue(args[15]);
+    if (norm < 0 || pairs < 0) return nullptr;
+    return without_gil([&] {
+        return f(ctx, &cache, q_heads > 0 ? &q_rows : nullptr, (int)q_heads, &k_rows, &v_rows, t, positions, slots, cos_p, sin_p, max_positions, (int)(2 * half), pairs,
+                 norm, q_weight, k_weight, (float)eps, out);
+    });
 }
 
 typedef PyObject *(*fast_function)(PyObject *, PyObject *const *, Py_ssize_t);
@@ -127,6 +273,8 @@ PyMethodDef methods[] = {{"address", (PyCFunction)(void (*)())(fast_function)gua
                          {"heads", (PyCFunction)(void (*)())(fast_function)guarded<heads>, METH_FASTCALL, nullptr},
                          {"rows", (PyCFunction)(void (*)())(fast_function)guarded<rows>, METH_FASTCALL, nullptr},
                          {"cache", (PyCFunction)(void (*)())(fast_function)guarded<cache>, METH_FASTCALL, nullptr},
+                         {"plan", (PyCFunction)(void (*)())(fast_function)guarded<plan>, METH_FASTCALL, nullptr},
+                         {"append", (PyCFunction)(void (*)())(fast_function)guarded<append>, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "tensor_views", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
