@@ -58,7 +58,7 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
     size_t ws_at = 0;
     few_line line = {};
     if (some_few) {
-        if (const int rc = few_prepare(ctx, a, WAVES, ws, &line, &ws_at)) return rc;
+        if (const int rc = few_prepare(ctx, a, WAVES, true, ws, &line, &ws_at)) return rc;
         if (line.row_waves > JOIN_ROWS) line.row_waves = JOIN_ROWS;
     } else if (ws > 0) {
         if (const int rc = buf_reserve(ctx, &ctx->read_ws, ws, "parts of the attention")) return rc;
@@ -71,10 +71,11 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
     if (some_few) {
         const int64_t all = chunk_blocks * split.splits + line.blocks;
         kv_attention_mixed_kernel<T, D, WAVES><<<(unsigned)all, 64 * WAVES, 0, ctx->stream>>>(a, split, (int)chunk_blocks, line);
-        const int slices = few_slices(line, FEW_ROWS, JOIN_ROWS);
+        const int slices = line.each ? 0 : few_slices(line, FEW_ROWS, JOIN_ROWS);
         const int64_t few_blocks = (int64_t)a.nreq * a.cache.heads * slices;
         if (few_blocks + joins > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", a.nreq);
-        kv_attention_mixed_join_kernel<T, D><<<(unsigned)(few_blocks + joins), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split, (int)few_blocks, slices, line);
+        if (few_blocks + joins > 0)
+            kv_attention_mixed_join_kernel<T, D><<<(unsigned)(few_blocks + joins), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split, (int)few_blocks, slices, line);
     } else {
         kv_attention_chunk_kernel<T, D, WAVES><<<dim3((unsigned)chunk_blocks, split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
         if (joins > 0) kv_attention_chunk_join_kernel<T, D><<<joins, 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split);

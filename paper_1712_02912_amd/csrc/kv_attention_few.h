@@ -21,6 +21,7 @@ constexpr int FEW_MAX = 1024;    // requests whose line a block adds up in share
 
 struct few_line {
     int unit;                // keys of a unit: FEW_TILE for each wave of a block
+    bool each;               // a block for each (request, head), no line
     const int64_t *starts;   // [nreq + 1] units of one head before each request, where the block does not add them up itself
     int64_t *starts_out;     // the same, for the kernel that joins the parts
     float *parts, *stats;    // [blocks][2][rows][D], [blocks][2][rows][2]
@@ -101,25 +102,29 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
     unsigned char *const mine = pool + wave * FEW_TILE * row::bytes;
 
-    const int64_t *starts = line.starts;
-    if (!starts) {
-        few_starts<THREADS>(a, UNIT, own_starts);
-        starts = own_starts;
-        if (block == 0)
-            for (int i = tid; i <= a.nreq; i += THREADS) line.starts_out[i] = own_starts[i];
-    }
     const int heads = a.cache.heads;
-    const int64_t total = starts[a.nreq] * heads;
-    const few_cut cut(total, line.blocks);
-    const int64_t begin = cut.begin(block), end = cut.begin(block + 1);
+    const int64_t *starts = line.starts;
+    int64_t begin = 0, end = 1;
+    if (!line.each) {
+        if (!starts) {
+            few_starts<THREADS>(a, UNIT, own_starts);
+            starts = own_starts;
+            if (block == 0)
+                for (int i = tid; i <= a.nreq; i += THREADS) line.starts_out[i] = own_starts[i];
+        }
+        const few_cut cut(starts[a.nreq] * heads, line.blocks);
+        begin = cut.begin(block);
+        end = cut.begin(block + 1);
+    }
 
     for (int64_t at = begin; at < end;) {
-        // the request and head at this place of the line
-        const int r = wave_search(a.nreq, [&](int i) { return starts[i] * heads <= at; });
+        // the request and head at this place of the line, or of this block
+        const int r = line.each ? block / heads : wave_search(a.nreq, [&](int i) { return starts[i] * heads <= at; });
         const few_range x = few_load(a, UNIT, r);
-        const int64_t in_request = at - starts[r] * heads;
+        if (x.units == 0) return;   // (of a block of its own)
+        const int64_t in_request = line.each ? (block - r * heads) * x.units : at - starts[r] * heads;
         const int h = (int)(in_request / x.units);
-        const int64_t first = in_request - h * x.units, count = min(x.units - first, end - at);
+        const int64_t first = in_request - h * x.units, count = line.each ? x.units : min(x.units - first, end - at);
         const bool whole = count == x.units;
         const int part = at == begin ? 0 : 1;
         at += count;
@@ -369,8 +374,8 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_join_bl
 }
 
 // The line's memory in read_ws (from its start on), its blocks and the waves that join a row; grows the buffer to hold `more` bytes
-// behind it.
-int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, few_line *line, size_t *ws_used);
+// behind it.  beside: in one launch with chunks.
+int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, bool beside, size_t more, few_line *line, size_t *ws_used);
 // Slices of the rows of a (request, head) for the kernel that joins, of `waves` waves.
 static inline int few_slices(const few_line &line, int most_rows, int waves) { return (most_rows * line.row_waves + waves - 1) / waves; }
 
