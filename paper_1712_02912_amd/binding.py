@@ -72,19 +72,14 @@ def load():
     lib.pq_rotate.argtypes = [vp, vp, vp, i64, ci, vp]
     lib.pq_encode.argtypes = [vp, vp, vp, i64, ci, ci, ci, ci, vp]
     lib.pq_derived_search.argtypes = [vp, vp, i64, vp, vp, ci, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, i64]
-    cf, cache, heads = ctypes.c_float, vp, vp   # (structures as their bytes, which the extension module makes)
-    lib.pq_kv_plan.argtypes = [vp, vp, vp, ci, vp, ci, vp, ci, ci, i64, vp, vp, vp, vp, vp]
-    lib.pq_kv_append.argtypes = [vp, cache, heads, ci, heads, heads, i64, vp, vp, vp, vp, i64, ci, ci, ci, vp, vp, cf, vp]
-    lib.pq_kv_attention.argtypes = [vp, cache, heads, ci, i64, vp, vp, ci, vp, ci, ci, cf, ci, vp, vp]
-    lib.pq_sample_tokens.argtypes = [vp, vp, ci, i64, ci, ci, vp, i64, vp, vp, vp, vp, vp, vp]
     lib.pq_calibration_copy.argtypes = [vp, vp, vp, ctypes.c_size_t]
     lib.pq_set_profiling.argtypes = [vp, ci]
     lib.pq_last_scan_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     for name in EXPORTS:
         if name not in ("pq_last_error", "pq_version"):
             getattr(lib, name).restype = ci
-    # the addresses of what the extension module calls by itself
-    for name in ("pq_kv_plan", "pq_kv_append"):
+    # the reading step is called from the extension module, by the functions' addresses
+    for name in ("pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens"):
         _entries[name] = ctypes.cast(getattr(lib, name), vp).value
     _lib = lib
     return lib
@@ -354,19 +349,12 @@ class Context:
     def pq_kv_attention(self, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new, scale=None, window=0, out=None,
                         lse=None):
         """Attention of q [tokens][q heads][dim] over the paged cache; scale None: 1 / sqrt(dim).  Returns (out, lse)."""
-        cache, _, dim = _views.cache(key_cache, value_cache)
-        dtype, i32, at = key_cache.dtype, torch.int32, _views.address
-        t, q_heads, _ = q.shape
-        nreq, width = block_tables.shape
-        shape = (t, q_heads, dim)
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=q.device)
+            out = torch.empty(q.shape, dtype=key_cache.dtype, device=q.device)
         if lse is None:
-            lse = torch.empty((t, q_heads), dtype=torch.float32, device=q.device)
-        rc = self.lib.pq_kv_attention(
-            self.handle, cache, _views.heads(q, dtype, "q", shape), q_heads, t, at(cu_new, i32, "cu_new", (nreq + 1,)),
-            at(kv_lens, i32, "kv_lens", (nreq,)), nreq, at(block_tables, i32, "block_tables", (nreq, width)), width, max_new,
-            dim ** -0.5 if scale is None else scale, window, at(out, dtype, "out", shape), at(lse, torch.float32, "lse", (t, q_heads)))
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        rc = _views.attention(_entries["pq_kv_attention"], self.handle.value, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new,
+                              scale, window, out, lse)
         if rc:
             self._check(rc)
         return out, lse
@@ -374,21 +362,10 @@ class Context:
     def pq_sample_tokens(self, logits, noise, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
         """One token for each row of logits [rows][vocab]; noise [rows][vocab] uniform in (0, 1), None: the largest logits.
         Returns (tokens, logprobs)."""
-        p, elem, stride, rows, vocab = _views.rows(logits, "logits")
-        noise_p, noise_stride, f32, at = None, 0, torch.float32, _views.address
-        if noise is not None:
-            noise_p, noise_elem, noise_stride, noise_rows, noise_vocab = _views.rows(noise, "noise")
-            if noise_elem != 0:
-                raise TypeError(f"noise must have dtype {f32}, got {noise.dtype}")
-            if (noise_rows, noise_vocab) != (rows, vocab):
-                raise ValueError(f"noise must have shape {[rows, vocab]}, got {list(noise.shape)}")
         if out is None:
-            out = (torch.empty(rows, dtype=torch.int64, device=logits.device), torch.empty(rows, dtype=f32, device=logits.device))
-        per_row = (rows,)
-        rc = self.lib.pq_sample_tokens(
-            self.handle, p, elem, stride, rows, vocab, noise_p, noise_stride, at(temperature, f32, "temperature", per_row),
-            at(top_k, torch.int32, "top_k", per_row), at(top_p, f32, "top_p", per_row), at(min_p, f32, "min_p", per_row),
-            at(out[0], torch.int64, "tokens", per_row), at(out[1], f32, "logprobs", per_row))
+            rows = logits.shape[0]
+            out = (torch.empty(rows, dtype=torch.int64, device=logits.device), torch.empty(rows, dtype=torch.float32, device=logits.device))
+        rc = _views.sample(_entries["pq_sample_tokens"], self.handle.value, logits, noise, temperature, top_k, top_p, min_p, *out)
         if rc:
             self._check(rc)
         return out

@@ -1,15 +1,14 @@
-// What the binding asks of tensors, as an extension module: checks, addresses and strides.  A call of the reading step takes up
-// to a dozen tensors and some microseconds; asked from Python, each tensor costs a third of a microsecond, here a tenth of
-// that.  The plan and the append of few tokens take less on the GPU than their arguments in Python, so these two are called from
-// here altogether (64 requests: 5.0 us a call of the plan by way of Python's foreign functions, 3.9 us from here).
-// Errors are raised here; no tensor is kept.
+// The calls of the reading step from Python, as an extension module: checks of the tensors, their addresses and strides, and the
+// library's function.  A call takes up to a dozen tensors, and where tokens are few its kernel takes less than these do if they are
+// asked from Python: the plan of 64 requests 5.0 us a call by way of Python's foreign functions, 3.5 us from here; the append of
+// 64 tokens 5.9 and 3.8 us.  Errors are raised here; no tensor is kept.
 #define PY_SSIZE_T_CLEAN   // (before any header of Python)
-#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
 
 #include "pq_read.h"
@@ -25,28 +24,6 @@ const at::Tensor *tensor_of(PyObject *o, const char *name) {
         return nullptr;
     }
     return &THPVariable_Unpack(o);
-}
-
-bool has_dtype(const at::Tensor &t, PyObject *dtype, const char *name) {
-    if (!THPDtype_Check(dtype)) {
-        PyErr_SetString(PyExc_TypeError, "not a dtype");
-        return false;
-    }
-    const at::ScalarType want = ((THPDtype *)dtype)->scalar_type;
-    if (t.scalar_type() == want) return true;
-    PyErr_Format(PyExc_TypeError, "%s must have dtype %s, got %s", name, dtype_name(want), dtype_name(t.scalar_type()));
-    return false;
-}
-
-bool has_shape(const at::Tensor &t, PyObject *shape, const char *name) {
-    if (PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == t.dim()) {
-        bool same = true;
-        for (int64_t i = 0; i < t.dim() && same; ++i) same = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i)) == t.size(i);
-        if (same) return true;
-        if (PyErr_Occurred()) return false;
-    }
-    PyErr_Format(PyExc_ValueError, "%s does not have shape %R", name, shape);
-    return false;
 }
 
 bool rows_contiguous(const at::Tensor &t, const char *name) {
@@ -65,41 +42,7 @@ int elem_of(const at::Tensor &t, const char *name) {
     }
 }
 
-// address(tensor, dtype, name, shape): of a contiguous tensor that the library reads and writes where it lies; None of None
-PyObject *address(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (n != 4) return PyErr_Format(PyExc_TypeError, "address takes a tensor, a dtype, a name and a shape");
-    if (args[0] == Py_None) Py_RETURN_NONE;
-    const char *name = PyUnicode_AsUTF8(args[2]);
-    const at::Tensor *t = name ? tensor_of(args[0], name) : nullptr;
-    if (!t || !has_dtype(*t, args[1], name)) return nullptr;
-    if (!t->is_contiguous()) return PyErr_Format(PyExc_ValueError, "%s must be contiguous", name);
-    if (!has_shape(*t, args[3], name)) return nullptr;
-    return PyLong_FromVoidPtr(t->data_ptr());
-}
-
-// heads(tensor, dtype, name, shape): rows [tokens][heads][dim] of any strides but the last, as the bytes of a pq_heads
-PyObject *heads(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (n != 4) return PyErr_Format(PyExc_TypeError, "heads takes a tensor, a dtype, a name and a shape");
-    const char *name = PyUnicode_AsUTF8(args[2]);
-    const at::Tensor *t = name ? tensor_of(args[0], name) : nullptr;
-    if (!t || !has_dtype(*t, args[1], name) || !has_shape(*t, args[3], name) || !rows_contiguous(*t, name)) return nullptr;
-    const pq_heads h = {t->data_ptr(), t->stride(0), t->stride(1)};
-    return PyBytes_FromStringAndSize((const char *)&h, sizeof(h));
-}
-
-// rows(tensor, name): a matrix of any strides but the last -> (address, pq_elem, row stride, rows, columns)
-PyObject *rows(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (n != 2) return PyErr_Format(PyExc_TypeError, "rows takes a tensor and a name");
-    const char *name = PyUnicode_AsUTF8(args[1]);
-    const at::Tensor *t = name ? tensor_of(args[0], name) : nullptr;
-    if (!t) return nullptr;
-    const int elem = elem_of(*t, name);
-    if (elem < 0) return nullptr;
-    if (t->dim() != 2) return PyErr_Format(PyExc_ValueError, "%s must be a matrix", name);
-    if (!rows_contiguous(*t, name)) return nullptr;
-    return Py_BuildValue("KiLLL", (unsigned long long)(uintptr_t)t->data_ptr(), elem, (long long)t->stride(0), (long long)t->size(0), (long long)t->size(1));
-}
-
+// Paged [blocks][block size][heads][dim] of any strides but the last.
 bool read_cache(PyObject *keys, PyObject *values, pq_kv_cache *c) {
     const at::Tensor *k = tensor_of(keys, "key_cache"), *v = k ? tensor_of(values, "value_cache") : nullptr;
     if (!v) return false;
@@ -123,15 +66,6 @@ bool read_cache(PyObject *keys, PyObject *values, pq_kv_cache *c) {
     return true;
 }
 
-// cache(keys, values): paged [blocks][block size][heads][dim] of any strides but the last -> (bytes of a pq_kv_cache, heads, dim)
-PyObject *cache(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (n != 2) return PyErr_Format(PyExc_TypeError, "cache takes keys and values");
-    pq_kv_cache c;
-    if (!read_cache(args[0], args[1], &c)) return nullptr;
-    return Py_BuildValue("y#ii", (const char *)&c, (Py_ssize_t)sizeof(c), c.heads, c.dim);
-}
-
-// ---- whole calls ------------------------------------------------------------------------------------------
 bool has_type(const at::Tensor &t, at::ScalarType want, const char *name) {
     if (t.scalar_type() == want) return true;
     PyErr_Format(PyExc_TypeError, "%s must have dtype %s, got %s", name, dtype_name(want), dtype_name(t.scalar_type()));
@@ -158,6 +92,7 @@ template <class P> bool in_place(PyObject *o, at::ScalarType type, at::IntArrayR
     *p = (P *)t->data_ptr();
     return true;
 }
+// Rows [tokens][heads][dim] of any strides but the last.
 bool in_rows(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const char *name, pq_heads *h) {
     const at::Tensor *t = tensor_of(o, name);
     if (!t || !has_type(*t, type, name) || !has_sizes(*t, sizes, name) || !rows_contiguous(*t, name)) return false;
@@ -259,6 +194,73 @@ PyObject *append(PyObject *, PyObject *const *args, Py_ssize_t n) {
     });
 }
 
+// attention(function, context, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new, scale, window, out, lse)
+PyObject *attention(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 13) return PyErr_Format(PyExc_TypeError, "attention takes 13 arguments");
+    decltype(pq_kv_attention) *f;
+    pq_ctx *ctx;
+    pq_kv_cache cache;
+    int64_t max_new, window;
+    if (!entry(args, &f, &ctx) || !read_cache(args[3], args[4], &cache) || !whole(args[8], &max_new) || !whole(args[10], &window)) return nullptr;
+    const at::ScalarType type = THPVariable_Unpack(args[3]).scalar_type();
+    const at::Tensor *q = tensor_of(args[2], "q"), *tables = q ? tensor_of(args[5], "block_tables") : nullptr;
+    if (!tables) return nullptr;
+    if (tables->dim() != 2) return PyErr_Format(PyExc_ValueError, "block_tables must be [requests][width]");
+    const int64_t t = q->dim() == 3 ? q->size(0) : 0, q_heads = q->dim() == 3 ? q->size(1) : 0, nreq = tables->size(0), width = tables->size(1);
+    for (const int64_t x : {q_heads, nreq, width, max_new, window})
+        if (x > INT32_MAX || x < INT32_MIN) return PyErr_Format(PyExc_ValueError, "sizes must be below 2^31");
+    const double scale = args[9] == Py_None ? 1.0 / std::sqrt((double)cache.dim) : PyFloat_AsDouble(args[9]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    pq_heads q_rows;
+    const int32_t *tables_p, *cu, *kv;
+    void *out;
+    float *lse;
+    if (!in_rows(args[2], type, {t, q_heads, cache.dim}, "q", &q_rows) || !in_place(args[5], at::kInt, {nreq, width}, "block_tables", &tables_p) ||
+        !in_place(args[6], at::kInt, {nreq + 1}, "cu_new", &cu) || !in_place(args[7], at::kInt, {nreq}, "kv_lens", &kv) ||
+        !in_place(args[11], type, {t, q_heads, cache.dim}, "out", &out) || !in_place(args[12], at::kFloat, {t, q_heads}, "lse", &lse))
+        return nullptr;
+    return without_gil([&] {
+        return f(ctx, &cache, &q_rows, (int)q_heads, t, cu, kv, (int)nreq, tables_p, (int)width, (int)max_new, (float)scale, (int)window, out, lse);
+    });
+}
+
+// sample(function, context, logits, noise, temperature, top_k, top_p, min_p, tokens, logprobs)
+PyObject *sample(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n != 10) return PyErr_Format(PyExc_TypeError, "sample takes 10 arguments");
+    decltype(pq_sample_tokens) *f;
+    pq_ctx *ctx;
+    if (!entry(args, &f, &ctx)) return nullptr;
+    const at::Tensor *logits = tensor_of(args[2], "logits");
+    if (!logits) return nullptr;
+    const int elem = elem_of(*logits, "logits");
+    if (elem < 0) return nullptr;
+    if (logits->dim() != 2) return PyErr_Format(PyExc_ValueError, "logits must be [rows][vocab]");
+    if (!rows_contiguous(*logits, "logits")) return nullptr;
+    const int64_t rows = logits->size(0), vocab = logits->size(1);
+    if (rows > INT32_MAX || vocab > INT32_MAX) return PyErr_Format(PyExc_ValueError, "sizes must be below 2^31");
+    const float *noise = nullptr;
+    int64_t noise_stride = 0;
+    if (args[3] != Py_None) {
+        const at::Tensor *u = tensor_of(args[3], "noise");
+        if (!u || !has_type(*u, at::kFloat, "noise") || !has_sizes(*u, {rows, vocab}, "noise") || !rows_contiguous(*u, "noise")) return nullptr;
+        noise = (const float *)u->data_ptr();
+        noise_stride = u->stride(0);
+    }
+    const float *temperature, *top_p, *min_p;
+    const int32_t *top_k;
+    int64_t *tokens;
+    float *logprobs;
+    if (!in_place(args[4], at::kFloat, {rows}, "temperature", &temperature, true) || !in_place(args[5], at::kInt, {rows}, "top_k", &top_k, true) ||
+        !in_place(args[6], at::kFloat, {rows}, "top_p", &top_p, true) || !in_place(args[7], at::kFloat, {rows}, "min_p", &min_p, true) ||
+        !in_place(args[8], at::kLong, {rows}, "tokens", &tokens) || !in_place(args[9], at::kFloat, {rows}, "logprobs", &logprobs, true))
+        return nullptr;
+    const void *const p = logits->data_ptr();
+    const int64_t row_stride = logits->stride(0);
+    return without_gil([&] {
+        return f(ctx, p, (pq_elem)elem, row_stride, (int)rows, (int)vocab, noise, noise_stride, temperature, top_k, top_p, min_p, tokens, logprobs);
+    });
+}
+
 typedef PyObject *(*fast_function)(PyObject *, PyObject *const *, Py_ssize_t);
 template <fast_function F> PyObject *guarded(PyObject *self, PyObject *const *args, Py_ssize_t n) {
     try {
@@ -269,13 +271,8 @@ template <fast_function F> PyObject *guarded(PyObject *self, PyObject *const *ar
     }
 }
 
-PyMethodDef methods[] = {{"address", (PyCFunction)(void (*)())(fast_function)guarded<address>, METH_FASTCALL, nullptr},
-                         {"heads", (PyCFunction)(void (*)())(fast_function)guarded<heads>, METH_FASTCALL, nullptr},
-                         {"rows", (PyCFunction)(void (*)())(fast_function)guarded<rows>, METH_FASTCALL, nullptr},
-                         {"cache", (PyCFunction)(void (*)())(fast_function)guarded<cache>, METH_FASTCALL, nullptr},
-                         {"plan", (PyCFunction)(void (*)())(fast_function)guarded<plan>, METH_FASTCALL, nullptr},
-                         {"append", (PyCFunction)(void (*)())(fast_function)guarded<append>, METH_FASTCALL, nullptr},
-                         {nullptr, nullptr, 0, nullptr}};
+#define METHOD(f) {#f, (PyCFunction)(void (*)())(fast_function)guarded<f>, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {METHOD(plan), METHOD(append), METHOD(attention), METHOD(sample), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "tensor_views", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
