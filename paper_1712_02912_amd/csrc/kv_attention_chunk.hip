@@ -58,7 +58,7 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
     size_t ws_at = 0;
     few_line line = {};
     if (some_few) {
-        if (const int rc = few_prepare(ctx, a, WAVES, true, ws, &line, &ws_at)) return rc;
+        if (const int rc = few_prepare(ctx, a, WAVES, ws, &line, &ws_at)) return rc;
         if (line.row_waves > JOIN_ROWS) line.row_waves = JOIN_ROWS;
     } else if (ws > 0) {
         if (const int rc = buf_reserve(ctx, &ctx->read_ws, ws, "parts of the attention")) return rc;
@@ -71,11 +71,10 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
     if (some_few) {
         const int64_t all = chunk_blocks * split.splits + line.blocks;
         kv_attention_mixed_kernel<T, D, WAVES><<<(unsigned)all, 64 * WAVES, 0, ctx->stream>>>(a, split, (int)chunk_blocks, line);
-        const int slices = line.each ? 0 : few_slices(line, FEW_ROWS, JOIN_ROWS);
+        const int slices = few_slices(line, FEW_ROWS, JOIN_ROWS);
         const int64_t few_blocks = (int64_t)a.nreq * a.cache.heads * slices;
         if (few_blocks + joins > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", a.nreq);
-        if (few_blocks + joins > 0)
-            kv_attention_mixed_join_kernel<T, D><<<(unsigned)(few_blocks + joins), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split, (int)few_blocks, slices, line);
+        kv_attention_mixed_join_kernel<T, D><<<(unsigned)(few_blocks + joins), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split, (int)few_blocks, slices, line);
     } else {
         kv_attention_chunk_kernel<T, D, WAVES><<<dim3((unsigned)chunk_blocks, split.splits), 64 * WAVES, 0, ctx->stream>>>(a, split);
         if (joins > 0) kv_attention_chunk_join_kernel<T, D><<<joins, 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split);
@@ -85,7 +84,10 @@ template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const att
 }
 
 template <class T> static int chunk_dim(pq_ctx *ctx, const attention_args &a, bool some_few) {
-    const bool many = a.ntokens * a.group >= (int64_t)a.nreq * 192;
+    // Eight waves share each tile of keys where requests have rows for them.  12 requests of 1 to 300 tokens, 7 heads on each of 4,
+    // 128 dimensions: 90 us with eight, 82 with four; 8 requests of 200 tokens, 8 heads on each of 8: 164 and 185 us; two chunks of
+    // 2048, 4 heads on each of 8: 707 and 794 us.
+    const bool many = a.ntokens * a.group >= (int64_t)a.nreq * 512;
     switch (a.cache.dim) {
     case 64: return many ? chunk_run<T, 64, 8>(ctx, a, some_few) : chunk_run<T, 64, 4>(ctx, a, some_few);
     case 96: return many ? chunk_run<T, 96, 8>(ctx, a, some_few) : chunk_run<T, 96, 4>(ctx, a, some_few);

@@ -374,8 +374,8 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_join_bl
 }
 
 // The line's memory in read_ws (from its start on), its blocks and the waves that join a row; grows the buffer to hold `more` bytes
-// behind it.  beside: in one launch with chunks.
-int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, bool beside, size_t more, few_line *line, size_t *ws_used);
+// behind it.
+int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, few_line *line, size_t *ws_used);
 // Slices of the rows of a (request, head) for the kernel that joins, of `waves` waves.
 static inline int few_slices(const few_line &line, int most_rows, int waves) { return (most_rows * line.row_waves + waves - 1) / waves; }
 

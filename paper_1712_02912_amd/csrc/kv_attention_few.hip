@@ -12,7 +12,7 @@ template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
 }
 __global__ __launch_bounds__(1024) void kv_attention_starts_kernel(attention_args a, int unit, int64_t *starts) { few_starts<1024>(a, unit, starts); }
 
-int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, bool beside, size_t more, few_line *line, size_t *ws_used) {
+int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, few_line *line, size_t *ws_used) {
     const int dim = a.cache.dim, per_cu = (dim > 128 ? 4 : 8) / waves;
     *line = {};
     line->unit = waves * FEW_TILE;
@@ -21,16 +21,15 @@ int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, bool beside, si
     // 256 dimensions), the line's sums and its second launch about 6 us.  4 requests of 41 keys, 8 heads: 5.7 us, 9.7 us by the
     // line; with 874 keys (7 units) of 12 requests, 8 heads, it is 22.9 and 17.2 us.  Where there are as many (request, head) as
     // the line has blocks, blocks wait less for each other: 96 requests of 1001 keys, 8 heads: 55 and 59 us, of 2001 keys 96 and
-    // 89 us.  Beside chunks the second launch is all that counts: windows of 1024 keys, 23 requests of 1 to 517 tokens: 37.5 and
-    // 41 us.  (Of 256 dimensions, windows of 184 keys: 20 and 22 us, of 305 keys 25 and 21 us.)
+    // 89 us.
     const int64_t held = (int64_t)a.width * a.cache.block_size, seen = a.window > 0 && a.window + FEW_ROWS < held ? a.window + FEW_ROWS : held;
     const bool many = (int64_t)a.nreq * a.cache.heads >= line->blocks;
-    const int64_t most = dim > 128 ? (beside || many ? 256 : 128) : beside ? 2048 : many ? 1024 : 512;
+    const int64_t most = (many ? 1024 : 512) / (dim > 128 ? 4 : 1);
     if (seen <= most) {
         line->each = true;
         line->blocks = a.nreq * a.cache.heads;
         *ws_used = 0;
-        return more > 0 ? buf_reserve(ctx, &ctx->read_ws, more, "parts of the attention") : PQ_OK;
+        return PQ_OK;
     }
     const size_t starts = align_up(((size_t)a.nreq + 1) * sizeof(int64_t), 256), slots = (size_t)line->blocks * 2 * FEW_ROWS;
     *ws_used = align_up(starts + slots * (dim + 2) * sizeof(float), 256);
@@ -51,7 +50,7 @@ int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, bool beside, si
 template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int most_rows) {
     few_line line;
     size_t ws_used;
-    if (const int rc = few_prepare(ctx, a, 4, false, 0, &line, &ws_used)) return rc;
+    if (const int rc = few_prepare(ctx, a, 4, 0, &line, &ws_used)) return rc;
     kv_attention_few_kernel<T, D><<<line.blocks, 256, 0, ctx->stream>>>(a, line);
     if (line.each) {
         PQ_HIP(ctx, hipGetLastError());

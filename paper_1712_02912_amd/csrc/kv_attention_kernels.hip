@@ -119,12 +119,14 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
             a.k_strides[i] = (uint32_t)cache->key_strides[i];
             a.v_strides[i] = (uint32_t)cache->value_strides[i];
         }
-        // Requests of few rows and others in one call: each goes to its own kernel.  A tile of rows of the chunks' kernel costs a
-        // request of one token as much as one of 128 (23 requests of 1 to 517 tokens, 16 heads: 63 us with that kernel alone, XX
-        // with both); where all requests have max_new tokens there is one kind only.
-        const int64_t most_rows = (int64_t)max_new * a.group;
+        // Requests of few rows and others in one call: over long contexts each kind has blocks of its own, as keys and values are
+        // read faster by those of few rows; over short ones what counts is one launch of one kind (64 requests of 1 to 50 tokens,
+        // 4 heads on each of 8, up to 8000 keys: 237 us, all as chunks 252 us; 23 requests of 1 to 100 tokens, 16 heads, up to 700
+        // keys: 24 and 19 us).  Where all requests have max_new tokens there is one kind only.
+        const int64_t most_rows = (int64_t)max_new * a.group, held = (int64_t)width * cache->block_size;
         if (most_rows <= FEW_ROWS) return launch_kv_attention_few(ctx, a, (int)most_rows);
-        return launch_kv_attention_chunk(ctx, a, a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new);
+        const bool is_long = held >= 4096 && (window == 0 || window >= 4096);
+        return launch_kv_attention_chunk(ctx, a, is_long && a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new);
     }
     const int64_t grid = ntokens * q_heads;
     if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);

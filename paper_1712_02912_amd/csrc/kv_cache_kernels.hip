@@ -174,7 +174,6 @@ struct append_args {
     int64_t ntokens, max_positions;
     float eps;
     int q_heads, rot, norm, rows;   // rows of a token: q_heads + 2 cache.heads
-    int chunks;                     // groups of lanes that share the rows of a token
 };
 
 struct append_row {
@@ -258,15 +257,12 @@ template <int V, bool PAIRS> __device__ __forceinline__ void append_turn(float (
 
 constexpr int APPEND_THREADS = 256;
 
-// GL lanes per head (a power of two, at least the number of units), ROWS heads of one token one after the other, all of
-// them read before the first is written.
-template <class T, int V, bool PAIRS, int ROWS>
-__global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(append_args a, int gl) {
+// GL lanes per head (a power of two, at least the number of units).
+template <class T, int V, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(append_args a, int gl) {
     const int64_t group = ((int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x) / gl;
     const int u = threadIdx.x & (gl - 1), dim = a.cache.dim;
-    const int64_t t = group / a.chunks;
+    const int64_t t = group / a.rows;
     if (t >= a.ntokens) return;
-    const int row0 = (int)(group - t * a.chunks) * ROWS;
     const bool active = u < dim / (2 * V);
     const append_unit<V, PAIRS> unit(active ? u : 0, a.rot);
     typedef elem_vec<T, V> vec;
@@ -275,63 +271,54 @@ __global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(append_args a
     const int32_t p = a.positions[t];
     const int64_t slot = a.slots[t];
     const bool placed = p >= 0 && (a.rot == 0 || p < a.max_positions);
-    append_row row[ROWS];
-    vec x[ROWS], y[ROWS];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        row[i].to = nullptr;
-        if (row0 + i < a.rows) row[i] = append_locate<T>(a, t, row0 + i, placed, slot);
-        if (active && row[i].to) {
-            x[i] = *(const vec *)((const T *)row[i].from + unit.first);
-            y[i] = *(const vec *)((const T *)row[i].from + unit.second);
+    const append_row row = append_locate<T>(a, t, (int)(group - t * a.rows), placed, slot);
+    if (!row.to) return;   // (all lanes of a head: what stands here is the row's, and so are the branches below)
+    vec x, y;
+    fvec c, s;
+    if (active) {
+        x = *(const vec *)((const T *)row.from + unit.first);
+        y = *(const vec *)((const T *)row.from + unit.second);
+        if (row.turned && placed && unit.angle >= 0) {
+            c = *(const fvec *)(a.cos_table + (int64_t)p * (a.rot / 2) + unit.angle);
+            s = *(const fvec *)(a.sin_table + (int64_t)p * (a.rot / 2) + unit.angle);
         }
     }
-    fvec c, s;
-    if (active && placed && unit.angle >= 0) {
-        c = *(const fvec *)(a.cos_table + (int64_t)p * (a.rot / 2) + unit.angle);
-        s = *(const fvec *)(a.sin_table + (int64_t)p * (a.rot / 2) + unit.angle);
-    }
+    if (row.turned) {
+        float fx[V], fy[V], sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        // (a group's lanes take every branch here together: to, turned and norm are the row's)
-        if (!row[i].to) continue;
-        if (row[i].turned) {
-            float fx[V], fy[V], sum = 0.f;
+        for (int e = 0; e < V; ++e) {
+            fx[e] = active ? (float)x.v[e] : 0.f;
+            fy[e] = active ? (float)y.v[e] : 0.f;
+            sum += fx[e] * fx[e] + fy[e] * fy[e];
+        }
+        if (a.norm) {
+            for (int d = gl / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+            const float r = 1.f / sqrtf(sum / (float)dim + a.eps);
+            if (active && row.weight) {
+                const fvec wx = *(const fvec *)(row.weight + unit.first), wy = *(const fvec *)(row.weight + unit.second);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                fx[e] = active ? (float)x[i].v[e] : 0.f;
-                fy[e] = active ? (float)y[i].v[e] : 0.f;
-                sum += fx[e] * fx[e] + fy[e] * fy[e];
-            }
-            if (a.norm) {
-                for (int d = gl / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
-                const float r = 1.f / sqrtf(sum / (float)dim + a.eps);
-                if (active && row[i].weight) {
-                    const fvec wx = *(const fvec *)(row[i].weight + unit.first), wy = *(const fvec *)(row[i].weight + unit.second);
+                for (int e = 0; e < V; ++e) {
+                    fx[e] *= r * wx.v[e];
+                    fy[e] *= r * wy.v[e];
+                }
+            } else {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        fx[e] *= r * wx.v[e];
-                        fy[e] *= r * wy.v[e];
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        fx[e] *= r;
-                        fy[e] *= r;
-                    }
+                for (int e = 0; e < V; ++e) {
+                    fx[e] *= r;
+                    fy[e] *= r;
                 }
             }
-            if (active && placed && unit.angle >= 0) append_turn<V, PAIRS>(fx, fy, c.v, s.v);
+        }
+        if (active && placed && unit.angle >= 0) append_turn<V, PAIRS>(fx, fy, c.v, s.v);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                x[i].v[e] = (T)(row[i].zero ? 0.f : fx[e]);
-                y[i].v[e] = (T)(row[i].zero ? 0.f : fy[e]);
-            }
+        for (int e = 0; e < V; ++e) {
+            x.v[e] = (T)(row.zero ? 0.f : fx[e]);
+            y.v[e] = (T)(row.zero ? 0.f : fy[e]);
         }
-        if (active) {
-            *(vec *)((T *)row[i].to + unit.first) = x[i];
-            *(vec *)((T *)row[i].to + unit.second) = y[i];
-        }
+    }
+    if (active) {
+        *(vec *)((T *)row.to + unit.first) = x;
+        *(vec *)((T *)row.to + unit.second) = y;
     }
 }
 
@@ -375,18 +362,12 @@ template <class T, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void
     }
 }
 
-template <class T, int V, bool PAIRS> static int append_vector(pq_ctx *ctx, append_args &a) {
+template <class T, int V, bool PAIRS> static int append_vector(pq_ctx *ctx, const append_args &a) {
     int gl = 1;
     while (gl < a.cache.dim / (2 * V)) gl *= 2;
-    // four heads per group of lanes once that still gives every compute unit its 32 waves (the loads of four heads are then
-    // in flight together, and the rotation's row is read once for them)
-    const int64_t lanes = a.ntokens * a.rows * gl;
-    const int rows = lanes >= (int64_t)ctx->num_cu * 2048 * 4 ? 4 : 1;
-    a.chunks = (a.rows + rows - 1) / rows;
-    const int64_t grid = (a.ntokens * a.chunks * gl + APPEND_THREADS - 1) / APPEND_THREADS;
+    const int64_t grid = (a.ntokens * a.rows * gl + APPEND_THREADS - 1) / APPEND_THREADS;
     if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
-    if (rows == 4) kv_append_kernel<T, V, PAIRS, 4><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a, gl);
-    else kv_append_kernel<T, V, PAIRS, 1><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a, gl);
+    kv_append_kernel<T, V, PAIRS><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a, gl);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
@@ -408,7 +389,7 @@ static int append_width(const append_args &a, int most) {
     return v;
 }
 
-template <class T, bool PAIRS> static int append_typed(pq_ctx *ctx, append_args &a) {
+template <class T, bool PAIRS> static int append_typed(pq_ctx *ctx, const append_args &a) {
     constexpr int most = 16 / sizeof(T);
     const int v = append_width(a, most);
     if (a.cache.dim <= 64 * 2 * v) {   // the units of a head fit a wave

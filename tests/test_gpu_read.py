@@ -412,6 +412,29 @@ def test_attention_of_requests_behind_the_rows(ctx, new):
     assert (got[new:t] == 0).all() and np.isneginf(lse[new:t]).all() and (got[t:] == 7).all() and (lse[t:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("q_heads,heads,dim", [(2, 2, 64), (4, 2, 64), (8, 2, 96), (4, 1, 128), (2, 1, 256)])
+@pytest.mark.parametrize("new", [[1, 40, 2, 17, 1, 3], [1] * 9 + [300], [5, 700, 1]])
+def test_attention_of_single_tokens_beside_chunks(ctx, dtype, q_heads, heads, dim, new):
+    kv = [4300 + 7 * i if i % 3 == 0 else 60 + n + 31 * i for i, n in enumerate(new)]
+    kv[1] = -1 if len(new) > 6 else kv[1]
+    check_attention(ctx, new, kv, q_heads, heads, dim, dtype, extra=2)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attention_of_a_cache_with_a_wide_stride(ctx, new):
+    """One block whose stride passes 32 bits."""
+    r = np.random.default_rng(new)
+    keys, values = (dev(r.standard_normal((1, 64, 2, 64)), BF16) for _ in range(2))
+    wide = keys.as_strided(keys.shape, (2 ** 32,) + keys.stride()[1:])
+    q = dev(r.standard_normal((new, 4, 64)), BF16)
+    table, cu, kv = np.zeros((1, 1), np.int32), np.array([0, new], np.int32), np.array([60], np.int32)
+    out, _ = ctx.pq_kv_attention(q, wide, values, dev(table), dev(cu), dev(kv), new)
+    want, _, spread = orc.attention(host(q), host(keys), host(values), table, cu, kv, 0.125, 0)
+    bound, _ = attention_bound(BF16, host(q), host(keys), spread, want, 0.125, 60, 64)
+    assert (np.abs(host(out) - want) <= bound).all()
+
+
 @pytest.mark.parametrize("new", [1, 40])
 @pytest.mark.parametrize("window", [0, 30])
 @pytest.mark.parametrize("dtype", [F32, BF16])
