@@ -8,6 +8,12 @@
 //
 // Keys and values go through registers into one of two buffers while the other one is computed on, so one barrier per tile is
 // enough and loads have a tile's time to arrive.  Places that hold no key become zeros on that way.
+//
+// Two chunks of 2048 over 14 336 keys, 32 heads of 128 dimensions on 8, bf16: 736 GFLOP in 700 us = 1.05 PFLOP/s (a large product
+// on this card: 1.23).  Matrix instructions take 52 % of the cycles there, vector instructions (a quarter of them the powers of
+// two, at a quarter of the rate) 48 %: the waves of a block meet at every tile and do the same at the same time, and giving half of
+// them priority did not change that.  64 dimensions: 0.75 PFLOP/s (as many powers for half the products); 256: 0.48, where a SIMD
+// has registers for one wave only.
 #pragma once
 #include <type_traits>
 
@@ -72,6 +78,8 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
     typedef lds_row<D> row;
     constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
     constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
+    // (Alone on its SIMD, a wave waits for every read of shared memory unless it reads ahead: 8 requests of 1024 tokens over 1024 to
+    // 8192 keys, 8 heads of 256 dimensions: 599 us, 663 without.  Where there are two waves it is no gain and costs registers.)
     constexpr int AT_ONCE = D > 128 ? 4 : 1;
     // a thread moves chunks of 16 bytes of one key (and value) of a tile, every LANES-th from its own on
     constexpr int LANES = THREADS / TILE, MOVES = (CHUNKS + LANES - 1) / LANES;

@@ -6,8 +6,8 @@ namespace pq {
 
 
 
-// Waves of a SIMD that registers are to be left for.  (Blocks of four waves over 64 dimensions come to 171 registers left alone, 168
-// for three: 44 and 40 us for 23 requests of 1 to 517 tokens, windows of 1024 keys.)
+// Waves of a SIMD that registers are to be left for.  (Left alone, blocks of four waves over 64 dimensions come to 168 to 171
+// registers; three waves have 168: 40 us for 23 requests of 1 to 517 tokens with windows of 1024 keys, 44 us with two waves.)
 template <int D, int WAVES> constexpr int CHUNK_RESIDENT = D > 128 ? 1 : D == 64 && WAVES == 4 ? 3 : 2;
 
 template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES, (CHUNK_RESIDENT<D, WAVES>)) void kv_attention_chunk_kernel(attention_args a, chunk_split split) {
@@ -38,12 +38,12 @@ __global__ __launch_bounds__(64 * JOIN_ROWS) void kv_attention_mixed_join_kernel
 template <class T, int D, int WAVES> static int chunk_run(pq_ctx *ctx, const attention_args &a, bool some_few) {
     constexpr int M = 32 * WAVES;
     const int64_t indexes = a.ntokens * a.group / M + a.nreq, rows = a.ntokens * a.q_heads;
-    // Tiles of rows that leave compute units without work: the keys of each are split, down to 256 keys a part (512 where there are two rounds), into one round of
+    // Tiles of rows that leave compute units without work: the keys of each are split, down to 256 keys a part, into one round of
     // the blocks that the chip holds.  Of blocks of eight waves over 96 and 128 dimensions two rounds are better, which end more
-    // evenly (512 rows of 8 heads over 30 512 keys of 128 dimensions: 121 us, 131 us in one round; 28 heads, 12 requests of 1 to
-    // 300 over 6000 keys: 91 and 103 us), of 64 they cost more in parts than that (700 rows of 8 heads over 9700 keys: 42 us, in
-    // one round 34 us).  Parts of 512 keys at least: 31 us for 4 requests of 1 to 20 tokens over windows of 305 keys, 256
-    // dimensions, 21 us with 256; in two rounds 45 us for 4 requests of 1 to 264 tokens over windows of 1388 keys, 50 us with 256.
+    // evenly (512 rows of 8 heads over 30 512 keys of 128 dimensions: 121 us, 131 us in one round), of 64 they cost more in parts
+    // than that (700 rows of 8 heads over 9700 keys: 42 us, in one round 34 us).  Parts of 512 keys at least: 31 us for 4 requests of
+    // 1 to 20 tokens over windows of 305 keys, 256 dimensions, 21 us with 256; in two rounds 45 us for 4 requests of 1 to 264 tokens
+    // over windows of 1388 keys, 50 us with 256.
     const int64_t tiles = ((a.ntokens * a.group + M - 1) / M + a.nreq / 2) * a.cache.heads;
     constexpr bool two_rounds = D > 64 && D <= 128 && WAVES == 8;
     constexpr int waves = D > 128 ? 4 : two_rounds ? 16 : 8, least = two_rounds ? 512 : 256;

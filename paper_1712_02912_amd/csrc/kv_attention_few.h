@@ -10,7 +10,14 @@
 // Work is cut by what it is, not by request: all keys of all requests and heads form one line of units of 128 keys, and every
 // block takes an equal stretch of it, so contexts of any lengths fill the chip evenly.  A (request, head) that lies
 // within one block is finished there; of others each block leaves a part (maximum, sum, weighted values), and a second kernel
-// joins the parts, always in the same order.
+// joins the parts, always in the same order.  (The block that leaves the last part could join them, without a second launch;
+// but what makes the parts visible across the chip's eight caches writes these back and empties them, in every block: 364 us instead
+// of 164 for the 64 tokens below.)
+//
+// 64 tokens over up to 8192 keys, 32 heads of 128 dimensions on 8, bf16: 823 MB in 160 us = 5.1 TB/s, and 6.6 us to join parts.
+// One token over 131 038 keys: 537 MB in 108 us = 5.0 TB/s, and 6.6 us.  Two blocks for each compute unit, as many as registers
+// allow (of 256 dimensions one): with one the 64 tokens take 175 us.  Short contexts are bound by latency: lengths, sums, the table's
+// entry, keys, values one after the other, about 8 us before the first result.
 #pragma once
 #include "kv_attention.h"
 

@@ -41,7 +41,8 @@ int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, fe
         kv_attention_starts_kernel<<<1, 1024, 0, ctx->stream>>>(a, line->unit, line->starts_out);
         line->starts = line->starts_out;
     }
-    // a wave for every fourth part of a row, about
+    // a wave for every fourth part of a row, about (2 requests of up to 30 000 keys, 2 heads of 64 dimensions: 19 us, with four waves
+    // 22 us)
     const int64_t parts = line->blocks / ((int64_t)a.nreq * a.cache.heads);
     line->row_waves = parts >= 32 ? 16 : parts >= 4 ? 4 : 1;
     return PQ_OK;

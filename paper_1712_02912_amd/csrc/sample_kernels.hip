@@ -16,6 +16,10 @@
 // the bins also finds the largest, and the row is read from memory once.  A row whose largest logit lies far above
 // that look is passed over again.
 //
+// 256 rows of 131 072 f32 logits with filters: 64 us (134 MB; 26 us at the rate of a large copy), bound by the adds to the bins and by
+// the steps behind that pass, of one block each.  8 rows of 32 000: 17 to 25 us by their filters, all latency: a dozen steps with
+// a barrier or a trip to memory each.
+//
 // A row is one block's work: 256 rows are one for each compute unit.  Only rows of calls without filters, which are one pass,
 // are shared by several blocks where they are few (see sample_typed).
 #include "elem.h"
