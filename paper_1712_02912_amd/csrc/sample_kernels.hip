@@ -9,7 +9,7 @@
 // Cuts: one pass puts every token into one of 2048 bins of 1/16 octave of weight, count and weight in one 64-bit word (all
 // weights of a bin have the same power of two, so they add up as whole numbers, in any order to the same sum).  The bin in
 // which a limit is reached is then known, and the next pass collects the tokens of the bins up to it, or of that bin alone
-// where those are too many for the list.  Finer bins of the list end at 64 keys or fewer, which one wave sorts.  Where the
+// where those are too many for the list.  Finer bins of the list end at 256 keys or fewer, which are ranked.  Where the
 // list holds all that stay, the draw is from it, else from one more pass over the row.
 //
 // Weights are relative to a logit that a first look at a part of the row has found, not to the largest: so the pass that fills
@@ -36,6 +36,7 @@ constexpr int SAMPLE_V = 8;                // tokens that a thread reads at once
 constexpr int SAMPLE_BINS = 2048;
 constexpr int SAMPLE_ABOVE = 1024;         // of them above weight 1: 64 octaves, and 64 below
 constexpr int SAMPLE_LIST = 4096;
+constexpr int SAMPLE_LAST = 256;           // keys among which a cut is found by their ranks
 constexpr int SAMPLE_COUNT_BIT = 44;       // a bin: count << 44 | weights in 2^-23 of the bin's power of two
 constexpr float SAMPLE_TOP = 60.f;         // octaves above the reference that weights and their sums stay in fp32
 constexpr int SAMPLE_NONE = 0x7fffffff;
@@ -64,7 +65,7 @@ struct op_max {
 };
 struct sample_shared {
     unsigned long long bins[SAMPLE_BINS], fine[SAMPLE_BINS];
-    unsigned long long list[SAMPLE_LIST], last[64];
+    unsigned long long list[SAMPLE_LIST], last[SAMPLE_LAST], sorted[SAMPLE_LAST];
     unsigned long long wave64[2][SAMPLE_WAVES];   // two of each, used in turn: one barrier per use
     double wave_d[2][SAMPLE_WAVES];
     uint32_t wave32[2][SAMPLE_WAVES];
@@ -522,9 +523,10 @@ template <class T> struct sample_row {
     }
 
     // The key in `bin` at which a limit is reached on top of c, m; the weight up to and with it in m.  The bin's keys are split
-    // into 2048 parts, the part with the limit again, until 64 or fewer are left, which a wave sorts (the range of
-    // keys shrinks to a 1024th at least, and no two keys are equal, so it ends after six rounds at most).  They come from the list of `listed` keys, or, where the bin has too many for
-    // it (listed < 0), from the row until the rest fits.
+    // into 2048 parts, the part with the limit again, until 256 or fewer are left, each of which is compared with all (the range of
+    // keys shrinks to a 1024th at least, and no two keys are equal, so it ends after six rounds at most).  They come from the list
+    // of `listed` keys, or, where the bin has too many for it (listed < 0), from the row until the rest fits.  (201 keys: 4 us, by a
+    // round of parts and a sort of 64 by one wave 7 us.)
     __device__ __forceinline__ uint64_t find_cut(const sample_scale &s, int bin, int listed, const sample_limit &limit, uint32_t c, double &m) {
         const int tid = threadIdx.x, octave = bin_octave(bin);
         auto in_bin = [&](float y) { return bin_of(y) == bin; };
@@ -548,13 +550,13 @@ template <class T> struct sample_row {
         };
         uint64_t low = 0, high = KEY_EMPTY;
         uint32_t n = bin_count(sh.bins[bin]);
-        if (n > 64) {
+        if (n > SAMPLE_LAST) {
             if (listed >= 0) from_list(range);
             else from_row(range);
             low = block_min(lo);
             high = ~block_min(~hi);
         }
-        while (n > 64) {
+        while (n > SAMPLE_LAST) {
             int shift = 0;
             while ((high - low) >> shift >= SAMPLE_BINS) ++shift;
             __syncthreads();
@@ -578,28 +580,57 @@ template <class T> struct sample_row {
         }
         if (listed < 0) listed = collect(s, bin, bin, low, high);   // (never: such a bin has more keys than the list)
         if (tid == 0) sh.nlast = 0;
-        if (tid < 64) sh.last[tid] = KEY_EMPTY;
         __syncthreads();
         from_list([&](uint64_t key, float) {
             if (key >= low && key <= high) sh.last[atomicAdd(&sh.nlast, 1u)] = key;
         });
         __syncthreads();
+        // ranks: of a few keys by the wave that goes on with them, else by as many lanes for each key as there are
+        const int left = (int)sh.nlast;
+        if (left <= 16) {
+            if (tid < 64) {
+                const uint64_t mine = sh.last[tid & 15];
+                int rank = 0;
+                for (int i = 0; i < left; ++i) rank += read_lane(mine, i) < mine;
+                __builtin_amdgcn_wave_barrier();
+                if (tid < left) sh.sorted[rank] = mine;
+                __builtin_amdgcn_wave_barrier();
+            }
+        } else {
+            const int lanes = left <= 64 ? 16 : 4, at = tid / lanes;
+            if (at < left) {   // (the lanes of a key together)
+                const uint64_t mine = sh.last[at];
+                int rank = 0;
+                for (int i = tid & (lanes - 1); i < left; i += lanes) rank += sh.last[i] < mine;
+                for (int d = lanes / 2; d > 0; d /= 2) rank += __shfl_xor(rank, d);
+                if ((tid & (lanes - 1)) == 0) sh.sorted[rank] = mine;
+            }
+            __syncthreads();
+        }
         if (tid < 64) {
-            const int n = (int)sh.nlast;
-            const uint64_t mine = sh.last[tid];
-            int rank = 0;
-            for (int i = 0; i < n; ++i) rank += read_lane(mine, i) < mine;
-            __builtin_amdgcn_wave_barrier();
-            if (tid < n) sh.last[rank] = mine;
-            __builtin_amdgcn_wave_barrier();
-            const uint64_t key = sh.last[tid];
-            const double w = tid < n ? (double)s.weight(s.y(sample_key_logit(key))) : 0.;
-            const double upto = wave_scan<op_add>(w) + m;
-            const uint64_t there = __ballot(tid < n && limit.reached(c + tid + 1, upto));
-            const int at = there ? __ffsll((unsigned long long)there) - 1 : n - 1;   // (not reached: rounding, the last one)
-            if (tid == at) {
-                sh.cut = key;
-                sh.mass = upto;
+            // (a lane has one key, or some one after the other)
+            constexpr int EACH = SAMPLE_LAST / 64;
+            const int each = left <= 64 ? 1 : EACH;
+            double upto[EACH], sum = 0.;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                if (e < each && each * tid + e < left) sum += (double)s.weight(s.y(sample_key_logit(sh.sorted[each * tid + e])));
+                upto[e] = sum;
+            }
+            const double before_lane = wave_scan<op_add>(sum) - sum + m;
+            int reached = EACH;
+#pragma unroll
+            for (int e = EACH - 1; e >= 0; --e)
+                if (e < each && each * tid + e < left && limit.reached(c + each * tid + e + 1, before_lane + upto[e])) reached = e;
+            const uint64_t there = __ballot(reached < EACH);
+            if (!there) reached = (left - 1) % each;   // (not reached: rounding, the last one)
+            if (tid == (there ? __ffsll((unsigned long long)there) - 1 : (left - 1) / each)) {
+                sh.cut = sh.sorted[each * tid + reached];
+                double all = upto[0];
+#pragma unroll
+                for (int e = 1; e < EACH; ++e)
+                    if (e <= reached) all = upto[e];
+                sh.mass = before_lane + all;
             }
         }
         __syncthreads();
