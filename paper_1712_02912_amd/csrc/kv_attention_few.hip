@@ -1,4 +1,6 @@
 // Launches of the attention of few rows per head (kv_attention_few.h).
+#include <algorithm>
+
 #include "kv_attention_few.h"
 
 namespace pq {
@@ -22,7 +24,7 @@ int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, fe
     // line; with 874 keys (7 units) of 12 requests, 8 heads, it is 22.9 and 17.2 us.  Where there are as many (request, head) as
     // the line has blocks, blocks wait less for each other: 96 requests of 1001 keys, 8 heads: 55 and 59 us, of 2001 keys 96 and
     // 89 us.
-    const int64_t held = (int64_t)a.width * a.cache.block_size, seen = a.window > 0 && a.window + FEW_ROWS < held ? a.window + FEW_ROWS : held;
+    const int64_t held = (int64_t)a.width * a.cache.block_size, seen = a.window > 0 ? std::min(held, (int64_t)a.window + FEW_ROWS) : held;
     const bool many = (int64_t)a.nreq * a.cache.heads >= line->blocks;
     const int64_t most = (many ? 1024 : 512) / (dim > 128 ? 4 : 1);
     if (seen <= most) {

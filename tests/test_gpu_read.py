@@ -461,6 +461,12 @@ def test_attention_of_lengths_that_no_plan_gives(ctx, new, window, dtype):
             assert (np.abs(got[row] - want[0]) <= bound[0]).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 40, 3]])
+def test_attention_of_the_largest_window(ctx, new, dtype):
+    check_attention(ctx, new, [70, 90, 3], 4, 2, 64, dtype, window=2 ** 31 - 1)
+
+
 @pytest.mark.parametrize("new", [1, 40])
 def test_attention_adds_up_small_weights(ctx, new):
     """One key of a large weight and value 0, thousands of 2^-25.5 of it whose values are large: in f16 those weights count."""
