@@ -1,4 +1,6 @@
 """The reading step (include/pq_read.h) against its oracle in 64 bits, at the sizes, layouts and masks where it can go wrong."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -18,6 +20,7 @@ def ctx():
     yield c
     torch.cuda.synchronize()
     c.close()
+    gc.collect()   # tensors that errors' frames hold: later tests watch the memory that is allocated
 
 
 def dev(a, dtype=None):

@@ -1,4 +1,5 @@
 """The example that retrieves and reads, against a decoder that computes every token anew from the whole sequence."""
+import gc
 import importlib.util
 import os
 
@@ -15,6 +16,13 @@ spec = importlib.util.spec_from_file_location(
     "read_passages", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "read_passages.py"))
 example = importlib.util.module_from_spec(spec)
 spec.loader.exec_module(example)
+
+
+@pytest.fixture(autouse=True)
+def collected():
+    """Tensors that errors' frames hold do not outlive a test: later ones watch the memory that is allocated."""
+    yield
+    gc.collect()
 
 
 def norm(x):
