@@ -13,8 +13,9 @@
 // list holds all that stay, the draw is from it, else from one more pass over the row.
 //
 // Weights are relative to a logit that a first look at a part of the row has found, not to the largest: so the pass that fills
-// the bins also finds the largest, and the row is read from memory once.  A row whose largest logit lies far above
-// that look is passed over again.
+// the bins also finds the largest, and the row is read from memory once.  A row whose largest logit lies more than
+// SAMPLE_TOP octaves above that look is passed over again, before a bin or a limit is taken from it: these are in the
+// reference's octaves, so it is the same from there on to the draw.
 //
 // 256 rows of 131 072 f32 logits with filters: 64 us (134 MB; 26 us at the rate of a large copy), bound by the adds to the bins and by
 // the steps behind that pass, of one block each.  8 rows of 32 000: 17 to 25 us by their filters, all latency: a dozen steps with
@@ -38,7 +39,8 @@ constexpr int SAMPLE_ABOVE = 1024;         // of them above weight 1: 64 octaves
 constexpr int SAMPLE_LIST = 4096;
 constexpr int SAMPLE_LAST = 256;           // keys among which a cut is found by their ranks
 constexpr int SAMPLE_COUNT_BIT = 44;       // a bin: count << 44 | weights in 2^-23 of the bin's power of two
-constexpr float SAMPLE_TOP = 60.f;         // octaves above the reference that weights and their sums stay in fp32
+constexpr float SAMPLE_TOP = 60.f;         // octaves above the reference up to which weights and their sums stay in fp32, and in the bins
+static_assert(SAMPLE_TOP < SAMPLE_ABOVE / 16, "what is taken lies below the end of the bins");
 constexpr int SAMPLE_NONE = 0x7fffffff;
 
 struct sample_args {
@@ -300,7 +302,7 @@ template <class T> struct sample_row {
         auto weight = [&](float y) { return y >= edge ? s.weight(y) : 0.f; };
         auto border = [&](int i) {   // a token of the cut's bin (indexes first, in the place of the keys)
             if (cut == KEY_EMPTY) {
-                sh.list[atomicAdd(&sh.nlist, 1u)] = (uint32_t)i;
+                list_index(i);
                 return;
             }
             const float l = (float)row[i], y = s.y(l);
@@ -367,9 +369,15 @@ template <class T> struct sample_row {
 #pragma unroll
         for (int e = 0; e < SAMPLE_V; ++e) mass += (double)sum[e];
         high = block_max(high);
-        if (cut == KEY_EMPTY) list_keys(sh.nlist);
+        if (cut == KEY_EMPTY) list_keys(list_size());
         return high;
     }
+    // Places of the list are given out in any order; what finds none is not listed.
+    __device__ __forceinline__ void list_index(int i) {
+        const uint32_t at = atomicAdd(&sh.nlist, 1u);
+        if (at < SAMPLE_LIST) sh.list[at] = (uint32_t)i;
+    }
+    __device__ __forceinline__ uint32_t list_size() { return min(sh.nlist, (uint32_t)SAMPLE_LIST); }
     // The list's n indexes become keys.
     __device__ __forceinline__ void list_keys(uint32_t n) {
         for (uint32_t i = threadIdx.x; i < n; i += SAMPLE_THREADS) {
@@ -428,10 +436,7 @@ template <class T> struct sample_row {
             uint32_t which = 0;
 #pragma unroll
             for (int e = 0; e < SAMPLE_V; ++e) which |= (uint32_t)(y[e] >= lowest) << e;
-            for (; which; which &= which - 1) {
-                const uint32_t at = atomicAdd(&sh.nlist, 1u);
-                if (at < SAMPLE_LIST) sh.list[at] = (uint32_t)(i + __ffs(which) - 1);
-            }
+            for (; which; which &= which - 1) list_index(i + __ffs(which) - 1);
         };
         if (first < whole) {
             float y[SAMPLE_V], most = -INFINITY;
@@ -453,10 +458,7 @@ template <class T> struct sample_row {
             const float y = s.y(l);
             high = fmaxf(high, y);
             add(y);
-            if (y >= lowest) {
-                const uint32_t at = atomicAdd(&sh.nlist, 1u);
-                if (at < SAMPLE_LIST) sh.list[at] = (uint32_t)i;
-            }
+            if (y >= lowest) list_index(i);
         });
         top = block_max(high);
         listed = sh.nlist <= SAMPLE_LIST ? last : -1;
@@ -516,10 +518,12 @@ template <class T> struct sample_row {
             const float y = s.y(l);
             if (!(y >= lowest && y < highest)) return;
             const uint64_t key = sample_key(l, i);
-            if (key >= low && key <= high) sh.list[atomicAdd(&sh.nlist, 1u)] = key;
+            if (key < low || key > high) return;
+            const uint32_t at = atomicAdd(&sh.nlist, 1u);
+            if (at < SAMPLE_LIST) sh.list[at] = key;
         });
         __syncthreads();
-        return (int)sh.nlist;
+        return (int)list_size();
     }
 
     // The key in `bin` at which a limit is reached on top of c, m; the weight up to and with it in m.  The bin's keys are split
@@ -582,11 +586,13 @@ template <class T> struct sample_row {
         if (tid == 0) sh.nlast = 0;
         __syncthreads();
         from_list([&](uint64_t key, float) {
-            if (key >= low && key <= high) sh.last[atomicAdd(&sh.nlast, 1u)] = key;
+            if (key < low || key > high) return;
+            const uint32_t at = atomicAdd(&sh.nlast, 1u);
+            if (at < SAMPLE_LAST) sh.last[at] = key;
         });
         __syncthreads();
         // ranks: of a few keys by the wave that goes on with them, else by as many lanes for each key as there are
-        const int left = (int)sh.nlast;
+        const int left = (int)min(sh.nlast, (uint32_t)SAMPLE_LAST);
         if (left <= 16) {
             if (tid < 64) {
                 const uint64_t mine = sh.last[tid & 15];
@@ -688,7 +694,7 @@ template <class T> struct sample_row {
             int complete;   // the list holds the tokens of all bins up to this one; -1: of none
             for (int round = 0; round < 2; ++round) {   // (the second with the largest logit for the reference)
                 fill_bins(s, wanted, top, complete);
-                if (top < (float)(SAMPLE_ABOVE / 16) || round == 1) break;
+                if (top <= SAMPLE_TOP || round == 1) break;
                 ref = largest();
                 s = sample_scale(ref, inv);
             }
@@ -729,16 +735,17 @@ template <class T> struct sample_row {
             // from the row: what lies before the bin of the cut stays, the bin itself is listed for later, or the cut is there
             const float lower = cut_bin < SAMPLE_BINS ? (float)(SAMPLE_ABOVE - 1 - cut_bin) * 0.0625f : -INFINITY;
             const float upper = cut_bin < SAMPLE_BINS ? lower + 0.0625f : -INFINITY;
-            for (int round = 0; round < 2; ++round) {   // (the second with the largest logit for the reference)
+            // (without limits, the second round with the largest logit for the reference; limits hold for the reference that they have)
+            for (int round = 0; round < 2; ++round) {
                 const float high = draw(s, upper, lower, least, later ? KEY_EMPTY : cut, cut_bin >= SAMPLE_BINS || c > (uint32_t)a.vocab / 32, best, mass);
-                if (high <= SAMPLE_TOP || round == 1) break;
+                if (high <= SAMPLE_TOP || by_k || by_p || round == 1) break;
                 s = sample_scale(largest(), inv);
                 best = race();
                 mass = 0.;
             }
             mass = block_sum(mass);
             if (later) {
-                listed = (int)sh.nlist;
+                listed = (int)list_size();
                 cut = min(cut, find_cut(s, cut_bin, listed, limit, c, m));
             }
         }

@@ -650,6 +650,33 @@ def test_sample_refusals(ctx):
         ctx.pq_sample_tokens(torch.zeros((2, 0), device="cuda"), torch.zeros((2, 0), device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("octaves", [59.0, 60.5, 61.0, 62.0, 63.0, 63.9, 65.0])
+@pytest.mark.parametrize("temperature", [1.0, 0.1])
+def test_sample_of_rows_whose_beginning_says_little(ctx, dtype, octaves, temperature):
+    """The largest logits lie so many octaves of weight above the first 8192 (rows are read in that order)."""
+    r = np.random.default_rng(int(octaves * 10))
+    vocab, high = 40000, octaves * np.log(2)
+    low = r.uniform(-3, -0.1, (5, vocab))
+    low[:, 5] = 0.0
+    # 0: few tokens count (top_k is not reached); 1 and 2: thousands do; 3 and 4: equal logits, thousands of them
+    low[0] = -60.0
+    low[0, :20] = -0.1 * np.arange(20)
+    low[0, 30000:30003] = high - 0.5 * np.arange(3)
+    low[1:3, 10000:30000] = high + r.uniform(-1, 0, (2, 20000))
+    low[1:3, 30000] = high
+    low[3:, 20000:24500] = high - np.log(2)
+    low[3, 25000:28000] = high - 2 * np.log(2)
+    low[3:, 31000] = high
+    logits = dev(low * temperature, dtype)
+    noise = dev(r.random((5, vocab)).astype(np.float32).clip(1e-7, 1 - 1e-7))
+    t = [temperature] * 5
+    for filters in (dict(top_k=[50, 6000, 9000, 4600, 4600], min_p=[0.05, 0.0, 0.01, 0.0, 0.0]), dict(top_k=[3, 4096, 4097, 4502, 5000]),
+                    dict(top_p=[0.9, 0.99, 0.5, 0.7, 0.99]), dict(top_k=[50, 15000, 5000, 6000, 20000], top_p=[0.7, 0.8, 0.95, 0.9, 0.999]),
+                    dict(top_k=[50] * 5, min_p=[0.05] * 5), dict(min_p=[0.05] * 5), dict(top_p=[0.999] * 5, min_p=[0.4] * 5), dict()):
+        check_sample(ctx, logits, noise, t, **filters)
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------
 def test_a_captured_step_replays(ctx):
     """Plan, append, attention and draw in one HIP graph, replayed on new inputs with eager work in between."""
