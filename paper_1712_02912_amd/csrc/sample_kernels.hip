@@ -262,7 +262,7 @@ template <class T> struct sample_row {
         return block_min(sample_key(high, at));
     }
 
-    // the best of a thread's race: largest w / e, then smallest index
+    // the best of a thread's race: largest w / e (logit without noise), then smallest index
     struct race {
         float best = -1.f;
         int token = SAMPLE_NONE;
@@ -273,14 +273,15 @@ template <class T> struct sample_row {
                 token = i;
             }
         }
-        __device__ __forceinline__ void enter_certain(float w, int i) {   // without noise: the largest weight
-            if (w > best || (w == best && i < token)) {
-                best = w;
+        // Without noise: the largest logit.  (Not the largest weight: different logits may round to one.)
+        __device__ __forceinline__ void enter_certain(float l, int i) {
+            if (token == SAMPLE_NONE || l > best || (l == best && i < token)) {
+                best = l;
                 token = i;
             }
         }
     };
-    // The winner of the block's races as a key, the largest w / e first; KEY_EMPTY: none (noise that is no number).
+    // The winner of the block's races as a key, the best first; KEY_EMPTY: none (noise that is no number).
     __device__ __forceinline__ uint64_t winner(const race &x) { return block_min(x.token == SAMPLE_NONE ? KEY_EMPTY : sample_key(x.best, x.token)); }
     // The winner's token, and the log of its share of the weights that stay.
     __device__ __forceinline__ void finish(uint64_t best, const sample_scale &s, double mass) {
@@ -310,7 +311,7 @@ template <class T> struct sample_row {
             const float w = s.weight(y);
             sum[0] += w;
             if (noise) best.enter(w, noise[i], i);
-            else best.enter_certain(w, i);
+            else best.enter_certain(l, i);
         };
         float bounded = 0.f;
         const int first = before + threadIdx.x * SAMPLE_V;
@@ -343,7 +344,7 @@ template <class T> struct sample_row {
             if (!noise) {
 #pragma unroll
                 for (int e = 0; e < SAMPLE_V; ++e)
-                    if (w[e] > 0.f) best.enter_certain(w[e], i + e);
+                    if (w[e] > 0.f) best.enter_certain(l[e], i + e);
                 return;
             }
             if (!many) u = *(const noises *)(noise + i);
@@ -364,7 +365,7 @@ template <class T> struct sample_row {
             if (y >= lower && y < upper) border(i);
             if (!(w > 0.f)) return;
             if (noise) best.enter(w, noise[i], i);
-            else best.enter_certain(w, i);
+            else best.enter_certain(l, i);
         });
 #pragma unroll
         for (int e = 0; e < SAMPLE_V; ++e) mass += (double)sum[e];
@@ -393,12 +394,12 @@ template <class T> struct sample_row {
         uint64_t mass = 0;
         for (int i = threadIdx.x; i < listed; i += SAMPLE_THREADS) {
             const uint64_t key = sh.list[i];
-            const float y = s.y(sample_key_logit(key)), w = s.weight(y);
+            const float l = sample_key_logit(key), y = s.y(l), w = s.weight(y);
             const int token = (int)(uint32_t)key;
             if (key > cut || !(y >= least)) continue;
             mass += (uint64_t)ldexp((double)w, 44 - shift);
             if (noise) best.enter(w, noise[token], token);
-            else best.enter_certain(w, token);
+            else best.enter_certain(l, token);
         }
         return ldexp((double)block_sum(mass), shift - 44);
     }

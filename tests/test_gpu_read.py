@@ -677,6 +677,24 @@ def test_sample_of_rows_whose_beginning_says_little(ctx, dtype, octaves, tempera
         check_sample(ctx, logits, noise, t, **filters)
 
 
+@pytest.mark.parametrize("temperature", [0.7, 50.0, 1e6, 1e30])
+@pytest.mark.parametrize("filters", [dict(), dict(top_k=3), dict(top_k=9000), dict(top_p=0.9), dict(top_p=0.2, min_p=0.5), dict(min_p=0.5)])
+@pytest.mark.parametrize("rows", [2, 130])
+def test_sample_without_noise_is_the_largest_logit(ctx, temperature, filters, rows):
+    """Also where the weights of different logits round to one number."""
+    r = np.random.default_rng(rows)
+    l = r.uniform(-1, 1, (rows, 12007)).astype(np.float32)
+    for k in range(rows):                                       # neighbours of the largest, before and behind it
+        at = np.sort(r.choice(12007, 5, replace=False))
+        l[k, at] = np.float32(5.0)
+        l[k, at[3 if k % 2 else 0]] = np.nextafter(np.float32(5.0), np.float32(6.0))
+    tokens = check_sample(ctx, dev(l), None, [temperature] * rows, **{k: [v] * rows for k, v in filters.items()})
+    assert np.array_equal(tokens, l.argmax(axis=1))
+    equal = torch.full((rows, 12007), 3.0, device="cuda")
+    equal[:, 17:] = 3.25
+    assert (check_sample(ctx, equal, None, [temperature] * rows, **{k: [v] * rows for k, v in filters.items()}) == 17).all()
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------
 def test_a_captured_step_replays(ctx):
     """Plan, append, attention and draw in one HIP graph, replayed on new inputs with eager work in between."""
