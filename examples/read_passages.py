@@ -75,7 +75,7 @@ class Reader:
                                                      self.block_size, len(tokens))
         self.used += blocks
         self.counts = [c + n for c, n in zip(self.counts, new)]
-        self.lens = kv
+        self.lens = kv                                    # (a refused request, of which there is none here, would stay refused)
         x = d.embedding[tokens]
         for w, (keys, values) in zip(d.layers, self.caches):
             qkv = (d.norm(x) @ w["qkv"]).view(len(tokens), d.q_heads + 2 * d.heads, d.dim)

@@ -11,7 +11,9 @@
  * grow: pq_kv_plan (for more than 4096 requests), pq_kv_attention and pq_sample_tokens use a buffer of the context that is
  * theirs alone, grown on demand (a HIP graph that captured a call holds its address, which stays valid until a call that
  * needs more).
- * Requests that the plan refuses have the length -1 from then on: their tokens are not written and see nothing.
+ * Requests that the plan refuses have the length -1: their tokens are not written and see nothing, and a plan that is given that
+ * length refuses them again, so one step's kv_lens can be the next one's cached_lens.  What a refused request holds in the cache and
+ * in its row of the table is left as it is; to try it again, give its length from before.
  */
 #ifndef PQ_READ_H
 #define PQ_READ_H
@@ -43,11 +45,12 @@ typedef struct {
     int64_t token_stride, head_stride;
 } pq_heads;
 
-/* Plan of one step.  Request r has cached_lens[r] tokens in the cache and brings new_lens[r] more (negative lengths count
- * as 0).  It needs the blocks that its new tokens begin, ceil((cached + new) / block_size) - ceil(cached / block_size) of
- * them; requests take theirs from free_blocks in order.  A request is refused if its blocks do not fit its row of the
- * table (then it needs none), if the free blocks are used up by its own and the earlier ones' needs, or if its tokens
- * end behind row ntokens of the outputs.
+/* Plan of one step.  Request r has cached_lens[r] tokens in the cache and brings new_lens[r] more (a negative number of new ones
+ * counts as 0).  It needs the blocks that its new tokens begin, ceil((cached + new) / block_size) - ceil(cached / block_size) of
+ * them; requests take theirs from free_blocks in order.  A request is refused if its cached length is negative or its blocks do not
+ * fit its row of the table (then it needs none), if the free blocks are used up by its own and the earlier ones' needs (those of
+ * earlier requests that are refused for that among them, and so it is refused even if it needs none itself: the ones that are to go
+ * on come first), or if its tokens end behind row ntokens of the outputs.
  *   new_lens, cached_lens [nreq] i32; block_tables [nreq][width] i32, in and out: the entries of the cached blocks are
  *   read, those of the fresh blocks written, the others left; free_blocks [nfree] i32
  *   -> cu_new [nreq+1] i32 = sums of the new lengths of the requests before (2^31-1 where they pass it);

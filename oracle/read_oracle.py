@@ -11,11 +11,12 @@ def plan(new_lens, cached_lens, tables, free_blocks, block_size, ntokens):
     positions, slots = np.full(ntokens, -1, np.int32), np.full(ntokens, -1, np.int64)
     counted = taken = 0
     for r, (n, c) in enumerate(zip(new_lens.tolist(), cached_lens.tolist())):
-        n, c = max(n, 0), max(c, 0)
+        n, refused, c = max(n, 0), c < 0, max(c, 0)
         have, full = -(-c // block_size), -(-(c + n) // block_size)
-        need = full - have if full <= width else 0
+        fits = not refused and full <= width
+        need = full - have if fits else 0
         counted += need
-        served = full <= width and counted <= len(free_blocks) and cu[-1] + n <= ntokens
+        served = fits and counted <= len(free_blocks) and cu[-1] + n <= ntokens
         if served:
             taken += need
             tables[r, have:full] = free_blocks[counted - need:counted]

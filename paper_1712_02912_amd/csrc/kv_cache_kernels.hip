@@ -57,10 +57,11 @@ __device__ __forceinline__ void plan_add_up(const plan_args &a, const plan_sums 
         bool fits = false;
         if (r < a.nreq) {
             fresh = (uint32_t)max(a.new_lens[r], 0);
-            cached = (uint32_t)max(a.cached_lens[r], 0);
+            const int32_t held = a.cached_lens[r];   // (negative: refused before, and again)
+            cached = (uint32_t)max(held, 0);
             const uint32_t all = fresh + cached;   // (below 2^32)
             const uint32_t full = all <= INT_MAX ? plan_blocks(a, all) : UINT_MAX;
-            fits = full <= (uint32_t)a.width;
+            fits = held >= 0 && full <= (uint32_t)a.width;
             need = fits ? full - plan_blocks(a, cached) : 0;
         }
         uint64_t t = wave_scan<op_add>((uint64_t)fresh), b = wave_scan<op_add>((uint64_t)need);

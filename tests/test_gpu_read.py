@@ -86,6 +86,27 @@ def test_plan_of_odd_lengths(ctx):
     assert cu.tolist() == [0] and taken[0] == 0 and (positions == -1).all() and (slots == -1).all()
 
 
+@pytest.mark.parametrize("nreq", [6, 700, 5000])
+def test_plan_of_lengths_that_a_plan_gave(ctx, nreq):
+    """Lengths of one step given to the next: a request that was refused stays so, its table and the pool are left alone."""
+    r = np.random.default_rng(nreq)
+    new, cached = r.integers(0, 20, nreq), r.integers(0, 40, nreq)
+    new[nreq // 2] = 1000
+    tables = r.integers(0, 10 ** 6, (nreq, 5)).astype(np.int32)
+    free = np.arange(10 ** 6, 10 ** 6 + 9 * nreq, dtype=np.int32)
+    free_at, before = 0, tables
+    for step in range(4):
+        nfree = len(free) - free_at if step != 1 else nreq // 4
+        want = orc.plan(new, cached, before, free[free_at:free_at + nfree], 16, int(new.sum()))
+        got = run_plan(ctx, new, cached, before, free[free_at:free_at + nfree], 16, int(new.sum()))
+        assert all(np.array_equal(np.atleast_1d(a), np.atleast_1d(b)) for a, b in zip(got, want)), step
+        refused = cached < 0
+        assert (got[2][refused] == -1).all() and np.array_equal(got[0][refused], before[refused])
+        before, cached, free_at = got[0].astype(np.int32), got[2], free_at + int(got[5][0])
+        new = r.integers(0, 3, nreq)
+    assert (cached < 0).sum() > 1 and (cached >= 0).any()
+
+
 def test_plan_refusals(ctx):
     i32 = dict(dtype=torch.int32, device="cuda")
     lens, table, free = torch.ones(2, **i32), torch.zeros((2, 4), **i32), torch.zeros(9, **i32)

@@ -33,6 +33,14 @@ def test_plan_refuses_in_order():
     assert kv.tolist() == [5, -1, -1, -1, -1] and taken == 2 and (positions[5:] == -1).all()
 
 
+def test_plan_refuses_again_what_it_refused():
+    tables = np.arange(15, dtype=np.int32).reshape(5, 3)
+    t, cu, kv, positions, slots, taken = orc.plan(np.array([1, 3, 0, 1, 2]), np.array([4, -1, -7, -2 ** 31, 4]), tables, np.arange(20, 30), 4, 9)
+    assert kv.tolist() == [5, -1, -1, -1, 6] and taken == 2 and cu.tolist() == [0, 1, 4, 4, 5, 7]
+    assert positions.tolist() == [4, -1, -1, -1, -1, 4, 5, -1, -1] and np.array_equal(t[1:4], tables[1:4])
+    assert slots.tolist() == [80, -1, -1, -1, -1, 84, 85, -1, -1]
+
+
 @pytest.mark.parametrize("pairs", [False, True])
 def test_turn_keeps_lengths_and_relative_angles(pairs):
     r = np.random.default_rng(2)
