@@ -104,7 +104,7 @@ def test_plan_of_lengths_that_a_plan_gave(ctx, nreq):
         assert (got[2][refused] == -1).all() and np.array_equal(got[0][refused], before[refused])
         before, cached, free_at = got[0].astype(np.int32), got[2], free_at + int(got[5][0])
         new = r.integers(0, 3, nreq)
-    assert (cached < 0).sum() > 1 and (cached >= 0).any()
+    assert (cached < 0).any() and (cached >= 0).any()
 
 
 def test_plan_refusals(ctx):
