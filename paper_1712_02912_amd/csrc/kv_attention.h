@@ -15,7 +15,7 @@ struct attention_args {
     void *out;
     float *lse;
     int64_t ntokens;
-    int q_heads, nreq, width, window;
+    int q_heads, nreq, width, window, max_new;
     int group;          // query heads that read one head of the cache
     uint32_t k_strides[2], v_strides[2];   // of blocks and places of the cache, where the matrix cores are taken
     fast_div by_block, by_group;
@@ -30,6 +30,10 @@ constexpr float NO_SCORE = -3e38f;
 // table can hold them (kv_lens is the caller's: memory is read by it).
 __device__ __forceinline__ int attention_length(const attention_args &a, int r) { return max(a.kv_lens[r], -1); }
 __device__ __forceinline__ int attention_keys(const attention_args &a, int r) { return min(attention_length(a, r), a.width * a.cache.block_size); }
+// New tokens of a request whose rows are computed: of all, those that have a row, up to max_new.
+__device__ __forceinline__ int attention_held(const attention_args &a, int r) {
+    return (int)min((int64_t)min(a.cu[r + 1] - a.cu[r], a.max_new), a.ntokens - a.cu[r]);
+}
 
 // A block table's entry; blocks outside the cache read as block 0 (memory stays in bounds, see pq_read.h).
 __device__ __forceinline__ int64_t attention_block(const attention_args &a, int32_t entry) { return (unsigned)entry < (uint64_t)a.cache.nblocks ? entry : 0; }
@@ -127,7 +131,7 @@ template <int D> struct lds_row {
 
 // Requests of so few rows per head of the cache have a kernel of their own.
 constexpr int FEW_ROWS = 16;
-__device__ __forceinline__ bool attention_is_few(const attention_args &a, int fresh) { return (int64_t)fresh * a.group <= FEW_ROWS; }
+__device__ __forceinline__ bool attention_is_few(const attention_args &a, int held) { return (int64_t)held * a.group <= FEW_ROWS; }
 
 // The last of 0 ... n - 1 for which f holds; f holds from 0 up to there.  By a whole wave, 64 places at once, so that a
 // search of a few hundred takes two loads one after the other, not nine.

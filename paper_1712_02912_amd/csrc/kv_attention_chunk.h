@@ -40,8 +40,8 @@ struct chunk_place {
 };
 template <int M> __device__ __forceinline__ chunk_place chunk_locate(const attention_args &a, bool without_few, int64_t index) {
     auto tiles_of = [&](int r) {
-        const int fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
-        return held <= 0 || (without_few && attention_is_few(a, fresh)) ? 0 : (int)(((int64_t)held * a.group + M - 1) / M);
+        const int held = attention_held(a, r);
+        return held <= 0 || (without_few && attention_is_few(a, held)) ? 0 : (int)(((int64_t)held * a.group + M - 1) / M);
     };
     if (a.nreq > CHUNK_ADDED) {
         const int r = wave_search(a.nreq, [&](int i) { return (int64_t)a.cu[i] * a.group / M + i <= index; });
@@ -91,7 +91,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
     const int heads = a.cache.heads, h = block % heads;
     const chunk_place at = chunk_locate<M>(a, split.without_few, block / heads);
     if (at.r < 0) return;
-    const int r = at.r, fresh = a.cu[r + 1] - a.cu[r], held = (int)min((int64_t)fresh, a.ntokens - a.cu[r]);
+    const int r = at.r, fresh = a.cu[r + 1] - a.cu[r], held = attention_held(a, r);
     const int64_t rows = (int64_t)held * a.group, mine = at.tiles - 1 - at.index;   // the last rows see the most keys: they come first
 
     const int kv = attention_length(a, r), nkeys = attention_keys(a, r);
@@ -361,10 +361,9 @@ template <class T, int D> __device__ __forceinline__ void chunk_join_block(const
     const int64_t row = (int64_t)block * JOIN_ROWS + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (row >= min(a.ntokens, (int64_t)a.cu[a.nreq]) * a.q_heads) return;
-    if (split.without_few) {
-        const int r = attention_request(a.cu, a.nreq, row / a.q_heads);
-        if (attention_is_few(a, a.cu[r + 1] - a.cu[r])) return;
-    }
+    const int64_t t = row / a.q_heads;
+    const int r = wave_search(a.nreq, [&](int i) { return a.cu[i] <= t; });
+    if (t - a.cu[r] >= a.max_new || (split.without_few && attention_is_few(a, attention_held(a, r)))) return;   // it has no parts
     const float *const stats = split.stats + 2 * row * split.splits, *const parts = split.parts + row * split.splits * D;
     float top = NO_SCORE, all = 0.f, o[E] = {};
     for (int s = lane; s < split.splits; s += 64) top = fmaxf(top, stats[2 * s]);

@@ -37,18 +37,18 @@ struct few_line {
 };
 
 struct few_range {
-    int fresh, held, keys, from;   // new tokens, those of them that have a row of the queries
+    int fresh, held, keys, from;   // new tokens, those of them whose rows are computed
     int64_t units;
 };
 // Keys that the rows of a request see; a request without any that still has rows is one unit (its rows are written).
 __device__ __forceinline__ few_range few_load(const attention_args &a, int unit, int r) {
     few_range x;
     x.fresh = a.cu[r + 1] - a.cu[r];
-    x.held = (int)min((int64_t)x.fresh, a.ntokens - a.cu[r]);
+    x.held = attention_held(a, r);
     const int kv = attention_length(a, r);
     x.keys = max(0, attention_keys(a, r));
     x.from = a.window > 0 ? (int)max((int64_t)0, (int64_t)kv - x.fresh - a.window + 1) : 0;
-    x.units = x.held <= 0 || !attention_is_few(a, x.fresh) ? 0 : max((int64_t)1, (int64_t)(((uint32_t)max(x.keys - x.from, 0) + unit - 1) / (uint32_t)unit));
+    x.units = x.held <= 0 || !attention_is_few(a, x.held) ? 0 : max((int64_t)1, (int64_t)(((uint32_t)max(x.keys - x.from, 0) + unit - 1) / (uint32_t)unit));
     return x;
 }
 

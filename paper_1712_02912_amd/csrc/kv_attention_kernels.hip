@@ -20,7 +20,7 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
     const int64_t t = blockIdx.x / a.q_heads;
     const int h = (int)(blockIdx.x - t * a.q_heads), kvh = h / (a.q_heads / a.cache.heads);
     const int r = attention_request(a.cu, a.nreq, t);
-    if (r < 0) return;
+    if (r < 0 || t - a.cu[r] >= a.max_new) return;
     const int position = attention_length(a, r) - (a.cu[r + 1] - (int)t), at = min(position, attention_keys(a, r) - 1);
     const int from = a.window > 0 ? (int)max((int64_t)0, (int64_t)position - a.window + 1) : 0;
     const T *qrow = (const T *)a.q.p + t * a.q.token_stride + h * a.q.head_stride;
@@ -113,6 +113,7 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
     a.nreq = nreq;
     a.width = width;
     a.window = window;
+    a.max_new = max_new;
     a.group = q_heads / cache->heads;
     a.by_block = fast_div((uint32_t)cache->block_size);
     a.by_group = fast_div((uint32_t)a.group);

@@ -436,6 +436,34 @@ def test_attention_of_requests_behind_the_rows(ctx, new):
     assert (got[new:t] == 0).all() and np.isneginf(lse[new:t]).all() and (got[t:] == 7).all() and (lse[t:] == 7).all()
 
 
+# few rows, whole and in parts; chunks, whole and in parts; both; the general kernel takes f32
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("new,kv,max_new", [([5, 3, 1], [200, 3, 90], 2), ([40, 3, 1, 9], [700, 90, 1, 9], 2), ([7, 40], [9000, 8000], 3),
+                                            ([300, 40, 0, 1], [310, 90, 7, 60], 100), ([90, 130], [3000, 2900], 60),
+                                            ([90, 1, 1, 30], [4400, 4300, 60, -1], 70), ([90, 9, 1, 30], [9000, 4300, 60, 30], 29),
+                                            ([1, 1], [100, 200], 0)])
+def test_attention_of_more_tokens_than_the_call_says(ctx, dtype, window, new, kv, max_new):
+    """Rows of a request behind max_new are left, those before it are as without the limit."""
+    r = np.random.default_rng(max_new)
+    tables, keys, values = make_cache(r, kv, 2, 64, 16, dtype, np.nan, "plain")
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    t = int(cu[-1])
+    q = dev(r.standard_normal((t, 4, 64)), dtype)
+    out, lse = torch.full((t, 4, 64), 7.0, dtype=dtype, device="cuda"), torch.full((t, 4), 7.0, device="cuda")
+    ctx.pq_kv_attention(q, keys, values, dev(tables), dev(cu), dev(np.array(kv, np.int32)), max_new, window=window, out=out, lse=lse)
+    want, want_lse, spread = orc.attention(host(q), host(keys), host(values), tables, cu, np.array(kv), 0.125, window)
+    got, got_lse = host(out), host(lse)
+    held = np.concatenate([np.arange(n) < max_new for n in new])
+    assert (got[~held] == 7).all() and (got_lse[~held] == 7).all()
+    held_keys = np.concatenate([host(keys)[tables[i, :-(-k // 16)]].reshape(-1, 2, 64)[:k] for i, k in enumerate(kv) if k > 0])
+    bound, fp32 = attention_bound(dtype, host(q), held_keys, spread, want, 0.125, max(kv), 64)
+    assert (np.abs(got - want) <= bound)[held].all()
+    seen = held[:, None] & np.isfinite(want_lse)
+    assert np.array_equal(np.isneginf(got_lse)[held], np.isneginf(want_lse)[held])
+    assert (np.abs(got_lse[seen] - want_lse[seen]) <= 2 * fp32 + 1e-6 * np.abs(want_lse[seen])).all()
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("q_heads,heads,dim", [(2, 2, 64), (4, 2, 64), (8, 2, 96), (4, 1, 128), (2, 1, 256)])
 @pytest.mark.parametrize("new", [[1, 40, 2, 17, 1, 3], [1] * 9 + [300], [5, 700, 1]])
