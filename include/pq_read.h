@@ -57,6 +57,7 @@ typedef struct {
  *      kv_lens [nreq] i32 = cached + new, -1 for a refused request;
  *      positions [ntokens] i32 and slots [ntokens] i64 of the new tokens, request after request, -1 for those of refused
  *      requests and for rows behind the last token; taken [1] i32 = number of blocks taken from free_blocks.
+ * Results and block_tables must overlap neither each other nor the other inputs (kv_lens is not cached_lens updated in place).
  * Requires width * block_size < 2^31, ntokens < 2^31. */
 int pq_kv_plan(pq_ctx *ctx, const int32_t *new_lens, const int32_t *cached_lens, int nreq, int32_t *block_tables, int width,
                const int32_t *free_blocks, int nfree, int block_size, int64_t ntokens, int32_t *cu_new, int32_t *kv_lens,

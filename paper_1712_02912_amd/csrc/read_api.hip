@@ -37,6 +37,15 @@ int check_heads(pq_ctx *ctx, const char *who, const char *what, const pq_heads *
     return PQ_OK;
 }
 
+// memory that a call takes
+struct span {
+    const void *p;
+    size_t bytes;
+};
+bool overlap(const span &a, const span &b) {
+    return a.bytes > 0 && b.bytes > 0 && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes && (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -51,6 +60,13 @@ int pq_kv_plan(pq_ctx *ctx, const int32_t *new_lens, const int32_t *cached_lens,
     if (!cu_new || !taken || (nreq > 0 && (!new_lens || !cached_lens || !kv_lens)) || (nreq > 0 && width > 0 && !block_tables) ||
         (nfree > 0 && !free_blocks) || (ntokens > 0 && (!positions || !slots)))
         return fail(ctx, PQ_EINVAL, "kv_plan: null pointer");
+    // (all blocks of the kernel read the lengths while others already write results; what is only read comes last)
+    const size_t n = (size_t)nreq, t = (size_t)ntokens;
+    const span spans[] = {{cu_new, 4 * (n + 1)}, {kv_lens, 4 * n},  {positions, 4 * t},   {slots, 8 * t},          {taken, 4},
+                          {block_tables, 4 * n * (size_t)width},   {new_lens, 4 * n}, {cached_lens, 4 * n}, {free_blocks, 4 * (size_t)nfree}};
+    for (int i = 0; i < 6; ++i)
+        for (int j = i + 1; j < 9; ++j)
+            if (overlap(spans[i], spans[j])) return fail(ctx, PQ_EINVAL, "kv_plan: results overlap each other or what is read");
     return launch_kv_plan(ctx, new_lens, cached_lens, nreq, block_tables, width, free_blocks, nfree, block_size, ntokens, cu_new, kv_lens,
                           positions, slots, taken);
 }

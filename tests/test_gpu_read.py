@@ -123,6 +123,29 @@ def test_plan_refusals(ctx):
         ctx.pq_kv_plan(lens, lens, torch.zeros((2, 8), **i32)[:, ::2], free, 16, 4)
 
 
+def test_plan_refuses_results_over_its_inputs(ctx):
+    """Lengths cannot be updated in place: blocks read them while another writes results."""
+    def whole(n, dtype=torch.int32):
+        return torch.full((n,), 2, dtype=dtype, device="cuda")
+    lens, cached, table, free = whole(3), whole(3), whole(12).view(3, 4), whole(9)
+    room, wide = whole(40), whole(40, torch.int64)
+    out = [room[:4], whole(3), whole(6), wide[:6], whole(1)]
+    ctx.pq_kv_plan(lens, cached, table, free, 16, 6, out=tuple(out))
+    for at, bad in ((1, cached), (1, lens), (0, free[2:6]), (1, room[3:6]), (2, table.view(-1)[6:]), (2, room[:6]), (4, lens[2:]),
+                    (4, wide.view(torch.int32)[11:12])):
+        with pytest.raises(binding.PqError) as e:
+            ctx.pq_kv_plan(lens, cached, table, free, 16, 6, out=tuple(bad if i == at else x for i, x in enumerate(out)))
+        assert e.value.code == -1
+    with pytest.raises(binding.PqError):
+        ctx.pq_kv_plan(lens, cached, table, table.view(-1)[3:], 16, 6, out=tuple(out))
+    with pytest.raises(binding.PqError):
+        ctx.pq_kv_plan(lens, table.view(-1)[:3], table, free, 16, 6, out=tuple(out))
+    assert (lens == 2).all() and (cached == 2).all()
+    # side by side is no overlap
+    ctx.pq_kv_plan(lens, cached, table, free, 16, 6, out=(room[:4], room[4:7], room[7:13], wide[:6], room[13:14]))
+    torch.cuda.synchronize()
+
+
 # ---- append -----------------------------------------------------------------------------------------------------------
 def check_append(ctx, tokens, q_heads, heads, dim, rot, pairs, dtype, norm=True, weights=True, layout="packed", block_size=16, eps=1e-6,
                  seed=0):
