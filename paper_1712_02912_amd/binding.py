@@ -12,10 +12,22 @@ import os
 
 import torch
 
+
+class _NoViews:
+    """In the extension module's place where it cannot be imported: the reading step's calls say why, the search goes without it."""
+
+    def __init__(self, error):
+        self.error = error
+
+    def __getattr__(self, name):
+        raise RuntimeError(f"the reading step's extension module tensor_views.so cannot be imported ({self.error}): build it for this "
+                           "Python and torch (python -m paper_1712_02912_amd.build)") from self.error
+
+
 try:
     from paper_1712_02912_amd import tensor_views as _views
-except ImportError:   # not built: load() says so
-    _views = None
+except ImportError as e:
+    _views = _NoViews(e)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpqadc.so")
@@ -48,8 +60,6 @@ def load():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: build it first (python -m paper_1712_02912_amd.build); "
                            "there is no fallback path")
-    if _views is None:
-        raise RuntimeError("tensor_views.so is missing: build it first (python -m paper_1712_02912_amd.build)")
     lib = ctypes.CDLL(LIB_PATH)
     vp, ci, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
     lib.pq_create.argtypes = [ctypes.POINTER(vp), ci, vp]
