@@ -127,11 +127,12 @@ class Context:
         if rc != 0:
             raise PqError(rc, "pq_create failed")
         self.handle = handle
+        self._address = handle.value   # the same, for the extension module
 
     def close(self):
         if getattr(self, "handle", None):
             self.lib.pq_destroy(self.handle)
-            self.handle = None
+            self.handle = self._address = None
 
     def __del__(self):
         try:
@@ -338,7 +339,7 @@ class Context:
             i32, nreq = torch.int32, block_tables.shape[0]
             out = tuple(torch.empty(n, dtype=dt, device=block_tables.device)
                         for n, dt in ((nreq + 1, i32), (nreq, i32), (ntokens, i32), (ntokens, torch.int64), (1, i32)))
-        rc = _views.plan(_entries["pq_kv_plan"], self.handle.value, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, *out)
+        rc = _views.plan(_entries["pq_kv_plan"], self._address, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, *out)
         if rc:
             self._check(rc)
         return out
@@ -350,7 +351,7 @@ class Context:
         (None if q is None)."""
         if q is not None and out is None:
             out = torch.empty(q.shape, dtype=key_cache.dtype, device=q.device)
-        rc = _views.append(_entries["pq_kv_append"], self.handle.value, q, k, v, positions, slots, key_cache, value_cache, cos, sin, q_weight,
+        rc = _views.append(_entries["pq_kv_append"], self._address, q, k, v, positions, slots, key_cache, value_cache, cos, sin, q_weight,
                            k_weight, eps, norm, pairs, out)
         if rc:
             self._check(rc)
@@ -363,7 +364,7 @@ class Context:
             out = torch.empty(q.shape, dtype=key_cache.dtype, device=q.device)
         if lse is None:
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        rc = _views.attention(_entries["pq_kv_attention"], self.handle.value, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new,
+        rc = _views.attention(_entries["pq_kv_attention"], self._address, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new,
                               scale, window, out, lse)
         if rc:
             self._check(rc)
@@ -375,7 +376,7 @@ class Context:
         if out is None:
             rows = logits.shape[0]
             out = (torch.empty(rows, dtype=torch.int64, device=logits.device), torch.empty(rows, dtype=torch.float32, device=logits.device))
-        rc = _views.sample(_entries["pq_sample_tokens"], self.handle.value, logits, noise, temperature, top_k, top_p, min_p, *out)
+        rc = _views.sample(_entries["pq_sample_tokens"], self._address, logits, noise, temperature, top_k, top_p, min_p, *out)
         if rc:
             self._check(rc)
         return out

@@ -103,12 +103,12 @@ bool whole(PyObject *o, int64_t *x) {
     *x = PyLong_AsLongLong(o);
     return *x != -1 || !PyErr_Occurred();
 }
-// The library's function and context, as the binding has them: addresses.
+// The library's function and context, as the binding has them: addresses (a closed context's is None: the library refuses it).
 template <class F> bool entry(PyObject *const *args, F **f, pq_ctx **ctx) {
     *f = (F *)PyLong_AsVoidPtr(args[0]);
-    *ctx = *f ? (pq_ctx *)PyLong_AsVoidPtr(args[1]) : nullptr;
-    if (*f && *ctx) return true;
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "the context is closed");
+    *ctx = !*f || args[1] == Py_None ? nullptr : (pq_ctx *)PyLong_AsVoidPtr(args[1]);
+    if (*f && (*ctx || !PyErr_Occurred())) return true;
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no function");
     return false;
 }
 template <class F> PyObject *without_gil(F f) {

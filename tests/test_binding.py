@@ -29,7 +29,7 @@ def test_the_search_goes_without_the_extension_module(monkeypatch):
     spec.loader.exec_module(alone)
     assert alone.load().pq_version().decode().startswith("pqadc")
     ctx = alone.Context.__new__(alone.Context)
-    ctx.lib, ctx.handle = alone.load(), ctypes.c_void_p()
+    ctx.lib, ctx.handle, ctx._address = alone.load(), ctypes.c_void_p(), None
     none = [None] * 6
     for call in (lambda: ctx.pq_kv_plan(*none, out=()), lambda: ctx.pq_kv_append(None, *none), lambda: ctx.pq_kv_attention(*none, 1, out=1, lse=1),
                  lambda: ctx.pq_sample_tokens(None, None, out=())):

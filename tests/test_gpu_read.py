@@ -767,6 +767,18 @@ def test_sample_without_noise_is_the_largest_logit(ctx, temperature, filters, ro
     assert (check_sample(ctx, equal, None, [temperature] * rows, **{k: [v] * rows for k, v in filters.items()}) == 17).all()
 
 
+def test_calls_of_a_closed_context_are_refused():
+    c = binding.Context(0)
+    c.close()
+    i32 = dict(dtype=torch.int32, device="cuda")
+    one, x, cache = torch.ones(1, **i32), torch.zeros((1, 1, 64), device="cuda"), torch.zeros((1, 16, 1, 64), device="cuda")
+    for call in (lambda: c.pq_kv_plan(one, one, one.view(1, 1), one, 16, 1), lambda: c.pq_kv_append(x, x, x, one, one.long(), cache, cache),
+                 lambda: c.pq_kv_attention(x, cache, cache, one.view(1, 1), torch.ones(2, **i32), one, 1),
+                 lambda: c.pq_sample_tokens(x[0], x[0]), lambda: c.pq_build_luts(torch.zeros((1, 8), device="cuda"), torch.zeros((8, 256, 1), device="cuda"))):
+        with pytest.raises(binding.PqError, match="null context"):
+            call()
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------
 def test_a_captured_step_replays(ctx):
     """Plan, append, attention and draw in one HIP graph, replayed on new inputs with eager work in between."""
