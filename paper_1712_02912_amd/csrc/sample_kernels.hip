@@ -480,14 +480,17 @@ template <class T> struct sample_row {
             sh.wave_d[turn][wave] = m;
         }
         __syncthreads();
-        const uint32_t cw = row_scan<op_add>(sh.wave32[turn][lane & 15]) + c0;
+        const uint32_t wave_count = sh.wave32[turn][lane & 15], cw = row_scan<op_add>(wave_count) + c0;
         const double mw = row_scan<op_add>(sh.wave_d[turn][lane & 15]) + m0;
         if (!limit.reached(read_lane(cw, 15), read_lane(mw, 15))) return SAMPLE_BINS;
-        // one wave: the first whose sum reaches the limit; in it the first bin that does (an empty one reaches nothing; if the
-        // rounding of the sums lets none, the last that is not empty)
-        const uint32_t cb = wave > 0 ? read_lane(cw, wave - 1) : c0;
-        const double mb = wave > 0 ? read_lane(mw, wave - 1) : m0;
-        if ((wave == 0 || !limit.reached(cb, mb)) && limit.reached(read_lane(cw, wave), read_lane(mw, wave))) {
+        // One wave: of those that hold a token the first whose sum reaches the limit; in it the first bin that does.  An empty one
+        // reaches nothing: sums of different waves are added up in different orders, so one may be the last bit above, or below, the
+        // sum that it adds nothing to.  Where rounding lets none reach the limit, the last that is not empty.
+        const uint32_t holds = (uint32_t)__ballot(wave_count > 0) & 0xffff, reach = (uint32_t)__ballot(limit.reached(cw, mw)) & holds;
+        if (holds == 0) return SAMPLE_BINS;
+        if (wave == (reach ? __ffs(reach) - 1 : 31 - __clz((int)holds))) {
+            const uint32_t cb = wave > 0 ? read_lane(cw, wave - 1) : c0;
+            const double mb = wave > 0 ? read_lane(mw, wave - 1) : m0;
             c += cb;
             m += mb;
             const uint32_t n0 = bin_count(v0), n1 = bin_count(v1);

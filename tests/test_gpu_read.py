@@ -767,6 +767,18 @@ def test_sample_without_noise_is_the_largest_logit(ctx, temperature, filters, ro
     assert (check_sample(ctx, equal, None, [temperature] * rows, **{k: [v] * rows for k, v in filters.items()}) == 17).all()
 
 
+@pytest.mark.parametrize("vocab", [9000, 131072])
+def test_sample_of_limits_within_the_last_bits_of_the_weight(ctx, vocab):
+    """Weights over 60 octaves in a few clusters, most of the bins empty, and top_p next to 1: sums that round where the limit is."""
+    r = np.random.default_rng(vocab)
+    l = np.full((60, vocab), -np.inf)
+    for row in l:
+        for cluster in r.choice(60, 5, replace=False):
+            row[r.integers(0, vocab, r.integers(1, 600))] = -cluster * np.log(2) + r.uniform(-0.3, 0.3)
+    noise = dev(r.random((60, vocab)).astype(np.float32).clip(1e-7, 1 - 1e-7))
+    check_sample(ctx, dev(l, F32), noise, top_p=[float(1 - 2.0 ** -r.integers(10, 25)) for _ in range(60)])
+
+
 def test_calls_of_a_closed_context_are_refused():
     c = binding.Context(0)
     c.close()
