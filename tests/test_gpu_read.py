@@ -459,6 +459,38 @@ def test_attention_of_requests_behind_the_rows(ctx, new):
     assert (got[new:t] == 0).all() and np.isneginf(lse[new:t]).all() and (got[t:] == 7).all() and (lse[t:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new,kv", [([1, 2, 1], [1, 35, 700]), ([1], [9000]), ([40, 40, 1], [40, 73, 1]), ([90], [3000]), ([90, 1, 1], [4400, 4300, 60])])
+def test_attention_leaves_unseen_keys_out_to_the_last_bits(ctx, dtype, dim, new, kv):
+    """Places that hold no key have -60000: the bound is that of the keys that are there, and the result is that of a cache of zeros."""
+    q = dev(np.random.default_rng(dim).standard_normal((sum(new), 4, dim)), dtype)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    found = []
+    for fill in (-60000.0, 0.0):
+        tables, keys, values = make_cache(np.random.default_rng(len(new)), kv, 2, dim, 64, dtype, fill, "plain")
+        found.append(ctx.pq_kv_attention(q, keys, values, dev(tables), dev(cu), dev(np.array(kv, np.int32)), max(new)))
+    want, want_lse, spread = orc.attention(host(q), host(keys), host(values), tables, cu, np.array(kv), dim ** -0.5, 0)
+    bound, fp32 = attention_bound(dtype, host(q), host(keys), spread, want, dim ** -0.5, max(kv), dim)
+    for out, lse in found:
+        assert (np.abs(host(out) - want) <= bound).all()
+        assert (np.abs(host(lse) - want_lse) <= 2 * fp32 + 1e-6 * np.abs(want_lse)).all()
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("new,kv", [([1, 2, 1], [1, 35, 700]), ([1, 3], [9000, 20000]), ([40, 40, 1], [40, 73, 1]), ([300, 200], [9000, 500]),
+                                    ([90, 1, 1, 7], [4400, 4300, 60, 9000])])
+def test_attention_repeats_itself_exactly(ctx, dtype, new, kv):
+    r = np.random.default_rng(len(new))
+    tables, keys, values = make_cache(r, kv, 2, 128, 16, dtype, np.nan, "plain")
+    args = (dev(r.standard_normal((sum(new), 8, 128)), dtype), keys, values, dev(tables), dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)),
+            dev(np.array(kv, np.int32)), max(new))
+    first = ctx.pq_kv_attention(*args)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(first, ctx.pq_kv_attention(*args)))
+
+
 # few rows, whole and in parts; chunks, whole and in parts; both; the general kernel takes f32
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("window", [0, 50])

@@ -86,3 +86,20 @@ def test_the_command_runs():
         example.answer(ctx, d, [torch.zeros(4, dtype=torch.int64, device="cuda")], 2, torch.rand((2, 1, 64), device="cuda"))
         reader = example.Reader(ctx, d, 1, 1, 1)
         reader.step(torch.zeros(17, dtype=torch.int64, device="cuda"), [17], torch.rand((1, 64), device="cuda"))
+
+
+def test_a_full_cache_is_refused_on_the_host():
+    """Too few blocks, or a row of the table too short: nothing is changed, and what fits is served afterwards."""
+    ctx = binding.Context(0)
+    d = example.Decoder(vocab=64, width=64, layers=1, q_heads=1, heads=1, positions=64)
+    tokens, noise = torch.zeros(40, dtype=torch.int64, device="cuda"), torch.rand((1, 64), device="cuda")
+    for blocks, width in ((1, 3), (3, 1)):
+        reader = example.Reader(ctx, d, 1, blocks, width)
+        with pytest.raises(RuntimeError, match="the cache is full"):
+            reader.step(tokens[:17], [17], noise)
+        drawn, _, _ = reader.step(tokens[:16], [16], noise)
+        assert drawn.shape == (1,) and reader.lens.tolist() == [16] and reader.used == 1
+        with pytest.raises(RuntimeError, match="the cache is full"):
+            reader.step(tokens[:1], [1], noise)
+        assert reader.lens.tolist() == [16] and reader.counts == [16]
+    ctx.close()
