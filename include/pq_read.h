@@ -48,9 +48,9 @@ typedef struct {
 /* Plan of one step.  Request r has cached_lens[r] tokens in the cache and brings new_lens[r] more (a negative number of new ones
  * counts as 0).  It needs the blocks that its new tokens begin, ceil((cached + new) / block_size) - ceil(cached / block_size) of
  * them; requests take theirs from free_blocks in order.  A request is refused if its cached length is negative or its blocks do not
- * fit its row of the table (then it needs none), if the free blocks are used up by its own and the earlier ones' needs (those of
- * earlier requests that are refused for that among them, and so it is refused even if it needs none itself: the ones that are to go
- * on come first), or if its tokens end behind row ntokens of the outputs.
+ * fit its row of the table (then it needs none), if the free blocks are used up by its own and the earlier ones' needs (of these
+ * all count, refused ones' too, so behind a request that found too few blocks all are refused, also those that need none: put
+ * first what must go on), or if its tokens end behind row ntokens of the outputs.
  *   new_lens, cached_lens [nreq] i32; block_tables [nreq][width] i32, in and out: the entries of the cached blocks are
  *   read, those of the fresh blocks written, the others left; free_blocks [nfree] i32
  *   -> cu_new [nreq+1] i32 = sums of the new lengths of the requests before (2^31-1 where they pass it);

@@ -333,8 +333,8 @@ class Context:
     # -- The reading step (include/pq_read.h).  Tensors are taken where they lie: what the library reads with strides may have any
     # but the last, all others are contiguous; nothing is copied. -------------------------------------------------------------
     def pq_kv_plan(self, new_lens, cached_lens, block_tables, free_blocks, block_size, ntokens, out=None):
-        """Positions and slots of the new tokens; block_tables [nreq][width] gets the fresh blocks.
-        Returns (cu_new, kv_lens, positions, slots, taken), `out` if it is given."""
+        """Positions and slots of the new tokens; block_tables [nreq][width] gets the fresh blocks.  A request with a negative cached
+        length is refused, as before; results go to memory of their own (kv_lens is not cached_lens updated in place).  Returns (cu_new, kv_lens, positions, slots, taken), `out` if it is given."""
         if out is None:
             i32, nreq = torch.int32, block_tables.shape[0]
             out = tuple(torch.empty(n, dtype=dt, device=block_tables.device)
@@ -359,7 +359,8 @@ class Context:
 
     def pq_kv_attention(self, q, key_cache, value_cache, block_tables, cu_new, kv_lens, max_new, scale=None, window=0, out=None,
                         lse=None):
-        """Attention of q [tokens][q heads][dim] over the paged cache; scale None: 1 / sqrt(dim).  Returns (out, lse)."""
+        """Attention of q [tokens][q heads][dim] over the paged cache; scale None: 1 / sqrt(dim).  Rows of a request behind max_new, and
+        behind the last one, are left as they are.  Returns (out, lse)."""
         if out is None:
             out = torch.empty(q.shape, dtype=key_cache.dtype, device=q.device)
         if lse is None:

@@ -1,4 +1,4 @@
-// Element types of the reading step (pq_elem): loads to fp32, stores rounded once to the nearest, and vectors of them.
+// Elements of the reading step (pq_elem): vectors of them, and their sizes.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -6,11 +6,6 @@
 #include "pq_read.h"
 
 namespace pq {
-
-template <int E> struct elem_of;
-template <> struct elem_of<PQ_ELEM_F32> { typedef float type; };
-template <> struct elem_of<PQ_ELEM_F16> { typedef _Float16 type; };
-template <> struct elem_of<PQ_ELEM_BF16> { typedef __bf16 type; };
 
 // N elements that one load or store moves
 template <class T, int N> struct __attribute__((aligned(sizeof(T) * N))) elem_vec { T v[N]; };

@@ -9,8 +9,8 @@
 // Keys and values go through registers into one of two buffers while the other one is computed on, so one barrier per tile is
 // enough and loads have a tile's time to arrive.  Places that hold no key become zeros on that way.
 //
-// Two chunks of 2048 over 14 336 keys, 32 heads of 128 dimensions on 8, bf16: 736 GFLOP in 700 us = 1.05 PFLOP/s (a large product
-// on this card: 1.23).  Matrix instructions take 52 % of the cycles there, vector instructions (a quarter of them the powers of
+// Two chunks of 2048 over 14 336 keys, 32 heads of 128 dimensions on 8, bf16: 736 GFLOP in 690 to 730 us, by the card = 1.01 to 1.06
+// PFLOP/s (a large product: 1.23).  Matrix instructions take 52 % of the cycles there, vector instructions (a quarter of them the powers of
 // two, at a quarter of the rate) 48 %: the waves of a block meet at every tile and do the same at the same time, and giving half of
 // them priority did not change that.  64 dimensions: 0.75 PFLOP/s (as many powers for half the products); 256: 0.48, where a SIMD
 // has registers for one wave only.

@@ -3,9 +3,6 @@
 
 namespace pq {
 
-
-
-
 // Waves of a SIMD that registers are to be left for.  (Left alone, blocks of four waves over 64 dimensions come to 168 to 171
 // registers; three waves have 168: 40 us for 23 requests of 1 to 517 tokens with windows of 1024 keys, 44 us with two waves.)
 template <int D, int WAVES> constexpr int CHUNK_RESIDENT = D > 128 ? 1 : D == 64 && WAVES == 4 ? 3 : 2;

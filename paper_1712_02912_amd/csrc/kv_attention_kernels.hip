@@ -10,7 +10,7 @@ namespace pq {
 // at the end.  Keys are read by one lane each and no row shares what another one reads: simple, not fast.  It is
 // for f32 and for layouts and dimensions that the other kernels do not take; the products' operands stay fp32 there.  64 single
 // tokens over up to 8192 keys, 32 heads of 128 dimensions on 8, bf16: 2.4 ms (kv_attention_few.h: 0.16); two chunks of 2048 over
-// 14 336 keys: 183 ms (kv_attention_chunk.h: 0.70).
+// 14 336 keys: 183 ms (kv_attention_chunk.h: 0.69 to 0.73).
 constexpr int GENERAL_WAVES = 4;
 constexpr int GENERAL_DIM = 512;
 
@@ -128,8 +128,9 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
         // 4 heads on each of 8, up to 8000 keys: 237 us, all as chunks 252 us; 23 requests of 1 to 100 tokens, 16 heads, up to 700
         // keys: 24 and 19 us).  Where all requests have max_new tokens there is one kind only.
         const int64_t most_rows = (int64_t)max_new * a.group, held = (int64_t)width * cache->block_size;
-        // (64 single tokens over up to 8192 keys, 4 heads on each of 8: 164 us, as chunks 233; one token over 131 038 keys: 115 and
-        // 109 us)
+        // (64 single tokens over up to 8192 keys, 4 heads on each of 8: 164 us, as chunks 233.  One token over 131 038 keys is the call
+        // that chunks serve faster, 109 us for 115: how many of a call's requests are as long is known on the GPU only, and a wrong
+        // guess costs more than that.)
         if (most_rows <= FEW_ROWS) return launch_kv_attention_few(ctx, a, (int)most_rows);
         const bool is_long = held >= 4096 && (window == 0 || window >= 4096);
         return launch_kv_attention_chunk(ctx, a, is_long && a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new);
