@@ -1,14 +1,17 @@
 /*
  * pq_read.h -- the reading step next to the search of pq_adc.h: what a language model does with the passages that a
- * search has found.  Four calls on the same context, stream and error rules as pq_adc.h, in the order of one step:
+ * search has found.  Calls on the same context, stream and error rules as pq_adc.h, in the order of one step:
  *
  *   pq_kv_plan        block tables, positions and slots of a paged cache of keys and values, from the requests' lengths
  *   pq_kv_append      norm and position rotation of queries and keys, keys and values written into the cache
  *   pq_kv_attention   attention of the new tokens over the cache
  *   pq_sample_tokens  the next tokens, drawn from the logits with given random numbers
  *
+ *   pq_kv_append8, pq_kv_attention8   the second and third over a cache that holds 8 bits an element
+ *   pq_token_logprobs                 log-probabilities, ranks and entropy of the logits, and the likeliest tokens
+ *
  * All data pointers are device pointers.  None of the calls waits for the stream, unless their scratch memory has to
- * grow: pq_kv_plan (for more than 4096 requests), pq_kv_attention and pq_sample_tokens use a buffer of the context that is
+ * grow: pq_kv_plan (for more than 4096 requests), the attention of either cache and pq_sample_tokens use a buffer of the context that is
  * theirs alone, grown on demand (a HIP graph that captured a call holds its address, which stays valid until a call that
  * needs more).
  * Requests that the plan refuses have the length -1: their tokens are not written and see nothing, and a plan that is given that
@@ -114,6 +117,54 @@ int pq_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, in
 int pq_sample_tokens(pq_ctx *ctx, const void *logits, pq_elem elem, int64_t row_stride, int rows, int vocab, const float *noise,
                      int64_t noise_stride, const float *temperature, const int32_t *top_k, const float *top_p,
                      const float *min_p, int64_t *tokens, float *logprobs);
+
+/* A paged cache of 8 bits: elements are e4m3 numbers (sign, 4 bits of exponent, 3 of fraction, largest 448, NaN, no infinities), laid out
+ * as in pq_kv_cache, with one scale for each block and head: an element stands for its number times
+ * key_scales[block * heads + head] (value_scales likewise).  Scales are powers of two from 2^-126 to 2^127: of another one only the
+ * exponent counts. */
+typedef struct {
+    void *keys, *values;
+    float *key_scales, *value_scales;
+    int64_t key_strides[3], value_strides[3];
+    int64_t nblocks;
+    int block_size, heads, dim;
+} pq_kv_cache8;
+
+/* pq_kv_append into a cache of 8 bits; queries, keys, values and q_out are of type elem, the other arguments as there.
+ * The tokens of a block that come in one call are neighbours, and their slots follow each other by one, as pq_kv_plan gives them: a run.
+ * The places of the block before a run's first are taken as held, those behind its last are left as they are.
+ *   scale of a (block, head): the smallest power of two s >= 2^-126 for which no finite element of the run is above 448 s, or the
+ *   block's scale from before, if that is larger and the run does not begin at place 0;
+ *   elements: e4m3(x / s), to the nearest, ties to the even one; infinities become +-448 s, NaN stays NaN;
+ *   where a block's scale grows, what its places before the run hold is rounded anew: e4m3(number * scale before / s).
+ * Keys are computed in fp64 up to x, which is rounded to fp32; queries in fp32 as in pq_kv_append.
+ * If a block's tokens are no run (an order of their own, one slot twice, a block in two requests' tables), its contents and scale are
+ * unspecified.  Tokens that pq_kv_append does not write are not written here, and no run goes over them. */
+int pq_kv_append8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const pq_heads *q, int q_heads, const pq_heads *k, const pq_heads *v,
+                  int64_t ntokens, const int32_t *positions, const int64_t *slots, const float *cos_table, const float *sin_table,
+                  int64_t max_positions, int rot, int pairs, int norm, const float *q_weight, const float *k_weight, float eps,
+                  void *q_out);
+
+/* pq_kv_attention over a cache of 8 bits: keys and values are what its elements stand for; q rows and out are of type elem, the other
+ * arguments and all rules as there.  Elements are multiplied as they are (16 bits hold them, for f16 values up to 2^16 and keys up to 2^17
+ * from 2^-23 on), so there is no rounding but that of the weights and of the result.
+ * dim 64, 96, 128 or 256 with f16 or bf16, rows of the queries, the cache and out on 16 bytes, takes the matrix cores, any other
+ * even dim <= 512 and f32 a general kernel. */
+int pq_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const pq_heads *q, int q_heads, int64_t ntokens,
+                     const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width, int max_new,
+                     float scale, int window, void *out, float *lse);
+
+/* Log-probabilities of each row of logits, log p_i = l_i - log sum_j exp(l_j).
+ *   logits [rows] rows of vocab elements at row_stride; tokens [rows] i64, may be NULL (then so are logprobs and ranks)
+ *   -> logprobs [rows] f32 = log p of the row's token;
+ *      ranks [rows] i32 = how many tokens come before it in order of falling logit (equal ones: the smaller index first);
+ *      entropy [rows] f32 = -sum p_i log p_i;
+ *      top_tokens [rows][top] i64, top_logprobs [rows][top] f32: the first `top` tokens of that order.
+ * Each result may be NULL.  NaN counts as -inf.  If some logits are +inf, those share the probability.  Tokens outside the vocabulary
+ * (padding) have log-probability -inf and rank -1.  Only tokens above -inf are listed: the rest of top_tokens is -1, of top_logprobs
+ * -inf.  A row without any has entropy 0 and log-probabilities -inf.  Sums are fp32.  Requires vocab < 2^20, top <= 128. */
+int pq_token_logprobs(pq_ctx *ctx, const void *logits, pq_elem elem, int64_t row_stride, int rows, int vocab, const int64_t *tokens, int top,
+                      float *logprobs, int32_t *ranks, float *entropy, int64_t *top_tokens, float *top_logprobs);
 
 #ifdef __cplusplus
 }

@@ -40,7 +40,8 @@ LUT_U8 = 1
 EXPORTS = ["pq_create", "pq_destroy", "pq_last_error", "pq_version", "pq_build_luts", "pq_quantize_luts",
            "pq_qmax_prescan", "pq_adc_scan_topk", "pq_rerank_f32", "ivf_adc_search", "pq_encode", "pq_rotate", "pq_derived_search", "pq_set_profiling",
            "pq_last_scan_kernel_ms", "pq_calibration_copy", "pq_set_option", "pq_unset_option", "pq_last_scan_info", "pq_adc_scan_topk_noalloc",
-           "ivf_quick_adc_search", "pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens"]
+           "ivf_quick_adc_search", "pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens", "pq_kv_append8",
+           "pq_kv_attention8", "pq_token_logprobs"]
 
 _lib = None
 _entries = {}
@@ -89,7 +90,7 @@ def load():
         if name not in ("pq_last_error", "pq_version"):
             getattr(lib, name).restype = ci
     # the reading step is called from the extension module, by the functions' addresses
-    for name in ("pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens"):
+    for name in ("pq_kv_plan", "pq_kv_append", "pq_kv_attention", "pq_sample_tokens", "pq_kv_append8", "pq_kv_attention8", "pq_token_logprobs"):
         _entries[name] = ctypes.cast(getattr(lib, name), vp).value
     _lib = lib
     return lib
@@ -378,6 +379,49 @@ class Context:
             rows = logits.shape[0]
             out = (torch.empty(rows, dtype=torch.int64, device=logits.device), torch.empty(rows, dtype=torch.float32, device=logits.device))
         rc = _views.sample(_entries["pq_sample_tokens"], self._address, logits, noise, temperature, top_k, top_p, min_p, *out)
+        if rc:
+            self._check(rc)
+        return out
+
+    # -- The reading step over a cache of 8 bits: key_cache and value_cache [blocks][block size][heads][dim] are float8_e4m3fn, the scales
+    # [blocks][heads] float32 --------------------------------------------------------------------------------------------------
+    def pq_kv_append8(self, q, k, v, positions, slots, key_cache, value_cache, key_scales, value_scales, cos=None, sin=None,
+                      q_weight=None, k_weight=None, eps=1e-6, norm=True, pairs=False, out=None):
+        """pq_kv_append into a cache of 8 bits; the blocks' scales are set, or grow, as their tokens need it.  The slots of a block's tokens
+        follow each other by one.  Returns the queries, of k's type (None if q is None)."""
+        if q is not None and out is None:
+            out = torch.empty(q.shape, dtype=k.dtype, device=q.device)
+        rc = _views.append8(_entries["pq_kv_append8"], self._address, q, k, v, positions, slots, key_cache, value_cache, key_scales,
+                            value_scales, cos, sin, q_weight, k_weight, eps, norm, pairs, out)
+        if rc:
+            self._check(rc)
+        return out if q is not None else None
+
+    def pq_kv_attention8(self, q, key_cache, value_cache, key_scales, value_scales, block_tables, cu_new, kv_lens, max_new, scale=None,
+                         window=0, out=None, lse=None):
+        """pq_kv_attention over a cache of 8 bits.  Returns (out, lse), out of q's type."""
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        rc = _views.attention8(_entries["pq_kv_attention8"], self._address, q, key_cache, value_cache, key_scales, value_scales, block_tables,
+                               cu_new, kv_lens, max_new, scale, window, out, lse)
+        if rc:
+            self._check(rc)
+        return out, lse
+
+    def pq_token_logprobs(self, logits, tokens=None, top=0, out=None):
+        """Log-probability and rank of a token for each row of logits [rows][vocab], the row's entropy, and its `top` likeliest tokens with
+        their log-probabilities.  Returns (logprobs, ranks, entropy, top_tokens, top_logprobs), the first two None without tokens; `out` if
+        it is given (None in it: a result that is not wanted)."""
+        if out is None:
+            rows, f32 = logits.shape[0], torch.float32
+            shape = (rows, max(top, 0))
+            out = tuple(torch.empty(n, dtype=dt, device=logits.device)
+                        for n, dt in ((rows, f32), (rows, torch.int32), (rows, f32), (shape, torch.int64), (shape, f32)))
+            if tokens is None:
+                out = (None, None) + out[2:]
+        rc = _views.logprobs(_entries["pq_token_logprobs"], self._address, logits, tokens, top, *out)
         if rc:
             self._check(rc)
         return out

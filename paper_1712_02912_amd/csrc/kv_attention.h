@@ -2,6 +2,7 @@
 #pragma once
 #include <limits.h>
 
+#include "e4m3.h"
 #include "elem.h"
 #include "pq_internal.h"
 #include "wave_sums.h"
@@ -9,7 +10,8 @@
 namespace pq {
 
 struct attention_args {
-    pq_kv_cache cache;
+    pq_kv_cache cache;   // (elem: the queries'; a cache of 8 bits has the same layout in its own elements, and scales)
+    const float *k_scales, *v_scales;   // [blocks][heads], of a cache of 8 bits
     pq_heads q;
     const int32_t *cu, *kv_lens, *tables;
     void *out;

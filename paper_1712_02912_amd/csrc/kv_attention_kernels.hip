@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache (pq_kv_attention).
+// Attention of new tokens over a paged cache (pq_kv_attention, pq_kv_attention8).
 #include "kv_attention.h"
 
 namespace pq {
@@ -14,7 +14,14 @@ namespace pq {
 constexpr int GENERAL_WAVES = 4;
 constexpr int GENERAL_DIM = 512;
 
-template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_attention_general_kernel(attention_args a) {
+// The scale of a head's keys or values in a block, one for elements without (e4m3.h: of a scale the exponent counts).
+template <class C> __device__ __forceinline__ float block_scale(const float *scales, int64_t block, int heads, int head) {
+    if constexpr (__is_same(C, e4m3)) return scale_of(scale_exponent(scales[block * heads + head]));
+    else return 1.f;
+}
+
+// T: elements of the queries and the result, C: of the cache
+template <class T, class C> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_attention_general_kernel(attention_args a) {
     __shared__ float q[GENERAL_DIM], acc[GENERAL_WAVES][GENERAL_DIM], stat[GENERAL_WAVES][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, dim = a.cache.dim;
     const int64_t t = blockIdx.x / a.q_heads;
@@ -30,15 +37,16 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
     float top = -INFINITY, sum = 0.f, part[GENERAL_DIM / 64] = {};
     for (int base = from + wave * 64; base <= at; base += 64 * GENERAL_WAVES) {
         const int j = base + lane;
-        float s = -INFINITY;
+        float s = -INFINITY, v_scale = 1.f;
         int64_t block = 0;
         int place = 0;
         if (j <= at) {
             attention_place(a, r, j, block, place);
-            const T *k = (const T *)a.cache.keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1] + kvh * a.cache.key_strides[2];
+            const C *k = (const C *)a.cache.keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1] + kvh * a.cache.key_strides[2];
             s = 0.f;
             for (int i = 0; i < dim; ++i) s += q[i] * (float)k[i];
-            s *= a.scale_log2;
+            s = s * block_scale<C>(a.k_scales, block, a.cache.heads, kvh) * a.scale_log2;
+            v_scale = block_scale<C>(a.v_scales, block, a.cache.heads, kvh);
         }
         float high = s;
         for (int d = 32; d > 0; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
@@ -52,8 +60,8 @@ template <class T> __global__ __launch_bounds__(64 * GENERAL_WAVES) void kv_atte
         for (int e = 0; e < GENERAL_DIM / 64; ++e) part[e] *= shrink;
         const int count = min(64, at - base + 1);
         for (int l = 0; l < count; ++l) {
-            const float wl = __shfl(w, l);
-            const T *v = (const T *)a.cache.values + __shfl((long long)row, l) + kvh * a.cache.value_strides[2];
+            const float wl = __shfl(w * v_scale, l);
+            const C *v = (const C *)a.cache.values + __shfl((long long)row, l) + kvh * a.cache.value_strides[2];
 #pragma unroll
             for (int e = 0; e < GENERAL_DIM / 64; ++e)
                 if (e * 64 + lane < dim) part[e] += wl * (float)v[e * 64 + lane];
@@ -97,11 +105,19 @@ static bool attention_on_matrix_cores(const attention_args &a) {
     return bits % 16 == 0;
 }
 
-int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
-                        const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width,
-                        int max_new, float scale, int window, void *out, float *lse) {
+template <class T, class C> static int attention_general(pq_ctx *ctx, const attention_args &a) {
+    const int64_t grid = a.ntokens * a.q_heads;
+    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
+    kv_attention_general_kernel<T, C><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
+}
+
+static attention_args attention_of(const pq_kv_cache &cache, const pq_heads *q, int q_heads, int64_t ntokens, const int32_t *cu_new,
+                                   const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width, int max_new, float scale, int window,
+                                   void *out, float *lse) {
     attention_args a = {};
-    a.cache = *cache;
+    a.cache = cache;
     a.q = *q;
     a.cu = cu_new;
     a.kv_lens = kv_lens;
@@ -114,10 +130,17 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
     a.width = width;
     a.window = window;
     a.max_new = max_new;
-    a.group = q_heads / cache->heads;
-    a.by_block = fast_div((uint32_t)cache->block_size);
+    a.group = q_heads / cache.heads;
+    a.by_block = fast_div((uint32_t)cache.block_size);
     a.by_group = fast_div((uint32_t)a.group);
     a.scale_log2 = scale * 1.4426950408889634f;
+    return a;
+}
+
+int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
+                        const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width,
+                        int max_new, float scale, int window, void *out, float *lse) {
+    attention_args a = attention_of(*cache, q, q_heads, ntokens, cu_new, kv_lens, nreq, block_tables, width, max_new, scale, window, out, lse);
     if (attention_on_matrix_cores(a)) {
         for (int i = 0; i < 2; ++i) {
             a.k_strides[i] = (uint32_t)cache->key_strides[i];
@@ -135,13 +158,27 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
         const bool is_long = held >= 4096 && (window == 0 || window >= 4096);
         return launch_kv_attention_chunk(ctx, a, is_long && a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new);
     }
-    const int64_t grid = ntokens * q_heads;
-    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
-    if (cache->elem == PQ_ELEM_F32) kv_attention_general_kernel<float><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
-    else if (cache->elem == PQ_ELEM_F16) kv_attention_general_kernel<_Float16><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
-    else kv_attention_general_kernel<__bf16><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
-    PQ_HIP(ctx, hipGetLastError());
-    return PQ_OK;
+    switch (cache->elem) {
+    case PQ_ELEM_F32: return attention_general<float, float>(ctx, a);
+    case PQ_ELEM_F16: return attention_general<_Float16, _Float16>(ctx, a);
+    default: return attention_general<__bf16, __bf16>(ctx, a);
+    }
+}
+
+int launch_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, int elem, const pq_heads *q, int q_heads, int64_t ntokens,
+                         const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width, int max_new,
+                         float scale, int window, void *out, float *lse) {
+    const pq_kv_cache layout = {cache->keys, cache->values, {cache->key_strides[0], cache->key_strides[1], cache->key_strides[2]},
+                                {cache->value_strides[0], cache->value_strides[1], cache->value_strides[2]},
+                                cache->nblocks, cache->block_size, cache->heads, cache->dim, (pq_elem)elem};
+    attention_args a = attention_of(layout, q, q_heads, ntokens, cu_new, kv_lens, nreq, block_tables, width, max_new, scale, window, out, lse);
+    a.k_scales = cache->key_scales;
+    a.v_scales = cache->value_scales;
+    switch (elem) {
+    case PQ_ELEM_F32: return attention_general<float, e4m3>(ctx, a);
+    case PQ_ELEM_F16: return attention_general<_Float16, e4m3>(ctx, a);
+    default: return attention_general<__bf16, e4m3>(ctx, a);
+    }
 }
 
 }  // namespace pq

@@ -137,5 +137,14 @@ int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q
 int launch_sample_tokens(pq_ctx *ctx, const void *logits, int elem, int64_t row_stride, int rows, int vocab, const float *noise,
                          int64_t noise_stride, const float *temperature, const int32_t *top_k, const float *top_p,
                          const float *min_p, int64_t *tokens, float *logprobs);
+int launch_kv_append8(pq_ctx *ctx, const pq_kv_cache8 *cache, int elem, const pq_heads *q, int q_heads, const pq_heads *k, const pq_heads *v,
+                      int64_t ntokens, const int32_t *positions, const int64_t *slots, const float *cos_table, const float *sin_table,
+                      int64_t max_positions, int rot, int pairs, int norm, const float *q_weight, const float *k_weight, float eps,
+                      void *q_out);
+int launch_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, int elem, const pq_heads *q, int q_heads, int64_t ntokens,
+                         const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width, int max_new,
+                         float scale, int window, void *out, float *lse);
+int launch_token_logprobs(pq_ctx *ctx, const void *logits, int elem, int64_t row_stride, int rows, int vocab, const int64_t *tokens, int top,
+                          float *logprobs, int32_t *ranks, float *entropy, int64_t *top_tokens, float *top_logprobs);
 
 }  // namespace pq
