@@ -146,8 +146,8 @@ int pq_kv_append8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const pq
                   void *q_out);
 
 /* pq_kv_attention over a cache of 8 bits: keys and values are what its elements stand for; q rows and out are of type elem, the other
- * arguments and all rules as there.  Elements are multiplied as they are (16 bits hold them, for f16 values up to 2^16 and keys up to 2^17
- * from 2^-23 on), so there is no rounding but that of the weights and of the result.
+ * arguments and all rules as there.  No element is rounded before the products (what they stand for fits 16 bits; for f16 if it is below
+ * 2^17 and, on the matrix cores, a multiple of 2^-23, to which others are rounded).
  * dim 64, 96, 128 or 256 with f16 or bf16, rows of the queries, the cache and out on 16 bytes, takes the matrix cores, any other
  * even dim <= 512 and f32 a general kernel. */
 int pq_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const pq_heads *q, int q_heads, int64_t ntokens,

@@ -1,6 +1,7 @@
 // What the attention kernels share (kv_attention_kernels.hip, kv_attention_few.h, kv_attention_chunk.h).
 #pragma once
 #include <limits.h>
+#include <math.h>
 
 #include "e4m3.h"
 #include "elem.h"
@@ -131,6 +132,41 @@ template <int D> struct lds_row {
     }
 };
 
+// ---- what the cache holds ---------------------------------------------------------------------------------
+//
+// The kernels on the matrix cores are built for caches of the queries' type T (C = T) and for e4m3 numbers (C = e4m3), which become
+// elements of T on their way from the cache: two a conversion, times a power of two, and exact, but for f16 at the ends of its range.
+// There a number times its scale may be 2^16, just above f16's largest, so f16 gets half of it, and twice the scale of the
+// scores (from the host) and twice the result.
+template <class T, class C> constexpr bool HALVED = __is_same(C, e4m3) && __is_same(T, _Float16);
+template <class T, class C> constexpr float VALUE_UNIT = HALVED<T, C> ? 2.f : 1.f;
+
+// Eight elements of two words of codes; scale: a power of two (only its exponent counts).
+template <class T> __device__ __forceinline__ u32x4 from_e4m3(uint32_t low, uint32_t high, float scale) {
+    if constexpr (__is_same(T, _Float16)) {
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)low, scale, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)low, scale, true)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)high, scale, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)high, scale, true))};
+    } else {
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)low, scale, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)low, scale, true)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)high, scale, false)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)high, scale, true))};
+    }
+}
+// A head's scale in a block, as the conversion takes it.
+template <class T> __device__ __forceinline__ float e4m3_scale(const attention_args &a, const float *scales, int64_t block, int head) {
+    return scales[block * a.cache.heads + head] * (HALVED<T, e4m3> ? 0.5f : 1.f);
+}
+
+// Adds those of four elements of a row of values that are NaN.
+template <class T, class V> __device__ __forceinline__ void add_not_finite(const e4m3 *v, V &out, int at) {
+    const elem_vec<e4m3, 4> x = *(const elem_vec<e4m3, 4> *)v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[at + e] += (x.v[e].bits & 0x7f) == 0x7f ? NAN : 0.f;
+}
+
 // Requests of so few rows per head of the cache have a kernel of their own.
 constexpr int FEW_ROWS = 16;
 __device__ __forceinline__ bool attention_is_few(const attention_args &a, int held) { return (int64_t)held * a.group <= FEW_ROWS; }
@@ -165,5 +201,8 @@ __device__ __forceinline__ int attention_request(const int32_t *cu, int nreq, in
 int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int most_rows);
 // All requests; some_few: those of few rows by the blocks of their own kind.
 int launch_kv_attention_chunk(pq_ctx *ctx, const attention_args &a, bool some_few);
+// The same over a cache of 8 bits.
+int launch_kv_attention8_few(pq_ctx *ctx, const attention_args &a, int most_rows);
+int launch_kv_attention8_chunk(pq_ctx *ctx, const attention_args &a, bool some_few);
 
 }  // namespace pq

@@ -68,21 +68,43 @@ template <int M> __device__ __forceinline__ chunk_place chunk_locate(const atten
     return {-1, 0, 0};
 }
 
+// What one load moves: eight elements of the queries' type, or 16 codes (eight where a row has fewer than 16 for each of `lanes`), which
+// become elements of the queries' type where they are stored.
+template <class C, int LANES, int D> struct chunk_of {
+    static constexpr int ELEMS = 8;
+    u32x4 x;
+    __device__ __forceinline__ void load(const C *p) { x = *(const u32x4 *)p; }
+    template <class T> __device__ __forceinline__ u32x4 eight(int, float) const { return x; }
+};
+template <int LANES, int D> struct chunk_of<e4m3, LANES, D> {
+    static constexpr int ELEMS = D >= 16 * LANES ? 16 : 8;
+    uint32_t x[ELEMS / 4];
+    __device__ __forceinline__ void load(const e4m3 *p) {
+        const elem_vec<uint32_t, ELEMS / 4> c = *(const elem_vec<uint32_t, ELEMS / 4> *)p;
+#pragma unroll
+        for (int i = 0; i < ELEMS / 4; ++i) x[i] = c.v[i];
+    }
+    template <class T> __device__ __forceinline__ u32x4 eight(int e, float scale) const { return from_e4m3<T>(x[2 * e], x[2 * e + 1], scale); }
+};
+
 // keys of a tile (of 256 dimensions, registers and shared memory hold half as many)
 template <int D> constexpr int CHUNK_TILE = D > 128 ? 32 : 64;
 template <int D> constexpr int CHUNK_POOL = 4 * CHUNK_TILE<D> * lds_row<D>::bytes;
 
 // One block's tile of rows (block: index * heads + head) and part of its keys; pool: CHUNK_POOL bytes of shared memory.
-template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block(const attention_args &a, const chunk_split &split, int block, int part, unsigned char *pool) {
+template <class T, class C, int D, int WAVES> __device__ __forceinline__ void chunk_block(const attention_args &a, const chunk_split &split, int block, int part, unsigned char *pool) {
     constexpr int TILE = CHUNK_TILE<D>;
     typedef lds_row<D> row;
     constexpr int M = 32 * WAVES, THREADS = 64 * WAVES;
-    constexpr int STEPS = D / 16, OUTS = D / 32, CHUNKS = D / 8;
+    constexpr int STEPS = D / 16, OUTS = D / 32;
     // (Alone on its SIMD, a wave waits for every read of shared memory unless it reads ahead: 8 requests of 1024 tokens over 1024 to
     // 8192 keys, 8 heads of 256 dimensions: 599 us, 663 without.  Where there are two waves it is no gain and costs registers.)
     constexpr int AT_ONCE = D > 128 ? 4 : 1;
-    // a thread moves chunks of 16 bytes of one key (and value) of a tile, every LANES-th from its own on
-    constexpr int LANES = THREADS / TILE, MOVES = (CHUNKS + LANES - 1) / LANES;
+    // a thread moves chunks of one key (and value) of a tile, every LANES-th from its own on: 16 bytes each, or 8 where eight-bit rows are
+    // shorter than that for all lanes
+    constexpr int LANES = THREADS / TILE;
+    typedef chunk_of<C, LANES, D> piece;
+    constexpr int CHUNKS = D / piece::ELEMS, MOVES = (CHUNKS + LANES - 1) / LANES;
     unsigned char *const lds_k[2] = {pool, pool + TILE * row::bytes}, *const lds_v[2] = {pool + 2 * TILE * row::bytes, pool + 3 * TILE * row::bytes};
     __shared__ int taken_out;   // values were (see below)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, g = lane >> 5;
@@ -138,10 +160,11 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
 
     // this thread's chunks of a tile
     const int my_key = tid / LANES, my_chunk = tid % LANES;
-    const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2] + 8 * my_chunk;
-    const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2] + 8 * my_chunk;
+    const C *const keys = (const C *)a.cache.keys + h * a.cache.key_strides[2] + piece::ELEMS * my_chunk;
+    const C *const values = (const C *)a.cache.values + h * a.cache.value_strides[2] + piece::ELEMS * my_chunk;
     const int32_t *const table = a.tables + (int64_t)r * a.width;
-    u32x4 mk[MOVES], mv[MOVES];
+    piece mk[MOVES], mv[MOVES];
+    float k_scale = 1.f, v_scale = 1.f;
     // (a tile's entry of the block table is read a tile before its keys are, so that nothing waits for it)
     int32_t entry = 0, place = 0;
     auto look_up = [&](int tile) {
@@ -151,13 +174,17 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
     };
     auto load = [&]() {
         const int64_t block = attention_block(a, entry);
-        const T *const k = keys + attention_key_at(a, block, place);
-        const T *const v = values + attention_value_at(a, block, place);
+        const C *const k = keys + attention_key_at(a, block, place);
+        const C *const v = values + attention_value_at(a, block, place);
+        if constexpr (__is_same(C, e4m3)) {
+            k_scale = e4m3_scale<T>(a, a.k_scales, block, h);
+            v_scale = e4m3_scale<T>(a, a.v_scales, block, h);
+        }
 #pragma unroll
         for (int i = 0; i < MOVES; ++i) {
             if (CHUNKS % LANES != 0 && my_chunk + LANES * i >= CHUNKS) continue;
-            mk[i] = *(const u32x4 *)(k + 8 * LANES * i);
-            mv[i] = *(const u32x4 *)(v + 8 * LANES * i);
+            mk[i].load(k + piece::ELEMS * LANES * i);
+            mv[i].load(v + piece::ELEMS * LANES * i);
         }
     };
     auto store = [&](int tile, int buffer) {
@@ -166,9 +193,12 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
         for (int i = 0; i < MOVES; ++i) {
             const int chunk = my_chunk + LANES * i;
             if (CHUNKS % LANES != 0 && chunk >= CHUNKS) continue;
-            const int at = my_key * row::bytes + 16 * row::chunk(my_key, chunk);
-            *(u32x4 *)(lds_k[buffer] + at) = mk[i];
-            *(u32x4 *)(lds_v[buffer] + at) = mv[i];
+#pragma unroll
+            for (int e = 0; e < piece::ELEMS / 8; ++e) {
+                const int at = my_key * row::bytes + 16 * row::chunk(my_key, chunk * (piece::ELEMS / 8) + e);
+                *(u32x4 *)(lds_k[buffer] + at) = mk[i].template eight<T>(e, k_scale);
+                *(u32x4 *)(lds_v[buffer] + at) = mv[i].template eight<T>(e, v_scale);
+            }
         }
         // Values that some row does not see must not reach it as 0 times inf: where a tile has rows that do not see all of it,
         // what is not finite is taken out, and added in the end to the rows that see it.  Places behind the last key become zeros.
@@ -177,9 +207,14 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
 #pragma unroll
             for (int i = 0; i < MOVES; ++i) {
                 const int chunk = my_chunk + LANES * i;
-                if ((CHUNKS % LANES != 0 && chunk >= CHUNKS) || (held && !any_not_finite<T>(mv[i]))) continue;
-                *(u32x4 *)(lds_v[buffer] + my_key * row::bytes + 16 * row::chunk(my_key, chunk)) = held ? finite_only<T>(mv[i]) : u32x4{0, 0, 0, 0};
-                if (held) taken_out = 1;
+                if (CHUNKS % LANES != 0 && chunk >= CHUNKS) continue;
+#pragma unroll
+                for (int e = 0; e < piece::ELEMS / 8; ++e) {
+                    const u32x4 x = mv[i].template eight<T>(e, v_scale);
+                    if (held && !any_not_finite<T>(x)) continue;
+                    *(u32x4 *)(lds_v[buffer] + my_key * row::bytes + 16 * row::chunk(my_key, chunk * (piece::ELEMS / 8) + e)) = held ? finite_only<T>(x) : u32x4{0, 0, 0, 0};
+                    if (held) taken_out = 1;
+                }
             }
         }
     };
@@ -315,11 +350,11 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
                 int64_t block;
                 int at;
                 attention_place(a, r, key, block, at);
-                const T *const v = (const T *)a.cache.values + h * a.cache.value_strides[2] + attention_value_at(a, block, at);
+                const C *const v = (const C *)a.cache.values + h * a.cache.value_strides[2] + attention_value_at(a, block, at);
 #pragma unroll
                 for (int f = 0; f < OUTS; ++f)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) add_not_finite(v + 32 * f + 8 * i + 4 * g, out[f], 4 * i);
+                    for (int i = 0; i < 4; ++i) add_not_finite<T>(v + 32 * f + 8 * i + 4 * g, out[f], 4 * i);
             }
         }
     }
@@ -340,7 +375,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
         }
         return;
     }
-    const float scale = sum != 0.f ? 1.f / sum : 0.f;
+    const float scale = sum != 0.f ? VALUE_UNIT<T, C> / sum : 0.f;
     T *const to_row = (T *)a.out + at_row * D;
 #pragma unroll
     for (int f = 0; f < OUTS; ++f)
@@ -356,7 +391,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void chunk_block
 
 // Joins the parts of rows, a wave for each row, in the order of the keys.
 constexpr int JOIN_ROWS = 4;
-template <class T, int D> __device__ __forceinline__ void chunk_join_block(const attention_args &a, const chunk_split &split, int block) {
+template <class T, class C, int D> __device__ __forceinline__ void chunk_join_block(const attention_args &a, const chunk_split &split, int block) {
     constexpr int E = (D + 63) / 64;
     const int64_t row = (int64_t)block * JOIN_ROWS + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -379,7 +414,7 @@ template <class T, int D> __device__ __forceinline__ void chunk_join_block(const
     T *const out = (T *)a.out + row * D;
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        if (D % 64 == 0 || e * 64 + lane < D) out[e * 64 + lane] = (T)(all != 0.f ? o[e] / all : 0.f);
+        if (D % 64 == 0 || e * 64 + lane < D) out[e * 64 + lane] = (T)(all != 0.f ? o[e] * VALUE_UNIT<T, C> / all : 0.f);
     if (lane == 0 && a.lse) a.lse[row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
 }
 

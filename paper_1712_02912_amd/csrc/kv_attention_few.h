@@ -90,15 +90,49 @@ struct few_cut {
     }
 };
 
-// where keys and values of a lane's two places of a tile are, in elements
+// where keys and values of a lane's two places of a tile are, in elements (and their blocks, of which a cache of 8 bits has the scales)
 struct few_places {
     int64_t k[2], v[2];
+    int64_t block[2];
+};
+
+// A lane's share of a row in registers: of the queries' type D / 4 elements, eight at 8 g + 32 t for each product t; of 8 bits
+// sixteen at 16 g + 64 u for two products, so that they come 16 bytes at a time, too, and eight at 8 g behind the last whole 64 (the
+// order of the dimensions within the products is free, and the queries' is the same).
+template <class C, int D> struct few_row {
+    static constexpr int STEPS = D / 32;
+    u32x4 x[STEPS];
+    static __device__ __forceinline__ int dim(int t, int g) { return 32 * t + 8 * g; }
+    __device__ __forceinline__ void load(const C *row, int g) {
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) x[t] = *(const u32x4 *)(row + dim(t, g));
+    }
+    template <class T> __device__ __forceinline__ u32x4 step(int t, float) const { return x[t]; }
+};
+template <int D> struct few_row<e4m3, D> {
+    static constexpr int STEPS = D / 32;
+    uint32_t x[2 * STEPS];
+    static __device__ __forceinline__ int dim(int t, int g) { return t < STEPS / 2 * 2 ? 64 * (t / 2) + 16 * g + 8 * (t % 2) : 32 * t + 8 * g; }
+    __device__ __forceinline__ void load(const e4m3 *row, int g) {
+#pragma unroll
+        for (int u = 0; u < STEPS / 2; ++u) {
+            const u32x4 c = *(const u32x4 *)(row + 64 * u + 16 * g);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * u + i] = c[i];
+        }
+        if constexpr (STEPS % 2 != 0) {
+            const uint2 c = *(const uint2 *)(row + dim(STEPS - 1, g));
+            x[2 * STEPS - 2] = c.x;
+            x[2 * STEPS - 1] = c.y;
+        }
+    }
+    template <class T> __device__ __forceinline__ u32x4 step(int t, float scale) const { return from_e4m3<T>(x[2 * t], x[2 * t + 1], scale); }
 };
 
 template <int D, int WAVES> constexpr int FEW_POOL = WAVES * FEW_TILE * lds_row<D>::bytes;
 
 // The block's stretch of the line; pool: FEW_POOL bytes of shared memory.
-template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(const attention_args &a, const few_line &line, int block, unsigned char *pool) {
+template <class T, class C, int D, int WAVES> __device__ __forceinline__ void few_block(const attention_args &a, const few_line &line, int block, unsigned char *pool) {
     typedef lds_row<D> row;
     constexpr int THREADS = 64 * WAVES, UNIT = WAVES * FEW_TILE;
     constexpr int STEPS = D / 32;   // products over the dimensions
@@ -147,9 +181,9 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
         const int64_t qrow = a.cu[r] + (n < rows ? token : 0);
         u32x4 q[STEPS];
         {
-            const T *p = (const T *)a.q.p + qrow * a.q.token_stride + (h * a.group + (n < rows ? sub : 0)) * a.q.head_stride + 8 * g;
+            const T *p = (const T *)a.q.p + qrow * a.q.token_stride + (h * a.group + (n < rows ? sub : 0)) * a.q.head_stride;
 #pragma unroll
-            for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + 32 * t);
+            for (int t = 0; t < STEPS; ++t) q[t] = *(const u32x4 *)(p + few_row<C, D>::dim(t, g));
         }
         f32x4 out[OUTS];
 #pragma unroll
@@ -159,8 +193,8 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
 
         const int tile0 = x.from + (int)first * UNIT + wave * FEW_TILE;   // this wave's first key; the next ones follow by units
         const int tiles = x.keys > tile0 ? (int)min(count, (int64_t)(x.keys - tile0 + UNIT - 1) / UNIT) : 0;
-        const T *const keys = (const T *)a.cache.keys + h * a.cache.key_strides[2] + 8 * g;
-        const T *const values = (const T *)a.cache.values + h * a.cache.value_strides[2] + 8 * g;
+        const C *const keys = (const C *)a.cache.keys + h * a.cache.key_strides[2];
+        const C *const values = (const C *)a.cache.values + h * a.cache.value_strides[2];
         auto places = [&](int i) {
             few_places p;
 #pragma unroll
@@ -170,21 +204,25 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
                 attention_place(a, r, min(tile0 + i * UNIT + 16 * s + n, x.keys - 1), page, place);
                 p.k[s] = (int64_t)attention_key_at(a, page, place);
                 p.v[s] = (int64_t)attention_value_at(a, page, place);
+                p.block[s] = page;
             }
             return p;
         };
-        u32x4 k[2][STEPS], v[2][STEPS];
+        few_row<C, D> k[2], v[2];
+        float k_scale[2] = {1.f, 1.f}, v_scale[2] = {1.f, 1.f};
         auto load_k = [&](const few_places &p) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int t = 0; t < STEPS; ++t) k[s][t] = *(const u32x4 *)(keys + p.k[s] + 32 * t);
+            for (int s = 0; s < 2; ++s) {
+                k[s].load(keys + p.k[s], g);
+                if constexpr (__is_same(C, e4m3)) k_scale[s] = e4m3_scale<T>(a, a.k_scales, p.block[s], h);
+            }
         };
         auto load_v = [&](const few_places &p) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int t = 0; t < STEPS; ++t) v[s][t] = *(const u32x4 *)(values + p.v[s] + 32 * t);
+            for (int s = 0; s < 2; ++s) {
+                v[s].load(values + p.v[s], g);
+                if constexpr (__is_same(C, e4m3)) v_scale[s] = e4m3_scale<T>(a, a.v_scales, p.block[s], h);
+            }
         };
         few_places next;
         if (tiles > 0) {
@@ -200,7 +238,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
             for (int j = 0; j < 2; ++j) {
                 s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int t = 0; t < STEPS; ++t) s[j] = mfma_of<T>::m16(k[j][t], q[t], s[j]);
+                for (int t = 0; t < STEPS; ++t) s[j] = mfma_of<T>::m16(k[j].template step<T>(t, k_scale[j]), q[t], s[j]);
             }
             if (i + 1 < tiles) load_k(next);
             // a lane's scores: keys 16 j + 4 g + e of the tile for row n
@@ -238,7 +276,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int t = 0; t < STEPS; ++t)
-                    *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = v[j][t];
+                    *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, few_row<C, D>::dim(t, g) / 8)) = v[j].template step<T>(t, v_scale[j]);
             // zeros for places that hold no key; what is not finite and not seen by all rows is taken out, see kv_attention_chunk.h
             if (!all_seen) {
                 bool found = false;
@@ -247,9 +285,10 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
                     const bool held = tile + 16 * j + n < x.keys;
 #pragma unroll
                     for (int t = 0; t < STEPS; ++t) {
-                        if (held && !any_not_finite<T>(v[j][t])) continue;
+                        const u32x4 x = v[j].template step<T>(t, v_scale[j]);
+                        if (held && !any_not_finite<T>(x)) continue;
                         found |= held;
-                        *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, 4 * t + g)) = held ? finite_only<T>(v[j][t]) : u32x4{0, 0, 0, 0};
+                        *(u32x4 *)(mine + (16 * j + n) * row::bytes + 16 * row::chunk(16 * j + n, few_row<C, D>::dim(t, g) / 8)) = held ? finite_only<T>(x) : u32x4{0, 0, 0, 0};
                     }
                 }
                 taken_out |= __any(found);
@@ -282,9 +321,9 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
                     int64_t page;
                     int place;
                     attention_place(a, r, key, page, place);
-                    const T *const row_v = values - 8 * g + attention_value_at(a, page, place);
+                    const C *const row_v = values + attention_value_at(a, page, place);
 #pragma unroll
-                    for (int f = 0; f < OUTS; ++f) add_not_finite(row_v + 16 * f + 4 * g, out[f], 0);
+                    for (int f = 0; f < OUTS; ++f) add_not_finite<T>(row_v + 16 * f + 4 * g, out[f], 0);
                 }
             }
         }
@@ -311,7 +350,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
             if (whole) {
                 const int tok = (int)a.by_group.div((uint32_t)m);
                 const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (m - tok * a.group);
-                ((T *)a.out)[at_row * D + d] = (T)(all != 0.f ? o / all : 0.f);
+                ((T *)a.out)[at_row * D + d] = (T)(all != 0.f ? o * VALUE_UNIT<T, C> / all : 0.f);
                 if (d == 0 && a.lse) a.lse[at_row] = all != 0.f ? (top + log2f(all)) * LN2 : -INFINITY;
             } else {
                 const int64_t at_row = ((int64_t)block * 2 + part) * FEW_ROWS + m;
@@ -328,7 +367,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_block(c
 
 // Joins the parts of rows of one (request, head), WAVES / row_waves of them: a row's waves sum up every so many-th part, and
 // their sums are added in the same order always.
-template <class T, int D, int WAVES> __device__ __forceinline__ void few_join_block(const attention_args &a, const few_line &line, int block, int slice) {
+template <class T, class C, int D, int WAVES> __device__ __forceinline__ void few_join_block(const attention_args &a, const few_line &line, int block, int slice) {
     __shared__ float sums[WAVES][D], alls[WAVES], tops[WAVES];
     constexpr int E = (D + 63) / 64;
     const int heads = a.cache.heads, r = block / heads, h = block - r * heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -375,7 +414,7 @@ template <class T, int D, int WAVES> __device__ __forceinline__ void few_join_bl
         }
         const int tok = (int)a.by_group.div((uint32_t)row);
         const int64_t at_row = (int64_t)(a.cu[r] + tok) * a.q_heads + h * a.group + (row - tok * a.group);
-        ((T *)a.out)[at_row * D + d] = (T)(total != 0.f ? sum / total : 0.f);
+        ((T *)a.out)[at_row * D + d] = (T)(total != 0.f ? sum * VALUE_UNIT<T, C> / total : 0.f);
         if (d == 0 && a.lse) a.lse[at_row] = total != 0.f ? (tops[at * row_waves] + log2f(total)) * LN2 : -INFINITY;
     }
 }

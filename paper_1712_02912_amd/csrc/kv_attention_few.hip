@@ -5,12 +5,12 @@
 
 namespace pq {
 
-template <class T, int D> __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void kv_attention_few_kernel(attention_args a, few_line line) {
+template <class T, class C, int D> __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void kv_attention_few_kernel(attention_args a, few_line line) {
     __shared__ __attribute__((aligned(16))) unsigned char pool[FEW_POOL<D, 4>];
-    few_block<T, D, 4>(a, line, blockIdx.x, pool);
+    few_block<T, C, D, 4>(a, line, blockIdx.x, pool);
 }
-template <class T, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) void kv_attention_few_join_kernel(attention_args a, few_line line) {
-    few_join_block<T, D, WAVES>(a, line, blockIdx.x, blockIdx.y);
+template <class T, class C, int D, int WAVES> __global__ __launch_bounds__(64 * WAVES) void kv_attention_few_join_kernel(attention_args a, few_line line) {
+    few_join_block<T, C, D, WAVES>(a, line, blockIdx.x, blockIdx.y);
 }
 __global__ __launch_bounds__(1024) void kv_attention_starts_kernel(attention_args a, int unit, int64_t *starts) { few_starts<1024>(a, unit, starts); }
 
@@ -50,33 +50,36 @@ int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, fe
     return PQ_OK;
 }
 
-template <class T, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int most_rows) {
+template <class T, class C, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int most_rows) {
     few_line line;
     size_t ws_used;
     if (const int rc = few_prepare(ctx, a, 4, 0, &line, &ws_used)) return rc;
-    kv_attention_few_kernel<T, D><<<line.blocks, 256, 0, ctx->stream>>>(a, line);
+    kv_attention_few_kernel<T, C, D><<<line.blocks, 256, 0, ctx->stream>>>(a, line);
     if (line.each) {
         PQ_HIP(ctx, hipGetLastError());
         return PQ_OK;
     }
     const int items = a.nreq * a.cache.heads;
-    if (line.row_waves > 4) kv_attention_few_join_kernel<T, D, 16><<<dim3(items, few_slices(line, most_rows, 16)), 1024, 0, ctx->stream>>>(a, line);
-    else kv_attention_few_join_kernel<T, D, 4><<<dim3(items, few_slices(line, most_rows, 4)), 256, 0, ctx->stream>>>(a, line);
+    if (line.row_waves > 4) kv_attention_few_join_kernel<T, C, D, 16><<<dim3(items, few_slices(line, most_rows, 16)), 1024, 0, ctx->stream>>>(a, line);
+    else kv_attention_few_join_kernel<T, C, D, 4><<<dim3(items, few_slices(line, most_rows, 4)), 256, 0, ctx->stream>>>(a, line);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
 
-template <class T> static int few_dim(pq_ctx *ctx, const attention_args &a, int most_rows) {
+template <class T, class C> static int few_dim(pq_ctx *ctx, const attention_args &a, int most_rows) {
     switch (a.cache.dim) {
-    case 64: return few_typed<T, 64>(ctx, a, most_rows);
-    case 96: return few_typed<T, 96>(ctx, a, most_rows);
-    case 128: return few_typed<T, 128>(ctx, a, most_rows);
-    default: return few_typed<T, 256>(ctx, a, most_rows);
+    case 64: return few_typed<T, C, 64>(ctx, a, most_rows);
+    case 96: return few_typed<T, C, 96>(ctx, a, most_rows);
+    case 128: return few_typed<T, C, 128>(ctx, a, most_rows);
+    default: return few_typed<T, C, 256>(ctx, a, most_rows);
     }
 }
 
 int launch_kv_attention_few(pq_ctx *ctx, const attention_args &a, int most_rows) {
-    return a.cache.elem == PQ_ELEM_F16 ? few_dim<_Float16>(ctx, a, most_rows) : few_dim<__bf16>(ctx, a, most_rows);
+    return a.cache.elem == PQ_ELEM_F16 ? few_dim<_Float16, _Float16>(ctx, a, most_rows) : few_dim<__bf16, __bf16>(ctx, a, most_rows);
+}
+int launch_kv_attention8_few(pq_ctx *ctx, const attention_args &a, int most_rows) {
+    return a.cache.elem == PQ_ELEM_F16 ? few_dim<_Float16, e4m3>(ctx, a, most_rows) : few_dim<__bf16, e4m3>(ctx, a, most_rows);
 }
 
 }  // namespace pq

@@ -92,12 +92,12 @@ template <class T, class C> __global__ __launch_bounds__(64 * GENERAL_WAVES) voi
     if (tid == 0 && a.lse) a.lse[t * a.q_heads + h] = total != 0.f ? (ref + log2f(total)) * LN2 : -INFINITY;
 }
 
-// rows of 16-bit elements that 16-byte accesses fit, in the dimensions that are built
-static bool attention_on_matrix_cores(const attention_args &a) {
+// rows that 16-byte accesses fit, in the dimensions that are built; e: bytes of an element of the cache
+static bool attention_on_matrix_cores(const attention_args &a, size_t e) {
     const pq_kv_cache &c = a.cache;
     if (c.elem == PQ_ELEM_F32 || (c.dim != 64 && c.dim != 96 && c.dim != 128 && c.dim != 256)) return false;
     uint64_t bits = (uint64_t)(uintptr_t)c.keys | (uint64_t)(uintptr_t)c.values | (uint64_t)(uintptr_t)a.q.p | (uint64_t)(uintptr_t)a.out;
-    for (int i = 0; i < 3; ++i) bits |= (uint64_t)(c.key_strides[i] | c.value_strides[i]) * 2;
+    for (int i = 0; i < 3; ++i) bits |= (uint64_t)(c.key_strides[i] | c.value_strides[i]) * e;
     // (strides of blocks and places are multiplied in 32 bits)
     for (int i = 0; i < 2; ++i)
         if (c.key_strides[i] > INT_MAX || c.value_strides[i] > INT_MAX) return false;
@@ -137,27 +137,30 @@ static attention_args attention_of(const pq_kv_cache &cache, const pq_heads *q, 
     return a;
 }
 
+// On the matrix cores, by the kernels of few rows or of chunks for the cache's elements.
+static int attention_fast(pq_ctx *ctx, attention_args &a, int (*few)(pq_ctx *, const attention_args &, int), int (*chunk)(pq_ctx *, const attention_args &, bool)) {
+    for (int i = 0; i < 2; ++i) {
+        a.k_strides[i] = (uint32_t)a.cache.key_strides[i];
+        a.v_strides[i] = (uint32_t)a.cache.value_strides[i];
+    }
+    // Requests of few rows and others in one call: over long contexts each kind has blocks of its own, as keys and values are
+    // read faster by those of few rows; over short ones what counts is one launch of one kind (64 requests of 1 to 50 tokens,
+    // 4 heads on each of 8, up to 8000 keys: 237 us, all as chunks 252 us; 23 requests of 1 to 100 tokens, 16 heads, up to 700
+    // keys: 24 and 19 us).  Where all requests have max_new tokens there is one kind only.
+    const int64_t most_rows = (int64_t)a.max_new * a.group, held = (int64_t)a.width * a.cache.block_size;
+    // (64 single tokens over up to 8192 keys, 4 heads on each of 8: 164 us, as chunks 233.  One token over 131 038 keys is the call
+    // that chunks serve faster, 109 us for 115: how many of a call's requests are as long is known on the GPU only, and a wrong
+    // guess costs more than that.)
+    if (most_rows <= FEW_ROWS) return few(ctx, a, (int)most_rows);
+    const bool is_long = held >= 4096 && (a.window == 0 || a.window >= 4096);
+    return chunk(ctx, a, is_long && a.group <= FEW_ROWS && a.ntokens < (int64_t)a.nreq * a.max_new);
+}
+
 int launch_kv_attention(pq_ctx *ctx, const pq_kv_cache *cache, const pq_heads *q, int q_heads, int64_t ntokens,
                         const int32_t *cu_new, const int32_t *kv_lens, int nreq, const int32_t *block_tables, int width,
                         int max_new, float scale, int window, void *out, float *lse) {
     attention_args a = attention_of(*cache, q, q_heads, ntokens, cu_new, kv_lens, nreq, block_tables, width, max_new, scale, window, out, lse);
-    if (attention_on_matrix_cores(a)) {
-        for (int i = 0; i < 2; ++i) {
-            a.k_strides[i] = (uint32_t)cache->key_strides[i];
-            a.v_strides[i] = (uint32_t)cache->value_strides[i];
-        }
-        // Requests of few rows and others in one call: over long contexts each kind has blocks of its own, as keys and values are
-        // read faster by those of few rows; over short ones what counts is one launch of one kind (64 requests of 1 to 50 tokens,
-        // 4 heads on each of 8, up to 8000 keys: 237 us, all as chunks 252 us; 23 requests of 1 to 100 tokens, 16 heads, up to 700
-        // keys: 24 and 19 us).  Where all requests have max_new tokens there is one kind only.
-        const int64_t most_rows = (int64_t)max_new * a.group, held = (int64_t)width * cache->block_size;
-        // (64 single tokens over up to 8192 keys, 4 heads on each of 8: 164 us, as chunks 233.  One token over 131 038 keys is the call
-        // that chunks serve faster, 109 us for 115: how many of a call's requests are as long is known on the GPU only, and a wrong
-        // guess costs more than that.)
-        if (most_rows <= FEW_ROWS) return launch_kv_attention_few(ctx, a, (int)most_rows);
-        const bool is_long = held >= 4096 && (window == 0 || window >= 4096);
-        return launch_kv_attention_chunk(ctx, a, is_long && a.group <= FEW_ROWS && ntokens < (int64_t)nreq * max_new);
-    }
+    if (attention_on_matrix_cores(a, elem_bytes(cache->elem))) return attention_fast(ctx, a, launch_kv_attention_few, launch_kv_attention_chunk);
     switch (cache->elem) {
     case PQ_ELEM_F32: return attention_general<float, float>(ctx, a);
     case PQ_ELEM_F16: return attention_general<_Float16, _Float16>(ctx, a);
@@ -174,6 +177,10 @@ int launch_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, int elem, const
     attention_args a = attention_of(layout, q, q_heads, ntokens, cu_new, kv_lens, nreq, block_tables, width, max_new, scale, window, out, lse);
     a.k_scales = cache->key_scales;
     a.v_scales = cache->value_scales;
+    if (attention_on_matrix_cores(a, 1)) {
+        if (elem == PQ_ELEM_F16) a.scale_log2 *= 2.f;   // (of keys that are half themselves, see HALVED)
+        return attention_fast(ctx, a, launch_kv_attention8_few, launch_kv_attention8_chunk);
+    }
     switch (elem) {
     case PQ_ELEM_F32: return attention_general<float, e4m3>(ctx, a);
     case PQ_ELEM_F16: return attention_general<_Float16, e4m3>(ctx, a);
