@@ -1,10 +1,9 @@
 // Log-probabilities of given tokens, their ranks, the entropy and the likeliest tokens (pq_token_logprobs).
 #include "elem.h"
 #include "pq_internal.h"
+#include "wave_sums.h"
 
 namespace pq {
-
-constexpr int LOGPROB_THREADS = 256;
 
 struct logprob_args {
     const void *logits;
@@ -29,77 +28,308 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
     return __builtin_bit_cast(float, b >> 31 ? b & 0x7fffffffu : ~b);
 }
 
-template <class V, class F> __device__ __forceinline__ V block_join(V v, F f) {
-    __shared__ V parts[LOGPROB_THREADS / 64];
-    for (int d = 32; d > 0; d /= 2) v = f(v, (V)__shfl_xor(v, d));
+// the next number above (of +inf: NaN, which nothing reaches)
+__device__ __forceinline__ float next_above(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    return __builtin_bit_cast(float, v == 0.f ? 1u : b >> 31 ? b - 1 : b + 1);
+}
+
+struct op_max {
+    template <class V> static __device__ __forceinline__ V none() {
+        if constexpr (__is_same(V, float)) return -INFINITY;
+        else return V(0);
+    }
+    template <class V> static __device__ __forceinline__ V of(V a, V b) { return a > b ? a : b; }
+};
+template <class OP, class V> __device__ __forceinline__ V wave_total(V v) { return read_lane(wave_scan<OP>(v), 63); }
+// over a block, for the rare paths
+template <int THREADS, class OP, class V> __device__ __forceinline__ V block_total(V v) {
+    __shared__ V parts[THREADS / 64];
+    v = wave_total<OP>(v);
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
     __syncthreads();
     v = parts[0];
-    for (int w = 1; w < LOGPROB_THREADS / 64; ++w) v = f(v, parts[w]);
+    for (int w = 1; w < THREADS / 64; ++w) v = OP::template of<V>(v, parts[w]);
     __syncthreads();
     return v;
 }
 
-// One block for each row, which reads it for the maximum, for the sums, and for every token that is listed.
-template <class T> __global__ __launch_bounds__(LOGPROB_THREADS) void token_logprobs_kernel(logprob_args a) {
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// The sums are formed of logits from -WILD on (what is less, -inf and NaN count as -WILD), and hold for rows whose largest is between
+// -WILD / 2 and WILD / 2: there what was raised has weight 0, 0 times it is 0, and a reference that is a logit times log2(e), rounded, is
+// off by less than one.  Other rows are summed once more, by differences.  (A power of two: -WILD times log2(e) is not rounded.)
+constexpr float WILD = 0x1p20f;
+
+constexpr int STRETCHES = 16;  // parts of its logits that a thread keeps the maximum of
+constexpr int GROUPS = 256;    // groups of threads whose maxima give the limit
+constexpr int CANDIDATES = 1024, LISTED = 512;   // logits that are sorted, stretches that are read again
+
+// One block for each row, which is read once.  A thread sums weights 2^y and y 2^y, y = logit * log2(e) - reference, by batches, and the
+// reference is the largest logit of the batches so far.  The entropy is log2(sum) - (sum of y 2^y) / sum, of terms of one sign.
+//
+// The likeliest tokens cost the pass one store of a maximum for each batch.  `top` groups of threads have a maximum of at
+// least the limit, the (top)th largest of the groups' maxima, so no smaller logit is listed, and nearly all that are as large are: for 20
+// of 256 groups 20.8 are expected.  The few stretches that reach the limit are read again, their logits of at least the limit are
+// sorted by counting.  Rows of too many (equal ones, or the largest all with one thread) are searched `top` times.
+//
+// Bound by memory where rows are many: 4096 rows of 131 072, bf16, 20 listed: 1.07 GB in 195 to 199 us = 5.4 TB/s; 1024 of these in f32
+// without a list: 537 MB in 93 us = 5.8 TB/s.  A logit takes a conversion, a bound, half a maximum, two multiply-adds, an addition and a
+// power of two (at a quarter of the rate), about 60 % of the cycles in bf16.  Few rows are bound by latency: the token's logit, the row,
+// two meetings (1.4 us), the stretches that are read again (2.7 us with the sort for 1 token, 4 us for 20).
+template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS) void token_logprobs_kernel(logprob_args a) {
+    constexpr int E = 16 / sizeof(T), WAVES = THREADS / 64;
+    typedef elem_vec<T, E> vec;
+    __shared__ float stretch_max[STRETCHES][THREADS];
+    __shared__ uint64_t candidates[CANDIDATES];
+    __shared__ uint32_t group_keys[GROUPS];
+    __shared__ uint16_t stretches[LISTED];
+    __shared__ float wave_high[WAVES], wave_sum[WAVES], wave_moment[WAVES], limit_at;
+    __shared__ int wave_before[WAVES];
+    __shared__ int nstretches, ncandidates;
     const int64_t r = blockIdx.x;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T *const row = (const T *)a.logits + r * a.row_stride;
-    auto most = [](auto x, auto y) { return x > y ? x : y; };
-    auto plus = [](auto x, auto y) { return x + y; };
+
+    // `head` logits before the first whole vector, and some behind the last, one for each of the first threads
+    const int head = min(a.vocab, (int)((0 - (uintptr_t)row / sizeof(T)) % E)), nvec = (a.vocab - head) / E, tail = a.vocab - head - nvec * E;
+    const vec *const vectors = (const vec *)(row + head);
+    const int odd = tid < head ? tid : tid >= E && tid - E < tail ? head + nvec * E + tid - E : -1;
+
+    // (the first batch is on its way before the token's logit is asked for)
+    const int batches = (nvec + BATCH * THREADS - 1) / (BATCH * THREADS), per_stretch = (batches + STRETCHES - 1) / STRETCHES;
+    vec next[BATCH];
+    auto load = [&](int b) {
+        const int j0 = b * BATCH * THREADS + tid;
+        if ((b + 1) * BATCH * THREADS <= nvec) {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) next[u] = vectors[j0 + u * THREADS];
+        } else {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                if (j0 + u * THREADS < nvec) next[u] = vectors[j0 + u * THREADS];
+                else
+#pragma unroll
+                    for (int e = 0; e < E; ++e) next[u].v[e] = (T)-INFINITY;
+            }
+        }
+    };
+    load(0);
     const int64_t token = a.tokens ? a.tokens[r] : -1;
     const bool given = token >= 0 && token < a.vocab;
-    const uint64_t chosen = given ? order_key(logit_of(row[token]), (int)token) : ~0ull;
-    float high = -INFINITY;
+    const float chosen = given ? logit_of(row[token]) : INFINITY, chosen_tame = fmaxf(chosen, -WILD), chosen_above = next_above(chosen);
     int before = 0;
-    for (int i = tid; i < a.vocab; i += LOGPROB_THREADS) {
-        const float v = logit_of(row[i]);
-        high = fmaxf(high, v);
-        before += order_key(v, i) > chosen;
+    auto count = [&](float v, int i) { before += v > chosen || (v == chosen && i < token); };
+
+    float high = -WILD, ref = -WILD * LOG2E, sum = 0.f, moment = 0.f;
+    if (odd >= 0) {
+        const float v = logit_of(row[odd]);
+        if (given) count(v, odd);
+        if (v > high) {
+            high = v;
+            ref = v * LOG2E;
+            const float y = fmaf(v, LOG2E, -ref), w = __builtin_amdgcn_exp2f(y);
+            sum = w;
+            moment = w * y;
+        }
     }
-    high = block_join(high, most);
-    before = block_join(before, plus);
-    // distance from the maximum; where that is infinite, 0 for those that are it
+    float stretch = -WILD;
+    int stretch_at = 0, left = per_stretch;
+    for (int b = 0; b < batches; ++b) {
+        vec v[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) v[u] = next[u];
+        if (b + 1 < batches) load(b + 1);
+        const int j0 = b * BATCH * THREADS + tid;
+        float x[BATCH * E], largest = -WILD;
+#pragma unroll
+        for (int i = 0; i < BATCH * E; ++i) {
+            x[i] = fmaxf((float)v[i / E].v[i % E], -WILD);
+            largest = fmaxf(largest, x[i]);
+        }
+        if (given && __any(largest >= chosen_tame)) {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const int i0 = head + (j0 + u * THREADS) * E;
+                if (chosen > -WILD && (i0 + E <= token || i0 > token)) {   // all before the token, or all behind it
+                    const float least = i0 > token ? chosen_above : chosen;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) before += x[u * E + e] >= least;
+                } else if (j0 + u * THREADS < nvec) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) count(logit_of(v[u].v[e]), i0 + e);
+                }
+            }
+        }
+        if (a.top > 0) {
+            stretch = fmaxf(stretch, largest);
+            if (--left == 0) {
+                stretch_max[stretch_at++][tid] = stretch;
+                stretch = -WILD;
+                left = per_stretch;
+            }
+        }
+        high = fmaxf(high, largest);
+        const float moved = high * LOG2E, by = ref - moved, shrink = __builtin_amdgcn_exp2f(by);
+        moment = fmaf(sum, by, moment) * shrink;
+        sum *= shrink;
+        ref = moved;
+#pragma unroll
+        for (int i = 0; i < BATCH * E; ++i) {
+            const float y = fmaf(x[i], LOG2E, -ref), w = __builtin_amdgcn_exp2f(y);
+            sum += w;
+            moment = fmaf(w, y, moment);
+        }
+    }
+    if (a.top > 0)
+        for (; stretch_at < STRETCHES; ++stretch_at) {
+            stretch_max[stretch_at][tid] = stretch;
+            stretch = -WILD;
+        }
+    const float own_high = high;
+
+    // one meeting for the maximum and the groups' keys, one for the sums and the limit
+    high = wave_total<op_max>(high);
+    if (lane == 0) wave_high[wave] = high;
+    if (a.top > 0) {
+        float group = own_high;
+        for (int d = THREADS / GROUPS / 2; d > 0; d /= 2) group = fmaxf(group, __shfl_xor(group, d));
+        if (tid % (THREADS / GROUPS) == 0) group_keys[tid / (THREADS / GROUPS)] = (uint32_t)(order_key(group, 0) >> 36);
+    }
+    if (tid == 0) nstretches = ncandidates = 0;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) high = fmaxf(high, wave_high[w]);
+    const float joint = high * LOG2E, by = ref - joint, shrink = __builtin_amdgcn_exp2f(by);
+    moment = wave_total<op_add>(fmaf(sum, by, moment) * shrink);
+    sum = wave_total<op_add>(sum * shrink);
+    if (given) before = wave_total<op_add>(before);
+    if (lane == 0) {
+        wave_sum[wave] = sum;
+        wave_moment[wave] = moment;
+        wave_before[wave] = before;
+    }
+    // the limit, by the upper 16 bits of the groups' maxima in their order: as high as `top` groups reach it
+    if (a.top > 0 && tid < 64) {
+        uint32_t keys[GROUPS / 64], found = 0;
+#pragma unroll
+        for (int i = 0; i < GROUPS / 64; ++i) keys[i] = group_keys[64 * i + tid];
+        for (int bit = 15; bit >= 0; --bit) {
+            const uint32_t next_key = found | 1u << bit;
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < GROUPS / 64; ++i) reach += __popcll(__ballot(keys[i] >= next_key));
+            if (reach >= a.top) found = next_key;
+        }
+        if (tid == 0) limit_at = key_logit((uint64_t)found << 36);
+    }
+    __syncthreads();
+    sum = moment = 0.f;
+    before = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        sum += wave_sum[w];
+        moment += wave_moment[w];
+        before += wave_before[w];
+    }
+    // log of the sum of exp(logit - high)
+    float log_sum = LN2 * (log2f(sum) - fmaf(high, LOG2E, -joint)), entropy = fmaxf(LN2 * (log2f(sum) - moment / sum), 0.f);
+    // distance from the largest; where that is infinite, 0 for those that are it
     auto below = [&](float v) { return v == high ? 0.f : v - high; };
-    float sum = 0.f, moment = 0.f;
-    for (int i = tid; i < a.vocab; i += LOGPROB_THREADS) {
-        const float d = below(logit_of(row[i])), w = expf(d);
-        sum += w;
-        if (w > 0.f) moment += w * d;
+    if (!(fabsf(high) < WILD / 2)) {
+        high = -INFINITY;
+        for (int i = tid; i < a.vocab; i += THREADS) high = fmaxf(high, logit_of(row[i]));
+        high = block_total<THREADS, op_max>(high);
+        sum = moment = 0.f;
+        for (int i = tid; i < a.vocab; i += THREADS) {
+            const float d = below(logit_of(row[i])), w = expf(d);
+            sum += w;
+            if (w > 0.f) moment += w * d;
+        }
+        sum = block_total<THREADS, op_add>(sum);
+        moment = block_total<THREADS, op_add>(moment);
+        log_sum = logf(sum);
+        entropy = high == -INFINITY ? 0.f : fmaxf(log_sum - moment / sum, 0.f);
     }
-    sum = block_join(sum, plus);
-    moment = block_join(moment, plus);
-    const float log_sum = logf(sum);
     const bool none = high == -INFINITY;
     if (tid == 0) {
-        if (a.logprobs) a.logprobs[r] = given && !none ? below(key_logit(chosen)) - log_sum : -INFINITY;
+        if (a.logprobs) a.logprobs[r] = given && !none ? below(chosen) - log_sum : -INFINITY;
         if (a.ranks) a.ranks[r] = given ? before : -1;
-        if (a.entropy) a.entropy[r] = none ? 0.f : log_sum - moment / sum;
+        if (a.entropy) a.entropy[r] = entropy;
     }
+    if (a.top == 0) return;
+    auto put = [&](int n, uint64_t key) {   // 0: no token
+        if (a.top_tokens) a.top_tokens[r * a.top + n] = key ? key_token(key) : -1;
+        if (a.top_logprobs) a.top_logprobs[r * a.top + n] = key ? below(key_logit(key)) - log_sum : -INFINITY;
+    };
+
+    const float limit = fmaxf(limit_at, -0x1.fffffep19f);   // (above -WILD: of what lies from there on down, see the end)
+    auto offer = [&](float v, int i) {
+        if (!(v >= limit)) return;
+        const int n = atomicAdd(&ncandidates, 1);
+        if (n < CANDIDATES) candidates[n] = order_key(v, i);
+    };
+    if (odd >= 0) offer(logit_of(row[odd]), odd);
+    if (own_high >= limit)
+#pragma unroll
+        for (int s = 0; s < STRETCHES; ++s)
+            if (stretch_max[s][tid] >= limit) {
+                const int n = atomicAdd(&nstretches, 1);
+                if (n < LISTED) stretches[n] = (uint16_t)(s * THREADS + tid);
+            }
+    __syncthreads();
+    const int per = per_stretch * BATCH, items = min(nstretches, LISTED) * per;
+    for (int k = tid; k < items; k += THREADS) {
+        const int s = stretches[k / per], j = (s / THREADS * per + k % per) * THREADS + s % THREADS;
+        if (j >= nvec) continue;
+        const vec v = vectors[j];
+#pragma unroll
+        for (int e = 0; e < E; ++e) offer(logit_of(v.v[e]), head + j * E + e);
+    }
+    __syncthreads();
     uint64_t last = ~0ull;
-    for (int n = 0; n < a.top; ++n) {
+    int done = 0;
+    if (ncandidates <= CANDIDATES && nstretches <= LISTED) {
+        const int n = ncandidates;
+        for (int k = tid; k < n; k += THREADS) {
+            const uint64_t mine = candidates[k];
+            int place = 0;
+            for (int i = 0; i < n; ++i) place += candidates[i] > mine;
+            if (place < a.top) put(place, mine);
+        }
+        if (n >= a.top) return;
+        for (int i = 0; i < n; ++i) last = min(last, candidates[i]);
+        done = n;
+    }
+    // too many candidates, or fewer than are listed: the rest one after the other
+    for (; done < a.top && last; ++done) {
         uint64_t best = 0;
-        for (int i = tid; i < a.vocab; i += LOGPROB_THREADS) {
+        for (int i = tid; i < a.vocab; i += THREADS) {
             const float v = logit_of(row[i]);
             const uint64_t key = order_key(v, i);
             if (v > -INFINITY && key < last && key > best) best = key;
         }
-        last = block_join(best, most);
-        if (tid == 0) {
-            if (a.top_tokens) a.top_tokens[r * a.top + n] = last ? key_token(last) : -1;
-            if (a.top_logprobs) a.top_logprobs[r * a.top + n] = last ? below(key_logit(last)) - log_sum : -INFINITY;
-        }
+        last = block_total<THREADS, op_max>(best);
+        if (tid == 0) put(done, last);
     }
+    for (int k = done + tid; k < a.top; k += THREADS) put(k, 0);
+}
+
+template <class T> static int logprobs_typed(pq_ctx *ctx, const logprob_args &a) {
+    // 16 logits of a thread at a time: with 32, longer rows gain 3 % at most and short ones lose as much in occupancy.
+    constexpr int E = 16 / sizeof(T), BATCH = 16 / E;
+    // Few rows: more threads for each, so long as all of them have logits (8 rows of 32 000, bf16: 10.0 us, 12.4 with 256 threads; 256 rows
+    // of 131 072: 20 and 29 us; but 300 rows of 50 021: 18.6 and 18.1 us).  Long rows: fewer ends, which are not hidden (4096 rows of
+    // 131 072, bf16: 195 us, 204 with 256 threads; of 32 000 it is 66 and 60 us).
+    if (a.rows <= ctx->num_cu && a.vocab >= 1024 * E) token_logprobs_kernel<T, 1024, BATCH><<<a.rows, 1024, 0, ctx->stream>>>(a);
+    else if (a.vocab >= 65536) token_logprobs_kernel<T, 512, BATCH><<<a.rows, 512, 0, ctx->stream>>>(a);
+    else token_logprobs_kernel<T, 256, BATCH><<<a.rows, 256, 0, ctx->stream>>>(a);
+    PQ_HIP(ctx, hipGetLastError());
+    return PQ_OK;
 }
 
 int launch_token_logprobs(pq_ctx *ctx, const void *logits, int elem, int64_t row_stride, int rows, int vocab, const int64_t *tokens, int top,
                           float *logprobs, int32_t *ranks, float *entropy, int64_t *top_tokens, float *top_logprobs) {
     const logprob_args a = {logits, tokens, logprobs, entropy, top_logprobs, ranks, top_tokens, row_stride, rows, vocab, top_tokens || top_logprobs ? top : 0};
-    if (elem == PQ_ELEM_F32) token_logprobs_kernel<float><<<rows, LOGPROB_THREADS, 0, ctx->stream>>>(a);
-    else if (elem == PQ_ELEM_F16) token_logprobs_kernel<_Float16><<<rows, LOGPROB_THREADS, 0, ctx->stream>>>(a);
-    else token_logprobs_kernel<__bf16><<<rows, LOGPROB_THREADS, 0, ctx->stream>>>(a);
-    PQ_HIP(ctx, hipGetLastError());
-    return PQ_OK;
+    if (elem == PQ_ELEM_F32) return logprobs_typed<float>(ctx, a);
+    return elem == PQ_ELEM_F16 ? logprobs_typed<_Float16>(ctx, a) : logprobs_typed<__bf16>(ctx, a);
 }
 
 }  // namespace pq

@@ -676,6 +676,26 @@ def test_logprobs_of_special_rows(ctx, dtype, vocab):
     check_logprobs(ctx, dev(l, dtype), [0, 39, 6, 12, 39, 3, 5, 4, 5, 21, 3, 0, vocab, -1], 3)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [7, 600, 40000])
+@pytest.mark.parametrize("mask", [-3e4, -6e5, -1.1e6, -1e9, -1e30, -3e38])
+def test_logprobs_of_masks_and_large_logits(ctx, dtype, vocab, mask):
+    """Masks that are numbers: most of a row, whole stretches of it, all of it but next to nothing; rows that lie as low or as high."""
+    if dtype == F16:
+        mask = max(mask, -65504.0)
+    l = np.random.default_rng(3).standard_normal((8, vocab))
+    l[0, : vocab // 2] = mask
+    l[1, vocab // 3:] = mask
+    l[2], l[2, 3] = mask, 1.0
+    l[3], l[3, 2], l[3, 5] = mask, -np.inf, mask / 2
+    l[4] = mask
+    l[5, : vocab // 2] = mask
+    l[5, vocab // 2:] = -np.inf
+    l[6, 1], l[6, 4] = -mask, -mask
+    l[7] += mask / 4
+    check_logprobs(ctx, dev(l, dtype), [0, vocab - 1, 3, 5, 1, 2, 4, 6], 5)
+
+
 def test_logprobs_layouts(ctx):
     """Rows of any stride, that begin at any element; results that are not wanted."""
     r = np.random.default_rng(3)
