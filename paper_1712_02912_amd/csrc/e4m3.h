@@ -19,6 +19,14 @@ __device__ __forceinline__ uint32_t e4m3_of(float x, float y) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xffffu;
 }
 
+// Four numbers in a word.
+__device__ __forceinline__ uint32_t e4m3_of(const float *x) { return e4m3_of(x[0], x[1]) | e4m3_of(x[2], x[3]) << 16; }
+
+// The same of numbers that are 448 at most, or NaN.
+__device__ __forceinline__ uint32_t e4m3_of_held(const float *x) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false), true);
+}
+
 // Scales are handled by their exponents, from -126 on.
 constexpr int LEAST_EXPONENT = -126;
 __device__ __forceinline__ int scale_exponent(float scale) {

@@ -102,9 +102,9 @@ template <int V, bool PAIRS, class F> __device__ __forceinline__ void append_tur
 
 constexpr int APPEND_THREADS = 256;
 
-// A block's heads, gl lanes for each (a power of two, at least the number of units).
-template <class T, int V, bool PAIRS> __device__ __forceinline__ void append_rows(const append_args &a, int gl, int64_t block) {
-    const int64_t group = (block * APPEND_THREADS + threadIdx.x) / gl;
+// The heads of a grid's threads, gl lanes for each (a power of two, at least the number of units).
+template <class T, int V, bool PAIRS> __device__ __forceinline__ void append_rows(const append_args &a, int gl, int64_t thread) {
+    const int64_t group = thread / gl;
     const int u = threadIdx.x & (gl - 1), dim = a.cache.dim;
     const int64_t t = group / a.rows;
     if (t >= a.ntokens) return;

@@ -168,7 +168,7 @@ int launch_kv_plan(pq_ctx *ctx, const int32_t *new_lens, const int32_t *cached_l
 // of 80 dimensions, f32, 95 MB in 24 us = 3.9 TB/s.  Four heads one after the other in a group of lanes, all read before the first
 // is written and the rotation's row read once for them, were slower (93 us).
 template <class T, int V, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void kv_append_kernel(append_args a, int gl) {
-    append_rows<T, V, PAIRS>(a, gl, blockIdx.x);
+    append_rows<T, V, PAIRS>(a, gl, (int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x);
 }
 template <class T, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void kv_append_general_kernel(append_args a) {
     append_rows_general<T, PAIRS>(a, blockIdx.x);

@@ -34,14 +34,6 @@ __device__ __forceinline__ float next_above(float v) {
     return __builtin_bit_cast(float, v == 0.f ? 1u : b >> 31 ? b - 1 : b + 1);
 }
 
-struct op_max {
-    template <class V> static __device__ __forceinline__ V none() {
-        if constexpr (__is_same(V, float)) return -INFINITY;
-        else return V(0);
-    }
-    template <class V> static __device__ __forceinline__ V of(V a, V b) { return a > b ? a : b; }
-};
-template <class OP, class V> __device__ __forceinline__ V wave_total(V v) { return read_lane(wave_scan<OP>(v), 63); }
 // over a block, for the rare paths
 template <int THREADS, class OP, class V> __device__ __forceinline__ V block_total(V v) {
     __shared__ V parts[THREADS / 64];
@@ -188,7 +180,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
     const float own_high = high;
 
     // one meeting for the maximum and the groups' keys, one for the sums and the limit
-    high = wave_total<op_max>(high);
+    high = wave_total<op_larger>(high);
     if (lane == 0) wave_high[wave] = high;
     if (a.top > 0) {
         float group = own_high;
@@ -236,7 +228,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
     if (!(fabsf(high) < WILD / 2)) {
         high = -INFINITY;
         for (int i = tid; i < a.vocab; i += THREADS) high = fmaxf(high, logit_of(row[i]));
-        high = block_total<THREADS, op_max>(high);
+        high = block_total<THREADS, op_larger>(high);
         sum = moment = 0.f;
         for (int i = tid; i < a.vocab; i += THREADS) {
             const float d = below(logit_of(row[i])), w = expf(d);
@@ -306,7 +298,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
             const uint64_t key = order_key(v, i);
             if (v > -INFINITY && key < last && key > best) best = key;
         }
-        last = block_total<THREADS, op_max>(best);
+        last = block_total<THREADS, op_larger>(best);
         if (tid == 0) put(done, last);
     }
     for (int k = done + tid; k < a.top; k += THREADS) put(k, 0);

@@ -1,6 +1,7 @@
 // Sums and the like over the lanes of a wave, in registers (lanes exchange by the data-parallel primitives, a few cycles a step).
 #pragma once
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace pq {
@@ -26,6 +27,13 @@ struct op_add {
     template <class V> static __device__ __forceinline__ V none() { return V(0); }
     template <class V> static __device__ __forceinline__ V of(V a, V b) { return a + b; }
 };
+struct op_larger {
+    template <class V> static __device__ __forceinline__ V none() {
+        if constexpr (__is_same(V, float)) return -INFINITY;
+        else return V(0);   // (of whole numbers from 0 on)
+    }
+    template <class V> static __device__ __forceinline__ V of(V a, V b) { return a > b ? a : b; }
+};
 // every lane gets what the lanes up to and with it come to, within its row of 16
 template <class OP, class V> __device__ __forceinline__ V row_scan(V v) {
     v = OP::template of<V>(v, from_lane<0x111, 0xf>(OP::template none<V>(), v));
@@ -37,6 +45,20 @@ template <class OP, class V> __device__ __forceinline__ V wave_scan(V v) {
     v = row_scan<OP>(v);
     v = OP::template of<V>(v, from_lane<0x142, 0xa>(OP::template none<V>(), v));
     return OP::template of<V>(v, from_lane<0x143, 0xc>(OP::template none<V>(), v));
+}
+
+// what all lanes come to
+template <class OP, class V> __device__ __forceinline__ V wave_total(V v) { return read_lane(wave_scan<OP>(v), 63); }
+
+// what the lanes of a group come to, each of them; lanes: of a group, a power of two (all lanes of the wave are here)
+template <class OP, class V> __device__ __forceinline__ V group_total(V v, int lanes) {
+    if (lanes > 1) v = OP::template of<V>(v, from_lane<0xb1, 0xf>(v, v));    // neighbours
+    if (lanes > 2) v = OP::template of<V>(v, from_lane<0x4e, 0xf>(v, v));    // pairs of four
+    if (lanes > 4) v = OP::template of<V>(v, from_lane<0x141, 0xf>(v, v));   // fours of eight, mirrored
+    if (lanes > 8) v = OP::template of<V>(v, from_lane<0x140, 0xf>(v, v));   // eights of sixteen, mirrored
+    if (lanes > 16) v = OP::template of<V>(v, __shfl_xor(v, 16));
+    if (lanes > 32) v = OP::template of<V>(v, __shfl_xor(v, 32));
+    return v;
 }
 
 // n / d for 0 <= n < 2^31, as a product
