@@ -1,11 +1,11 @@
 """Retrieve and read: the search finds passages for each question, a small decoder reads them and answers.
 
-    python examples/read_passages.py [--questions 16] [--passages 100000] [--tokens 32] [--dtype bf16]
+    python examples/read_passages.py [--questions 16] [--passages 100000] [--tokens 32] [--dtype bf16] [--cache8]
 
 Passages are embeddings in a PQ 8x8 index; a question's nearest ones come from the tables and scan calls.  Their tokens and the
 question's are one chunk of new tokens of a request, then every step adds one drawn token to each.  A step is the plan of
 the paged cache, for every layer the append and the attention (between torch's products with the layer's weights), and the
-draw.  Data and weights are random: what is shown is how the calls go together, and what a step takes.
+draw.  With --cache8 the cache holds 8 bits an element.  Data and weights are random: what is shown is how the calls go together, and what a step takes.
 """
 import argparse
 import os
@@ -53,10 +53,17 @@ class Decoder:
 class Reader:
     """Requests in a paged cache: the state of a batch that is being served."""
 
-    def __init__(self, ctx, decoder, requests, blocks, width, block_size=16):
+    def __init__(self, ctx, decoder, requests, blocks, width, block_size=16, cache8=False):
         self.ctx, self.decoder, self.block_size = ctx, decoder, block_size
         shape = (blocks, block_size, decoder.heads, decoder.dim)
-        self.caches = [tuple(torch.zeros(shape, dtype=decoder.dtype, device="cuda") for _ in range(2)) for _ in decoder.layers]
+        # of each layer keys and values, of 8 bits also their scales
+        if cache8:
+            self.append, self.attention = ctx.pq_kv_append8, ctx.pq_kv_attention8
+            self.caches = [tuple(torch.zeros(shape, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2)) +
+                           tuple(torch.ones((blocks, decoder.heads), device="cuda") for _ in range(2)) for _ in decoder.layers]
+        else:
+            self.append, self.attention = ctx.pq_kv_append, ctx.pq_kv_attention
+            self.caches = [tuple(torch.zeros(shape, dtype=decoder.dtype, device="cuda") for _ in range(2)) for _ in decoder.layers]
         self.tables = torch.full((requests, width), -1, dtype=torch.int32, device="cuda")
         self.lens = torch.zeros(requests, dtype=torch.int32, device="cuda")
         self.counts = [0] * requests                      # the same on the host, which hands out the blocks
@@ -77,11 +84,11 @@ class Reader:
         self.counts = [c + n for c, n in zip(self.counts, new)]
         self.lens = kv                                    # (a refused request, of which there is none here, would stay refused)
         x = d.embedding[tokens]
-        for w, (keys, values) in zip(d.layers, self.caches):
+        for w, cache in zip(d.layers, self.caches):
             qkv = (d.norm(x) @ w["qkv"]).view(len(tokens), d.q_heads + 2 * d.heads, d.dim)
             q, k, v = qkv.split((d.q_heads, d.heads, d.heads), dim=1)       # (views: the append reads them with their strides)
-            q = ctx.pq_kv_append(q, k, v, positions, slots, keys, values, d.cos, d.sin, w["q_norm"], w["k_norm"])
-            out, _ = ctx.pq_kv_attention(q, keys, values, self.tables, cu, kv, max(new))
+            q = self.append(q, k, v, positions, slots, *cache, d.cos, d.sin, w["q_norm"], w["k_norm"])
+            out, _ = self.attention(q, *cache, self.tables, cu, kv, max(new))
             x = x + out.view(len(tokens), -1) @ w["out"]
             x = x + torch.nn.functional.silu(d.norm(x) @ w["up"]) @ w["down"]
         logits = d.norm(x[(cu[1:] - 1).long()]) @ d.head
@@ -89,12 +96,12 @@ class Reader:
         return drawn, logprobs, logits
 
 
-def answer(ctx, decoder, prompts, tokens, noise, **filters):
+def answer(ctx, decoder, prompts, tokens, noise, cache8=False, **filters):
     """Draws `tokens` tokens for each prompt (lists of token tensors) with noise [tokens][prompts][vocab].  Returns the tokens
     [prompts][tokens], their logprobs and every step's logits."""
     block_size, longest = 16, max(len(p) for p in prompts) + tokens
     width = -(-longest // block_size)
-    reader = Reader(ctx, decoder, len(prompts), len(prompts) * width, width, block_size)
+    reader = Reader(ctx, decoder, len(prompts), len(prompts) * width, width, block_size, cache8)
     drawn, logprobs, logits = [], [], []
     for i in range(tokens):
         inputs, new = (torch.cat(prompts), [len(p) for p in prompts]) if i == 0 else (drawn[-1], [1] * len(prompts))
@@ -111,6 +118,7 @@ def main(argv=None):
     parser.add_argument("--passages", type=int, default=100000)
     parser.add_argument("--tokens", type=int, default=32, help="tokens of each answer")
     parser.add_argument("--dtype", choices=sorted(DTYPES), default="bf16")
+    parser.add_argument("--cache8", action="store_true", help="keys and values in 8 bits")
     args = parser.parse_args(argv)
 
     ctx = binding.Context(0)
@@ -134,12 +142,15 @@ def main(argv=None):
     for run in ("first", "second"):
         torch.cuda.synchronize()
         start = time.perf_counter()
-        tokens, logprobs, _ = answer(ctx, decoder, prompts, args.tokens, noise, **filters)
+        tokens, logprobs, logits = answer(ctx, decoder, prompts, args.tokens, noise, args.cache8, **filters)
         torch.cuda.synchronize()
         print(f"{run} run: {args.questions} answers of {args.tokens} tokens over {sum(len(p) for p in prompts)} tokens of passages and "
               f"questions: {1e3 * (time.perf_counter() - start):.2f} ms")
     print(f"the passage that was meant is among the four found for {found} of {args.questions} questions")
     print("first answer:", tokens[0].tolist(), f"log-likelihood {logprobs[0].sum().item():.2f}")
+    # what the model itself says of the drawn tokens, without temperature and filters, and which it had found likeliest
+    _, ranks, entropy, likeliest, _ = ctx.pq_token_logprobs(logits[0], tokens[:, 0].contiguous(), 3)
+    print(f"its first token is number {ranks[0].item()} of {decoder.vocab} (likeliest: {likeliest[0].tolist()}), entropy {entropy[0].item():.2f}")
     ctx.close()
     return tokens
 

@@ -413,7 +413,9 @@ template <class T, int QV, bool PAIRS> static int append8_vector(pq_ctx *ctx, co
     const int64_t chunks = (a.in.ntokens + tokens - 1) / tokens, held = ctx->num_cu * (1024 / threads) / 2, most = (held + chunks - 1) / chunks;
     // (as many blocks as the chip holds, four waves on a SIMD, half of them for keys: fewer lists each begin more often)
     const int each = most >= heads ? 1 : most <= 1 ? heads : (int)((heads + most - 1) / most), groups = (heads + each - 1) / each;
-    const bool merged = a.in.ntokens <= 1024;
+    // Up to 96 MiB of queries in the same launch: 4099 tokens of 12 heads of 80 dimensions 31 us, 36 with a launch of their own.  More of
+    // them want the waves that this kernel's registers do not leave (16 384 tokens of 32 heads of 128, bf16: 111 and 100 us).
+    const bool merged = a.in.ntokens * a.in.q_heads * a.cache.dim * (int64_t)sizeof(T) <= (int64_t)96 << 20;
     const int64_t kv = chunks * groups * 2, queries = (a.in.ntokens * a.in.q_heads * q_gl + APPEND_THREADS - 1) / APPEND_THREADS;
     if (kv + queries > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
     const int64_t with = merged ? (queries * APPEND_THREADS + threads - 1) / threads : 0;

@@ -161,16 +161,18 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
             }
         }
         high = fmaxf(high, largest);
+        // (summed for itself first: a long chain of additions would be off by ten times as much)
         const float moved = high * LOG2E, by = ref - moved, shrink = __builtin_amdgcn_exp2f(by);
-        moment = fmaf(sum, by, moment) * shrink;
-        sum *= shrink;
         ref = moved;
+        float batch_sum = 0.f, batch_moment = 0.f;
 #pragma unroll
         for (int i = 0; i < BATCH * E; ++i) {
             const float y = fmaf(x[i], LOG2E, -ref), w = __builtin_amdgcn_exp2f(y);
-            sum += w;
-            moment = fmaf(w, y, moment);
+            batch_sum += w;
+            batch_moment = fmaf(w, y, batch_moment);
         }
+        moment = fmaf(fmaf(sum, by, moment), shrink, batch_moment);
+        sum = fmaf(sum, shrink, batch_sum);
     }
     if (a.top > 0)
         for (; stretch_at < STRETCHES; ++stretch_at) {

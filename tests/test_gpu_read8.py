@@ -190,6 +190,38 @@ def test_append_of_special_values(ctx, dtype, dim):
     assert held[1, 0] == 2.0 ** -126 and np.isnan(values[5]).sum() == dim + 1
 
 
+@pytest.mark.parametrize("dim", [64, 80, 10])
+def test_append_counts_the_exponents_of_scales(ctx, dim):
+    """A block's scale from before that is no power of two is taken as the one below; a run that keeps it writes that."""
+    x = dev(np.random.default_rng(dim).standard_normal((2, 1, dim)), F32)
+    found = []
+    for scale in (4.0, 7.9):
+        caches = [torch.full((1, 16, 1, dim), 0x51, dtype=torch.uint8, device="cuda").view(E4M3) for _ in range(2)]
+        scales = [torch.full((1, 1), scale, device="cuda") for _ in range(2)]
+        ctx.pq_kv_append8(None, x, x, whole([0, 0]), dev(np.array([3, 4])), *caches, *scales, norm=False)
+        assert all(float(s) == 4.0 for s in scales)
+        found.append([host(c) for c in caches])
+    assert np.array_equal(found[0], found[1])
+
+
+@pytest.mark.parametrize("dim", [64, 10])
+def test_append_of_rows_without_a_size(ctx, dim):
+    """Keys of zeros under a norm: zeros with eps, no numbers without it; values are not touched by that."""
+    x = torch.zeros((2, 1, dim), device="cuda")
+    for eps in (1e-6, 0.0):
+        caches = [torch.full((1, 4, 1, dim), 0x51, dtype=torch.uint8, device="cuda").view(E4M3) for _ in range(2)]
+        scales = [torch.ones((1, 1), device="cuda") for _ in range(2)]
+        ctx.pq_kv_append8(None, x, x, whole([0, 0]), dev(np.array([0, 1])), *caches, *scales, eps=eps)
+        assert np.array_equal(np.isnan(host(caches[0])[0, :2]), np.full((2, 1, dim), eps == 0)) and (host(caches[1])[0, :2] == 0).all()
+        assert all(float(s) == 2.0 ** -126 for s in scales) and (host(caches[0])[0, 2:] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens", [1100, 20000])
+def test_append_of_single_tokens_of_many_requests(ctx, dtype, tokens):
+    check_append(ctx, tokens, tokens, 2, 2, 64, 64, False, dtype, block_size=4, seed=tokens)
+
+
 def test_append_refusals(ctx):
     x = torch.zeros((4, 2, 64), device="cuda")
     cache, scales = torch.zeros((2, 4, 2, 64), dtype=torch.uint8, device="cuda").view(E4M3), torch.ones((2, 2), device="cuda")
@@ -501,6 +533,20 @@ def test_attention_of_scales_of_all_sizes(ctx, new, dtype, exponents):
                 bound += 2.0 ** -24 * 512 * 2.0 ** ve + 2.0 ** -24
             assert (np.abs(host(out) - want) <= bound).all()
             assert (np.abs(host(lse) - want_lse) <= 2 * fp32 + 1e-6 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("dim", [64, 80])
+def test_attention_counts_the_exponents_of_scales(ctx, new, dtype, dim):
+    """Scales between powers of two give the result of the power below, to the last bit."""
+    r = np.random.default_rng(new)
+    tables, kc, vc, ks, vs, _, _ = make_cache(r, [new + 77, new], 2, dim, 16, 0)
+    q = dev(r.standard_normal((2 * new, 4, dim)), dtype)
+    rest = (dev(tables), whole([0, new, 2 * new]), whole([new + 77, new]), new)
+    want = ctx.pq_kv_attention8(q, kc, vc, ks, vs, *rest)
+    got = ctx.pq_kv_attention8(q, kc, vc, ks * 1.75, vs * 1.25, *rest)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
 @pytest.mark.parametrize("new", [1, 40])
