@@ -70,7 +70,7 @@ __device__ __forceinline__ append8_place append8_locate(const append8_args &a, c
 // ---- any layout ---------------------------------------------------------------------------------------
 //
 // One wave for each token and head (of the cache: one for keys, one for values), which holds the run that begins there.  It goes over
-// the run's rows twice, for the largest element and to write them; no row is kept between.
+// the run's rows twice, for the largest element and to write them; no row is kept between.  (The 16 384 tokens below take 1430 us here.)
 template <class T, bool PAIRS> __device__ __forceinline__ void append8_general_head(const append8_args &a, int64_t t, int h, bool is_key) {
     const int64_t slot = append8_slot(a, t);
     if (!append8_begins(a, slot, t > 0 ? append8_slot(a, t - 1) : -1)) return;
@@ -138,12 +138,21 @@ template <class T, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void
 
 // ---- by groups of lanes ---------------------------------------------------------------------------------
 //
-// A block looks at a chunk of tokens and takes the runs that begin among them, as many one after the other as it has rows for (gl lanes
-// hold a row, kv_append.h), list by list: the keys or the values of a head.  A row stays in registers from the norm over the largest
-// element to the codes, what the rows of a run need of a scale they tell each other in shared memory; the next list's rows are on their
+// A block looks at a chunk of tokens and takes the runs that begin among them, as many side by side as it has rows for (gl lanes
+// hold a row, kv_append.h), head by head, keys or values.  A row stays in registers from the norm over the largest
+// element to the codes, what the rows of a run need of a scale they tell each other in shared memory; the next head's rows are on their
 // way meanwhile, and a token's rotation is read once for all its heads.  Rows of a run that is longer than the block holds are read
 // a second time.
-constexpr int APPEND8_V = 4;       // (eight elements a lane: sixteen, in fp64, leave registers for two waves of a SIMD)
+//
+// Scales are powers of two: a scale that grows moves the exponents of what is there, and only what falls below the least exponent is
+// rounded again; a number's own exponent makes a finer scale of little use.  fp64 up to a key's x costs 2 us of 40 (below) and makes
+// its code a matter of the definition, not of the order in which a norm is summed: next to a border of e4m3 the last bit of x decides
+// over a sixteenth of it.
+//
+// 16 384 tokens of 32 + 8 + 8 heads of 128 dimensions, bf16: 378 MB in 96 us, 41 us keys and values (101 MB; bound by vector instructions
+// and by their meetings: a list of 16 rows takes a wave about 250 to 350 of them) and 54 us queries (268 MB = 5.0 TB/s); 4099 tokens of 36 heads of
+// 80 dimensions, f16, 25 us; 64 single tokens 6.5 us, a chain of slots, rows and rotations, scales.
+constexpr int APPEND8_V = 4;       // of keys (eight elements a lane: sixteen, in fp64, leave registers for two waves of a SIMD)
 constexpr int APPEND8_MOST = 1024; // threads of a block
 constexpr int APPEND8_ROWS = APPEND8_MOST;
 
@@ -189,11 +198,11 @@ struct append8_shared {
 };
 
 // The keys or the values of heads first ... end - 1, from head `at` on.
-template <class T, bool PAIRS, bool KEYS, bool LONG>
+template <class T, int V, bool PAIRS, bool KEYS, bool LONG>
 __device__ __forceinline__ void append8_heads(const append8_args &a, int gl, const append8_tile &tile, const append8_row &mine, int first, int end, int at, append8_shared &shared, int &turn) {
-    constexpr int V = APPEND8_V;
     typedef elem_vec<T, V> vec;
     typedef elem_vec<float, V> fvec;
+    typedef elem_vec<uint32_t, V / 4> codes;
     const int u = threadIdx.x & (gl - 1), rows = blockDim.x / gl, row = threadIdx.x / gl;
     const bool active = u < a.cache.dim / (2 * V), normed = KEYS && a.in.norm, weighted = normed && a.in.k_weight;
     const append_unit<V, PAIRS> unit(active ? u : 0, KEYS ? a.in.rot : 0);
@@ -319,8 +328,14 @@ __device__ __forceinline__ void append8_heads(const append8_args &a, int gl, con
                 y[e] = __builtin_amdgcn_ldexpf(y[e], -e8);
             }
             uint8_t *const p = out + begin * strides[1] + h * strides[2];
-            *(uint32_t *)p = odd ? e4m3_of(x) : e4m3_of_held(x);
-            *(uint32_t *)(p + second) = odd ? e4m3_of(y) : e4m3_of_held(y);
+            codes cx, cy;
+#pragma unroll
+            for (int e = 0; e < V / 4; ++e) {
+                cx.v[e] = odd ? e4m3_of(x + 4 * e) : e4m3_of_held(x + 4 * e);
+                cy.v[e] = odd ? e4m3_of(y + 4 * e) : e4m3_of_held(y + 4 * e);
+            }
+            *(codes *)p = cx;
+            *(codes *)(p + second) = cy;
         }
         const bool there = active && row < tile.n;
         // The scale has grown: what the block held before, rounded anew.
@@ -328,11 +343,16 @@ __device__ __forceinline__ void append8_heads(const append8_args &a, int gl, con
             for (int p = row - mine.begin; p < mine.place; p += mine.end - mine.begin)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    uint32_t *const codes = (uint32_t *)(block + p * strides[1] + h * strides[2] + half * second);
-                    float f[V];
+                    codes *const at_codes = (codes *)(block + p * strides[1] + h * strides[2] + half * second);
+                    codes held = *at_codes;
 #pragma unroll
-                    for (int e = 0; e < V; ++e) f[e] = __builtin_amdgcn_ldexpf((float)e4m3{(uint8_t)(*codes >> 8 * e)}, before - e8);
-                    *codes = e4m3_of_held(f);
+                    for (int e = 0; e < V / 4; ++e) {
+                        float f[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_ldexpf((float)e4m3{(uint8_t)(held.v[e] >> 8 * i)}, before - e8);
+                        held.v[e] = e4m3_of_held(f);
+                    }
+                    *at_codes = held;
                 }
         if (there && u == 0 && row == mine.begin) scales[h] = scale_of(e8);
         h = next_h;
@@ -340,7 +360,7 @@ __device__ __forceinline__ void append8_heads(const append8_args &a, int gl, con
 }
 
 // The runs that begin in a chunk, of as many tokens as the block has rows (64 at most): heads first ... end - 1 of their keys or values.
-template <class T, bool PAIRS, bool KEYS, bool LONG>
+template <class T, int V, bool PAIRS, bool KEYS, bool LONG>
 __device__ __forceinline__ void append8_chunk(const append8_args &a, int gl, int64_t chunk, int first, int end, append8_shared &shared) {
     const int lane = threadIdx.x & 63, rows = blockDim.x / gl, tokens = min(rows, 64);
     const int64_t t0 = chunk * tokens, t = t0 + lane;
@@ -376,27 +396,37 @@ __device__ __forceinline__ void append8_chunk(const append8_args &a, int gl, int
             }
         }
         const append8_row mine = append8_row_of(a, tile, threadIdx.x / gl, rows);
-        append8_heads<T, PAIRS, KEYS, LONG>(a, gl, tile, mine, first, end, first, shared, turn);
+        append8_heads<T, V, PAIRS, KEYS, LONG>(a, gl, tile, mine, first, end, first, shared, turn);
     }
 }
 
-// Blocks for the keys and the values of each group of `each` heads of a chunk, side by side; behind kv_blocks of them those of the
-// queries, QV of whose elements are accessed at once.  LONG: blocks of the cache have more places than there are rows.
-template <class T, int QV, bool PAIRS, int THREADS, bool LONG>
-__global__ __launch_bounds__(THREADS) void kv_append8_kernel(append8_args a, int gl, int q_gl, unsigned kv_blocks, int groups, int each) {
+// The blocks of one side, keys or values: `groups` of them share a chunk's heads, `each` of these a block.
+struct append8_side {
+    unsigned blocks;
+    int gl, groups, each;
+};
+// Blocks of keys, of values, and of queries, W elements of both of which are accessed at once.  LONG: blocks of the cache have more
+// places than there are rows.
+template <class T, int W, bool PAIRS, int THREADS, bool LONG>
+__global__ __launch_bounds__(THREADS) void kv_append8_kernel(append8_args a, append8_side keys, append8_side values) {
     __shared__ append8_shared shared;
-    if (blockIdx.x >= kv_blocks) {
-        append_rows<T, QV, PAIRS>(a.in, q_gl, (int64_t)(blockIdx.x - kv_blocks) * blockDim.x + threadIdx.x);
+    unsigned block = blockIdx.x;
+    if (block < keys.blocks) {
+        const unsigned chunk = block / keys.groups, first = (block - chunk * keys.groups) * keys.each;
+        append8_chunk<T, APPEND8_V, PAIRS, true, LONG>(a, keys.gl, chunk, first, min(a.cache.heads, (int)first + keys.each), shared);
         return;
     }
-    const unsigned side = blockIdx.x & 1, chunk = blockIdx.x / 2 / groups, group = blockIdx.x / 2 - chunk * groups;
-    const int first = group * each, end = min(a.cache.heads, first + each);
-    if (side == 0) append8_chunk<T, PAIRS, true, LONG>(a, gl, chunk, first, end, shared);
-    else append8_chunk<T, PAIRS, false, LONG>(a, gl, chunk, first, end, shared);
+    block -= keys.blocks;
+    if (block < values.blocks) {
+        const unsigned chunk = block / values.groups, first = (block - chunk * values.groups) * values.each;
+        append8_chunk<T, W, PAIRS, false, LONG>(a, values.gl, chunk, first, min(a.cache.heads, (int)first + values.each), shared);
+        return;
+    }
+    append_rows<T, W, PAIRS>(a.in, values.gl, (int64_t)(block - values.blocks) * blockDim.x + threadIdx.x);
 }
 
-template <class T, int QV, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void kv_append8_queries_kernel(append_args a, int q_gl) {
-    append_rows<T, QV, PAIRS>(a, q_gl, (int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x);
+template <class T, int W, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void kv_append8_queries_kernel(append_args a, int gl) {
+    append_rows<T, W, PAIRS>(a, gl, (int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x);
 }
 
 static int lanes_of(int units) {
@@ -405,53 +435,53 @@ static int lanes_of(int units) {
     return gl;
 }
 
-template <class T, int QV, bool PAIRS> static int append8_vector(pq_ctx *ctx, const append8_args &a) {
-    const int gl = lanes_of(a.cache.dim / (2 * APPEND8_V)), q_gl = lanes_of(a.cache.dim / (2 * QV)), heads = a.cache.heads;
+template <class T, int W, bool PAIRS> static int append8_vector(pq_ctx *ctx, const append8_args &a) {
+    const int key_gl = lanes_of(a.cache.dim / (2 * APPEND8_V)), gl = lanes_of(a.cache.dim / (2 * W)), heads = a.cache.heads;
     int threads = APPEND_THREADS;
-    while (threads < APPEND8_MOST && threads / gl < a.cache.block_size) threads *= 2;
-    const int tokens = threads / gl < 64 ? threads / gl : 64;
-    const int64_t chunks = (a.in.ntokens + tokens - 1) / tokens, held = ctx->num_cu * (1024 / threads) / 2, most = (held + chunks - 1) / chunks;
-    // (as many blocks as the chip holds, four waves on a SIMD, half of them for keys: fewer lists each begin more often)
-    const int each = most >= heads ? 1 : most <= 1 ? heads : (int)((heads + most - 1) / most), groups = (heads + each - 1) / each;
-    // Up to 96 MiB of queries in the same launch: 4099 tokens of 12 heads of 80 dimensions 31 us, 36 with a launch of their own.  More of
+    while (threads < APPEND8_MOST && threads / key_gl < a.cache.block_size) threads *= 2;
+    auto side = [&](int lanes) {
+        const int tokens = threads / lanes < 64 ? threads / lanes : 64;
+        // (as many blocks as the chip holds, four waves on a SIMD, half of them for keys: fewer heads each begin more often)
+        const int64_t chunks = (a.in.ntokens + tokens - 1) / tokens, held = ctx->num_cu * (1024 / threads) / 2, most = (held + chunks - 1) / chunks;
+        const int each = most >= heads ? 1 : most <= 1 ? heads : (int)((heads + most - 1) / most), groups = (heads + each - 1) / each;
+        const append8_side s = {(unsigned)(chunks * groups), lanes, groups, each};
+        return chunks * groups > INT_MAX / 4 ? append8_side{0, 0, 0, 0} : s;
+    };
+    const append8_side keys = side(key_gl), values = side(gl);
+    const int64_t queries = (a.in.ntokens * a.in.q_heads * gl + APPEND_THREADS - 1) / APPEND_THREADS;
+    if (keys.groups == 0 || values.groups == 0 || queries > INT_MAX / 4) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
+    // Up to 96 MiB of queries in the same launch: 4099 tokens of 12 heads of 80 dimensions 29 us, 36 with a launch of their own.  More of
     // them want the waves that this kernel's registers do not leave (16 384 tokens of 32 heads of 128, bf16: 111 and 100 us).
     const bool merged = a.in.ntokens * a.in.q_heads * a.cache.dim * (int64_t)sizeof(T) <= (int64_t)96 << 20;
-    const int64_t kv = chunks * groups * 2, queries = (a.in.ntokens * a.in.q_heads * q_gl + APPEND_THREADS - 1) / APPEND_THREADS;
-    if (kv + queries > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
-    const int64_t with = merged ? (queries * APPEND_THREADS + threads - 1) / threads : 0;
-    const unsigned grid = (unsigned)(kv + with);
-    if (a.cache.block_size > threads / gl) kv_append8_kernel<T, QV, PAIRS, APPEND8_MOST, true><<<grid, threads, 0, ctx->stream>>>(a, gl, q_gl, (unsigned)kv, groups, each);
-    else if (threads > APPEND_THREADS) kv_append8_kernel<T, QV, PAIRS, APPEND8_MOST, false><<<grid, threads, 0, ctx->stream>>>(a, gl, q_gl, (unsigned)kv, groups, each);
-    else kv_append8_kernel<T, QV, PAIRS, APPEND_THREADS, false><<<grid, threads, 0, ctx->stream>>>(a, gl, q_gl, (unsigned)kv, groups, each);
-    if (!merged && queries > 0) kv_append8_queries_kernel<T, QV, PAIRS><<<(unsigned)queries, APPEND_THREADS, 0, ctx->stream>>>(a.in, q_gl);
+    const unsigned grid = keys.blocks + values.blocks + (merged ? (unsigned)((queries * APPEND_THREADS + threads - 1) / threads) : 0);
+    if (a.cache.block_size > threads / key_gl) kv_append8_kernel<T, W, PAIRS, APPEND8_MOST, true><<<grid, threads, 0, ctx->stream>>>(a, keys, values);
+    else if (threads > APPEND_THREADS) kv_append8_kernel<T, W, PAIRS, APPEND8_MOST, false><<<grid, threads, 0, ctx->stream>>>(a, keys, values);
+    else kv_append8_kernel<T, W, PAIRS, APPEND_THREADS, false><<<grid, threads, 0, ctx->stream>>>(a, keys, values);
+    if (!merged && queries > 0) kv_append8_queries_kernel<T, W, PAIRS><<<(unsigned)queries, APPEND_THREADS, 0, ctx->stream>>>(a.in, gl);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }
 
-// whether rows, pairs and the rest of the head allow accesses of v elements: of queries, or of keys, values and codes
-static bool append8_fits(const append8_args &a, int v, size_t e, bool of_queries) {
+// whether rows, pairs and the rest of the head allow accesses of v elements: of keys, or of queries and values, whose codes they are too
+static bool append8_fits(const append8_args &a, int v, size_t e, bool of_keys) {
     const pq_kv_cache8 &c = a.cache;
-    uint64_t of_elems = 0, of_codes = 0, of_tables = (uint64_t)(uintptr_t)(of_queries ? a.in.q_weight : a.in.k_weight);
-    auto rows = [&](const pq_heads &h) { of_elems |= (uint64_t)(uintptr_t)h.p | (uint64_t)h.token_stride * e | (uint64_t)h.head_stride * e; };
-    if (of_queries) {
+    uint64_t elems = 0, codes = (uint64_t)(uintptr_t)(of_keys ? c.keys : c.values), tables = (uint64_t)(uintptr_t)(of_keys ? a.in.k_weight : a.in.q_weight);
+    for (int i = 0; i < 3; ++i) codes |= (uint64_t)(of_keys ? c.key_strides[i] : c.value_strides[i]);
+    auto rows = [&](const pq_heads &h) { elems |= (uint64_t)(uintptr_t)h.p | (uint64_t)h.token_stride * e | (uint64_t)h.head_stride * e; };
+    rows(of_keys ? a.in.k : a.in.v);
+    if (!of_keys && a.in.q_heads > 0) {
         rows(a.in.q);
-        of_elems |= (uint64_t)(uintptr_t)a.in.q_out;   // (dim is a multiple of v, as its parts are)
-    } else {
-        rows(a.in.k);
-        rows(a.in.v);
-        of_codes = (uint64_t)(uintptr_t)c.keys | (uint64_t)(uintptr_t)c.values;
-        for (int i = 0; i < 3; ++i) of_codes |= (uint64_t)c.key_strides[i] | (uint64_t)c.value_strides[i];
+        elems |= (uint64_t)(uintptr_t)a.in.q_out;   // (dim is a multiple of v, as its parts are)
     }
-    if (a.in.rot > 0) of_tables |= (uint64_t)(uintptr_t)a.in.cos_table | (uint64_t)(uintptr_t)a.in.sin_table;
-    return a.in.rot / 2 % v == 0 && (c.dim - a.in.rot) / 2 % v == 0 && c.dim <= 64 * 2 * v && of_elems % (v * e) == 0 && of_codes % v == 0 &&
-           of_tables % (v * 4) == 0;
+    if (a.in.rot > 0) tables |= (uint64_t)(uintptr_t)a.in.cos_table | (uint64_t)(uintptr_t)a.in.sin_table;
+    return a.in.rot / 2 % v == 0 && (c.dim - a.in.rot) / 2 % v == 0 && c.dim <= 64 * 2 * v && elems % (v * e) == 0 && codes % v == 0 && tables % (v * 4) == 0;
 }
 
 template <class T, bool PAIRS> static int append8_typed(pq_ctx *ctx, const append8_args &a) {
     constexpr int most = 16 / sizeof(T);
-    if (append8_fits(a, APPEND8_V, sizeof(T), false)) {
-        if (a.in.q_heads == 0 || append8_fits(a, most, sizeof(T), true)) return append8_vector<T, most, PAIRS>(ctx, a);
-        if (append8_fits(a, 4, sizeof(T), true)) return append8_vector<T, 4, PAIRS>(ctx, a);
+    if (append8_fits(a, APPEND8_V, sizeof(T), true)) {
+        if (append8_fits(a, most, sizeof(T), false)) return append8_vector<T, most, PAIRS>(ctx, a);
+        if (append8_fits(a, 4, sizeof(T), false)) return append8_vector<T, 4, PAIRS>(ctx, a);
     }
     constexpr int WAVES = APPEND_THREADS / 64;
     const int64_t queries = (a.in.ntokens * a.in.q_heads + WAVES - 1) / WAVES, items = (a.in.ntokens * 2 * a.cache.heads + WAVES - 1) / WAVES;
