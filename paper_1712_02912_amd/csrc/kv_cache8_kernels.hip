@@ -241,6 +241,10 @@ __device__ __forceinline__ void append8_heads(const append8_args &a, int gl, con
 #pragma unroll 1
     for (int left = end - first, h = at; left > 0; --left) {
         const int next_h = h + 1 < end ? h + 1 : first;
+        if (parts > 1 && left < end - first) {   // (of one part they are on their way since the head before)
+            fetch(h, 0);
+            angles(0);
+        }
         const int before = mine.place > 0 ? scale_exponent(next_scale) : LEAST_EXPONENT;
         float amax = 0.f;
         int e8 = before;
@@ -250,7 +254,7 @@ __device__ __forceinline__ void append8_heads(const append8_args &a, int gl, con
         for (int n = 0; n < (parts > 1 ? 2 * parts : 1); ++n) {
             const int begin = (n < parts ? n : n - parts) * rows;
             const bool there = active && begin + row < tile.n;
-            if (parts > 1 && (n > 0 || left < end - first)) {
+            if (n > 0) {
                 fetch(h, begin);
                 angles(begin);
             }

@@ -132,6 +132,11 @@ def test_append_of_large_blocks(ctx, dtype, dim):
     check_append(ctx, 900, 2, 2, 1, dim, dim, False, dtype, block_size=400, seed=dim)
 
 
+@pytest.mark.parametrize("dim,heads", [(64, 40), (128, 24), (256, 12), (512, 8)])
+def test_append_of_many_heads_of_large_blocks(ctx, dim, heads):
+    check_append(ctx, 1900, 3, 2, heads, dim, dim, False, BF16, block_size=400, seed=dim)
+
+
 @pytest.mark.parametrize("tokens,requests", [(1, 1), (6, 6), (1031, 300), (9000, 11)])
 def test_append_of_many_tokens(ctx, tokens, requests):
     check_append(ctx, tokens, requests, 8, 2, 64, 64, False, BF16, block_size=24, seed=tokens)
