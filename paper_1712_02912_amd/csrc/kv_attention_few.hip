@@ -51,6 +51,8 @@ int few_prepare(pq_ctx *ctx, const attention_args &a, int waves, size_t more, fe
 }
 
 template <class T, class C, int D> static int few_typed(pq_ctx *ctx, const attention_args &a, int most_rows) {
+    const int64_t items = (int64_t)a.nreq * a.cache.heads;
+    if (!grid_fits(items, 256)) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", a.nreq);
     few_line line;
     size_t ws_used;
     if (const int rc = few_prepare(ctx, a, 4, 0, &line, &ws_used)) return rc;
@@ -59,9 +61,8 @@ template <class T, class C, int D> static int few_typed(pq_ctx *ctx, const atten
         PQ_HIP(ctx, hipGetLastError());
         return PQ_OK;
     }
-    const int items = a.nreq * a.cache.heads;
-    if (line.row_waves > 4) kv_attention_few_join_kernel<T, C, D, 16><<<dim3(items, few_slices(line, most_rows, 16)), 1024, 0, ctx->stream>>>(a, line);
-    else kv_attention_few_join_kernel<T, C, D, 4><<<dim3(items, few_slices(line, most_rows, 4)), 256, 0, ctx->stream>>>(a, line);
+    if (line.row_waves > 4) kv_attention_few_join_kernel<T, C, D, 16><<<dim3((unsigned)items, few_slices(line, most_rows, 16)), 1024, 0, ctx->stream>>>(a, line);
+    else kv_attention_few_join_kernel<T, C, D, 4><<<dim3((unsigned)items, few_slices(line, most_rows, 4)), 256, 0, ctx->stream>>>(a, line);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
 }

@@ -107,7 +107,7 @@ static bool attention_on_matrix_cores(const attention_args &a, size_t e) {
 
 template <class T, class C> static int attention_general(pq_ctx *ctx, const attention_args &a) {
     const int64_t grid = a.ntokens * a.q_heads;
-    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
+    if (!grid_fits(grid, 64 * GENERAL_WAVES)) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)grid);
     kv_attention_general_kernel<T, C><<<(int)grid, 64 * GENERAL_WAVES, 0, ctx->stream>>>(a);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;

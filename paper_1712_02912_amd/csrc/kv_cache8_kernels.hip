@@ -406,7 +406,7 @@ __device__ __forceinline__ void append8_chunk(const append8_args &a, int gl, int
 
 // The blocks of one side, keys or values: `groups` of them share a chunk's heads, `each` of these a block.
 struct append8_side {
-    unsigned blocks;
+    int64_t blocks;
     int gl, groups, each;
 };
 // Blocks of keys, of values, and of queries, W elements of both of which are accessed at once.  LONG: blocks of the cache have more
@@ -448,16 +448,16 @@ template <class T, int W, bool PAIRS> static int append8_vector(pq_ctx *ctx, con
         // (as many blocks as the chip holds, four waves on a SIMD, half of them for keys: fewer heads each begin more often)
         const int64_t chunks = (a.in.ntokens + tokens - 1) / tokens, held = ctx->num_cu * (1024 / threads) / 2, most = (held + chunks - 1) / chunks;
         const int each = most >= heads ? 1 : most <= 1 ? heads : (int)((heads + most - 1) / most), groups = (heads + each - 1) / each;
-        const append8_side s = {(unsigned)(chunks * groups), lanes, groups, each};
-        return chunks * groups > INT_MAX / 4 ? append8_side{0, 0, 0, 0} : s;
+        return append8_side{chunks * groups, lanes, groups, each};
     };
     const append8_side keys = side(key_gl), values = side(gl);
     const int64_t queries = (a.in.ntokens * a.in.q_heads * gl + APPEND_THREADS - 1) / APPEND_THREADS;
-    if (keys.groups == 0 || values.groups == 0 || queries > INT_MAX / 4) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
     // Up to 96 MiB of queries in the same launch: 4099 tokens of 12 heads of 80 dimensions 29 us, 36 with a launch of their own.  More of
     // them want the waves that this kernel's registers do not leave (16 384 tokens of 32 heads of 128, bf16: 111 and 100 us).
     const bool merged = a.in.ntokens * a.in.q_heads * a.cache.dim * (int64_t)sizeof(T) <= (int64_t)96 << 20;
-    const unsigned grid = keys.blocks + values.blocks + (merged ? (unsigned)((queries * APPEND_THREADS + threads - 1) / threads) : 0);
+    const int64_t all = keys.blocks + values.blocks + (merged ? (queries * APPEND_THREADS + threads - 1) / threads : 0);
+    if (!grid_fits(all, threads) || !grid_fits(queries, APPEND_THREADS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
+    const unsigned grid = (unsigned)all;
     if (a.cache.block_size > threads / key_gl) kv_append8_kernel<T, W, PAIRS, APPEND8_MOST, true><<<grid, threads, 0, ctx->stream>>>(a, keys, values);
     else if (threads > APPEND_THREADS) kv_append8_kernel<T, W, PAIRS, APPEND8_MOST, false><<<grid, threads, 0, ctx->stream>>>(a, keys, values);
     else kv_append8_kernel<T, W, PAIRS, APPEND_THREADS, false><<<grid, threads, 0, ctx->stream>>>(a, keys, values);
@@ -489,7 +489,7 @@ template <class T, bool PAIRS> static int append8_typed(pq_ctx *ctx, const appen
     }
     constexpr int WAVES = APPEND_THREADS / 64;
     const int64_t queries = (a.in.ntokens * a.in.q_heads + WAVES - 1) / WAVES, items = (a.in.ntokens * 2 * a.cache.heads + WAVES - 1) / WAVES;
-    if (queries + items > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
+    if (!grid_fits(queries + items, APPEND_THREADS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
     kv_append8_general_kernel<T, PAIRS><<<(unsigned)(queries + items), APPEND_THREADS, 0, ctx->stream>>>(a, (unsigned)queries);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;

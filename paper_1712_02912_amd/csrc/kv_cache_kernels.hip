@@ -178,7 +178,7 @@ template <class T, int V, bool PAIRS> static int append_vector(pq_ctx *ctx, cons
     int gl = 1;
     while (gl < a.cache.dim / (2 * V)) gl *= 2;
     const int64_t grid = (a.ntokens * a.rows * gl + APPEND_THREADS - 1) / APPEND_THREADS;
-    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
+    if (!grid_fits(grid, APPEND_THREADS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
     kv_append_kernel<T, V, PAIRS><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a, gl);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;
@@ -209,7 +209,7 @@ template <class T, bool PAIRS> static int append_typed(pq_ctx *ctx, const append
         if (v >= 4) return append_vector<T, 4, PAIRS>(ctx, a);
     }
     const int64_t grid = (a.ntokens * a.rows + APPEND_THREADS / 64 - 1) / (APPEND_THREADS / 64);
-    if (grid > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
+    if (!grid_fits(grid, APPEND_THREADS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_append: %lld tokens in one call", (long long)a.ntokens);
     kv_append_general_kernel<T, PAIRS><<<(int)grid, APPEND_THREADS, 0, ctx->stream>>>(a);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;

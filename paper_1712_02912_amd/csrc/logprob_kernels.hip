@@ -312,8 +312,10 @@ template <class T> static int logprobs_typed(pq_ctx *ctx, const logprob_args &a)
     // Few rows: more threads for each, so long as all of them have logits (8 rows of 32 000, bf16: 10.0 us, 12.4 with 256 threads; 256 rows
     // of 131 072: 20 and 29 us; but 300 rows of 50 021: 18.6 and 18.1 us).  Long rows: fewer ends, which are not hidden (4096 rows of
     // 131 072, bf16: 195 us, 204 with 256 threads; of 32 000 it is 66 and 60 us).
-    if (a.rows <= ctx->num_cu && a.vocab >= 1024 * E) token_logprobs_kernel<T, 1024, BATCH><<<a.rows, 1024, 0, ctx->stream>>>(a);
-    else if (a.vocab >= 65536) token_logprobs_kernel<T, 512, BATCH><<<a.rows, 512, 0, ctx->stream>>>(a);
+    const int threads = a.rows <= ctx->num_cu && a.vocab >= 1024 * E ? 1024 : a.vocab >= 65536 ? 512 : 256;
+    if (!grid_fits(a.rows, threads)) return fail(ctx, PQ_EUNSUPPORTED, "token_logprobs: %d rows in one call", a.rows);
+    if (threads == 1024) token_logprobs_kernel<T, 1024, BATCH><<<a.rows, 1024, 0, ctx->stream>>>(a);
+    else if (threads == 512) token_logprobs_kernel<T, 512, BATCH><<<a.rows, 512, 0, ctx->stream>>>(a);
     else token_logprobs_kernel<T, 256, BATCH><<<a.rows, 256, 0, ctx->stream>>>(a);
     PQ_HIP(ctx, hipGetLastError());
     return PQ_OK;

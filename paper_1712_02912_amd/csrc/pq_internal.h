@@ -83,6 +83,8 @@ static inline void note_plain_scan(pq_ctx *ctx, const char *name, int queries_pe
     ctx->stat_onehot = nullptr;
 }
 
+// A grid has less than 2^32 threads along an axis (of one that has more the remainder alone runs, without an error).
+static inline bool grid_fits(int64_t blocks, int threads) { return blocks <= (int64_t)UINT32_MAX / threads; }
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // ---- launchers implemented in the kernel files -------------------------------------

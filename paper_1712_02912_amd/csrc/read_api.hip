@@ -65,6 +65,7 @@ int check_append(pq_ctx *ctx, const char *who, const append_call &c, int dim, si
     if (c.q_heads < 0 || c.ntokens < 0 || c.rot < 0 || c.max_positions < 0) return fail(ctx, PQ_EINVAL, "%s: bad size", who);
     if (c.rot % 2 != 0 || c.rot > dim) return fail(ctx, PQ_ESHAPE, "%s: rot=%d of dim=%d", who, c.rot, dim);
     if (!(c.eps >= 0.f)) return fail(ctx, PQ_EINVAL, "%s: eps must not be negative", who);
+    if (c.ntokens > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "%s: %lld tokens in one call", who, (long long)c.ntokens);
     if (c.ntokens == 0) return PQ_OK;
     if (const int rc = check_heads(ctx, who, "keys", c.k, e)) return rc;
     if (const int rc = check_heads(ctx, who, "values", c.v, e)) return rc;

@@ -826,6 +826,7 @@ template <class T> __global__ __launch_bounds__(SAMPLE_THREADS) void sample_join
 }
 
 template <class T> static int sample_typed(pq_ctx *ctx, const sample_args &a, int rows) {
+    if (!grid_fits(rows, SAMPLE_THREADS)) return fail(ctx, PQ_EUNSUPPORTED, "sample_tokens: %d rows in one call", rows);
     // Rows without filters that leave half of the compute units idle are drawn in parts of 8192 tokens or more (33 rows of 50 021:
     // 11.8 us in parts, 14.1 us by a block each; 8 rows of 131 072: 12.1 and 22.9 us).  Sharing the last pass of rows with
     // filters was no gain: 256 rows of 131 072 took 97 us with it, 73 us without.

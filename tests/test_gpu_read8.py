@@ -637,6 +637,32 @@ def test_attention_refusals(ctx):
         ctx.pq_kv_attention8(q, cache, cache.transpose(2, 3), scales, scales, table, cu, kv, 1)
 
 
+@pytest.mark.parametrize("dim,dtype,tokens", [(2, F32, 2 ** 25 + 4), (64, BF16, 2 ** 29)])
+def test_append_of_more_tokens_than_a_launch_takes(ctx, dim, dtype, tokens):
+    x = torch.ones((1, 1, dim), dtype=dtype, device="cuda").expand(tokens, 1, dim)
+    positions, slots = torch.zeros(tokens, dtype=torch.int32, device="cuda"), torch.full((tokens,), -1, dtype=torch.int64, device="cuda")
+    cache = torch.zeros((2, 4, 1, dim), device="cuda").to(E4M3)
+    with pytest.raises(binding.PqError, match="kv_append8") as e:
+        ctx.pq_kv_append8(None, x, x, positions, slots, cache, cache, *torch.ones((2, 2, 1), device="cuda"))
+    assert e.value.code == -3
+    with pytest.raises(binding.PqError, match="kv_append") as e:
+        ctx.pq_kv_append(None, x, x, positions, slots, *torch.zeros((2, 2, 4, 1, dim), dtype=dtype, device="cuda"))
+    assert e.value.code == -3
+
+
+@pytest.mark.parametrize("dim,dtype,tokens,requests", [(2, F32, 2 ** 24, 1), (64, BF16, 1, 2 ** 24), (64, BF16, 40, 2 ** 24)])
+def test_attention_of_more_rows_than_a_launch_takes(ctx, dim, dtype, tokens, requests):
+    i32 = dict(dtype=torch.int32, device="cuda")
+    q, cache, ones = torch.ones((tokens, 1, dim), dtype=dtype, device="cuda"), torch.zeros((2, 16, 1, dim), device="cuda"), torch.ones((2, 1), device="cuda")
+    where = (torch.zeros((requests, 1), **i32), torch.zeros(requests + 1, **i32), torch.zeros(requests, **i32), tokens)
+    with pytest.raises(binding.PqError, match="kv_attention") as e:
+        ctx.pq_kv_attention8(q, cache.to(E4M3), cache.to(E4M3), ones, ones, *where)
+    assert e.value.code == -3
+    with pytest.raises(binding.PqError, match="kv_attention") as e:
+        ctx.pq_kv_attention(q, cache.to(dtype), cache.to(dtype), *where)
+    assert e.value.code == -3
+
+
 # ---- log-probabilities ------------------------------------------------------------------------------------------------
 def check_logprobs(ctx, logits, tokens, top):
     """fp32 sums of up to 2^20 terms in parts of at most 2^12, each term off by a few units and by its distance from the maximum (up
@@ -679,6 +705,22 @@ def test_logprobs(ctx, dtype, vocab, top):
 def test_logprobs_of_many_rows(ctx, dtype, rows):
     r = np.random.default_rng(rows)
     check_logprobs(ctx, rows_of(r, rows, 1003, dtype), r.integers(-1, 1005, rows), 7)
+
+
+def test_logprobs_of_more_rows_than_a_launch_takes(ctx):
+    """The most rows that 2^32 - 1 threads hold, all of them answered, and one more."""
+    rows = 2 ** 24 - 1
+    logits = torch.tensor([[1.0, 2.0, -1.0]], device="cuda").expand(rows + 1, 3)
+    want = host(ctx.pq_token_logprobs(logits[:1], top=1)[4])[0, 0]
+    out = (None, None, None, torch.full((rows, 1), -7, device="cuda"), torch.zeros((rows, 1), device="cuda"))
+    ctx.pq_token_logprobs(logits[:rows], top=1, out=out)
+    assert bool((out[3] == 1).all()) and bool((out[4] == float(want)).all())
+    with pytest.raises(binding.PqError, match="token_logprobs") as e:
+        ctx.pq_token_logprobs(logits, top=1)
+    assert e.value.code == -3
+    with pytest.raises(binding.PqError, match="sample_tokens") as e:
+        ctx.pq_sample_tokens(logits, None)
+    assert e.value.code == -3
 
 
 def test_logprobs_of_the_largest_vocabulary(ctx):
