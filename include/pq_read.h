@@ -146,8 +146,9 @@ int pq_kv_append8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const pq
                   void *q_out);
 
 /* pq_kv_attention over a cache of 8 bits: keys and values are what its elements stand for; q rows and out are of type elem, the other
- * arguments and all rules as there.  No element is rounded before the products (what they stand for fits 16 bits; for f16 if it is below
- * 2^17 and, on the matrix cores, a multiple of 2^-23, to which others are rounded).
+ * arguments and all rules as there.  What elements stand for must be below 2^128, for f16 below 2^17 (more counts as infinite, and may miss
+ * rows that see it).  No element is rounded before the products (16 bits hold it; in f16, on the matrix cores, those that are no multiple
+ * of 2^-23 are rounded to one, and what is below 2^-126 may count as 0).
  * dim 64, 96, 128 or 256 with f16 or bf16, rows of the queries, the cache and out on 16 bytes, takes the matrix cores, any other
  * even dim <= 512 and f32 a general kernel. */
 int pq_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const pq_heads *q, int q_heads, int64_t ntokens,

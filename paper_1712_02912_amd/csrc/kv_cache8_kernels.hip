@@ -1,6 +1,4 @@
 // The append to a paged cache of 8 bits (pq_kv_append8).
-#include <limits.h>
-
 #include "e4m3.h"
 #include "kv_append.h"
 #include "wave_sums.h"
