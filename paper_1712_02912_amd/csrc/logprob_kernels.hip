@@ -18,10 +18,11 @@ struct logprob_args {
 // A logit as its order counts it: NaN as -inf, one zero.
 template <class T> __device__ __forceinline__ float logit_of(T v) { return fmaxf((float)v, -INFINITY) + 0.f; }
 // One whole number for each token of a row, in the order of its logits, of equal ones the smaller index first; 0 is none.
-__device__ __forceinline__ uint64_t order_key(float v, int i) {
+__device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t b = __builtin_bit_cast(uint32_t, v);
-    return (uint64_t)(b >> 31 ? ~b : b | 0x80000000u) << 20 | (uint32_t)((1 << 20) - 1 - i);
+    return b >> 31 ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ uint64_t order_key(float v, int i) { return (uint64_t)key_of(v) << 20 | (uint32_t)((1 << 20) - 1 - i); }
 __device__ __forceinline__ int key_token(uint64_t key) { return (1 << 20) - 1 - (int)(key & ((1 << 20) - 1)); }
 __device__ __forceinline__ float key_logit(uint64_t key) {
     const uint32_t b = (uint32_t)(key >> 20);
@@ -52,6 +53,8 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // off by less than one.  Other rows are summed once more, by differences.  (A power of two: -WILD times log2(e) is not rounded.)
 constexpr float WILD = 0x1p20f;
 
+// the lowest bit of a logit, as fp32, that its type has (f16 numbers have 10 bits of fraction, bf16 7)
+template <class T> constexpr int LEAST_BIT = __is_same(T, float) ? 0 : __is_same(T, _Float16) ? 13 : 16;
 constexpr int STRETCHES = 16;  // parts of its logits that a thread keeps the maximum of
 constexpr int GROUPS = 256;    // groups of threads whose maxima give the limit
 constexpr int CANDIDATES = 1024, LISTED = 512;   // logits that are sorted, stretches that are read again
@@ -62,7 +65,8 @@ constexpr int CANDIDATES = 1024, LISTED = 512;   // logits that are sorted, stre
 // The likeliest tokens cost the pass one store of a maximum for each batch.  `top` groups of threads have a maximum of at
 // least the limit, the (top)th largest of the groups' maxima, so no smaller logit is listed, and nearly all that are as large are: for 20
 // of 256 groups 20.8 are expected.  The few stretches that reach the limit are read again, their logits of at least the limit are
-// sorted by counting.  Rows of too many (equal ones, or the largest all with one thread) are searched `top` times.
+// sorted by counting.  Of too many (equal ones, or the largest all with one thread) those above the limit
+// are, by one more pass, and the rest is searched by a pass for each different logit.
 //
 // Bound by memory where rows are many: 4096 rows of 131 072, bf16, 20 listed: 1.07 GB in 195 to 199 us = 5.4 TB/s; 1024 of these in f32
 // without a list: 537 MB in 93 us = 5.8 TB/s.  A logit takes a conversion, a bound, half a maximum, two multiply-adds, an addition and a
@@ -187,7 +191,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
     if (a.top > 0) {
         float group = own_high;
         for (int d = THREADS / GROUPS / 2; d > 0; d /= 2) group = fmaxf(group, __shfl_xor(group, d));
-        if (tid % (THREADS / GROUPS) == 0) group_keys[tid / (THREADS / GROUPS)] = (uint32_t)(order_key(group, 0) >> 36);
+        if (tid % (THREADS / GROUPS) == 0) group_keys[tid / (THREADS / GROUPS)] = key_of(group);
     }
     if (tid == 0) nstretches = ncandidates = 0;
     __syncthreads();
@@ -201,19 +205,19 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
         wave_moment[wave] = moment;
         wave_before[wave] = before;
     }
-    // the limit, by the upper 16 bits of the groups' maxima in their order: as high as `top` groups reach it
+    // the limit, by the bits of the groups' maxima in their order (those that T has): as high as `top` groups reach it
     if (a.top > 0 && tid < 64) {
         uint32_t keys[GROUPS / 64], found = 0;
 #pragma unroll
         for (int i = 0; i < GROUPS / 64; ++i) keys[i] = group_keys[64 * i + tid];
-        for (int bit = 15; bit >= 0; --bit) {
+        for (int bit = 31; bit >= LEAST_BIT<T>; --bit) {
             const uint32_t next_key = found | 1u << bit;
             int reach = 0;
 #pragma unroll
             for (int i = 0; i < GROUPS / 64; ++i) reach += __popcll(__ballot(keys[i] >= next_key));
             if (reach >= a.top) found = next_key;
         }
-        if (tid == 0) limit_at = key_logit((uint64_t)found << 36);
+        if (tid == 0) limit_at = key_logit((uint64_t)found << 20);
     }
     __syncthreads();
     sum = moment = 0.f;
@@ -256,11 +260,13 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
 
     const float limit = fmaxf(limit_at, -0x1.fffffep19f);   // (above -WILD: of what lies from there on down, see the end)
     auto offer = [&](float v, int i) {
-        if (!(v >= limit)) return;
         const int n = atomicAdd(&ncandidates, 1);
         if (n < CANDIDATES) candidates[n] = order_key(v, i);
     };
-    if (odd >= 0) offer(logit_of(row[odd]), odd);
+    auto look = [&](float v, int i) {
+        if (v >= limit) offer(v, i);
+    };
+    if (odd >= 0) look(logit_of(row[odd]), odd);
     if (own_high >= limit)
 #pragma unroll
         for (int s = 0; s < STRETCHES; ++s)
@@ -275,12 +281,24 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
         if (j >= nvec) continue;
         const vec v = vectors[j];
 #pragma unroll
-        for (int e = 0; e < E; ++e) offer(logit_of(v.v[e]), head + j * E + e);
+        for (int e = 0; e < E; ++e) look(logit_of(v.v[e]), head + j * E + e);
     }
     __syncthreads();
-    uint64_t last = ~0ull;
+    bool listed = ncandidates <= CANDIDATES && nstretches <= LISTED;
+    if (!listed) {   // too many are as large as the limit: those that are larger
+        __syncthreads();
+        if (tid == 0) ncandidates = 0;
+        __syncthreads();
+        for (int i = tid; i < a.vocab; i += THREADS) {
+            const float v = logit_of(row[i]);
+            if (v > limit) offer(v, i);
+        }
+        __syncthreads();
+        listed = ncandidates <= CANDIDATES;
+    }
+    uint32_t last = ~0u;   // the least logit of those that are done
     int done = 0;
-    if (ncandidates <= CANDIDATES && nstretches <= LISTED) {
+    if (listed) {
         const int n = ncandidates;
         for (int k = tid; k < n; k += THREADS) {
             const uint64_t mine = candidates[k];
@@ -289,19 +307,43 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
             if (place < a.top) put(place, mine);
         }
         if (n >= a.top) return;
-        for (int i = 0; i < n; ++i) last = min(last, candidates[i]);
+        for (int i = 0; i < n; ++i) last = min(last, (uint32_t)(candidates[i] >> 20));
         done = n;
     }
-    // too many candidates, or fewer than are listed: the rest one after the other
-    for (; done < a.top && last; ++done) {
+    // the rest one logit after the other, its tokens in their order
+    while (done < a.top) {
         uint64_t best = 0;
+        int times = 0;
         for (int i = tid; i < a.vocab; i += THREADS) {
             const float v = logit_of(row[i]);
-            const uint64_t key = order_key(v, i);
-            if (v > -INFINITY && key < last && key > best) best = key;
+            const uint32_t key = key_of(v), so_far = (uint32_t)(best >> 20);
+            if (v == -INFINITY || key >= last || key < so_far) continue;
+            times = key == so_far ? times + 1 : 1;
+            if (key > so_far) best = order_key(v, i);
         }
-        last = block_total<THREADS, op_larger>(best);
-        if (tid == 0) put(done, last);
+        const uint64_t all = block_total<THREADS, op_larger>(best);
+        if (!all) break;
+        last = (uint32_t)(all >> 20);
+        times = block_total<THREADS, op_add>((uint32_t)(best >> 20) == last ? times : 0);
+        if (times == 1) {
+            if (tid == 0) put(done, all);
+            ++done;
+            continue;
+        }
+        for (int i0 = key_token(all), until = min(a.top, done + times); done < until && i0 < a.vocab; i0 += THREADS) {
+            const int i = i0 + tid;
+            const bool is = i < a.vocab && key_of(logit_of(row[i])) == last;
+            const uint64_t same = __ballot(is);
+            __syncthreads();   // (what was read here before is)
+            if (lane == 0) wave_before[wave] = __popcll(same);
+            __syncthreads();
+            int place = done + __popcll(same & ((1ull << lane) - 1));
+            for (int w = 0; w < WAVES; ++w) {
+                if (w < wave) place += wave_before[w];
+                done += wave_before[w];
+            }
+            if (is && place < a.top) put(place, order_key(key_logit(all), i));
+        }
     }
     for (int k = done + tid; k < a.top; k += THREADS) put(k, 0);
 }

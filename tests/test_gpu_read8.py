@@ -744,6 +744,24 @@ def test_logprobs_of_equal_and_ordered_logits(ctx, dtype, vocab, top):
     check_logprobs(ctx, dev(np.stack(rows), dtype), r.integers(0, vocab, len(rows)), top)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [3000, 70001])
+@pytest.mark.parametrize("top", [1, 50, 128])
+def test_logprobs_of_close_logits(ctx, dtype, vocab, top):
+    """Logits that lie close together, and a few that stand out of thousands of equal ones, in runs, far apart, in pairs."""
+    r = np.random.default_rng(vocab)
+    l = np.stack([r.uniform(0.99, 1, vocab), 20 + r.standard_normal(vocab) * 0.01, -r.uniform(300, 301, vocab)] + [np.full(vocab, 0.25)] * 6)
+    out = r.permutation(vocab)
+    l[3, out[:60]] = 1 + np.arange(60) / 16
+    l[4, out[:60]] = 1 + np.arange(60) // 2 / 16
+    l[5, ::300] = 2.0
+    l[6, vocab // 2:] = -1.0
+    l[7, out[:40]], l[7, vocab // 3:vocab // 3 + 1500] = 3 + np.arange(40) / 16, 2.5
+    l[8] = -3e4
+    l[8, out[:30]] = -5 - np.arange(30) / 16
+    check_logprobs(ctx, dev(l, dtype), r.integers(0, vocab, 9), top)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("vocab", [40, 20000])
 def test_logprobs_of_special_rows(ctx, dtype, vocab):
