@@ -217,6 +217,8 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
             for (int i = 0; i < GROUPS / 64; ++i) reach += __popcll(__ballot(keys[i] >= next_key));
             if (reach >= a.top) found = next_key;
         }
+        // (the bits that T has not are ones in the key of a negative number: with zeros the limit would lie below the logit that it is)
+        if (!(found >> 31)) found |= (1u << LEAST_BIT<T>) - 1;
         if (tid == 0) limit_at = key_logit((uint64_t)found << 20);
     }
     __syncthreads();
