@@ -48,6 +48,12 @@ template <int THREADS, class OP, class V> __device__ __forceinline__ V block_tot
 }
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// A reference: a logit times log2(e), rounded.  (The compiler may not take the product into what it is subtracted from: the difference of two
+// references would be one of numbers that the sums are not formed with, and rows of 30 000 off by a thousandth.)
+__device__ __forceinline__ float reference_of(float v) {
+#pragma clang fp contract(off)
+    return v * LOG2E;
+}
 // The sums are formed of logits from -WILD on (what is less, -inf and NaN count as -WILD), and hold for rows whose largest is between
 // -WILD / 2 and WILD / 2: there what was raised has weight 0, 0 times it is 0, and a reference that is a logit times log2(e), rounded, is
 // off by less than one.  Other rows are summed once more, by differences.  (A power of two: -WILD times log2(e) is not rounded.)
@@ -122,7 +128,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
         if (given) count(v, odd);
         if (v > high) {
             high = v;
-            ref = v * LOG2E;
+            ref = reference_of(v);
             const float y = fmaf(v, LOG2E, -ref), w = __builtin_amdgcn_exp2f(y);
             sum = w;
             moment = w * y;
@@ -166,7 +172,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
         }
         high = fmaxf(high, largest);
         // (summed for itself first: a long chain of additions would be off by ten times as much)
-        const float moved = high * LOG2E, by = ref - moved, shrink = __builtin_amdgcn_exp2f(by);
+        const float moved = reference_of(high), by = ref - moved, shrink = __builtin_amdgcn_exp2f(by);
         ref = moved;
         float batch_sum = 0.f, batch_moment = 0.f;
 #pragma unroll
@@ -196,7 +202,7 @@ template <class T, int THREADS, int BATCH> __global__ __launch_bounds__(THREADS)
     if (tid == 0) nstretches = ncandidates = 0;
     __syncthreads();
     for (int w = 0; w < WAVES; ++w) high = fmaxf(high, wave_high[w]);
-    const float joint = high * LOG2E, by = ref - joint, shrink = __builtin_amdgcn_exp2f(by);
+    const float joint = reference_of(high), by = ref - joint, shrink = __builtin_amdgcn_exp2f(by);
     moment = wave_total<op_add>(fmaf(sum, by, moment) * shrink);
     sum = wave_total<op_add>(sum * shrink);
     if (given) before = wave_total<op_add>(before);

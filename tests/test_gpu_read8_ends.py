@@ -56,3 +56,63 @@ def test_logprobs_of_masked_rows_take_no_pass_for_each_token(ctx, dtype, mask):
             assert np.array_equal(first[i], want) and (np.abs(lp[i] - want_lp) <= 3e-6 * (1 + np.abs(want_lp))).all()
         found.append(least_time(lambda: ctx.pq_token_logprobs(logits, top=50)))
     assert found[0] <= 2.5 * found[1], found
+
+
+def check_closely(ctx, logits, tokens, top, rows=None):
+    """As the definition has it, with bounds that masks and the size of a row's logits do not widen.
+
+    A row's sum S of weights w = exp(-d), d = distance from the largest, and M of d w: terms are off by 2 + d units (power, distance), chains
+    of up to n additions by n.  n: 64 and one for each 4096 logits; rows whose largest is beyond 2^19 are summed in more bits.  So log S is off by
+    n + 2 + D, D = M / S the mean distance, and M / S by (2 n + 4) D + D2, D2 the mean square; then come roundings of what is
+    put together."""
+    lp, ranks, entropy, first, top_lp = (None if x is None else host(x) for x in ctx.pq_token_logprobs(logits, whole(tokens, np.int64), top))
+    for r in range(len(tokens)) if rows is None else rows:
+        l = host(logits[r])
+        want_lp, rank, want_entropy, want_first, want_top = orc.logprobs(l, int(tokens[r]), top)
+        assert ranks[r] == rank and np.array_equal(first[r], want_first), r
+        high = l[~np.isnan(l)].max()
+        d = high - l[l >= high - 200]
+        w = np.exp(-d)
+        mean, square = (w @ d) / w.sum(), (w @ d ** 2) / w.sum()
+        n = 4 if abs(high) >= 2 ** 19 else 64 + len(l) / 4096
+        sure = n + 4 + mean + 2 * np.log(w.sum())
+        assert lp[r] == want_lp or abs(lp[r] - want_lp) <= HALF_UNIT * (sure + 2 * abs(want_lp)), (r, lp[r], want_lp)
+        assert abs(entropy[r] - want_entropy) <= HALF_UNIT * (sure + (2 * n + 4) * mean + square + 2 * want_entropy), (r, entropy[r], want_entropy)
+        some = np.isfinite(want_top)
+        assert np.array_equal(top_lp[r][~some], want_top[~some])
+        assert (np.abs(top_lp[r][some] - want_top[some]) <= HALF_UNIT * (sure + 2 * np.abs(want_top[some]))).all(), r
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+@pytest.mark.parametrize("vocab", [9, 3000, 40000, 2 ** 20 - 1])
+@pytest.mark.parametrize("base", [21.0, -300.0, 30003.0, -500000.0])
+def test_logprobs_of_rows_away_from_zero(ctx, rows, vocab, base):
+    """One logit over equal ones, and logits of all distances, away from zero: as exact as rows next to it."""
+    r = np.random.default_rng(vocab)
+    for low in (np.full(vocab, 9.875), np.full(vocab, 2.375), r.integers(0, 200, vocab) / 8):
+        l = base - low
+        l[vocab // 2] = base
+        logits = dev(l[None], F32).expand(rows, vocab)
+        check_closely(ctx, logits, np.full(rows, vocab - 1), 3, rows=[0, rows - 1])
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [7, 600, 40000])
+@pytest.mark.parametrize("mask", [-3e4, -6e5, -1.1e6, -1e9, -1e30, -3e38])
+def test_logprobs_of_logits_beside_a_mask(ctx, dtype, vocab, mask):
+    """A mask's size, which the results do not depend on, is not in the bounds either."""
+    if dtype == F16:
+        mask = max(mask, -65504.0)
+    r = np.random.default_rng(vocab)
+    l = r.standard_normal((6, vocab)) * 3
+    l[0, : vocab // 2] = mask
+    l[1, vocab // 3:] = mask
+    l[2, r.random(vocab) < 0.9] = mask
+    l[3, r.random(vocab) < 0.5] = -np.inf
+    l[3, r.random(vocab) < 0.5] = mask
+    l[4] += 100
+    l[4, ::2] = mask
+    l[5, 1:] = mask
+    logits = dev(l, dtype)
+    for tokens in ([0, vocab - 1, 3, 5, 1, 0], [vocab - 1, 0, 1, 2, 3, 1]):
+        check_closely(ctx, logits, tokens, 5)
