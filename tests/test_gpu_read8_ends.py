@@ -96,6 +96,14 @@ def test_logprobs_of_rows_away_from_zero(ctx, rows, vocab, base):
         check_closely(ctx, logits, np.full(rows, vocab - 1), 3, rows=[0, rows - 1])
 
 
+@pytest.mark.parametrize("rows", [3, 300])
+@pytest.mark.parametrize("vocab", [9, 3000, 40000, 2 ** 20 - 1])
+@pytest.mark.parametrize("base", [2.0 ** 20, -2.0 ** 20 + 64, 2.0 ** 19, -2.0 ** 19 - 8])
+def test_logprobs_of_rows_far_from_zero(ctx, rows, vocab, base):
+    """The same a million from zero, where rows are summed a second time."""
+    test_logprobs_of_rows_away_from_zero(ctx, rows, vocab, base)
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("vocab", [7, 600, 40000])
 @pytest.mark.parametrize("mask", [-3e4, -6e5, -1.1e6, -1e9, -1e30, -3e38])
