@@ -37,15 +37,16 @@ template <class T, class C> __global__ __launch_bounds__(64 * GENERAL_WAVES) voi
     float top = -INFINITY, sum = 0.f, part[GENERAL_DIM / 64] = {};
     for (int base = from + wave * 64; base <= at; base += 64 * GENERAL_WAVES) {
         const int j = base + lane;
-        float s = -INFINITY, v_scale = 1.f;
+        float s = -INFINITY, v_scale = 1.f;   // (a scale goes to the element, which stays exact; with a sum or a weight it may leave fp32)
         int64_t block = 0;
         int place = 0;
         if (j <= at) {
             attention_place(a, r, j, block, place);
             const C *k = (const C *)a.cache.keys + block * a.cache.key_strides[0] + place * a.cache.key_strides[1] + kvh * a.cache.key_strides[2];
             s = 0.f;
-            for (int i = 0; i < dim; ++i) s += q[i] * (float)k[i];
-            s = s * block_scale<C>(a.k_scales, block, a.cache.heads, kvh) * a.scale_log2;
+            const float k_scale = block_scale<C>(a.k_scales, block, a.cache.heads, kvh);
+            for (int i = 0; i < dim; ++i) s += q[i] * ((float)k[i] * k_scale);
+            s = s * a.scale_log2;
             v_scale = block_scale<C>(a.v_scales, block, a.cache.heads, kvh);
         }
         float high = s;
@@ -60,11 +61,11 @@ template <class T, class C> __global__ __launch_bounds__(64 * GENERAL_WAVES) voi
         for (int e = 0; e < GENERAL_DIM / 64; ++e) part[e] *= shrink;
         const int count = min(64, at - base + 1);
         for (int l = 0; l < count; ++l) {
-            const float wl = __shfl(w * v_scale, l);
+            const float wl = __shfl(w, l), vl = __is_same(C, e4m3) ? __shfl(v_scale, l) : 1.f;
             const C *v = (const C *)a.cache.values + __shfl((long long)row, l) + kvh * a.cache.value_strides[2];
 #pragma unroll
             for (int e = 0; e < GENERAL_DIM / 64; ++e)
-                if (e * 64 + lane < dim) part[e] += wl * (float)v[e * 64 + lane];
+                if (e * 64 + lane < dim) part[e] += wl * ((float)v[e * 64 + lane] * vl);
         }
     }
     for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);

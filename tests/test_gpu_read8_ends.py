@@ -7,8 +7,9 @@ import pytest
 import torch
 
 from oracle import read8_oracle as orc
+from oracle import read_oracle
 from paper_1712_02912_amd import binding
-from test_gpu_read8 import BF16, F16, F32, dev, host, whole
+from test_gpu_read8 import BF16, E4M3, F16, F32, attention_bound, dev, host, make_cache, whole
 
 pytestmark = pytest.mark.gpu
 
@@ -22,6 +23,43 @@ def ctx():
     torch.cuda.synchronize()
     c.close()
     gc.collect()
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype,dim", [(F32, 64), (F32, 80), (BF16, 64), (BF16, 80)])
+def test_attention_of_keys_of_the_least_scale(ctx, new, dtype, dim):
+    """Large queries and small keys: products of a query with the keys' codes alone would leave fp32."""
+    r = np.random.default_rng(new)
+    tables, kc, vc, _, vs, keys, values = make_cache(r, [new + 77, new], 2, dim, 16, 0)
+    ks = torch.full_like(vs, 2.0 ** -126)
+    keys = host(kc) * 2.0 ** -126
+    q = dev(r.standard_normal((2 * new, 4, dim)) * 1e37, dtype)
+    scale, cu, kv = 0.1 * dim ** -0.5, np.array([0, new, 2 * new]), np.array([new + 77, new])
+    out, lse = ctx.pq_kv_attention8(q, kc, vc, ks, vs, dev(tables), whole(cu), whole(kv), new, scale=scale)
+    want, want_lse, spread = read_oracle.attention(host(q), keys, values, tables, cu, kv, scale, 0)
+    bound, fp32 = attention_bound(dtype, host(q), keys, spread, want, scale, 0, dim)
+    assert (np.abs(host(out) - want) <= bound).all()
+    assert (np.abs(host(lse) - want_lse) <= 2 * fp32 + 1e-6 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("dtype,dim", [(F32, 64), (F32, 80), (BF16, 80)])
+def test_attention_adds_up_small_weights_of_a_small_scale(ctx, dtype, dim):
+    """One key of a large weight and value 0, thousands of exp(-18) of it whose values are 256 times 2^-120: a weight times the scale alone has
+    three bits left in fp32."""
+    count, scale = 8191, 2.0 ** -120
+    tables = np.arange(512, dtype=np.int32)[None]
+    keys, values = (np.zeros((512, 16, 1, dim)) for _ in range(2))
+    keys.reshape(-1, dim)[1:, 0], values.reshape(-1, dim)[1:] = -18.0, 256.0
+    q = np.zeros((1, 1, dim))
+    q[0, 0, 0] = 1.0
+    ones, small = torch.ones((512, 1), device="cuda"), torch.full((512, 1), scale, device="cuda")
+    out, _ = ctx.pq_kv_attention8(dev(q, dtype), dev(keys, F32).to(E4M3), dev(values, F32).to(E4M3), ones, small, dev(tables), whole([0, 1]), whole([8192]),
+                                  1, scale=1.0)
+    term = np.exp(-18.0) * 256 * scale
+    want = count * term / (1 + count * np.exp(-18.0))
+    # each addition of a term is off by half a unit of the sum, or half of fp32's least step; rounding of the result
+    assert (np.abs(host(out) - want) <= want * (8192 * HALF_UNIT + 2.0 ** -150 / term + (2.0 ** -8 if dtype == BF16 else 0.0))).all()
 
 
 # ---- log-probabilities ------------------------------------------------------------------------------------------------
