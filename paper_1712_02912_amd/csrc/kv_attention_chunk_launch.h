@@ -52,7 +52,7 @@ template <class T, class C, int D, int WAVES> static int chunk_run(pq_ctx *ctx, 
     if (splits > most) splits = most;
     chunk_split split = {splits < 1 ? 1 : (int)splits, some_few, nullptr, nullptr};
     const int64_t chunk_blocks = indexes * a.cache.heads;
-    if (!grid_fits(chunk_blocks * split.splits + (1 << 20), 64 * WAVES) || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
+    if (!grid_fits(chunk_blocks, 64 * WAVES) || rows > INT_MAX) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %lld rows in one call", (long long)rows);
     const size_t slots = split.splits > 1 ? (size_t)rows * split.splits : 0, ws = slots * (D + 2) * sizeof(float);
     size_t ws_at = 0;
     few_line line = {};
@@ -67,10 +67,9 @@ template <class T, class C, int D, int WAVES> static int chunk_run(pq_ctx *ctx, 
         split.stats = split.parts + slots * D;
     }
     const int joins = split.splits > 1 ? (int)((rows + JOIN_ROWS - 1) / JOIN_ROWS) : 0, slices = some_few ? few_slices(line, FEW_ROWS, JOIN_ROWS) : 0;
-    const int64_t few_blocks = (int64_t)a.nreq * a.cache.heads * slices;
-    if (!grid_fits(few_blocks + joins, 64 * JOIN_ROWS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", a.nreq);
+    const int64_t few_blocks = (int64_t)a.nreq * a.cache.heads * slices, all = chunk_blocks * split.splits + line.blocks;   // (of both kinds)
+    if ((some_few && !grid_fits(all, 64 * WAVES)) || !grid_fits(few_blocks + joins, 64 * JOIN_ROWS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_attention: %d requests in one call", a.nreq);
     if (some_few) {
-        const int64_t all = chunk_blocks * split.splits + line.blocks;
         kv_attention_mixed_kernel<T, C, D, WAVES><<<(unsigned)all, 64 * WAVES, 0, ctx->stream>>>(a, split, (int)chunk_blocks, line);
         kv_attention_mixed_join_kernel<T, C, D><<<(unsigned)(few_blocks + joins), 64 * JOIN_ROWS, 0, ctx->stream>>>(a, split, (int)few_blocks, slices, line);
     } else {

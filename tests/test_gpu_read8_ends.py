@@ -62,6 +62,29 @@ def test_attention_adds_up_small_weights_of_a_small_scale(ctx, dtype, dim):
     assert (np.abs(host(out) - want) <= want * (8192 * HALF_UNIT + 2.0 ** -150 / term + (2.0 ** -8 if dtype == BF16 else 0.0))).all()
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("requests", [2 ** 24 - 2, 2 ** 24 - 2 ** 19])
+def test_attention_of_as_many_requests_as_a_launch_takes(ctx, eight, requests):
+    """Chunks of so many requests, all but one of them empty: 2^32 threads are not passed, so the rows are written."""
+    new, dim, heads = 40, 64, 1
+    r = np.random.default_rng(1)
+    tables, *cache, keys, values = make_cache(r, [new + 9], heads, dim, 16)
+    q = dev(r.standard_normal((new, 2, dim)), BF16)
+    if not eight:
+        cache = [dev(np.nan_to_num(x), BF16) for x in (keys, values)]
+        keys, values = (host(x) for x in cache)
+    cu = torch.zeros(requests + 1, dtype=torch.int32, device="cuda")
+    cu[-1] = new
+    kv = torch.zeros(requests, dtype=torch.int32, device="cuda")
+    kv[-1] = new + 9
+    table = torch.full((requests, tables.shape[1]), -1, dtype=torch.int32, device="cuda")
+    table[-1] = dev(tables[0])
+    out, lse = (ctx.pq_kv_attention8 if eight else ctx.pq_kv_attention)(q, *cache, table, cu, kv, new)
+    want, want_lse, spread = read_oracle.attention(host(q), keys, values, tables, np.array([0, new]), np.array([new + 9]), dim ** -0.5, 0)
+    bound, fp32 = attention_bound(BF16, host(q), np.nan_to_num(keys), spread, want, dim ** -0.5, new + 9, dim)
+    assert (np.abs(host(out) - want) <= bound).all() and (np.abs(host(lse) - want_lse) <= 2 * fp32 + 1e-6 * np.abs(want_lse)).all()
+
+
 # ---- log-probabilities ------------------------------------------------------------------------------------------------
 def least_time(f, calls=3, tries=5):
     """Milliseconds of a call, the least of some tries."""
