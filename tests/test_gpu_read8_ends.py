@@ -9,7 +9,7 @@ import torch
 from oracle import read8_oracle as orc
 from oracle import read_oracle
 from paper_1712_02912_amd import binding
-from test_gpu_read8 import BF16, E4M3, F16, F32, attention_bound, dev, host, make_cache, whole
+from test_gpu_read8 import BF16, E4M3, F16, F32, UNIT, attention_bound, dev, host, make_cache, whole
 
 pytestmark = pytest.mark.gpu
 
@@ -23,6 +23,63 @@ def ctx():
     torch.cuda.synchronize()
     c.close()
     gc.collect()
+
+
+# ---- append -----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dtype,dim,q_heads,heads,tokens", [(BF16, 128, 192, 1, 2048), (F16, 80, 192, 2, 3276), (F32, 64, 192, 1, 2048), (BF16, 512, 96, 2, 1024)])
+@pytest.mark.parametrize("more", [0, 1, 70])
+def test_append_of_queries_about_96_mib(ctx, dtype, pairs, dim, q_heads, heads, tokens, more):
+    """Up to 96 MiB of queries go with the keys and values, more of them by themselves: either way as the same tokens in two calls, with
+    tokens without a position, and as the definition."""
+    assert tokens * q_heads * dim * dtype.itemsize <= 96 * 2 ** 20 < (tokens + 1) * q_heads * dim * dtype.itemsize
+    tokens += more
+    r = np.random.default_rng(dim + more)
+    gen = torch.Generator(device="cuda").manual_seed(dim + more)
+    q, k, v = (torch.randn((tokens, n, dim), device="cuda", generator=gen).mul_(3).to(dtype) for n in (q_heads, heads, heads))
+    positions = r.integers(0, 50, tokens).astype(np.int32)
+    # requests of 1 to 300 tokens, each from the beginning of a block on
+    slots, at = np.empty(tokens, np.int64), 0
+    begins = []
+    while at < tokens:
+        n = min(tokens - at, int(r.integers(1, 301)))
+        begins.append(at)
+        slots[at:at + n] = (max(slots[:at], default=-16) // 16 + 1) * 16 + np.arange(n)
+        at += n
+    cut = begins[len(begins) // 2]
+    unplaced = np.array([begins[1], begins[2], cut, tokens]) - 1   # (the last tokens of requests: a run ends before them)
+    positions[unplaced] = [-1, 50, 2 ** 31 - 1, -2 ** 31]
+    blocks = int(slots.max()) // 16 + 1
+    rot = dim // 2
+    angle = r.uniform(-3, 3, (50, rot // 2))
+    cos, sin = np.cos(angle).astype(np.float32), np.sin(angle).astype(np.float32)
+    qw, kw = (r.uniform(0.5, 2, dim).astype(np.float32) for _ in range(2))
+
+    def append(parts):
+        cache = [torch.full((blocks, 16, heads, dim), 0x7f, dtype=torch.uint8, device="cuda").view(E4M3) for _ in range(2)]
+        scales = [torch.full((blocks, heads), float("nan"), device="cuda") for _ in range(2)]
+        out = torch.full((tokens, q_heads, dim), 7.0, dtype=dtype, device="cuda")
+        for a, b in parts:
+            ctx.pq_kv_append8(q[a:b], k[a:b], v[a:b], dev(positions[a:b]), dev(slots[a:b]), *cache, *scales, dev(cos), dev(sin), q_weight=dev(qw),
+                              k_weight=dev(kw), pairs=pairs, out=out[a:b])
+        return [out] + [c.view(torch.uint8) for c in cache] + [s.view(torch.int32) for s in scales]
+
+    whole_call, halves = append([(0, tokens)]), append([(0, cut), (cut, tokens)])
+    assert all(torch.equal(a, b) for a, b in zip(whole_call, halves))
+    # of the queries some tokens, against the definition
+    some = np.unique(np.concatenate([unplaced, [1, tokens - 1], r.integers(0, tokens, 5)]))
+    p = np.where((positions >= 0) & (positions < 50), positions, 0)
+    want = read_oracle.turn(host(q[some]), p[some], cos, sin, qw, 1e-6, True, pairs)
+    size = np.abs(read_oracle.turn(host(q[some]), p[some], None, None, qw, 1e-6, True, pairs)).max(axis=2, keepdims=True)
+    placed = ~np.isin(some, unplaced)[:, None, None]
+    bound = UNIT[dtype] * np.abs(want) * 1.01 + (8 + dim / 64) * HALF_UNIT * 2 * size + 2.0 ** -25 * (dtype == F16)
+    assert (np.abs(host(whole_call[0][some]) - np.where(placed, want, 0)) <= np.where(placed, bound, 0)).all()
+    # codes and scales, all of them
+    keys = read_oracle.turn(host(k), p, cos, sin, kw, float(np.float32(1e-6)), True, pairs).astype(np.float32)
+    for rows, codes, scale in zip((keys, host(v)), whole_call[1:3], whole_call[3:]):
+        values, held = np.full((blocks, 16, heads, dim), np.nan), np.full((blocks, heads), np.nan)
+        orc.store(values, held, rows, slots, ~np.isin(np.arange(tokens), unplaced))
+        assert np.array_equal(host(scale.view(F32)), held, equal_nan=True) and np.array_equal(host(codes.view(E4M3)), values, equal_nan=True)
 
 
 # ---- attention --------------------------------------------------------------------------------------------------------
