@@ -450,9 +450,10 @@ template <class T, int W, bool PAIRS> static int append8_vector(pq_ctx *ctx, con
     };
     const append8_side keys = side(key_gl), values = side(gl);
     const int64_t queries = (a.in.ntokens * a.in.q_heads * gl + APPEND_THREADS - 1) / APPEND_THREADS;
-    // Up to 96 MiB of queries in the same launch: 4099 tokens of 12 heads of 80 dimensions 29 us, 36 with a launch of their own.  More of
-    // them want the waves that this kernel's registers do not leave (16 384 tokens of 32 heads of 128, bf16: 111 and 100 us).
-    const bool merged = a.in.ntokens * a.in.q_heads * a.cache.dim * (int64_t)sizeof(T) <= (int64_t)96 << 20;
+    // Up to 64 MiB of queries in the same launch, which saves one: 32 + 8 + 8 heads of 128 dimensions, bf16, 34 MB of queries 30 us, 33 with a
+    // launch of their own, 67 MB 55 and 60; 12 heads each of 80, f16, 8 MB 25 and 30, 58 MB 147 and 147.  More of them want the waves that
+    // this kernel's registers do not leave: 98 MB of the former 79 and 74 us, 134 MB 106 and 97; 96 MB in f32 (28 + 4 + 4 heads) 60 and 57.
+    const bool merged = a.in.ntokens * a.in.q_heads * a.cache.dim * (int64_t)sizeof(T) <= (int64_t)64 << 20;
     const int64_t all = keys.blocks + values.blocks + (merged ? (queries * APPEND_THREADS + threads - 1) / threads : 0);
     if (!grid_fits(all, threads) || !grid_fits(queries, APPEND_THREADS)) return fail(ctx, PQ_EUNSUPPORTED, "kv_append8: %lld tokens in one call", (long long)a.in.ntokens);
     const unsigned grid = (unsigned)all;
