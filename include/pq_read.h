@@ -163,7 +163,8 @@ int pq_kv_attention8(pq_ctx *ctx, const pq_kv_cache8 *cache, pq_elem elem, const
  *      top_tokens [rows][top] i64, top_logprobs [rows][top] f32: the first `top` tokens of that order.
  * Each result may be NULL.  NaN counts as -inf.  If some logits are +inf, those share the probability.  Tokens outside the vocabulary
  * (padding) have log-probability -inf and rank -1.  Only tokens above -inf are listed: the rest of top_tokens is -1, of top_logprobs
- * -inf.  A row without any has entropy 0 and log-probabilities -inf.  Sums are fp32.  Requires vocab < 2^20, top <= 128, and
+ * -inf.  A row without any has entropy 0 and log-probabilities -inf.  Sums are fp32, in fp64
+ * where the largest logit is beyond 2^19 either way.  Requires vocab < 2^20, top <= 128, and
  * rows < 2^23 (more are refused where a launch does not take them: PQ_EUNSUPPORTED). */
 int pq_token_logprobs(pq_ctx *ctx, const void *logits, pq_elem elem, int64_t row_stride, int rows, int vocab, const int64_t *tokens, int top,
                       float *logprobs, int32_t *ranks, float *entropy, int64_t *top_tokens, float *top_logprobs);

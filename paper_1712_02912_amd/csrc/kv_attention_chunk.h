@@ -17,8 +17,9 @@
 //
 // Over a cache of 8 bits (C = e4m3) a tile's codes become 16-bit elements on their way into shared memory, once for all waves of a block
 // (products of 8 bits at twice the rate would need queries and weights in two halves each, twice the products, and instructions for every
-// weight of every row, where a converted element serves all rows): the two chunks take 690 to 705 us.  33 requests of 2 to 6 tokens, 7 heads on each of 4, up to 5009 keys: 48 us, and 9 us to join parts; most
-// rows of a block are empty there, and the longest request's blocks end last.  (Parts of equal length instead of equal shares of a
+// weight of every row, where a converted element serves all rows): the two chunks take 715 us a call, 722 over 16 bits.  33 requests of 2 to 6
+// tokens, 7 heads on each of 4, up to 5009 keys: 46 us, and 9 us to join parts; a tile of 128 rows has 14 to 42 there, so one wave or two
+// carry the chain of every tile of keys (1.3 TB/s, 73 TFLOP/s) and the others only move keys.  (Parts of equal length instead of equal shares of a
 // request: 63 rows 46 us, not 64, but equal contexts 43 to 53 us; tiles of 32 rows in kv_attention_few.h: 28 rows 57 us, not 49.)
 #pragma once
 #include <type_traits>

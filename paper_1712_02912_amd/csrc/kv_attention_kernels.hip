@@ -10,7 +10,8 @@ namespace pq {
 // at the end.  Keys are read by one lane each and no row shares what another one reads: simple, not fast.  It is
 // for f32 and for layouts and dimensions that the other kernels do not take; the products' operands stay fp32 there.  64 single
 // tokens over up to 8192 keys, 32 heads of 128 dimensions on 8, bf16: 2.4 ms (kv_attention_few.h: 0.16); two chunks of 2048 over
-// 14 336 keys: 183 ms (kv_attention_chunk.h: 0.69 to 0.73).
+// 14 336 keys: 183 ms (kv_attention_chunk.h: 0.69 to 0.73).  Over 8 bits a lane loads its key byte by byte: the 64 tokens with f32
+// queries 2.0 ms, with 80 dimensions in f16 1.7 ms.
 constexpr int GENERAL_WAVES = 4;
 constexpr int GENERAL_DIM = 512;
 

@@ -147,9 +147,9 @@ template <class T, bool PAIRS> __global__ __launch_bounds__(APPEND_THREADS) void
 // its code a matter of the definition, not of the order in which a norm is summed: next to a border of e4m3 the last bit of x decides
 // over a sixteenth of it.
 //
-// 16 384 tokens of 32 + 8 + 8 heads of 128 dimensions, bf16: 378 MB in 96 us, 41 us keys and values (101 MB; bound by vector instructions
-// and by their meetings: a list of 16 rows takes a wave about 250 to 350 of them) and 54 us queries (268 MB = 5.0 TB/s); 4099 tokens of 36 heads of
-// 80 dimensions, f16, 25 us; 64 single tokens 6.5 us, a chain of slots, rows and rotations, scales.
+// 16 384 tokens of 32 + 8 + 8 heads of 128 dimensions, bf16: 378 MB in 97 us, 44 us keys and values (101 MB; bound by vector instructions
+// and by their meetings: a list of 16 rows takes a wave about 250 to 350 of them) and 53 us queries (268 MB = 5.0 TB/s); 4099 tokens of 36 heads of
+// 80 dimensions, f16, 25 us; 64 single tokens 8.6 us a call, a chain of slots, rows and rotations, scales.
 constexpr int APPEND8_V = 4;       // of keys (eight elements a lane: sixteen, in fp64, leave registers for two waves of a SIMD)
 constexpr int APPEND8_MOST = 1024; // threads of a block
 constexpr int APPEND8_ROWS = APPEND8_MOST;

@@ -72,7 +72,8 @@ constexpr int CANDIDATES = 1024, LISTED = 512;   // logits that are sorted, stre
 // least the limit, the (top)th largest of the groups' maxima, so no smaller logit is listed, and nearly all that are as large are: for 20
 // of 256 groups 20.8 are expected.  The few stretches that reach the limit are read again, their logits of at least the limit are
 // sorted by counting.  Of too many (equal ones, or the largest all with one thread) those above the limit
-// are, by one more pass, and the rest is searched by a pass for each different logit.
+// are, by one more pass, and the rest is searched by a pass for each different logit (1024 rows of 131 072, bf16, all but 20 logits -9984:
+// 56 us with 10 listed, 410 with 50).
 //
 // Bound by memory where rows are many: 4096 rows of 131 072, bf16, 20 listed: 1.07 GB in 195 to 199 us = 5.4 TB/s; 1024 of these in f32
 // without a list: 537 MB in 93 us = 5.8 TB/s.  A logit takes a conversion, a bound, half a maximum, two multiply-adds, an addition and a
@@ -361,8 +362,9 @@ template <class T> static int logprobs_typed(pq_ctx *ctx, const logprob_args &a)
     // 16 logits of a thread at a time: with 32, longer rows gain 3 % at most and short ones lose as much in occupancy.
     constexpr int E = 16 / sizeof(T), BATCH = 16 / E;
     // Few rows: more threads for each, so long as all of them have logits (8 rows of 32 000, bf16: 10.0 us, 12.4 with 256 threads; 256 rows
-    // of 131 072: 20 and 29 us; but 300 rows of 50 021: 18.6 and 18.1 us).  Long rows: fewer ends, which are not hidden (4096 rows of
-    // 131 072, bf16: 195 us, 204 with 256 threads; of 32 000 it is 66 and 60 us).
+    // of 131 072: 20 and 29 us); with more rows than compute units not (300 rows of 50 021: 23.6 us, 18.8 with 256).  Long rows: fewer ends, which
+    // are not hidden (131 072, bf16: 4096 rows 195 us with 512 threads, 205 with 256, 517 rows 38 and 42; but 1024 rows 67 and 58, and of 32 000
+    // 4096 rows 72 and 63).
     const int threads = a.rows <= ctx->num_cu && a.vocab >= 1024 * E ? 1024 : a.vocab >= 65536 ? 512 : 256;
     if (!grid_fits(a.rows, threads)) return fail(ctx, PQ_EUNSUPPORTED, "token_logprobs: %d rows in one call", a.rows);
     if (threads == 1024) token_logprobs_kernel<T, 1024, BATCH><<<a.rows, 1024, 0, ctx->stream>>>(a);
